@@ -371,6 +371,89 @@ nmd_status nmd_nn_workspace_bytes(int64_t N, int32_t d, size_t* bytes);
 nmd_status nmd_nearest_neighbors(const float* d_x, int64_t N, int32_t d, const int32_t* d_labels, int32_t* d_nn,
                                  float* d_best, int64_t* errors, void* d_workspace, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Fine-tuning a fitted model.  Row i of the model L = W H scores the n columns;
+ * softmax(L_i) is its distribution over them (the next word of a bigram table,
+ * the partner of a cell).  The calls below train such scores on preferences or
+ * rewards.  They take no handle: every pointer is a device pointer unless said
+ * otherwise, caller-owned, on the current device; the work is enqueued on
+ * `stream` (a cudaStream_t, NULL = legacy default stream) and nothing waits.
+ * Workspaces are 256-byte aligned, of at least the size that the *_bytes call
+ * gives (NMD_ERR_WORKSPACE otherwise), and free again once the call's work on
+ * the stream is done.  Bad arguments: NMD_ERR_INVALID, before anything is
+ * enqueued.
+ *
+ * Logits: T rows (0 <= T <= 2^27) of V columns (1 <= V < 2^31), row t at
+ * element t ld (ld >= 0), the columns of a row adjacent, any alignment of an
+ * element.  d_targets[t] is row t's column.  A target below zero leaves its
+ * row out: its logits and its entries of the other arrays are not read (they
+ * may hold anything), its log-probability is 0 and its gradient row is zero.
+ * A target of V or more gives NaN.  With tau = temperature > 0,
+ *   lp_t = x_ty / tau - log sum_v exp(x_tv / tau),   p_tv = exp(x_tv/tau) / sum.
+ * Logits of -inf have probability 0; a row of nothing else, and a NaN or +inf
+ * in a row, give NaN.  Gradients d loss / d x_tv = g_t (1[v = y_t] - p_tv) / tau
+ * are written for all T rows in the logits' type (rounded once), row t at
+ * element t grad_ld (grad_ld >= V); they may not overlap the logits.  Sums are
+ * kept in 32 bits or more and taken in an order that the sizes, strides and
+ * alignments fix: equal calls give equal bits. */
+typedef enum { NMD_DT_FP32 = 0, NMD_DT_BF16 = 1, NMD_DT_FP16 = 2 } nmd_dtype;
+
+/* d_logps[t] = lp_t (T fp32). */
+nmd_status nmd_token_logprobs(const void* d_logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                              const int64_t* d_targets, double temperature, float* d_logps, void* stream);
+
+/* Paired preference loss over P >= 1 pairs of sequences packed into the rows:
+ * sequence k is rows [d_offsets[k], d_offsets[k + 1]) (2 P + 1 ascending
+ * borders), pair p prefers sequence 2p to sequence 2p + 1; a sequence may be
+ * empty, and rows outside all of them take no part.  d_reference[t]: the
+ * reference model's log-probability of row t's column.
+ *   R_k    = sum over the live rows of k of (lp_t - reference_t)
+ *            (average != 0: divided by their number, if any)   -> d_ratios, 2 P
+ *   h_p    = beta (R_2p - R_2p+1)                              -> d_margins, P
+ *   loss   = mean_p -(1 - smoothing) log sigma(h_p) - smoothing log sigma(-h_p)
+ * with smoothing in [0, 1).  d_loss: 1 fp32; d_logps: T; d_grad may be NULL. */
+nmd_status nmd_preference_workspace_bytes(int64_t T, int64_t P, size_t* bytes);
+nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                               const int64_t* d_targets, const int64_t* d_offsets, int64_t P,
+                               const float* d_reference, double beta, double smoothing, int32_t average,
+                               double temperature, float* d_loss, float* d_logps, float* d_ratios, float* d_margins,
+                               void* d_grad, int64_t grad_ld, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Clipped policy loss with a KL term.  With rho_t = exp(lp_t - old_t),
+ * A = d_advantages and lo = 1 - clip_low, hi = 1 + clip_high:
+ *   l_t = -min(rho_t A_t, clamp(rho_t, lo, hi) A_t) + kl_coef k_t,
+ *   k_t = exp(ref_t - lp_t) - (ref_t - lp_t) - 1   (>= 0; estimates the KL
+ *         divergence from the reference),
+ *   loss = sum_t w_t l_t over the live rows, w_t = 1 / (live rows) without
+ *   d_offsets, else 1 / (S x live rows of the row's sequence) for the S
+ *   sequences with borders d_offsets (S + 1, as above); a row is cut off (no
+ *   gradient through its first term) when A_t > 0 and rho_t > hi or A_t < 0
+ *   and rho_t < lo.
+ * d_stats: 3 fp32: loss, sum w_t k_t, sum of w_t over the rows cut off.
+ * d_reference may be NULL if kl_coef is 0 (k_t then counts as 0).  clip_low in
+ * [0, 1], clip_high >= 0, kl_coef >= 0.  d_logps: T; d_grad may be NULL. */
+nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes);
+nmd_status nmd_policy_loss(const void* d_logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                           const int64_t* d_targets, const float* d_old, const float* d_reference,
+                           const float* d_advantages, const int64_t* d_offsets, int64_t S, double clip_low,
+                           double clip_high, double kl_coef, double temperature, float* d_stats, float* d_logps,
+                           void* d_grad, int64_t grad_ld, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Global norm of `count` gradients and the gradients scaled to a largest norm:
+ *   norm = sqrt(sum of all squares),  out = grad min(1, max_norm / norm).
+ * d_grads, sizes (elements, >= 0), dtypes (nmd_dtype) and d_out are host
+ * arrays of `count` entries, read before the call returns; the tensors are
+ * contiguous, of any alignment of an element.  d_out NULL: in place (nothing
+ * is written when the norm is within max_norm); otherwise each out[k] has its
+ * gradient's type and is either the gradient itself or apart from every other
+ * tensor.  d_norm: 1 fp32.  A norm that is NaN makes every gradient NaN; an
+ * infinite one makes its infinite entries NaN and the others 0.  The squares
+ * neither overflow nor vanish over the whole range of fp32. */
+nmd_status nmd_clip_workspace_bytes(int64_t count, size_t* bytes);
+nmd_status nmd_clip_grad_norm(int64_t count, const void* const* d_grads, const int64_t* sizes, const int32_t* dtypes,
+                              double max_norm, void* const* d_out, float* d_norm, void* d_workspace, size_t ws_bytes,
+                              void* stream);
+
 const char* nmd_status_string(nmd_status s);
 const char* nmd_last_error(const nmd_handle* h);
 void nmd_destroy(nmd_handle* h);

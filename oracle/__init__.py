@@ -9,3 +9,4 @@ from .salsa import (ROW, COL, EXACT, STOCH, ALTERNATE, PHASED, NotSPD, Options, 
                     solve_normal, update_z, loss, splitmix64_mix, SplitMix64,
                     positive_set, range_search_set)
 from . import embed  # noqa: F401,E402  (Sec. 5.3: cell embedding and 1-NN error)
+from . import tuning  # noqa: F401,E402  (fine-tuning operators)

@@ -25,6 +25,7 @@ NMD_BF16, NMD_FP32, NMD_SIMT = 0, 1, 2
 NMD_EPI_Z, NMD_EPI_DELTA = 0, 1
 NMD_K_DENSE, NMD_K_SPARSE, NMD_K_GRAM, NMD_K_UPDATE, NMD_K_LOSS = 0, 1, 2, 3, 4
 NMD_SKIP_NONE, NMD_SKIP_VOTE, NMD_SKIP_RANGE = 0, 1, 2
+NMD_DT_FP32, NMD_DT_BF16, NMD_DT_FP16 = 0, 1, 2
 
 # every symbol include/nmd.h declares
 EXPORTS = [
@@ -34,6 +35,8 @@ EXPORTS = [
     "nmd_launch_count", "nmd_skip_count", "nmd_selftest_wait_timeout", "nmd_profile", "nmd_profile_read", "nmd_status_string", "nmd_last_error",
     "nmd_destroy", "nmd_gram_noalloc", "nmd_support_term", "nmd_block_update_combined", "nmd_range_mask",
     "nmd_embed", "nmd_nn_workspace_bytes", "nmd_nearest_neighbors",
+    "nmd_token_logprobs", "nmd_preference_workspace_bytes", "nmd_preference_loss", "nmd_policy_workspace_bytes",
+    "nmd_policy_loss", "nmd_clip_workspace_bytes", "nmd_clip_grad_norm",
 ]
 
 
@@ -105,6 +108,18 @@ def lib() -> C.CDLL:
             "nmd_nn_workspace_bytes": (C.c_int, [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]),
             "nmd_nearest_neighbors": (C.c_int, [_P, C.c_int64, C.c_int32, _P, _P, _P, _i64p, _P, C.c_size_t,
                                                 _P]),
+            "nmd_token_logprobs": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, C.c_double, _P,
+                                             _P]),
+            "nmd_preference_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+            "nmd_preference_loss": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, _P, C.c_int64, _P,
+                                              C.c_double, C.c_double, C.c_int32, C.c_double, _P, _P, _P, _P, _P,
+                                              C.c_int64, _P, C.c_size_t, _P]),
+            "nmd_policy_workspace_bytes": (C.c_int, [C.c_int64, C.POINTER(C.c_size_t)]),
+            "nmd_policy_loss": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, _P, _P, _P, _P,
+                                          C.c_int64, C.c_double, C.c_double, C.c_double, C.c_double, _P, _P, _P,
+                                          C.c_int64, _P, C.c_size_t, _P]),
+            "nmd_clip_workspace_bytes": (C.c_int, [C.c_int64, C.POINTER(C.c_size_t)]),
+            "nmd_clip_grad_norm": (C.c_int, [C.c_int64, _P, _P, _P, C.c_double, _P, _P, _P, C.c_size_t, _P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
