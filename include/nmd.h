@@ -402,6 +402,22 @@ typedef enum { NMD_DT_FP32 = 0, NMD_DT_BF16 = 1, NMD_DT_FP16 = 2 } nmd_dtype;
 nmd_status nmd_token_logprobs(const void* d_logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                               const int64_t* d_targets, double temperature, float* d_logps, void* stream);
 
+/* The same from the factors, with no T x n matrix of scores anywhere: row t's
+ * scores are z_tj = a_t . b_j for the T rows of A and the n rows of B, r
+ * columns each (1 <= n < 2^31, 1 <= r <= 256), of one type.  Element (t, k) of
+ * A is at t a_row + k a_col, of B at j b_row + k b_col (any strides >= 0; the
+ * r x n matrix H is B with b_row = 1, b_col = n).  16-bit factors with
+ * adjacent columns, rows a multiple of 8 elements apart and a 16-byte aligned
+ * start are read where they are; others are first packed into the workspace.
+ * 16-bit factors are multiplied exactly, fp32 ones to about 2^-24 of |a_t| |b_j|
+ * (three bf16 pieces each); products are accumulated in fp32.  A wait in the
+ * kernel that runs out (2 s) makes the rows concerned NaN. */
+nmd_status nmd_factor_workspace_bytes(const void* d_A, int64_t a_row, int64_t a_col, const void* d_B, int64_t b_row,
+                                      int64_t b_col, int32_t dtype, int64_t T, int64_t n, int64_t r, size_t* bytes);
+nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, const void* d_B, int64_t b_row,
+                               int64_t b_col, int32_t dtype, int64_t T, int64_t n, int64_t r, const int64_t* d_targets,
+                               double temperature, float* d_logps, void* d_workspace, size_t ws_bytes, void* stream);
+
 /* Paired preference loss over P >= 1 pairs of sequences packed into the rows:
  * sequence k is rows [d_offsets[k], d_offsets[k + 1]) (2 P + 1 ascending
  * borders), pair p prefers sequence 2p to sequence 2p + 1; a sequence may be

@@ -5,7 +5,7 @@
 // For row t with logits x_tv, temperature tau, c = log2(e) / tau and the row's
 // maximum m,
 //   e_tv = 2^(c (x_tv - m)),  S = sum_v e_tv,  p_tv = e_tv / S,
-//   log p_ty = ln 2 c (x_ty - m) - ln S,
+//   log p_ty = (x_ty - m) / tau - ln S,
 //   d loss / d x_tv = g_t (1[v = y_t] - p_tv) / tau.
 // (The difference is taken before the product: c m alone would pass fp32's
 // range where a row is masked with the type's lowest value.)  m and S come
@@ -30,7 +30,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr float kLn2 = 0.693147180559945309f;
 constexpr double kLog2e = 1.4426950408889634074;
 
 // 2^x by the SFU (relative error about 2^-22; results below 2^-126 become 0,
@@ -271,7 +270,7 @@ __global__ void __launch_bounds__(512) row_kernel(const Rows a) {
     float lp = 0.f;
     if (live) {
       // a target past the last column has no log-probability: NaN, so that the mistake shows
-      lp = y < a.V ? kLn2 * ((Vec<T>::get(x[y]) - st.m) * a.c) - logf(st.S) : NAN;
+      lp = y < a.V ? (Vec<T>::get(x[y]) - st.m) * a.inv_temp - logf(st.S) : NAN;
     }
     if (tid == 0) {
       a.logps[t] = lp;

@@ -36,7 +36,8 @@ EXPORTS = [
     "nmd_destroy", "nmd_gram_noalloc", "nmd_support_term", "nmd_block_update_combined", "nmd_range_mask",
     "nmd_embed", "nmd_nn_workspace_bytes", "nmd_nearest_neighbors",
     "nmd_token_logprobs", "nmd_preference_workspace_bytes", "nmd_preference_loss", "nmd_policy_workspace_bytes",
-    "nmd_policy_loss", "nmd_clip_workspace_bytes", "nmd_clip_grad_norm",
+    "nmd_policy_loss", "nmd_clip_workspace_bytes", "nmd_clip_grad_norm", "nmd_factor_workspace_bytes",
+    "nmd_factor_logprobs",
 ]
 
 
@@ -110,6 +111,10 @@ def lib() -> C.CDLL:
                                                 _P]),
             "nmd_token_logprobs": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, C.c_double, _P,
                                              _P]),
+            "nmd_factor_workspace_bytes": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int64, C.c_int32,
+                                                     C.c_int64, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+            "nmd_factor_logprobs": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int64, C.c_int32, C.c_int64,
+                                              C.c_int64, C.c_int64, _P, C.c_double, _P, _P, C.c_size_t, _P]),
             "nmd_preference_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
             "nmd_preference_loss": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, _P, C.c_int64, _P,
                                               C.c_double, C.c_double, C.c_int32, C.c_double, _P, _P, _P, _P, _P,

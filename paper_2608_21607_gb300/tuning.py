@@ -103,6 +103,31 @@ def token_logprobs(logits, targets, *, temperature: float = 1.0) -> torch.Tensor
     return logps
 
 
+def factor_logprobs(A, B, targets, *, temperature: float = 1.0) -> torch.Tensor:
+    """token_logprobs of the scores A @ B^T without forming them (T fp32).
+
+    ``A`` (T x r) and ``B`` (n x r, r <= 256) have one type and any strides: the model's rows are A = W[rows] and
+    B = H.t().  16-bit factors are read where they are if their rows are contiguous, 16-byte aligned and a multiple
+    of 8 elements apart; others are packed first.
+    """
+    for x, name in ((A, "A"), (B, "B")):
+        if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda or x.dtype not in _DTYPES:
+            _invalid("%s: a two-dimensional float32, bfloat16 or float16 CUDA tensor is wanted" % name)
+    device, (T, r), n = A.device, A.shape, B.shape[0]
+    if B.device != device or B.dtype != A.dtype or B.shape[1] != r:
+        _invalid("B: %s of %d columns on %s is wanted, as A" % (A.dtype, r, device))
+    if not 1 <= r <= 256 or n < 1:
+        _invalid("A, B: 1 to 256 columns and at least one row of B are wanted")
+    targets = _vector(targets, "targets", T, torch.int64, device)
+    logps = torch.empty(T, dtype=torch.float32, device=device)
+    factors = (A.data_ptr(), *A.stride(), B.data_ptr(), *B.stride(), _DTYPES[A.dtype], T, n, r)
+    nbytes = _bytes("nmd_factor_workspace_bytes", *factors)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _call(device, "nmd_factor_logprobs", *factors, targets.data_ptr(), temperature, logps.data_ptr(), ws.data_ptr(),
+          nbytes)
+    return logps
+
+
 def preference_loss(logits, targets, offsets, reference, *, beta: float = 0.1, label_smoothing: float = 0.0,
                     average: bool = False, temperature: float = 1.0, grad: bool = True) -> PreferenceLoss:
     """Paired preference loss -log sigma(beta (R_chosen - R_rejected)), mean over the pairs, and its gradient.

@@ -8,6 +8,10 @@ finite z = x / temperature and lp its log-probability:
   64 u by its order and 40 u by the rescalings of ten merges; the logarithm and
   the last difference add 2 u (|lp| + R).  Together below
   u (128 + 4 R + 4 |lp|), called TOL(lp) here.
+* factors: a score's products are exact for 16-bit factors and the fp32 additions
+  lose at most (r + 8) 2 u sum |a b|; fp32 factors, as six products of three
+  pieces, (6 r + 8) 2 u and 8 u for what the pieces leave out.  A log-probability
+  takes twice the largest of that over its row's columns, over temperature.
 * preference: a ratio sums TOL(lp) + u |lp| over its rows (the log-probability
   is stored in fp32 first), the margin takes beta of two of them, the logistic
   function has slope at most 1/4, and coefficients are rounded once.
@@ -155,6 +159,80 @@ def test_no_rows_and_equal_bits():
             for _ in range(2)]
     for a, b in zip(*runs):
         assert torch.equal(a, b)
+
+
+def make_factors(seed, T, n, r, dtype, scale=1.0):
+    rng = np.random.default_rng(seed)
+    f = scale * np.sqrt(2.5 / np.sqrt(r))
+    A = cuda(f * rng.standard_normal((T, r))).to(DTYPES[dtype])
+    B = cuda(f * rng.standard_normal((n, r))).to(DTYPES[dtype])
+    y = rng.integers(0, n, T)
+    y[0], y[-1] = n - 1, 0
+    y[rng.random(T) < 0.2] = -3
+    return A, B, y
+
+
+def check_factors(A, B, y, dtype, temperature, got):
+    a, b, r = A.double().cpu().numpy(), B.double().cpu().numpy(), A.shape[1]
+    a = np.where((y >= 0)[:, None], a, 0.0)
+    want = O.tuning.factor_logprobs(a, b, y, temperature)
+    worst = (np.abs(a) @ np.abs(b).T).max(axis=1)
+    ez = worst * ((6 * r + 8) * 2 * U + 8 * U if dtype == "fp32" else (r + 8) * 2 * U)
+    tol = 2 * ez / temperature + tol_lp(a @ b.T, y, want, temperature) + U * np.abs(want)
+    check("logps", got.cpu().numpy(), want, np.where(y >= 0, tol, 0.0))
+
+
+FACTORS = [  # T, n, r
+    (1, 1, 1), (1, 2, 3), (5, 127, 16), (128, 128, 64), (129, 129, 17), (300, 1000, 65), (7, 20001, 64),
+    (1000, 257, 100), (33, 5000, 128), (257, 3001, 129), (64, 4097, 200), (513, 2500, 256), (2, 139255, 64),
+    (40000, 40, 8),
+]
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("shape", FACTORS, ids=lambda s: "x".join(map(str, s)))
+def test_factor_logprobs(shape, dtype):
+    T, n, r = shape
+    for temperature in (1.0, 0.6):
+        A, B, y = make_factors(T + n, T, n, r, dtype)
+        got = tuning().factor_logprobs(A, B, cuda(y, torch.int64), temperature=temperature)
+        check_factors(A, B, y, dtype, temperature, got)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_factor_layouts(dtype):
+    """Every layout gives what contiguous factors give: H as it is stored (r x n), rows cut out of wider ones,
+    unaligned starts, broadcast rows."""
+    A, B, y = make_factors(3, 200, 777, 40, dtype)
+    yt = cuda(y, torch.int64)
+    H = B.t().contiguous()
+    wide = torch.zeros(777, 64, dtype=B.dtype, device="cuda")
+    odd = torch.zeros(777 * 41 + 1, dtype=B.dtype, device="cuda")[1:].view(777, 41)
+    wide[:, 8:48] = B
+    odd[:, 1:] = B
+    want = tuning().factor_logprobs(A, B, yt)
+    check_factors(A, B, y, dtype, 1.0, want)
+    for given in (H.t(), wide[:, 8:48], odd[:, 1:]):
+        assert torch.equal(tuning().factor_logprobs(A, given, yt), want)
+    assert torch.equal(tuning().factor_logprobs(A.t().contiguous().t(), B, yt), want)
+    same = A[5:6].expand(200, 40)
+    check_factors(same, B, y, dtype, 1.0, tuning().factor_logprobs(same, B, yt))
+
+
+def test_factor_rows_that_are_no_numbers():
+    """A NaN or infinite row of A spoils its own result only, unless it is left out."""
+    A, B, y = make_factors(4, 150, 300, 64, "bf16")
+    y[:] = np.arange(150)
+    y[9] = -1
+    A[9], A[20], A[21, 3] = float("nan"), float("nan"), float("inf")
+    yt = cuda(y, torch.int64)
+    yt[33] = 300                          # past the last column
+    got = tuning().factor_logprobs(A, B, yt).cpu()
+    bad = torch.zeros(150, dtype=torch.bool)
+    bad[[20, 21, 33]] = True
+    assert torch.equal(torch.isnan(got), bad) and got[9] == 0.0
+    A, B, y = make_factors(4, 3, 300, 64, "fp32")
+    assert tuning().factor_logprobs(A[:0], B, torch.empty(0, dtype=torch.int64, device="cuda")).shape == (0,)
 
 
 PREFERENCE = [  # T, V, pad, shift, borders
@@ -447,6 +525,12 @@ def test_refusals():
     for kw in (dict(clip_low=-0.1), dict(clip_low=1.5), dict(clip_high=-1.0), dict(clip_high=float("inf")),
                dict(kl_coef=-0.1), dict(kl_coef=float("nan"))):
         refused(t.policy_loss, x, y, v, v, v, **kw)
+    A, B = torch.zeros(4, 8, device="cuda"), torch.zeros(9, 8, device="cuda")
+    for a, b in ((A, B[:, :7]), (A, B.bfloat16()), (A, B.cpu()), (A.double(), B.double()), (A[0], B), (A, B[:0]),
+                 (A[:, :0], B[:, :0]), (torch.zeros(4, 257, device="cuda"), torch.zeros(9, 257, device="cuda"))):
+        refused(t.factor_logprobs, a, b, y)
+    refused(t.factor_logprobs, A, B, y[:3])
+    refused(t.factor_logprobs, A, B, y, temperature=0.0)
     for max_norm in (0.0, -1.0, float("nan"), float("inf")):
         refused(t.clip_grad_norm, [x.clone()], max_norm)
     refused(t.clip_grad_norm, [], 1.0)
