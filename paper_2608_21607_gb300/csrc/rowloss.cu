@@ -11,72 +11,134 @@
 // range where a row is masked with the type's lowest value.)  m and S come
 // from one pass with a running maximum: a thread keeps its own (m, S),
 // rescales S when a group of vectors raises m, and the threads' pairs are
-// merged by (m1, S1) + (m2, S2) = (m, S1 2^(c (m1 - m)) + S2 2^(c (m2 - m)))
-// in a fixed order.  All sums are fp32; the only rounding to fewer bits is that of
+// merged in a fixed order.  All sums are fp32; the only rounding to fewer bits is that of
 // the gradient to the logits' type, once, when it is stored.
 //
 // Everything here is bound by HBM: a row is read once (twice where the
 // gradient's coefficient depends on other rows) and its gradient written once.
-#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <cmath>
 
 #include "nmd_internal.cuh"
+#include "tc_pipe.cuh"
+#include "tc_ptx.cuh"
 
 namespace nmd {
 namespace {
 
-namespace cg = cooperative_groups;
-
+constexpr float kLn2 = 0.693147180559945309f;
 constexpr double kLog2e = 1.4426950408889634074;
 
-// 2^x by the SFU (relative error about 2^-22; results below 2^-126 become 0,
-// which no sum of probabilities can tell from the exact value)
+// 2^x by the SFU (results below 2^-126 become 0, which no sum of
+// probabilities can tell from the exact value)
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// the larger value, NaN if one is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
 
-// 16-byte vectors of the three element types
+// Pairs of fp32 values (fp32x2 instructions: one issue slot for two)
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t pair_of(float a, float b) {
+  pair_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 halves(pair_t p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+  pair_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
+  pair_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+  pair_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// c = log2(e) / tau as hi + lo, hi of 12 bits, so that a 16-bit x times hi less
+// an integer is exact and the exponent is rounded once, without a leaning that
+// the sum over a long sequence would show.  lo > 0: both products of -inf are
+// -inf.  `whole` is c in one fp32 value.
+struct Scale {
+  float hi, lo, whole;
+};
+// 2^(c (x - m))
+__device__ __forceinline__ float power(float x, float m, Scale c) {
+  const float d = x - m;
+  return ex2(fmaf(d, c.hi, d * c.lo));
+}
+__device__ __forceinline__ pair_t exponent2(pair_t x, float m, Scale c) {
+  const pair_t d = add2(x, pair_of(-m, -m));
+  return fma2(d, pair_of(c.hi, c.hi), mul2(d, pair_of(c.lo, c.lo)));
+}
+__device__ __forceinline__ pair_t power2(pair_t x, float m, Scale c) {
+  const float2 e = halves(exponent2(x, m, c));
+  return pair_of(ex2(e.x), ex2(e.y));
+}
+
+// 16-byte vectors of the three element types: N values, the largest of them (NaN
+// if one is), pairs of them
 template <class T>
 struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[4]) {
-    f[0] = __uint_as_float(v.x);
-    f[1] = __uint_as_float(v.y);
-    f[2] = __uint_as_float(v.z);
-    f[3] = __uint_as_float(v.w);
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }   // -inf
+  static __device__ __forceinline__ pair_t pair(const uint4& v, int i) {
+    return i == 0 ? pair_of(__uint_as_float(v.x), __uint_as_float(v.y))
+                  : pair_of(__uint_as_float(v.z), __uint_as_float(v.w));
   }
-  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  static __device__ __forceinline__ float top(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
+                   max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  static __device__ __forceinline__ uint4 pack(const pair_t (&f)[2]) {
+    const float2 a = halves(f[0]), b = halves(f[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
   }
   static __device__ __forceinline__ float get(float x) { return x; }
   static __device__ __forceinline__ float put(float x) { return x; }
 };
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) {
+  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+}
 template <>
 struct Vec<bf16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }   // -inf
+  static __device__ __forceinline__ pair_t pair(const uint4& v, int i) {
+    const uint32_t w = word(v, i);
+    return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
-  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-    uint32_t w[4];
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __nv_bfloat162* h = (const __nv_bfloat162*)&v;
+    const float2 f = __bfloat1622float2(__hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    return max_nan(f.x, f.y);
+  }
+  static __device__ __forceinline__ uint4 pack(const pair_t (&f)[4]) {
+    uint4 w;
+    __nv_bfloat162* h = (__nv_bfloat162*)&w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      w[i] = *(const uint32_t*)&h;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 4; ++i) h[i] = __float22bfloat162_rn(halves(f[i]));
+    return w;
   }
   static __device__ __forceinline__ float get(bf16 x) { return __bfloat162float(x); }
   static __device__ __forceinline__ bf16 put(float x) { return __float2bfloat16_rn(x); }
@@ -84,54 +146,146 @@ struct Vec<bf16> {
 template <>
 struct Vec<__half> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 g = __half22float2(*(const __half2*)&w[i]);
-      f[2 * i] = g.x;
-      f[2 * i + 1] = g.y;
-    }
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u); }   // -inf
+  static __device__ __forceinline__ pair_t pair(const uint4& v, int i) {
+    const uint32_t w = word(v, i);
+    const float2 f = __half22float2(*(const __half2*)&w);
+    return pair_of(f.x, f.y);
   }
-  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-    uint32_t w[4];
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __half2* h = (const __half2*)&v;
+    const float2 f = __half22float2(__hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    return max_nan(f.x, f.y);
+  }
+  static __device__ __forceinline__ uint4 pack(const pair_t (&f)[4]) {
+    uint4 w;
+    __half2* h = (__half2*)&w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-      w[i] = *(const uint32_t*)&h;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 4; ++i) h[i] = __float22half2_rn(halves(f[i]));
+    return w;
   }
   static __device__ __forceinline__ float get(__half x) { return __half2float(x); }
   static __device__ __forceinline__ __half put(float x) { return __float2half_rn(x); }
 };
 
-// (m, S) of a set of elements: the maximum and the sum of 2^(c (x - m))
-struct Stat {
+// (m, S) of a set of elements: a value near their maximum (NaN if one is; -inf
+// of none) and the sum of 2^(c x - ref), where ref is the integer ceil(c m) if
+// that is within +-1024, and c m otherwise.  An integer reference makes every
+// rescaling exact.
+struct __align__(8) Stat {
   float m, S;
 };
-// -inf until a finite element has been seen: the sum is 0 and stays 0
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ Stat merge(const Stat& a, const Stat& b, float c) {
-  const float m = fmaxf(a.m, b.m), z = base_of(m);
-  return {m, a.S * ex2((a.m - z) * c) + b.S * ex2((b.m - z) * c)};
+__device__ __forceinline__ bool is_near(float m, Scale c) { return fabsf(m * c.hi) <= 1024.f; }
+__device__ __forceinline__ float ref_of(float m, Scale c) { return ceilf(m * c.hi); }
+// ref - c m: what the reference is above the maximum
+__device__ __forceinline__ float above(float m, Scale c) {
+  return is_near(m, c) ? fmaf(-m, c.lo, fmaf(-m, c.hi, ref_of(m, c))) : 0.f;
 }
-// adds the values f[0..N) to the pair
-template <int N>
-__device__ __forceinline__ void add(Stat& s, const float (&f)[N], float c) {
-  float m = f[0];
+// 2^(reference of m - reference of to), m <= to
+__device__ __forceinline__ float rescale(float m, float to, Scale c) {
+  if (is_near(m, c) && is_near(to, c)) return ex2(ref_of(m, c) - ref_of(to, c));   // exact
+  if (m == to) return 1.f;
+  const float d = m - to;
+  return ex2(fmaf(d, c.hi, d * c.lo) + (above(m, c) - above(to, c)));
+}
+// Merges over groups of `width` lanes (a power of two); every lane of a group
+// gets the same result.
+template <int width>
+__device__ __forceinline__ Stat merge_lanes(Stat st, Scale c) {
+  float m = st.m;
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, f[i]);
-  if (m > s.m) {
-    s.S *= ex2((s.m - m) * c);
-    s.m = m;
+  for (int o = width / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float S = st.S * rescale(st.m, m, c);
+#pragma unroll
+  for (int o = width / 2; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+  return {m, S};
+}
+
+// A running pair.  The reference is the maximum of the first elements and stays
+// until a group of elements exceeds it by much (its sum passes kHigh), so that
+// the usual group costs a product, a correction, an exponential and an addition
+// per element and no comparison.  The SFU's exponential is low by 5e-8 on
+// average for negative arguments and high by 3.5e-8 for positive ones (measured
+// over many arguments), which the sum over a long sequence would show; every
+// second element is therefore taken 2^kLift larger, and its sum reduced by that,
+// exactly.
+template <class T>
+struct Running {
+  static constexpr float kHigh = 4096.f, kLift = 24.f, kDrop = 1.f / (1 << 24);
+  Stat s{-INFINITY, 0.f};
+  float r = 0.f;
+  bool usual = false;   // the reference is an integer
+
+  // four vectors: get(0) to get(3), asked for again where the group is not a usual one
+  template <class G>
+  __device__ __forceinline__ void add(G get, Scale c) {
+    constexpr int P = Vec<T>::N / 2, H = 4 * P;
+    for (;;) {
+      if (usual) {
+        const pair_t hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo), k0 = pair_of(-r, kLift - r);
+        // all products, then all exponentials, then the sums: enough of each
+        // under way to cover their latencies
+        pair_t x[H];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint4 v = get(k);
+#pragma unroll
+          for (int i = 0; i < P; ++i) x[k * P + i] = Vec<T>::pair(v, i);
+        }
+#pragma unroll
+        for (int i = 0; i < H; ++i) x[i] = fma2(x[i], lo, fma2(x[i], hi, k0));
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const float2 e = halves(x[i]);
+          x[i] = pair_of(ex2(e.x), ex2(e.y));
+        }
+#pragma unroll
+        for (int d = H / 2; d > 0; d /= 2)
+#pragma unroll
+          for (int i = 0; i < d; ++i) x[i] = add2(x[i], x[i + d]);
+        const float2 t = halves(x[0]);
+        const float group = fmaf(t.y, kDrop, t.x);
+        if (group < kHigh) {
+          s.S += group;
+          return;
+        }
+      }
+      // the first group, one with larger values, or one with NaN or infinities
+      float m = s.m;
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) m = max_nan(m, Vec<T>::top(get(k)));
+      raise(m, c);
+      if (usual) continue;
+      // huge, infinite or no numbers; only -inf so far: the sum is 0 and stays 0
+      const float z = s.m == -INFINITY ? 0.f : s.m;
+      pair_t sum = pair_of(0.f, 0.f);
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {
+        const uint4 v = get(k);
+#pragma unroll
+        for (int i = 0; i < P; ++i) sum = add2(sum, power2(Vec<T>::pair(v, i), z, c));
+      }
+      const float2 t = halves(sum);
+      s.S += t.x + t.y;
+      return;
+    }
   }
-  const float z = base_of(s.m);
-  float t = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) t += ex2((f[i] - z) * c);
-  s.S += t;
-}
+  // one value
+  __device__ __forceinline__ void add(float x, Scale c) {
+    raise(max_nan(s.m, x), c);
+    if (usual) s.S += ex2(fmaf(x, c.hi, -r) + x * c.lo);
+    else s.S += power(x, s.m == -INFINITY ? 0.f : s.m, c);
+  }
+
+ private:
+  __device__ __forceinline__ void raise(float m, Scale c) {
+    if (m == s.m) return;
+    s.S *= rescale(s.m, m, c);
+    s.m = m;
+    r = ref_of(m, c);
+    usual = is_near(m, c);
+  }
+};
 
 struct Policy {
   const float* old;      // T: log-probabilities under the policy that produced the tokens
@@ -146,13 +300,16 @@ struct Rows {
   const void* x;
   int64_t T, V, ld;
   const int64_t* y;
-  float c, inv_temp;
+  Scale c;
+  float inv_temp;
   float* logps;          // T
   Stat* stats;           // T (the statistics pass writes, the gradient pass reads) or nullptr
   float* coef;           // T: g_t; zeroed by the statistics pass
   void* grad;            // T x V with row stride gld, or nullptr
   int64_t gld;
+  int64_t each;          // vectors of a row that one CTA of its cluster takes
   int same_phase;        // rows of x and grad start at the same offset from a 16-byte boundary
+  unsigned* done;        // count of finished CTAs: zeroed by the kernel before the one that counts
   Policy p;
 };
 
@@ -172,178 +329,6 @@ __device__ __forceinline__ Span span_of(const T* row, int64_t V) {
   return s;
 }
 
-enum { kStats = 0, kPolicy = 1, kGrad = 2 };
-
-// One group of threads per row: a warp (GROUP 32), or a CTA or cluster of
-// CTAs (GROUP 0; the cluster shares one row).
-template <class T, int GROUP, int MODE>
-__global__ void __launch_bounds__(512) row_kernel(const Rows a) {
-  constexpr int N = Vec<T>::N;
-  __shared__ Stat red[16];
-  __shared__ Stat cred;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t t;
-  int64_t tid, nthr;
-  unsigned csize = 1;
-  if constexpr (GROUP == 32) {
-    t = (int64_t)blockIdx.x * (blockDim.x / 32) + warp;
-    if (t >= a.T) return;
-    tid = lane;
-    nthr = 32;
-  } else {
-    csize = cg::this_cluster().num_blocks();
-    t = blockIdx.x / csize;
-    tid = (int64_t)(blockIdx.x % csize) * blockDim.x + threadIdx.x;
-    nthr = (int64_t)csize * blockDim.x;
-  }
-  const int64_t y = a.y[t];
-  const T* x = (const T*)a.x + t * a.ld;
-  T* g = (T*)a.grad + t * a.gld;
-  const Span sp = span_of(x, a.V);
-  const uint4* xv = (const uint4*)(x + sp.head);
-  // the row's scalar elements: at most one per thread
-  const int64_t scalar = tid < sp.head ? tid : (tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1);
-
-  Stat st{-INFINITY, 0.f};
-  float coef = 0.f;
-  const bool live = y >= 0;
-  if (MODE == kStats && tid == 0 && a.coef != nullptr) a.coef[t] = 0.f;
-  if (MODE != kGrad && live) {
-    constexpr int U = 32 / N;   // vectors in flight per thread
-    int64_t i = tid;
-    for (; i + (U - 1) * nthr < sp.nvec; i += U * nthr) {
-      uint4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = xv[i + u * nthr];
-      float f[U * N];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float h[N];
-        Vec<T>::unpack(v[u], h);
-#pragma unroll
-        for (int k = 0; k < N; ++k) f[u * N + k] = h[k];
-      }
-      add(st, f, a.c);
-    }
-    for (; i < sp.nvec; i += nthr) {
-      float f[N];
-      Vec<T>::unpack(xv[i], f);
-      add(st, f, a.c);
-    }
-    if (scalar >= 0) {
-      float f[1] = {Vec<T>::get(x[scalar])};
-      add(st, f, a.c);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const Stat other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.S, o)};
-      st = merge(st, other, a.c);
-    }
-    if constexpr (GROUP != 32) {
-      if (lane == 0) red[warp] = st;
-      __syncthreads();
-      st = lane < (int)(blockDim.x / 32) ? red[lane] : Stat{-INFINITY, 0.f};
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) {
-        const Stat other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.S, o)};
-        st = merge(st, other, a.c);
-      }
-      st.m = __shfl_sync(0xffffffffu, st.m, 0);
-      st.S = __shfl_sync(0xffffffffu, st.S, 0);
-      if (csize > 1) {
-        cg::cluster_group cl = cg::this_cluster();
-        if (threadIdx.x == 0) cred = st;
-        cl.sync();
-        st = lane < (int)csize ? *cl.map_shared_rank(&cred, lane) : Stat{-INFINITY, 0.f};
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) {
-          const Stat other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.S, o)};
-          st = merge(st, other, a.c);
-        }
-        st.m = __shfl_sync(0xffffffffu, st.m, 0);
-        st.S = __shfl_sync(0xffffffffu, st.S, 0);
-        cl.sync();   // the peers' copies stay until everybody has read them
-      }
-    }
-  }
-  if (MODE != kGrad) {
-    float lp = 0.f;
-    if (live) {
-      // a target past the last column has no log-probability: NaN, so that the mistake shows
-      lp = y < a.V ? (Vec<T>::get(x[y]) - st.m) * a.inv_temp - logf(st.S) : NAN;
-    }
-    if (tid == 0) {
-      a.logps[t] = lp;
-      if (a.stats != nullptr) a.stats[t] = st;
-    }
-    if (MODE == kPolicy) {
-      float term = 0.f, kl = 0.f, cut = 0.f;
-      if (live) {
-        const Policy& p = a.p;
-        const float w = p.weight[t], adv = p.adv[t];
-        const float ratio = expf(lp - p.old[t]);
-        const float bound = fminf(fmaxf(ratio, p.lo), p.hi);
-        const bool off = (adv > 0.f && ratio > p.hi) || (adv < 0.f && ratio < p.lo);
-        const float ra = ratio * adv, ba = bound * adv;
-        term = -(ra < ba || ra != ra ? ra : ba);
-        coef = off ? 0.f : -ra;
-        if (p.ref != nullptr) {
-          const float gap = p.ref[t] - lp;
-          const float q = expm1f(gap);
-          kl = q - gap;
-          if (p.kl != 0.f) {
-            term += p.kl * kl;
-            coef -= p.kl * q;
-          }
-        }
-        term *= w;
-        kl *= w;
-        coef *= w;
-        cut = off ? w : 0.f;
-      }
-      if (tid == 0) {
-        a.p.terms[t] = term;
-        a.p.terms[a.T + t] = kl;
-        a.p.terms[2 * a.T + t] = cut;
-      }
-    }
-  } else {
-    if (live) {
-      coef = a.coef[t];
-      st = a.stats[t];
-    }
-  }
-  if (MODE == kStats || a.grad == nullptr) return;
-
-  // the gradient row; a zero coefficient (a row left out or cut off) needs no logits
-  const bool zero = !live || coef == 0.f;
-  const float up = coef * a.inv_temp, down = -up / st.S, m = st.m;
-  for (int64_t i = tid; i < sp.nvec; i += nthr) {
-    float d[N];
-    if (zero) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) d[k] = 0.f;
-    } else {
-      float f[N];
-      Vec<T>::unpack(xv[i], f);
-      const int64_t at = y - (sp.head + i * N);
-#pragma unroll
-      for (int k = 0; k < N; ++k) d[k] = fmaf(down, ex2((f[k] - m) * a.c), k == at ? up : 0.f);
-    }
-    T* to = g + sp.head + i * N;
-    if (a.same_phase) {
-      *(uint4*)to = Vec<T>::pack(d);
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k) to[k] = Vec<T>::put(d[k]);
-    }
-  }
-  if (scalar >= 0) {
-    const float d = zero ? 0.f : fmaf(down, ex2((Vec<T>::get(x[scalar]) - m) * a.c), scalar == y ? up : 0.f);
-    g[scalar] = Vec<T>::put(d);
-  }
-}
-
 // Fixed-order sum over one CTA of up to 1024 threads; every thread gets it.
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
@@ -356,6 +341,578 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+// Whether this CTA is the last of the grid to come here; what the others wrote before is then visible.
+__device__ __forceinline__ bool last_cta(unsigned* done) {
+  __shared__ int last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(done, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (last) __threadfence();
+  return last != 0;
+}
+
+// A row's gradient: d_v = down 2^(c (x_v - m)) + up [v = y].  16-bit gradients
+// take the factor |down| into the exponent, where its rounding (2^-14 at most)
+// is far below theirs.
+struct Slope {
+  float m, down, up, k, sign;
+  bool zero, fold;
+};
+template <class T>
+__device__ __forceinline__ Slope slope_of(bool live, float coef, Stat st, float inv_temp, Scale c) {
+  Slope d;
+  d.zero = !live || coef == 0.f;   // left out, cut off, in no sequence: the logits are not needed
+  d.m = st.m;
+  d.up = coef * inv_temp;
+  d.down = -d.up / st.S;
+  const float l = log2f(fabsf(d.down));
+  d.k = fmaf(-st.m, c.whole, l);
+  d.sign = d.down < 0.f ? -1.f : 1.f;
+  d.fold = sizeof(T) == 2 && is_near(st.m, c) && fabsf(l) < 1024.f;
+  return d;
+}
+// One element of it.
+template <class T>
+__device__ __forceinline__ float slope_at(T x, const Slope& s, Scale c, bool target) {
+  return fmaf(s.down, power(Vec<T>::get(x), s.m, c), target ? s.up : 0.f);
+}
+// K vectors of it, read `apart` and written `stride` vectors apart.
+template <class T, bool FOLD, bool ALIGNED, int K>
+__device__ __forceinline__ void write_vectors(const uint4* v, int apart, int stride, T* g, const Slope& s, Scale c) {
+  constexpr int N = Vec<T>::N, H = N / 2;
+  uint4 w[K];
+#pragma unroll
+  for (int q = 0; q < K; ++q) w[q] = v[q * apart];
+  const pair_t mul = FOLD ? pair_of(s.sign, s.sign) : pair_of(s.down, s.down);
+  const pair_t cc = pair_of(c.whole, c.whole), kk = pair_of(s.k, s.k);
+  // all products, then all exponentials, ...: enough of each under way to cover their latencies
+  pair_t d[K][H];
+#pragma unroll
+  for (int q = 0; q < K; ++q)
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const pair_t x = Vec<T>::pair(w[q], h);
+      d[q][h] = FOLD ? fma2(x, cc, kk) : exponent2(x, s.m, c);
+    }
+#pragma unroll
+  for (int q = 0; q < K; ++q)
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const float2 e = halves(d[q][h]);
+      d[q][h] = pair_of(ex2(e.x), ex2(e.y));
+    }
+#pragma unroll
+  for (int q = 0; q < K; ++q) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) d[q][h] = mul2(d[q][h], mul);
+    const uint4 r = Vec<T>::pack(d[q]);
+    if (ALIGNED) {
+      __stcs((uint4*)g + q * stride, r);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) g[(int64_t)q * stride * N + k] = ((const T*)&r)[k];
+    }
+  }
+}
+template <class T, bool FOLD, bool ALIGNED>
+__device__ __forceinline__ void write_run(const uint4* v, int apart, int n, int tid, int stride, T* g, const Slope& s,
+                                          Scale c) {
+  constexpr int N = Vec<T>::N, K = ALIGNED ? 4 : 1;
+  int i = tid;
+  for (; i + (K - 1) * stride < n; i += K * stride, v += K * apart)
+    write_vectors<T, FOLD, ALIGNED, K>(v, apart, stride, g + (int64_t)i * N, s, c);
+  if (K > 1)
+    for (; i < n; i += stride, v += apart)
+      write_vectors<T, FOLD, ALIGNED, 1>(v, apart, stride, g + (int64_t)i * N, s, c);
+}
+// n vectors of a gradient row from g on, by `stride` threads.  v: this thread's
+// first vector, its next ones `apart` further each.  `target`: the target's
+// place among the elements, or anything outside of them.
+template <class T>
+__device__ __forceinline__ void write_slope(const uint4* v, int n, int tid, int stride, T* g, const Slope& s, Scale c,
+                                            int64_t target, bool aligned, int apart) {
+  constexpr int N = Vec<T>::N;
+  if (s.zero) {
+    const uint4 w = make_uint4(0, 0, 0, 0);
+    if (aligned)
+      for (int i = tid; i < n; i += stride) __stcs((uint4*)g + i, w);
+    else
+      for (int64_t i = tid; i < (int64_t)n * N; i += stride) g[i] = Vec<T>::put(0.f);
+    return;
+  }
+  if (!aligned) write_run<T, false, false>(v, apart, n, tid, stride, g, s, c);
+  else if (sizeof(T) == 2 && s.fold) write_run<T, sizeof(T) == 2, true>(v, apart, n, tid, stride, g, s, c);
+  else write_run<T, false, true>(v, apart, n, tid, stride, g, s, c);
+  // the thread that wrote the target's vector puts its value right
+  if (target >= 0 && target < (int64_t)n * N) {
+    const int i = (int)(target / N);
+    if (i % stride == tid) {
+      const T* e = (const T*)(v + (int64_t)(i / stride) * apart);
+      g[target] = Vec<T>::put(slope_at(e[target % N], s, c, true));
+    }
+  }
+}
+
+enum { kStats = 0, kPolicy = 1 };
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// What a row's single values make of its statistics.
+struct RowOut {
+  float lp, term, kl, cut, coef;
+};
+template <int MODE, class W>
+__device__ __forceinline__ RowOut row_out(const Rows& a, bool live, float xy, float adv, float old, float ref, W weight,
+                                          Stat& st) {
+  RowOut o{0.f, 0.f, 0.f, 0.f, 0.f};
+  if (!live) return o;
+  if (st.m == INFINITY) st.m = NAN;   // no distribution
+  const float over = above(st.m, a.c);
+  o.lp = (xy - st.m) * a.inv_temp - (logf(st.S) + kLn2 * over);
+  st.S *= ex2(over);   // from here on against the maximum itself, as the gradient takes it
+  if (MODE == kPolicy) {
+    const Policy& p = a.p;
+    const float ratio = expf(o.lp - old);
+    const float bound = fminf(fmaxf(ratio, p.lo), p.hi);
+    const bool off = (adv > 0.f && ratio > p.hi) || (adv < 0.f && ratio < p.lo);
+    const float ra = ratio * adv, ba = bound * adv;
+    o.term = -(ra < ba || ra != ra ? ra : ba);
+    o.coef = off ? 0.f : -ra;
+    if (p.ref != nullptr) {
+      const float gap = ref - o.lp;
+      const float q = expm1f(gap);
+      o.kl = q - gap;
+      if (p.kl != 0.f) {
+        o.term += p.kl * o.kl;
+        o.coef -= p.kl * q;
+      }
+    }
+    const float w = weight();
+    o.term *= w;
+    o.kl *= w;
+    o.coef *= w;
+    o.cut = off ? w : 0.f;
+  }
+  return o;
+}
+template <int MODE>
+__device__ __forceinline__ void write_row(const Rows& a, int64_t t, const RowOut& o, const Stat& st) {
+  a.logps[t] = o.lp;
+  if (MODE == kStats && a.stats != nullptr) {
+    a.stats[t] = st;
+    a.coef[t] = 0.f;
+    if (t == 0) *a.done = 0;
+  }
+  if (MODE == kPolicy) {
+    a.p.terms[t] = o.term;
+    a.p.terms[a.T + t] = o.kl;
+    a.p.terms[2 * a.T + t] = o.cut;
+  }
+}
+
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int left>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(left) : "memory"); }
+
+// Log-probabilities, and for the policy loss everything of a row: one warp per
+// row (WARP), or one CTA or cluster of CTAs, each with one run of its vectors.
+// A thread's vectors come through slots of its own in shared memory, DEPTH
+// groups of four ahead, so that the loads under way take no registers.  For a
+// policy row's gradient (KEEP) all groups stay there, and the row is read once.
+template <class T, bool WARP, int MODE, int DEPTH, bool KEEP>
+__global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Rows a) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ uint4 slots[];
+  __shared__ Stat red[16], peers[8];
+  __shared__ Slope shared_slope;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (MODE == kStats) asm volatile("griddepcontrol.launch_dependents;");
+  unsigned csize = 1, rank = 0;
+  if (!WARP) {
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    if (csize > 1) cluster_arrive();   // waited for before a peer's shared memory is written
+  }
+  const int64_t t = WARP ? (int64_t)blockIdx.x * (blockDim.x / 32) + warp : blockIdx.x / csize;
+  if (WARP && t >= a.T) return;
+  const int tid = WARP ? lane : threadIdx.x, nthr = WARP ? 32 : blockDim.x;
+
+  const int64_t y = a.y[t];
+  const bool live = y >= 0;
+  const T* x = (const T*)a.x + t * a.ld;
+  const Span sp = span_of(x, a.V);
+  // this CTA's vectors: [0, n) from xv, the first of them vector v0 of the row
+  const int64_t v0 = min(sp.nvec, rank * a.each);
+  const int n = (int)min(a.each, sp.nvec - v0);
+  const uint4* xv = (const uint4*)(x + sp.head) + v0;
+  // the elements before and after the vectors: at most one per thread of the first CTA
+  const int64_t scalar = rank != 0 ? -1 : tid < sp.head ? tid
+                         : tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1;
+  // slot i of a thread is slots[i blockDim + thread]
+  const uint4* mine = slots + threadIdx.x;
+  // the row's single values, under way with the vectors; a target past the
+  // last column has no log-probability: NaN, so that the mistake shows
+  float xy = NAN, adv = 0.f, old = 0.f, ref = 0.f;
+  T xs = Vec<T>::put(0.f);
+  Stat st{-INFINITY, 0.f};
+  if (live) {
+    int ahead = tid;   // next vector to be loaded
+    auto load = [&](int slot) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q, ahead += nthr)
+        if (ahead < n) copy_async(tc::smem_u32(mine + (slot * 4 + q) * blockDim.x), xv + ahead);
+      copy_commit();
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(d);
+    if (scalar >= 0) xs = x[scalar];
+    if (y < a.V) xy = Vec<T>::get(x[y]);
+    if (MODE == kPolicy) {
+      adv = a.p.adv[t];
+      old = a.p.old[t];
+      if (a.p.ref != nullptr) ref = a.p.ref[t];
+    }
+    Running<T> run;
+    int d = 0;
+    for (int i = tid; i < n; i += 4 * nthr) {
+      copy_wait<DEPTH - 1>();
+      if (i + 3 * nthr < n)
+        run.add([&](int q) { return mine[(d * 4 + q) * blockDim.x]; }, a.c);
+      else   // -inf past the end of the run
+        run.add([&](int q) { return i + q * nthr < n ? mine[(d * 4 + q) * blockDim.x] : Vec<T>::none(); }, a.c);
+      if (KEEP) {
+        copy_commit();
+        ++d;
+      } else {
+        load(d);
+        if (++d == DEPTH) d = 0;
+      }
+    }
+    if (scalar >= 0) run.add(Vec<T>::get(xs), a.c);
+    st = merge_lanes<32>(run.s, a.c);
+  }
+  auto weight = [&] {   // the weights are the previous kernel's
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return a.p.weight[t];
+  };
+  Slope d;
+  if constexpr (WARP) {
+    const RowOut o = row_out<MODE>(a, live, xy, adv, old, ref, weight, st);
+    if (lane == 0) write_row<MODE>(a, t, o, st);
+    if (MODE == kStats || a.grad == nullptr) return;
+    d = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
+  } else {
+    if (lane == 0) red[warp] = st;
+    __syncthreads();
+    if (warp == 0) st = merge_lanes<16>(lane < (int)(blockDim.x / 32) ? red[lane] : Stat{-INFINITY, 0.f}, a.c);
+    if (csize > 1) {   // every CTA writes its pair to all of them
+      cluster_wait();
+      if (threadIdx.x < csize) {
+        uint32_t to;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;"
+            : "=r"(to)
+            : "r"((uint32_t)__cvta_generic_to_shared(peers + rank)), "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(st.m), "f"(st.S) : "memory");
+      }
+      __syncwarp();
+      cluster_arrive();
+      cluster_wait();
+      if (warp == 0) st = merge_lanes<8>(lane < (int)csize ? peers[lane] : Stat{-INFINITY, 0.f}, a.c);
+    }
+    if (warp == 0) {
+      const RowOut o = row_out<MODE>(a, live, xy, adv, old, ref, weight, st);
+      if (threadIdx.x == 0) {
+        if (rank == 0) write_row<MODE>(a, t, o, st);
+        if (MODE == kPolicy) shared_slope = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
+      }
+    }
+    if (MODE == kStats || a.grad == nullptr) return;
+    __syncthreads();
+    d = shared_slope;
+  }
+  T* g = (T*)a.grad + t * a.gld;
+  const int64_t target = y - sp.head - v0 * N;
+  if (KEEP)   // (a thread writes the vectors that it holds)
+    write_slope<T>(mine, n, tid, nthr, g + sp.head + v0 * N, d, a.c, target, a.same_phase, blockDim.x);
+  else
+    write_slope<T>(xv + tid, n, tid, nthr, g + sp.head + v0 * N, d, a.c, target, a.same_phase, nthr);
+  if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(xs, d, a.c, scalar == y));
+  if (MODE == kPolicy) asm volatile("griddepcontrol.wait;" ::: "memory");   // rows left out have not waited
+}
+
+// The policy loss with its gradient for batches that fill the GPU: one
+// persistent CTA per SM (each cluster takes every so many rows), whose warps
+// share the work of a row so that no part of it waits for another row's:
+//   producer   (1 warp)  keeps the next vectors coming into a ring of
+//                        shared-memory slots by bulk copies
+//   summing    (8 warps) the row's maximum and sum
+//   scalar     (1 warp)  merges the warps' and the cluster's pairs, takes the
+//                        row's terms and its slope
+//   writing    (8 warps) the gradient from the slots, which it then frees
+// The ring has to hold a CTA's whole run of a row.
+constexpr int kSlotVec = 1024, kSlots = 13;          // 16 KB each
+constexpr int kGroup = 256, kGroupWarps = kGroup / 32;
+constexpr int kScalarWarp = 2 * kGroupWarps, kProducerWarp = kScalarWarp + 1;
+constexpr int kStreamThreads = (kProducerWarp + 1) * 32;
+constexpr int kSlopes = 4;                           // rows between the scalar and the writing warps
+constexpr size_t kRingBytes = (size_t)kSlots * kSlotVec * 16;
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// Bounded wait (2 s); false once any wait of this CTA has run out.
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = tc::globaltimer_ns();
+  while (!tc::mbar_try_wait(bar, parity)) {
+    if (*stop) return false;
+    if (tc::globaltimer_ns() - t0 > tc::kTimeoutNs) {
+      *stop = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const __grid_constant__ Rows a) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ __align__(128) uint4 ring[];
+  __shared__ __align__(8) uint64_t bars[2 * kSlots + 4 + 2 * kSlopes + 2];
+  __shared__ Stat red[2][kGroupWarps], peers[2][8];
+  __shared__ Slope slopes[kSlopes];
+  __shared__ int stop_flag;
+  volatile int* stop = &stop_flag;
+  const uint32_t b_full = tc::smem_u32(bars), b_empty = b_full + 8 * kSlots;   // slots
+  const uint32_t b_sum = b_empty + 8 * kSlots, b_sumfree = b_sum + 16;         // pairs of the summing warps
+  const uint32_t b_slope = b_sumfree + 16, b_slopefree = b_slope + 8 * kSlopes;
+  const uint32_t b_peers = b_slopefree + 8 * kSlopes;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned csize, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      tc::mbar_init(b_full + 8 * i, 1);
+      tc::mbar_init(b_empty + 8 * i, kGroupWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(b_sum + 8 * i, kGroupWarps);
+      tc::mbar_init(b_sumfree + 8 * i, 1);
+      tc::mbar_init(b_peers + 8 * i, 1);
+    }
+    for (int i = 0; i < kSlopes; ++i) {
+      tc::mbar_init(b_slope + 8 * i, 1);
+      tc::mbar_init(b_slopefree + 8 * i, kGroupWarps);
+    }
+    stop_flag = 0;
+    tc::fence_mbar_init();
+  }
+  __syncthreads();
+  if (csize > 1) {   // a peer's barriers exist before anything is sent to them
+    cluster_arrive();
+    cluster_wait();
+  }
+  const int64_t t0 = blockIdx.x / csize, step = gridDim.x / csize;
+  int slot = 0;
+  uint32_t phase = 0;          // of the slot's next use
+  uint32_t k = 0;              // live rows so far
+  int64_t next = t0 < a.T ? a.y[t0] : -1;
+  auto advance = [&] {
+    if (++slot == kSlots) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  };
+  const bool sums = warp < kGroupWarps, writes = warp >= kGroupWarps && warp < 2 * kGroupWarps;
+  int64_t issued = 0;
+  if (warp == kScalarWarp) asm volatile("griddepcontrol.wait;" ::: "memory");   // the weights are the previous kernel's
+  for (int64_t t = t0; t < a.T; t += step) {
+    const int64_t y = next;
+    if (t + step < a.T) next = a.y[t + step];
+    const bool live = y >= 0;
+    const T* x = (const T*)a.x + t * a.ld;
+    const Span sp = span_of(x, a.V);
+    // this CTA's run of the row, and the elements outside of the vectors (the first CTA's)
+    const int64_t v0 = min(sp.nvec, rank * a.each);
+    const int n = (int)min(a.each, sp.nvec - v0);
+    const uint4* xv = (const uint4*)(x + sp.head) + v0;
+    const int tid = threadIdx.x & (kGroup - 1);
+    const int64_t scalar = rank != 0 ? -1 : tid < sp.head ? tid
+                           : tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1;
+    bool ok = true;
+    if (sums) {
+      if (!live) continue;
+      Running<T> run;
+      const float xs = scalar >= 0 ? Vec<T>::get(x[scalar]) : -INFINITY;
+      for (int c = 0; c < n; c += kSlotVec) {
+        if (!(ok = ring_wait(b_full + 8 * slot, phase, stop))) break;
+        const uint4* v = ring + slot * kSlotVec + tid;
+        const int left = n - c - tid;
+        if (n - c >= kSlotVec) run.add([&](int q) { return v[q * kGroup]; }, a.c);
+        else run.add([&](int q) { return left > q * kGroup ? v[q * kGroup] : Vec<T>::none(); }, a.c);   // -inf past its end
+        advance();
+      }
+      if (scalar >= 0) run.add(xs, a.c);
+      const Stat st = merge_lanes<32>(run.s, a.c);
+      ok = ok && ring_wait(b_sumfree + 8 * (k & 1), ((k >> 1) & 1u) ^ 1u, stop);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (lane == 0) {
+        red[k & 1][warp] = st;
+        tc::mbar_arrive(b_sum + 8 * (k & 1));
+      }
+    } else if (writes) {
+      T* g = (T*)a.grad + t * a.gld;
+      Slope d{};
+      d.zero = true;
+      T xs = Vec<T>::put(0.f);
+      if (live) {
+        if (scalar >= 0) xs = x[scalar];
+        ok = ring_wait(b_slope + 8 * (k % kSlopes), (k / kSlopes) & 1u, stop);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        d = slopes[k % kSlopes];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(b_slopefree + 8 * (k % kSlopes));
+        for (int c = 0; c < n; c += kSlotVec) {
+          if (!(ok = ring_wait(b_full + 8 * slot, phase, stop))) break;
+          const int64_t col = sp.head + (v0 + c) * N;
+          write_slope<T>(ring + slot * kSlotVec + tid, min(kSlotVec, n - c), tid, kGroup, g + col, d, a.c, y - col,
+                         a.same_phase, kGroup);
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(b_empty + 8 * slot);
+          advance();
+        }
+        if (!__all_sync(0xffffffffu, ok)) break;
+      } else {
+        write_slope<T>(nullptr, n, tid, kGroup, g + sp.head + v0 * N, d, a.c, -1, a.same_phase, kGroup);
+      }
+      if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(xs, d, a.c, scalar == y));
+    } else if (warp == kScalarWarp) {
+      float xy = NAN, adv = 0.f, old = 0.f, ref = 0.f, w = 0.f;
+      Stat st{0.f, 1.f};
+      if (live) {
+        if (y < a.V) xy = Vec<T>::get(x[y]);
+        adv = a.p.adv[t];
+        old = a.p.old[t];
+        w = a.p.weight[t];
+        if (a.p.ref != nullptr) ref = a.p.ref[t];
+        ok = ring_wait(b_sum + 8 * (k & 1), (k >> 1) & 1u, stop);
+        st = merge_lanes<8>(lane < kGroupWarps ? red[k & 1][lane] : Stat{-INFINITY, 0.f}, a.c);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(b_sumfree + 8 * (k & 1));
+        if (!ok) st.m = st.S = NAN;   // a wait ran out: no result
+        if (csize > 1) {              // every CTA sends its pair to all of them
+          const uint32_t bar = b_peers + 8 * (k & 1);
+          if (lane == 0) tc::mbar_expect_tx(bar, csize * (uint32_t)sizeof(Stat));
+          __syncwarp();
+          st.m = __shfl_sync(0xffffffffu, st.m, 0);
+          st.S = __shfl_sync(0xffffffffu, st.S, 0);
+          if (lane < (int)csize) {
+            uint32_t to, tobar;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(tc::smem_u32(&peers[k & 1][rank])), "r"(lane));
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(tobar) : "r"(bar), "r"(lane));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to),
+                         "f"(st.m), "f"(st.S), "r"(tobar)
+                         : "memory");
+          }
+          ok = ring_wait(bar, (k >> 1) & 1u, stop) && ok;
+          st = merge_lanes<8>(lane < (int)csize ? peers[k & 1][lane] : Stat{-INFINITY, 0.f}, a.c);
+          if (!ok) st.m = st.S = NAN;
+        }
+        if (lane < kGroupWarps) ok = ok && ring_wait(b_slopefree + 8 * (k % kSlopes), ((k / kSlopes) & 1u) ^ 1u, stop);
+        ok = __all_sync(0xffffffffu, ok);
+      }
+      const RowOut o = row_out<kPolicy>(a, live, xy, adv, old, ref, [&] { return w; }, st);
+      if (lane == 0) {
+        if (rank == 0) write_row<kPolicy>(a, t, o, st);
+        if (live) {
+          slopes[k % kSlopes] = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
+          tc::mbar_arrive(b_slope + 8 * (k % kSlopes));
+        }
+      }
+      __syncwarp();
+    } else if (lane == 0) {
+      if (!live) continue;
+      for (int c = 0; c < n; c += kSlotVec) {
+        if (!(ok = ring_wait(b_empty + 8 * slot, phase ^ 1u, stop))) break;
+        const uint32_t bytes = min(kSlotVec, n - c) * 16u;
+        tc::mbar_expect_tx(b_full + 8 * slot, bytes);
+        bulk_load(tc::smem_u32(ring + slot * kSlotVec), xv + c, bytes, b_full + 8 * slot);
+        ++issued;
+        advance();
+      }
+      if (!ok) break;
+    } else {
+      break;   // the producer warp's other lanes
+    }
+    if (live) ++k;
+  }
+  if (warp == kProducerWarp && lane == 0 && *stop)   // the copies in flight end before shared memory goes away
+    for (int64_t q = issued > kSlots ? issued - kSlots : 0; q < issued; ++q) {
+      const uint64_t from = tc::globaltimer_ns();
+      while (!tc::mbar_try_wait(b_full + 8 * (int)(q % kSlots), (uint32_t)((q / kSlots) & 1)) &&
+             tc::globaltimer_ns() - from < 100000000ull) {
+      }
+    }
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // rows left out have not waited
+  __syncwarp();
+  if (csize > 1) {   // no CTA's shared memory goes away while a peer may write to it
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+// The sums of the policy rows' terms, in their order.
+__global__ void __launch_bounds__(1024) terms_kernel(const float* terms, int64_t T, float* stats) {
+  __shared__ double red[32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const float* v = terms + blockIdx.x * T;
+  double s = 0.0;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < T; i += blockDim.x) s += (double)v[i];
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) stats[blockIdx.x] = (float)s;
+}
+
+// The gradient rows from the statistics and coefficients of earlier kernels:
+// one warp per row, or `pieces` CTAs per row of 4 vectors per thread.  The rows
+// are taken from the last to the first: the statistics pass read those last,
+// and part of them is still in L2.
+template <class T, bool WARP>
+__global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ Rows a, unsigned pieces) {
+  constexpr int N = Vec<T>::N, K = 4;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int64_t rows = WARP ? 8 : 1;
+  const int64_t t = a.T - 1 - (WARP ? (int64_t)blockIdx.x * rows + (threadIdx.x >> 5) : blockIdx.x / pieces);
+  if (t < 0) return;
+  const int64_t y = a.y[t];
+  const float coef = y >= 0 ? a.coef[t] : 0.f;
+  const Stat st = a.stats[t];
+  const T* x = (const T*)a.x + t * a.ld;
+  T* g = (T*)a.grad + t * a.gld;
+  const Span sp = span_of(x, a.V);
+  const uint4* xv = (const uint4*)(x + sp.head);
+  const Slope d = slope_of<T>(y >= 0, coef, st, a.inv_temp, a.c);
+  const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, nthr = WARP ? 32 : blockDim.x;
+  const unsigned piece = WARP ? 0 : blockIdx.x % pieces;
+  const int64_t first = (int64_t)piece * K * nthr;
+  const int n = (int)(WARP ? sp.nvec : min((int64_t)K * nthr, sp.nvec - first));
+  const int64_t col = sp.head + first * N;
+  write_slope<T>(xv + first + tid, n, tid, nthr, g + col, d, a.c, y - col, a.same_phase, nthr);
+  if (piece == 0) {
+    const int64_t scalar = tid < sp.head ? tid
+                           : tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1;
+    if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(x[scalar], d, a.c, scalar == y));
+  }
+}
+
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -372,54 +929,52 @@ __device__ __forceinline__ int64_t border(const int64_t* offsets, int64_t k, int
 __global__ void __launch_bounds__(256)
     pair_kernel(const int64_t* y, const float* logps, const float* ref, const int64_t* offsets, int64_t T, int64_t P,
                 double beta, double smoothing, int average, float* ratios, float* margins, double* pair_loss,
-                float* coef) {
-  const int64_t p = (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (p >= P) return;
-  double ratio[2], share[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
-    double sum = 0.0, count = 0.0;
-    for (int64_t t = a + lane; t < b; t += 32)
-      if (y[t] >= 0) {
-        sum += (double)logps[t] - (double)ref[t];
-        count += 1.0;
-      }
-    sum = warp_sum(sum);
-    count = warp_sum(count);
-    share[k] = average && count > 1.0 ? 1.0 / count : 1.0;
-    ratio[k] = sum * share[k];
-  }
-  const double h = beta * (ratio[0] - ratio[1]);
-  // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|)
-  const double l = log1p(exp(-fabs(h)));
-  const double down = fmax(-h, 0.0) + l, up = fmax(h, 0.0) + l;
-  if (lane == 0) {
-    ratios[2 * p] = (float)ratio[0];
-    ratios[2 * p + 1] = (float)ratio[1];
-    margins[p] = (float)h;
-    pair_loss[p] = smoothing > 0.0 ? (1.0 - smoothing) * down + smoothing * up : down;   // no 0 x inf
-  }
-  if (coef == nullptr) return;
-  const double slope = beta * (smoothing - 1.0 / (1.0 + exp(h))) / (double)P;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
-    const float g = (float)((k ? -slope : slope) * share[k]);
-    for (int64_t t = a + lane; t < b; t += 32) coef[t] = y[t] >= 0 ? g : 0.f;
-  }
-}
-
-// out[k] = scale sum_i v[k n + i], k < gridDim.x
-template <class T>
-__global__ void __launch_bounds__(1024) sum_kernel(const T* v, int64_t n, double scale, float* out) {
+                float* coef, unsigned* done, float* loss) {
   __shared__ double red[32];
-  v += (int64_t)blockIdx.x * n;
+  const int lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int64_t p = (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5); p < P;
+       p += (int64_t)gridDim.x * (blockDim.x / 32)) {
+    double ratio[2], share[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
+      double sum = 0.0, count = 0.0;
+      for (int64_t t = a + lane; t < b; t += 32)
+        if (y[t] >= 0) {
+          sum += (double)logps[t] - (double)ref[t];
+          count += 1.0;
+        }
+      sum = warp_sum(sum);
+      count = warp_sum(count);
+      share[k] = average && count > 1.0 ? 1.0 / count : 1.0;
+      ratio[k] = sum * share[k];
+    }
+    const double h = beta * (ratio[0] - ratio[1]);
+    // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|)
+    const double l = log1p(exp(-fabs(h)));
+    const double down = fmax(-h, 0.0) + l, up = fmax(h, 0.0) + l;
+    if (lane == 0) {
+      ratios[2 * p] = (float)ratio[0];
+      ratios[2 * p + 1] = (float)ratio[1];
+      margins[p] = (float)h;
+      pair_loss[p] = smoothing > 0.0 ? (1.0 - smoothing) * down + smoothing * up : down;   // no 0 x inf
+    }
+    if (coef == nullptr) continue;
+    const double gain = beta * (smoothing - 1.0 / (1.0 + exp(h))) / (double)P;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
+      const float g = (float)((k ? -gain : gain) * share[k]);
+      for (int64_t t = a + lane; t < b; t += 32) coef[t] = y[t] >= 0 ? g : 0.f;
+    }
+  }
+  if (!last_cta(done)) return;
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += (double)v[i];
+  for (int64_t i = threadIdx.x; i < P; i += blockDim.x) s += __ldcg(pair_loss + i);
   s = block_sum(s, red);
-  if (threadIdx.x == 0) out[blockIdx.x] = (float)(s * scale);
+  if (threadIdx.x == 0) *loss = (float)(s / (double)P);
 }
 
 // Each row's share of the policy loss: 1 / (live rows), or 1 / (sequences x
@@ -427,10 +982,13 @@ __global__ void __launch_bounds__(1024) sum_kernel(const T* v, int64_t n, double
 __global__ void __launch_bounds__(1024)
     weight_kernel(const int64_t* y, const int64_t* offsets, int64_t T, int64_t S, float* weight) {
   __shared__ double red[32];
+  // the rows' statistics do not need the weights, and the logits are older than this kernel
+  asm volatile("griddepcontrol.launch_dependents;");
   if (offsets == nullptr) {
-    double n = 0.0;
-    for (int64_t t = threadIdx.x; t < T; t += blockDim.x) n += y[t] >= 0 ? 1.0 : 0.0;
-    n = block_sum(n, red);
+    int64_t count = 0;
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < T; t += blockDim.x) count += y[t] >= 0;
+    const double n = block_sum((double)count, red);
     const float w = (float)(1.0 / fmax(n, 1.0));
     for (int64_t t = threadIdx.x; t < T; t += blockDim.x) weight[t] = w;
     return;
@@ -462,32 +1020,140 @@ int num_sms() {
   });
 }
 
+// Launches `kernel`; with `overlap` it may start before the kernel ahead of it
+// in the stream has finished (it waits for that one itself, where it needs it).
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, size_t smem, unsigned cluster, bool overlap,
+                   cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2]{};
+  int n = 0;
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (overlap) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+constexpr int kMaxKeep = 220 * 1024;   // shared memory of a run that is kept
+
+// The same with up to kMaxKeep of dynamic shared memory.
+template <class... P, class... A>
+cudaError_t launch_row(void (*kernel)(P...), size_t smem, int64_t grid, int block, unsigned cluster, bool overlap,
+                       cudaStream_t s, const A&... args) {
+  if (smem > 40 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxKeep);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(kernel, grid, block, smem, cluster, overlap, s, args...);
+}
+
+// The statistics pass, or a policy batch without its gradient.
 template <class T, int MODE>
-nmd_status launch_rows_t(const Rows& a, cudaStream_t s) {
-  if (a.T == 0) return NMD_OK;
+cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
+  constexpr bool late = MODE == kPolicy;   // the weights' kernel is ahead of it
+  // A warp per row of up to 8192 16-bit columns where there are rows enough (at
+  // V = 4096: 61 us against 113 us for 48,828 rows by CTAs of 128 threads).
+  if (nvec <= 256 || (nvec <= 1024 && a.T >= 16 * sms))
+    return launch_row(row_kernel<T, true, MODE, 2, false>, 32 * 1024, (a.T + 7) / 8, 256, 1, late, s, a);
+  // A CTA per row, and clusters of up to eight where there are too few to fill the SMs
+  int64_t cs = 1;
+  while (cs < 8 && a.T * cs < 2 * sms && nvec >= cs * 2 * 256) cs *= 2;
+  int block = 128;
+  if (a.T * cs < 2 * sms) {
+    block = 512;
+    while (block > 64 && (nvec + cs - 1) / cs < block) block /= 2;
+  }
+  a.each = (nvec + cs - 1) / cs;
+  return launch_row(row_kernel<T, false, MODE, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, late, s, a);
+}
+
+// A policy batch with its gradient.
+template <class T>
+cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
+  // a warp per row of up to 4096 16-bit columns (V = 4096, 48,828 rows: 195 us against 234 us by CTAs)
+  if (nvec <= 256 || (nvec <= 513 && a.T >= 16 * sms)) {
+    const int groups = (int)((nvec + 127) / 128);
+    if (groups <= 2)
+      return launch_row(row_kernel<T, true, kPolicy, 2, true>, groups * 16384, (a.T + 7) / 8, 256, 1, true, s, a);
+    return launch_row(row_kernel<T, true, kPolicy, 8, true>, groups * 16384, (a.T + 7) / 8, 256, 1, true, s, a);
+  }
+  // Long rows in batches that fill the GPU: the streaming kernel, its clusters'
+  // runs at most nine of the ring's thirteen slots (V = 32768, 6103 rows: 158 us
+  // against 161 us by clusters of row_kernel; V = 139255: 163 us against 171 us;
+  // V = 16384: 198 us against 153 us).
+  const int64_t slots = (nvec + kSlotVec - 1) / kSlotVec;
+  int64_t cs = std::min<int64_t>(8, (slots + 8) / 9);
+  if (nvec > 3072 && a.T * cs >= 4 * sms && slots <= cs * kSlots) {
+    static std::atomic<int> ready[kMaxDevices], room[9][kMaxDevices];
+    if (!per_device(ready, [] {
+          return cudaFuncSetAttribute(policy_stream_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      (int)kRingBytes) == cudaSuccess ? 1 : 0;
+        }))
+      return cudaErrorInvalidValue;
+    // as many clusters as run at the same time
+    const int clusters = per_device(room[cs], [&] {
+      cudaLaunchConfig_t cfg{};
+      cudaLaunchAttribute at{};
+      at.id = cudaLaunchAttributeClusterDimension;
+      at.val.clusterDim.x = (unsigned)cs;
+      at.val.clusterDim.y = at.val.clusterDim.z = 1;
+      cfg.gridDim = dim3((unsigned)(sms / cs * cs));
+      cfg.blockDim = dim3(kStreamThreads);
+      cfg.dynamicSmemBytes = kRingBytes;
+      cfg.attrs = &at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      return cudaOccupancyMaxActiveClusters(&n, policy_stream_kernel<T>, &cfg) == cudaSuccess ? n : 0;
+    });
+    if (clusters == 0) return cudaErrorInvalidValue;
+    a.each = (nvec + cs - 1) / cs;
+    return launch(policy_stream_kernel<T>, std::min<int64_t>(a.T, clusters) * cs, kStreamThreads, kRingBytes,
+                  (unsigned)cs, true, s, a);
+  }
+  // A CTA per row, or a cluster with runs of 32 KB, or where the rows are too few to fill the SMs
+  cs = nvec * 16 <= 48 * 1024 ? 1 : std::min<int64_t>(8, (nvec * 16 + 32767) / 32768);
+  int block = 128;
+  while (cs < 8 && a.T * cs < 2 * sms && nvec >= cs * 2 * 256) cs = std::min<int64_t>(8, cs * 2);
+  if (a.T * cs < 2 * sms) {
+    block = 512;
+    while (block > 64 && (nvec + cs - 1) / cs < block) block /= 2;
+  }
+  a.each = (nvec + cs - 1) / cs;
+  while (block < 512 && a.each > 32 * block) block *= 2;   // up to eight groups per thread are kept
+  const int64_t groups = (a.each + 4 * block - 1) / (4 * block);
+  const size_t smem = (size_t)block * 64 * groups;
+  if (groups <= 2)
+    return launch_row(row_kernel<T, false, kPolicy, 2, true>, smem, a.T * cs, block, (unsigned)cs, true, s, a);
+  if (groups <= 8 && smem <= kMaxKeep)
+    return launch_row(row_kernel<T, false, kPolicy, 8, true>, smem, a.T * cs, block, (unsigned)cs, true, s, a);
+  // too long to be kept: read again
+  return launch_row(row_kernel<T, false, kPolicy, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, true,
+                    s, a);
+}
+
+template <class T, int MODE>
+nmd_status launch_rows_t(Rows a, cudaStream_t s) {
   const int sms = num_sms();
   if (sms == 0) return NMD_ERR_CUDA;
+  const int64_t nvec = a.V / Vec<T>::N + 1;
+  a.each = nvec;
   cudaError_t e;
-  if (a.V <= 1024) {   // a warp per row
-    row_kernel<T, 32, MODE><<<(unsigned)((a.T + 7) / 8), 256, 0, s>>>(a);
-    e = cudaGetLastError();
-  } else {
-    // a CTA per row, or a cluster where there are too few rows to fill the
-    // SMs and each CTA still gets two vectors per thread
-    unsigned cs = 1;
-    while (cs < 8 && a.T * cs < 2 * sms && a.V >= (int64_t)cs * 4 * 512 * Vec<T>::N) cs *= 2;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(a.T * cs));
-    cfg.blockDim = dim3(512);
-    cfg.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = cs;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, row_kernel<T, 0, MODE>, a);
-  }
+  if constexpr (MODE == kPolicy) e = a.grad ? launch_policy<T>(a, nvec, sms, s) : launch_sums<T, MODE>(a, nvec, sms, s);
+  else e = launch_sums<T, MODE>(a, nvec, sms, s);
   return e == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
@@ -496,9 +1162,29 @@ nmd_status launch_rows(int dtype, const Rows& a, cudaStream_t s) {
   switch (dtype) {
     case NMD_DT_FP32: return launch_rows_t<float, MODE>(a, s);
     case NMD_DT_BF16: return launch_rows_t<bf16, MODE>(a, s);
-    case NMD_DT_FP16: return launch_rows_t<__half, MODE>(a, s);
+    default: return launch_rows_t<__half, MODE>(a, s);
   }
-  return NMD_ERR_INVALID;
+}
+
+template <class T>
+nmd_status launch_grad_t(const Rows& a, cudaStream_t s) {
+  const int64_t nvec = a.V / Vec<T>::N;
+  cudaError_t e;
+  if (nvec <= 256) {
+    e = launch(grad_kernel<T, true>, (a.T + 7) / 8, 256, 0, 1, true, s, a, 1u);
+  } else {
+    const int64_t pieces = (nvec + 4 * 256 - 1) / (4 * 256);
+    e = launch(grad_kernel<T, false>, a.T * pieces, 256, 0, 1, true, s, a, (unsigned)pieces);
+  }
+  return e == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+}
+
+nmd_status launch_grad(int dtype, const Rows& a, cudaStream_t s) {
+  switch (dtype) {
+    case NMD_DT_FP32: return launch_grad_t<float>(a, s);
+    case NMD_DT_BF16: return launch_grad_t<bf16>(a, s);
+    default: return launch_grad_t<__half>(a, s);
+  }
 }
 
 int dtype_bytes(int dtype) { return dtype == NMD_DT_FP32 ? 4 : 2; }
@@ -511,8 +1197,14 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
   if (dtype < NMD_DT_FP32 || dtype > NMD_DT_FP16 || T < 0 || T > kMaxRows || V < 1 || V >= (int64_t(1) << 31) ||
       ld < 0 || !(temperature > 0.0) || !std::isfinite(temperature))
     return NMD_ERR_INVALID;
-  const float c = (float)(kLog2e / temperature), it = (float)(1.0 / temperature);
-  if (!(c > 0.f) || !std::isfinite(c) || !std::isfinite(it)) return NMD_ERR_INVALID;
+  const double c = kLog2e / temperature;
+  const float whole = (float)c, it = (float)(1.0 / temperature);
+  if (!(whole >= 1e-30f) || !(whole <= 1e30f)) return NMD_ERR_INVALID;
+  int e = 0;
+  const double f = std::frexp(c, &e);   // in [1/2, 1)
+  double head = std::floor(f * 4096.0);
+  if (head == f * 4096.0) head -= 1.0;   // hi is below c, so that lo > 0
+  const float hi = (float)std::ldexp(head, e - 12);
   if (T > 0 && (!x || !y || !logps)) return NMD_ERR_INVALID;
   const int es = dtype_bytes(dtype);
   if (((uintptr_t)x | (uintptr_t)grad) & (uintptr_t)(es - 1)) return NMD_ERR_INVALID;
@@ -522,7 +1214,7 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
   a->V = V;
   a->ld = ld;
   a->y = y;
-  a->c = c;
+  a->c = Scale{hi, (float)(c - (double)hi), whole};
   a->inv_temp = it;
   a->logps = logps;
   if (grad) {
@@ -552,13 +1244,14 @@ nmd_status nmd_token_logprobs(const void* d_logits, int32_t dtype, int64_t T, in
                               const int64_t* d_targets, double temperature, float* d_logps, void* stream) {
   Rows a;
   const nmd_status st = fill(d_logits, dtype, T, V, ld, d_targets, temperature, d_logps, nullptr, 0, &a);
-  if (st != NMD_OK) return st;
+  if (st != NMD_OK || T == 0) return st;
   return launch_rows<kStats>(dtype, a, (cudaStream_t)stream);
 }
 
 nmd_status nmd_preference_workspace_bytes(int64_t T, int64_t P, size_t* bytes) {
   if (T < 0 || T > kMaxRows || P < 1 || P > kMaxRows || !bytes) return NMD_ERR_INVALID;
-  *bytes = align256((size_t)T * sizeof(Stat)) + align256((size_t)T * sizeof(float)) + align256((size_t)P * sizeof(double));
+  *bytes = align256((size_t)T * sizeof(Stat)) + align256((size_t)T * sizeof(float)) + align256((size_t)P * sizeof(double)) +
+           256;
   return NMD_OK;
 }
 
@@ -579,20 +1272,27 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
   cudaStream_t s = (cudaStream_t)stream;
   char* w = (char*)d_workspace;
   a.stats = (Stat*)w;
-  a.coef = (float*)(w + align256((size_t)T * sizeof(Stat)));
-  double* pair_loss = (double*)(w + align256((size_t)T * sizeof(Stat)) + align256((size_t)T * sizeof(float)));
-  if ((st = launch_rows<kStats>(dtype, a, s)) != NMD_OK) return st;
-  pair_kernel<<<(unsigned)((P + 7) / 8), 256, 0, s>>>(d_targets, d_logps, d_reference, d_offsets, T, P, beta,
-                                                      smoothing, average, d_ratios, d_margins, pair_loss,
-                                                      d_grad ? a.coef : nullptr);
-  sum_kernel<double><<<1, 1024, 0, s>>>(pair_loss, P, 1.0 / (double)P, d_loss);
-  if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
-  return d_grad ? launch_rows<kGrad>(dtype, a, s) : NMD_OK;
+  w += align256((size_t)T * sizeof(Stat));
+  a.coef = (float*)w;
+  w += align256((size_t)T * sizeof(float));
+  double* pair_loss = (double*)w;
+  a.done = (unsigned*)(w + align256((size_t)P * sizeof(double)));
+  if (T > 0) {
+    if ((st = launch_rows<kStats>(dtype, a, s)) != NMD_OK) return st;   // zeroes the count too
+  } else if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) {
+    return NMD_ERR_CUDA;
+  }
+  const int64_t grid = std::min<int64_t>((P + 7) / 8, 1024);
+  if (launch(pair_kernel, grid, 256, 0, 1, true, s, d_targets, (const float*)d_logps, d_reference, d_offsets, T, P, beta,
+             smoothing, (int)average, d_ratios, d_margins, pair_loss, d_grad ? a.coef : (float*)nullptr, a.done,
+             d_loss) != cudaSuccess)
+    return NMD_ERR_CUDA;
+  return d_grad && T > 0 ? launch_grad(dtype, a, s) : NMD_OK;
 }
 
 nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes) {
   if (T < 0 || T > kMaxRows || !bytes) return NMD_ERR_INVALID;
-  *bytes = align256((size_t)T * sizeof(float)) + align256((size_t)T * 3 * sizeof(float)) + 256;
+  *bytes = align256((size_t)T * sizeof(float)) + align256((size_t)T * 3 * sizeof(float));
   return NMD_OK;
 }
 
@@ -610,17 +1310,19 @@ nmd_status nmd_policy_loss(const void* d_logits, int32_t dtype, int64_t T, int64
       (d_offsets && (S < 1 || S > kMaxRows)) || !(clip_low >= 0.0 && clip_low <= 1.0) ||
       !(clip_high >= 0.0 && std::isfinite(clip_high)) || !(kl_coef >= 0.0 && std::isfinite(kl_coef)))
     return NMD_ERR_INVALID;
-  if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
+  if (T == 0) return cudaMemsetAsync(d_stats, 0, 3 * sizeof(float), s) == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   char* w = (char*)d_workspace;
   float* weight = (float*)w;
+  w += align256((size_t)T * sizeof(float));
   a.p = Policy{d_old, d_reference, d_advantages, weight, (float)(1.0 - clip_low), (float)(1.0 + clip_high),
-               (float)kl_coef, (float*)(w + align256((size_t)T * sizeof(float)))};
+               (float)kl_coef, (float*)w};
   weight_kernel<<<1, 1024, 0, s>>>(d_targets, d_offsets, T, S, weight);
   if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
   if ((st = launch_rows<kPolicy>(dtype, a, s)) != NMD_OK) return st;
-  sum_kernel<float><<<3, 1024, 0, s>>>(a.p.terms, T, 1.0, d_stats);
-  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  return launch(terms_kernel, 3, 1024, 0, 0, true, s, (const float*)a.p.terms, T, d_stats) == cudaSuccess
+             ? NMD_OK : NMD_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -143,6 +143,19 @@ def test_logprobs_of_unusual_rows(V):
     assert torch.isnan(got[[3, 4, 5, 7]]).all() and got[6] == float("-inf")
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("temperature", [1e-3, 0.05, 30.0, 3000.0])
+def test_temperatures(dtype, temperature):
+    """Sharp and flat distributions, with banned columns and large common offsets of the logits."""
+    for V, shift in ((700, 0.0), (9000, 0.0), (9000, -3000.0), (9000, 900.0)):
+        g, x, y = make_logits(V, 12, V, dtype, banned=0.1)
+        g += shift
+        x = g.double().cpu().numpy()
+        got = tuning().token_logprobs(g, cuda(y, torch.int64), temperature=temperature)
+        want = O.tuning.token_logprobs(x, y, temperature)
+        check("logps", got.cpu().numpy(), want, tol_lp(x, y, want, temperature) + U * np.abs(want))
+
+
 def test_no_rows_and_equal_bits():
     t = tuning()
     x = torch.empty(0, 12, device="cuda")
@@ -328,6 +341,43 @@ def test_policy_loss(case, dtype):
         only = tuning().policy_loss(g, cuda(y, torch.int64), hide(old), hide(ref), hide(adv), offsets=off, grad=False,
                                     **args)
         assert only.grad is None and torch.equal(only.loss, r.loss) and torch.equal(only.kl, r.kl)
+
+
+# batches that fill the GPU take other kernels than the ones above: long rows stream through a ring of shared-memory
+# slots (one CTA or a cluster of them per row), short ones take a warp each
+LARGE = [(611, 30001, 0, 1, "bf16"), (620, 25000, 0, 0, "fp16"), (615, 12301, 3, 2, "fp32"), (310, 100003, 5, 0, "bf16"),
+         (205, 200005, 0, 3, "fp16"), (2500, 3001, 0, 1, "bf16"), (2440, 4096, 0, 0, "fp16"), (2440, 1500, 1, 0, "fp32"),
+         (1300, 9000, 0, 0, "bf16"), (2433, 6000, 0, 5, "fp16")]
+
+
+@pytest.mark.parametrize("shape", LARGE, ids=lambda s: "x".join(map(str, s)))
+def test_large_batches(shape):
+    T, V, pad, shift, dtype = shape
+    g, x, y = make_logits(V, T, V, dtype, pad=pad, shift=shift, banned=0.05, masked=0.3)
+    rng = np.random.default_rng(T)
+    lp = O.tuning.token_logprobs(x, y, 0.9)
+    yt = cuda(y, torch.int64)
+    e = tol_lp(x, y, lp, 0.9) + U * np.abs(lp)
+    check("logps", tuning().token_logprobs(g, yt, temperature=0.9).cpu().numpy(), lp, e)
+    old = np.float32(lp - rng.choice([-0.7, -0.1, 0.05, 0.6], T))
+    ref = np.float32(lp + 0.4 * rng.standard_normal(T))
+    adv = np.float32(rng.standard_normal(T))
+    want = O.tuning.policy_loss(x, y, old, ref, adv, kl_coef=0.2, temperature=0.9)
+    hide = lambda v: cuda(np.where(y >= 0, v, np.float32(np.nan)))  # noqa: E731
+    runs = [tuning().policy_loss(g, yt, hide(old), hide(ref), hide(adv), kl_coef=0.2, temperature=0.9)
+            for _ in range(2)]
+    r = runs[0]
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    check("logps", r.logps.cpu().numpy(), lp, e)
+    w = O.tuning.policy_weights(y)
+    rho = np.where(y >= 0, np.exp(lp - old), 0.0)
+    erho = rho * (e + U * (np.abs(lp) + np.abs(old) + 8))
+    gap = np.where(y >= 0, ref - lp, 0.0)
+    egap = e + U * (np.abs(gap) + np.abs(lp))
+    dcoef = w * (erho * np.abs(adv) + 4 * U * np.abs(rho * adv) + 0.2 * (np.exp(gap) * egap + 8 * U * np.exp(gap)))
+    check("loss", r.loss.cpu().numpy(), want["loss"], dcoef.sum() + 4 * U * np.sum(w * (np.abs(rho * adv) + 1)))
+    check_grad(r.grad, x, y, lp, want["coef"], dcoef, want["grad"], dtype, 0.9)
 
 
 def test_all_rows_left_out():
