@@ -386,7 +386,7 @@ nmd_status nmd_nearest_neighbors(const float* d_x, int64_t N, int32_t d, const i
  * Logits: T rows (0 <= T <= 2^27) of V columns (1 <= V < 2^31), row t at
  * element t ld (ld >= 0), the columns of a row adjacent, any alignment of an
  * element.  d_targets[t] is row t's column.  A target below zero leaves its
- * row out: its logits and its entries of the other arrays are not read (they
+ * row out: its logits and its entries of the other arrays take no part (they
  * may hold anything), its log-probability is 0 and its gradient row is zero.
  * A target of V or more gives NaN.  With tau = temperature > 0,
  *   lp_t = x_ty / tau - log sum_v exp(x_tv / tau),   p_tv = exp(x_tv/tau) / sum.

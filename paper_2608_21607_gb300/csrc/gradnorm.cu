@@ -9,11 +9,10 @@
 // needed.  The list travels in the kernel's parameters (up to kTable tensors
 // per launch), so that nothing is copied to the device first.
 //
-// Squares are summed in fp32 by each thread, in fp64 from there on.  So that
-// no square leaves fp32's range, a vector of elements whose largest
-// magnitude is above 2^56 or below 2^-50 is scaled by 2^-80 or 2^80 and summed
-// apart; the three sums are put together in fp64, and norms over all of
-// fp32's range come out right.
+// Squares are summed in fp32 by each thread, in fp64 from there on.  A group of
+// elements whose squares leave fp32's range, or come near its ends, is scaled
+// by 2^-80 or 2^80 and summed apart; the three sums are put together in fp64,
+// and norms over all of fp32's range come out right.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -25,8 +24,10 @@ namespace nmd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunkBytes = 32768;     // one CTA's piece of a tensor at a time
-constexpr int kMaxCtas = 2048;         // CTAs of the norm pass over all launches
+constexpr int kVecs = 8;               // 16-byte loads of a thread under way together
+constexpr int kChunkBytes = kThreads * kVecs * 16;   // one CTA's piece of a tensor at a time (32 KB)
+constexpr int kCtasPerSm = 3, kScaleCtasPerSm = 4;
+constexpr int kMaxCtas = 1024;         // CTAs of the norm pass over all launches
 
 template <int K>
 struct Table {
@@ -39,10 +40,6 @@ struct Table {
   int dtype[K];
 };
 
-struct Sums {
-  double mid, big, small;
-};
-
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(bf16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
@@ -50,83 +47,117 @@ __device__ __forceinline__ void from_float(float v, float* x) { *x = v; }
 __device__ __forceinline__ void from_float(float v, bf16* x) { *x = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_float(float v, __half* x) { *x = __float2half_rn(v); }
 
-// the squares of N values into one of the three sums
-template <int N>
-__device__ __forceinline__ void add_squares(const float (&f)[N], float (&acc)[3]) {
-  float m = 0.f;
+// Squares of elements: of the usual groups, of those whose sum is above 2^96
+// (scaled by 2^-80) and of those whose sum is below 2^-60 (by 2^80).
+struct Squares {
+  float usual = 0.f, big = 0.f, small = 0.f;
+  template <class T, int V>
+  __device__ __forceinline__ void add(const uint4 (&v)[V]) {
+    constexpr int N = 16 / sizeof(T);
+    float t[2] = {0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(f[k]));
-  const int which = m > 0x1p56f ? 1 : (m < 0x1p-50f ? 2 : 0);
-  const float sc = which == 0 ? 1.f : (which == 1 ? 0x1p-80f : 0x1p80f);
-  float t = 0.f;
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const float v = f[k] * sc;
-    t = fmaf(v, v, t);
-  }
-  acc[0] += which == 0 ? t : 0.f;
-  acc[1] += which == 1 ? t : 0.f;
-  acc[2] += which == 2 ? t : 0.f;
-}
-
-// Elements [e0, e1) of a tensor, walked by one CTA: f(i, N) is called with
-// the first element of each 16-byte vector (N of them) and of each single
-// element before and after them (1)
-template <class T, class F>
-__device__ __forceinline__ void walk(const T* x, int64_t e0, int64_t e1, F f) {
-  constexpr int N = 16 / sizeof(T);
-  const int off = (int)((uintptr_t)(x + e0) & 15);
-  const int64_t n = e1 - e0;
-  const int64_t h = off ? (16 - off) / (int)sizeof(T) : 0;
-  const int head = (int)(h < n ? h : n);
-  const int64_t nvec = (n - head) / N;
-  const int tail = (int)(n - head - nvec * N);
-  for (int64_t i = threadIdx.x; i < nvec; i += kThreads) f(e0 + head + i * N, true);
-  const int t = threadIdx.x;
-  if (t < head) f(e0 + t, false);
-  else if (t - head < tail) f(e0 + head + nvec * N + t - head, false);
-}
-
-template <class T>
-__device__ __forceinline__ void chunk_squares(const T* x, int64_t e0, int64_t e1, float (&acc)[3]) {
-  constexpr int N = 16 / sizeof(T);
-  walk(x, e0, e1, [&](int64_t i, bool vec) {
-    if (vec) {
-      const uint4 v = *(const uint4*)(x + i);
-      const T* e = (const T*)&v;
-      float f[N];
-#pragma unroll
-      for (int k = 0; k < N; ++k) f[k] = as_float(e[k]);
-      add_squares(f, acc);
-    } else {
-      const float f[1] = {as_float(x[i])};
-      add_squares(f, acc);
-    }
-  });
-}
-
-template <class T>
-__device__ __forceinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e1, float scale) {
-  constexpr int N = 16 / sizeof(T);
-  const bool same = ((uintptr_t)x & 15) == ((uintptr_t)o & 15);
-  walk(x, e0, e1, [&](int64_t i, bool vec) {
-    if (vec) {
-      const uint4 v = *(const uint4*)(x + i);
-      const T* e = (const T*)&v;
-      uint4 w;
-      T* d = (T*)&w;
-#pragma unroll
-      for (int k = 0; k < N; ++k) from_float(as_float(e[k]) * scale, d + k);
-      if (same) {
-        *(uint4*)(o + i) = w;
-      } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) o[i + k] = d[k];
+      for (int k = 0; k < N; ++k) {
+        const float f = as_float(((const T*)&v[i])[k]);
+        t[k & 1] = fmaf(f, f, t[k & 1]);
       }
-    } else {
-      from_float(as_float(x[i]) * scale, o + i);
+    const float sum = t[0] + t[1];
+    if (sum >= 0x1p-60f && sum <= 0x1p96f) {
+      usual += sum;
+      return;
     }
-  });
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(as_float(((const T*)&v[i])[k])));
+    const float scale = m > 1.f ? 0x1p-80f : 0x1p80f;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float f = as_float(((const T*)&v[i])[k]) * scale;
+        s = fmaf(f, f, s);
+      }
+    if (m > 1.f) big += s;
+    else small += s;
+  }
+};
+
+// Elements [e0, e1) of a tensor by one CTA: the 16-byte vectors of the chunk
+// (at most kVecs per thread), and single elements before and after them.
+struct Piece {
+  int head, nvec, tail;
+};
+template <class T>
+__device__ __forceinline__ Piece piece_of(const T* x, int64_t e0, int64_t e1) {
+  const int off = (int)((uintptr_t)(x + e0) & 15), n = (int)(e1 - e0);
+  Piece p;
+  p.head = min(off ? (16 - off) / (int)sizeof(T) : 0, n);
+  p.nvec = (n - p.head) / (16 / (int)sizeof(T));
+  p.tail = n - p.head - p.nvec * (16 / (int)sizeof(T));
+  return p;
+}
+// the single element of this thread within the piece, or -1
+template <class T>
+__device__ __forceinline__ int single_of(const Piece& p) {
+  const int t = threadIdx.x;
+  return t < p.head ? t : t - p.head < p.tail ? p.nvec * (16 / (int)sizeof(T)) + t : -1;
+}
+
+template <class T>
+__device__ __noinline__ void chunk_squares(const T* x, int64_t e0, int64_t e1, Squares& acc) {
+  const Piece p = piece_of(x, e0, e1);
+  const uint4* xv = (const uint4*)(x + e0 + p.head) + threadIdx.x;
+  uint4 v[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i)
+    v[i] = (int)threadIdx.x + i * kThreads < p.nvec ? xv[i * kThreads] : make_uint4(0, 0, 0, 0);
+  if ((int)threadIdx.x < p.nvec) acc.template add<T, kVecs>(v);
+  const int s = single_of<T>(p);
+  if (s >= 0) {
+    uint4 w[1] = {make_uint4(0, 0, 0, 0)};
+    *(T*)w = x[e0 + s];
+    acc.template add<T, 1>(w);
+  }
+}
+
+template <class T, bool SAME>
+__device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e1, float scale) {
+  constexpr int N = 16 / sizeof(T), K = 8;
+  const Piece p = piece_of(x, e0, e1);
+  const uint4* xv = (const uint4*)(x + e0 + p.head);
+  T* to = o + e0 + p.head;
+  auto put = [&](const uint4& v, int i) {
+    uint4 w;
+#pragma unroll
+    for (int k = 0; k < N; ++k) from_float(as_float(((const T*)&v)[k]) * scale, (T*)&w + k);
+    if (SAME) {
+      __stcs((uint4*)to + i, w);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) to[i * N + k] = ((const T*)&w)[k];
+    }
+  };
+  int i = threadIdx.x;
+  for (; i + (K - 1) * kThreads < p.nvec; i += K * kThreads) {
+    uint4 v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = xv[i + k * kThreads];
+#pragma unroll
+    for (int k = 0; k < K; ++k) put(v[k], i + k * kThreads);
+  }
+  for (; i < p.nvec; i += kThreads) put(xv[i], i);
+  const int s = single_of<T>(p);
+  if (s >= 0) from_float(as_float(x[e0 + s]) * scale, o + e0 + s);
+}
+template <class T>
+__device__ __forceinline__ void scale_piece(const void* in, void* out, int64_t e0, int64_t e1, float scale) {
+  // vectors on both sides where they start at the same offset from a 16-byte boundary
+  if ((((uintptr_t)in ^ (uintptr_t)out) & 15) == 0) chunk_scale<T, true>((const T*)in, (T*)out, e0, e1, scale);
+  else chunk_scale<T, false>((const T*)in, (T*)out, e0, e1, scale);
 }
 
 // the entry that holds chunk c: the last whose first chunk is not past c
@@ -154,9 +185,11 @@ __device__ __forceinline__ double cta_sum(double v, double* red) {
 }
 
 template <int K>
-__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Table<K> tab, Sums* parts) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+    norm_kernel(const __grid_constant__ Table<K> tab, double* parts) {
   __shared__ double red[kThreads / 32];
-  float acc[3] = {0.f, 0.f, 0.f};
+  asm volatile("griddepcontrol.launch_dependents;");
+  Squares acc;
   for (int64_t c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
     const int e = entry_of(tab, c);
     const int es = tab.dtype[e] == NMD_DT_FP32 ? 4 : 2;
@@ -166,37 +199,34 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     else if (tab.dtype[e] == NMD_DT_BF16) chunk_squares((const bf16*)tab.in[e], e0, e1, acc);
     else chunk_squares((const __half*)tab.in[e], e0, e1, acc);
   }
-  Sums s;
-  s.mid = cta_sum((double)acc[0], red);
-  s.big = cta_sum((double)acc[1], red);
-  s.small = cta_sum((double)acc[2], red);
+  // fp64 holds all three together
+  const double s = cta_sum((double)acc.usual + (double)acc.big * 0x1p160 + (double)acc.small * 0x1p-160, red);
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
+// The chunks are taken from the last to the first: the norm pass read those
+// last, and they are still in L2.
 template <int K>
-__global__ void __launch_bounds__(kThreads)
-    scale_kernel(const __grid_constant__ Table<K> tab, const Sums* parts, int nparts, double max_norm, int in_place,
+__global__ void __launch_bounds__(kThreads, kScaleCtasPerSm)
+    scale_kernel(const __grid_constant__ Table<K> tab, const double* parts, int nparts, double max_norm, int in_place,
                  float* norm_out) {
   __shared__ double red[kThreads / 32];
-  double mid = 0.0, big = 0.0, small = 0.0;
-  for (int i = threadIdx.x; i < nparts; i += kThreads) {
-    mid += parts[i].mid;
-    big += parts[i].big;
-    small += parts[i].small;
-  }
-  const double norm = sqrt(cta_sum(mid, red) + cta_sum(big, red) * 0x1p160 + cta_sum(small, red) * 0x1p-160);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < nparts; i += kThreads) sum += parts[i];
+  const double norm = sqrt(cta_sum(sum, red));
   if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   // a norm that is not a number makes every gradient so
   const float scale = norm <= max_norm ? 1.f : (float)(max_norm / norm);
   if (in_place && scale == 1.f) return;
-  for (int64_t c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
+  for (int64_t c = tab.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
     const int e = entry_of(tab, c);
     const int es = tab.dtype[e] == NMD_DT_FP32 ? 4 : 2;
     const int64_t e0 = (c - tab.first[e]) * (kChunkBytes / es);
     const int64_t e1 = min(tab.n[e], e0 + kChunkBytes / es);
-    if (tab.dtype[e] == NMD_DT_FP32) chunk_scale((const float*)tab.in[e], (float*)tab.out[e], e0, e1, scale);
-    else if (tab.dtype[e] == NMD_DT_BF16) chunk_scale((const bf16*)tab.in[e], (bf16*)tab.out[e], e0, e1, scale);
-    else chunk_scale((const __half*)tab.in[e], (__half*)tab.out[e], e0, e1, scale);
+    if (tab.dtype[e] == NMD_DT_FP32) scale_piece<float>(tab.in[e], tab.out[e], e0, e1, scale);
+    else if (tab.dtype[e] == NMD_DT_BF16) scale_piece<bf16>(tab.in[e], tab.out[e], e0, e1, scale);
+    else scale_piece<__half>(tab.in[e], tab.out[e], e0, e1, scale);
   }
 }
 
@@ -232,12 +262,12 @@ void fill(Table<K>& t, const void* const* in, void* const* out, const int64_t* n
 
 template <int K>
 nmd_status run(int64_t count, const void* const* in, const int64_t* n, const int32_t* dtype, double max_norm,
-               void* const* out, float* d_norm, Sums* parts, cudaStream_t s) {
+               void* const* out, float* d_norm, double* parts, cudaStream_t s) {
   const int sms = sm_count();
   if (sms == 0) return NMD_ERR_CUDA;
   const int64_t groups = std::max<int64_t>(1, (count + K - 1) / K);
   // CTAs of each launch: the partial sums of all launches fit the workspace
-  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(sms * 8, kMaxCtas / groups));
+  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(sms * kCtasPerSm, kMaxCtas / groups));
   int nparts = 0;
   Table<K> t;
   for (int64_t g = 0; g < groups; ++g) {
@@ -246,10 +276,21 @@ nmd_status run(int64_t count, const void* const* in, const int64_t* n, const int
     norm_kernel<K><<<grid, kThreads, 0, s>>>(t, parts + nparts);
     nparts += grid;
   }
-  for (int64_t g = 0; g < groups; ++g) {
+  // the last group first, in line with the order of the chunks
+  for (int64_t g = groups - 1; g >= 0; --g) {
     if (groups > 1) fill(t, in, out, n, dtype, g * K, std::min(count, (g + 1) * K));
-    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(t.chunks, sms * 8));
-    scale_kernel<K><<<grid, kThreads, 0, s>>>(t, parts, nparts, max_norm, out == nullptr, g == 0 ? d_norm : nullptr);
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(t.chunks, sms * kScaleCtasPerSm)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = groups == 1 ? 1 : 0;   // it waits for the launch just ahead only
+    if (cudaLaunchKernelEx(&cfg, scale_kernel<K>, t, (const double*)parts, nparts, max_norm, (int)(out == nullptr),
+                           g == 0 ? d_norm : (float*)nullptr) != cudaSuccess)
+      return NMD_ERR_CUDA;
   }
   return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
@@ -266,7 +307,7 @@ extern "C" {
 
 nmd_status nmd_clip_workspace_bytes(int64_t count, size_t* bytes) {
   if (count < 0 || count > (int64_t)kTable * kMaxCtas || !bytes) return NMD_ERR_INVALID;
-  *bytes = kMaxCtas * sizeof(Sums);
+  *bytes = kMaxCtas * sizeof(double);
   return NMD_OK;
 }
 
@@ -287,7 +328,7 @@ nmd_status nmd_clip_grad_norm(int64_t count, const void* const* d_grads, const i
   }
   if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
-  Sums* parts = (Sums*)d_workspace;
+  double* parts = (double*)d_workspace;
   if (count <= kSmallTable) return run<kSmallTable>(count, d_grads, sizes, dtypes, max_norm, d_out, d_norm, parts, s);
   return run<kTable>(count, d_grads, sizes, dtypes, max_norm, d_out, d_norm, parts, s);
 }

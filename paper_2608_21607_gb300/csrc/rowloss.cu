@@ -924,57 +924,65 @@ __device__ __forceinline__ int64_t border(const int64_t* offsets, int64_t k, int
   return o < 0 ? 0 : (o > T ? T : o);
 }
 
-// One warp per pair: the two sequences' sums of log ratios, the margin, the
-// pair's loss and the coefficient of each of its rows.
+// One warp (GROUP 32) or one CTA (GROUP 256) per pair: the two sequences' sums
+// of log ratios, the margin, the pair's loss and the coefficient of each of its
+// rows.  Latency is all there is to it, so long sequences get a CTA.
+template <int GROUP>
 __global__ void __launch_bounds__(256)
     pair_kernel(const int64_t* y, const float* logps, const float* ref, const int64_t* offsets, int64_t T, int64_t P,
-                double beta, double smoothing, int average, float* ratios, float* margins, double* pair_loss,
-                float* coef, unsigned* done, float* loss) {
+                double inv_pairs, double beta, double smoothing, int average, float* ratios, float* margins,
+                double* pair_loss, float* coef, unsigned* done, float* loss) {
   __shared__ double red[32];
-  const int lane = threadIdx.x & 31;
+  constexpr int per = 256 / GROUP;   // pairs at a time per CTA
+  const int tid = threadIdx.x % GROUP;
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int64_t p = (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5); p < P;
-       p += (int64_t)gridDim.x * (blockDim.x / 32)) {
+  for (int64_t p = (int64_t)blockIdx.x * per + threadIdx.x / GROUP; p < P; p += (int64_t)gridDim.x * per) {
+    int64_t at[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) at[k] = border(offsets, 2 * p + k, T);
     double ratio[2], share[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
-      double sum = 0.0, count = 0.0;
-      for (int64_t t = a + lane; t < b; t += 32)
-        if (y[t] >= 0) {
-          sum += (double)logps[t] - (double)ref[t];
-          count += 1.0;
+      double sum = 0.0;
+      int count = 0;
+      for (int64_t t = at[k] + tid; t < at[k + 1]; t += GROUP) {
+        const int64_t yt = y[t];
+        const float d = logps[t] - ref[t];
+        if (yt >= 0) {
+          sum += (double)d;
+          ++count;
         }
-      sum = warp_sum(sum);
-      count = warp_sum(count);
-      share[k] = average && count > 1.0 ? 1.0 / count : 1.0;
+      }
+      double n = (double)count;
+      sum = GROUP == 32 ? warp_sum(sum) : block_sum(sum, red);
+      n = GROUP == 32 ? warp_sum(n) : block_sum(n, red);
+      share[k] = average && n > 1.0 ? 1.0 / n : 1.0;
       ratio[k] = sum * share[k];
     }
     const double h = beta * (ratio[0] - ratio[1]);
-    // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|)
-    const double l = log1p(exp(-fabs(h)));
-    const double down = fmax(-h, 0.0) + l, up = fmax(h, 0.0) + l;
-    if (lane == 0) {
+    // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|), in fp32 from here on
+    const float hf = (float)h, l = log1pf(expf(-fabsf(hf)));
+    const double down = (double)(fmaxf(-hf, 0.f) + l), up = (double)(fmaxf(hf, 0.f) + l);
+    if (tid == 0) {
       ratios[2 * p] = (float)ratio[0];
       ratios[2 * p + 1] = (float)ratio[1];
       margins[p] = (float)h;
       pair_loss[p] = smoothing > 0.0 ? (1.0 - smoothing) * down + smoothing * up : down;   // no 0 x inf
     }
     if (coef == nullptr) continue;
-    const double gain = beta * (smoothing - 1.0 / (1.0 + exp(h))) / (double)P;
+    const double gain = beta * (smoothing - (double)(1.f / (1.f + expf(hf)))) * inv_pairs;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int64_t a = border(offsets, 2 * p + k, T), b = border(offsets, 2 * p + k + 1, T);
       const float g = (float)((k ? -gain : gain) * share[k]);
-      for (int64_t t = a + lane; t < b; t += 32) coef[t] = y[t] >= 0 ? g : 0.f;
+      for (int64_t t = at[k] + tid; t < at[k + 1]; t += GROUP) coef[t] = y[t] >= 0 ? g : 0.f;
     }
   }
   if (!last_cta(done)) return;
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < P; i += blockDim.x) s += __ldcg(pair_loss + i);
   s = block_sum(s, red);
-  if (threadIdx.x == 0) *loss = (float)(s / (double)P);
+  if (threadIdx.x == 0) *loss = (float)(s * inv_pairs);
 }
 
 // Each row's share of the policy loss: 1 / (live rows), or 1 / (sequences x
@@ -1072,7 +1080,7 @@ cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
   // A CTA per row, and clusters of up to eight where there are too few to fill the SMs
   int64_t cs = 1;
   while (cs < 8 && a.T * cs < 2 * sms && nvec >= cs * 2 * 256) cs *= 2;
-  int block = 128;
+  int block = nvec > 8192 && a.T >= 8 * sms ? 256 : 128;   // (V = 139,255, 4096 rows: 166 us against 172 us)
   if (a.T * cs < 2 * sms) {
     block = 512;
     while (block > 64 && (nvec + cs - 1) / cs < block) block /= 2;
@@ -1169,8 +1177,10 @@ nmd_status launch_rows(int dtype, const Rows& a, cudaStream_t s) {
 template <class T>
 nmd_status launch_grad_t(const Rows& a, cudaStream_t s) {
   const int64_t nvec = a.V / Vec<T>::N;
+  const int sms = num_sms();
+  if (sms == 0) return NMD_ERR_CUDA;
   cudaError_t e;
-  if (nvec <= 256) {
+  if (nvec <= 256 || (nvec <= 1024 && a.T >= 16 * sms)) {
     e = launch(grad_kernel<T, true>, (a.T + 7) / 8, 256, 0, 1, true, s, a, 1u);
   } else {
     const int64_t pieces = (nvec + 4 * 256 - 1) / (4 * 256);
@@ -1282,10 +1292,11 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
   } else if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) {
     return NMD_ERR_CUDA;
   }
-  const int64_t grid = std::min<int64_t>((P + 7) / 8, 1024);
-  if (launch(pair_kernel, grid, 256, 0, 1, true, s, d_targets, (const float*)d_logps, d_reference, d_offsets, T, P, beta,
-             smoothing, (int)average, d_ratios, d_margins, pair_loss, d_grad ? a.coef : (float*)nullptr, a.done,
-             d_loss) != cudaSuccess)
+  const bool large = T > 128 * P;   // long sequences
+  const int64_t grid = std::min<int64_t>(large ? P : (P + 7) / 8, 1024);
+  if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, d_targets, (const float*)d_logps,
+             d_reference, d_offsets, T, P, 1.0 / (double)P, beta, smoothing, (int)average, d_ratios, d_margins, pair_loss,
+             d_grad ? a.coef : (float*)nullptr, a.done, d_loss) != cudaSuccess)
     return NMD_ERR_CUDA;
   return d_grad && T > 0 ? launch_grad(dtype, a, s) : NMD_OK;
 }

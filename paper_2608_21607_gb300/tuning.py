@@ -11,7 +11,9 @@ tensors' device and does not wait.  What is wrong with the arguments raises
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import functools
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -48,40 +50,45 @@ def _matrix(x, name: str) -> int:
     dt = _DTYPES.get(x.dtype)
     if dt is None:
         _invalid("%s: float32, bfloat16 or float16 is wanted, not %s" % (name, x.dtype))
-    if x.shape[1] < 1 or (x.shape[1] > 1 and x.stride(1) != 1):
+    V = x.shape[1]
+    if V < 1 or (V > 1 and x.stride(1) != 1):
         _invalid("%s: at least one column, and the columns of a row adjacent (stride 1)" % name)
     return dt
 
 
-def _vector(v, name: str, length: int, dtype, device) -> torch.Tensor:
-    if not isinstance(v, torch.Tensor) or v.dim() != 1 or v.shape[0] != length or v.dtype != dtype \
-            or v.device != device:
-        _invalid("%s: a %s vector of %d on %s is wanted" % (name, str(dtype).replace("torch.", ""), length, device))
+def _vector(v, name: str, length: int, dtype, index: int) -> torch.Tensor:
+    if not isinstance(v, torch.Tensor) or v.dim() != 1 or v.numel() != length or v.dtype != dtype \
+            or not v.is_cuda or v.get_device() != index:
+        _invalid("%s: a %s vector of %d on cuda:%d is wanted" % (name, str(dtype).replace("torch.", ""), length, index))
     return v if v.is_contiguous() else v.contiguous()
 
 
-def _offsets(offsets, device, name: str = "offsets") -> torch.Tensor:
+def _offsets(offsets, index: int, name: str = "offsets") -> torch.Tensor:
     if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1:
         _invalid("%s: a vector of sequence borders is wanted" % name)
-    return _vector(offsets, name, offsets.shape[0], torch.int64, device)
+    return _vector(offsets, name, offsets.numel(), torch.int64, index)
 
 
-def _grad_like(logits) -> torch.Tensor:
+def _grad_like(logits, T: int, V: int, ld: int) -> torch.Tensor:
     """The gradient's tensor: the logits' row stride, so that both are reached by the same 16-byte vectors."""
-    T, V = logits.shape
-    ld = logits.stride(0) if T > 1 else V
-    if ld <= V:
+    if T <= 1 or ld <= V:
         return torch.empty((T, V), dtype=logits.dtype, device=logits.device)
     return torch.empty((T, ld), dtype=logits.dtype, device=logits.device)[:, :V]
 
 
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+_calls = {}
 
 
-def _call(device, name: str, *args):
-    with torch.cuda.device(device):
-        st = getattr(nmd.lib(), name)(*args, _stream(device))
+def _call(index: int, name: str, *args):
+    """The C call of that name with the stream that is current on the device, and its status checked."""
+    f = _calls.get(name)
+    if f is None:
+        f = _calls[name] = getattr(nmd.lib(), name)
+    if torch.cuda.current_device() == index:
+        st = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != nmd.NMD_OK:
         nmd._check(None, st, name)
 
@@ -92,14 +99,19 @@ def _bytes(name: str, *args) -> int:
     return out.value
 
 
+@functools.lru_cache(maxsize=256)
+def _bytes_of_sizes(name: str, *sizes) -> int:
+    return _bytes(name, *sizes)
+
+
 def token_logprobs(logits, targets, *, temperature: float = 1.0) -> torch.Tensor:
     """log softmax(logits / temperature) at one column per row (T fp32; 0 where the target is below zero)."""
     dt = _matrix(logits, "logits")
-    T, V = logits.shape
-    targets = _vector(targets, "targets", T, torch.int64, logits.device)
+    index, (T, V) = logits.get_device(), logits.shape
+    targets = _vector(targets, "targets", T, torch.int64, index)
     logps = torch.empty(T, dtype=torch.float32, device=logits.device)
-    _call(logits.device, "nmd_token_logprobs", logits.data_ptr(), dt, T, V, logits.stride(0), targets.data_ptr(),
-          temperature, logps.data_ptr())
+    _call(index, "nmd_token_logprobs", logits.data_ptr(), dt, T, V, logits.stride(0), targets.data_ptr(), temperature,
+          logps.data_ptr())
     return logps
 
 
@@ -113,17 +125,17 @@ def factor_logprobs(A, B, targets, *, temperature: float = 1.0) -> torch.Tensor:
     for x, name in ((A, "A"), (B, "B")):
         if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda or x.dtype not in _DTYPES:
             _invalid("%s: a two-dimensional float32, bfloat16 or float16 CUDA tensor is wanted" % name)
-    device, (T, r), n = A.device, A.shape, B.shape[0]
+    device, index, (T, r), n = A.device, A.get_device(), A.shape, B.shape[0]
     if B.device != device or B.dtype != A.dtype or B.shape[1] != r:
         _invalid("B: %s of %d columns on %s is wanted, as A" % (A.dtype, r, device))
     if not 1 <= r <= 256 or n < 1:
         _invalid("A, B: 1 to 256 columns and at least one row of B are wanted")
-    targets = _vector(targets, "targets", T, torch.int64, device)
+    targets = _vector(targets, "targets", T, torch.int64, index)
     logps = torch.empty(T, dtype=torch.float32, device=device)
     factors = (A.data_ptr(), *A.stride(), B.data_ptr(), *B.stride(), _DTYPES[A.dtype], T, n, r)
     nbytes = _bytes("nmd_factor_workspace_bytes", *factors)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _call(device, "nmd_factor_logprobs", *factors, targets.data_ptr(), temperature, logps.data_ptr(), ws.data_ptr(),
+    _call(index, "nmd_factor_logprobs", *factors, targets.data_ptr(), temperature, logps.data_ptr(), ws.data_ptr(),
           nbytes)
     return logps
 
@@ -138,23 +150,23 @@ def preference_loss(logits, targets, offsets, reference, *, beta: float = 0.1, l
     model's log-probability of the same column (fp32, one per row).
     """
     dt = _matrix(logits, "logits")
-    device, (T, V) = logits.device, logits.shape
-    targets = _vector(targets, "targets", T, torch.int64, device)
-    reference = _vector(reference, "reference", T, torch.float32, device)
-    offsets = _offsets(offsets, device)
-    P = offsets.shape[0] // 2
-    if offsets.shape[0] != 2 * P + 1 or P < 1:
-        _invalid("offsets: 2 P + 1 borders of P >= 1 pairs are wanted, got %d" % offsets.shape[0])
-    nbytes = _bytes("nmd_preference_workspace_bytes", T, P)
+    device, index, (T, V), ld = logits.device, logits.get_device(), logits.shape, logits.stride(0)
+    targets = _vector(targets, "targets", T, torch.int64, index)
+    reference = _vector(reference, "reference", T, torch.float32, index)
+    offsets = _offsets(offsets, index)
+    P = offsets.numel() // 2
+    if offsets.numel() != 2 * P + 1 or P < 1:
+        _invalid("offsets: 2 P + 1 borders of P >= 1 pairs are wanted, got %d" % offsets.numel())
+    nbytes = _bytes_of_sizes("nmd_preference_workspace_bytes", T, P)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    out = torch.empty(1 + T + 3 * P, dtype=torch.float32, device=device)
-    loss, logps, ratios, margins = out[0], out[1:1 + T], out[1 + T:1 + T + 2 * P], out[1 + T + 2 * P:]
-    g = _grad_like(logits) if grad else None
-    _call(device, "nmd_preference_loss", logits.data_ptr(), dt, T, V, logits.stride(0), targets.data_ptr(),
-          offsets.data_ptr(), P, reference.data_ptr(), beta, label_smoothing, int(average), temperature,
-          loss.data_ptr(), logps.data_ptr(), ratios.data_ptr(), margins.data_ptr(), g.data_ptr() if grad else None,
-          g.stride(0) if grad else 0, ws.data_ptr(), nbytes)
-    return PreferenceLoss(loss, logps, ratios, margins, g)
+    loss = torch.empty((), dtype=torch.float32, device=device)
+    out = torch.empty(T + 3 * P, dtype=torch.float32, device=device)
+    at = out.data_ptr()
+    g = _grad_like(logits, T, V, ld) if grad else None
+    _call(index, "nmd_preference_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), offsets.data_ptr(), P,
+          reference.data_ptr(), beta, label_smoothing, int(average), temperature, loss.data_ptr(), at, at + 4 * T,
+          at + 4 * (T + 2 * P), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws.data_ptr(), nbytes)
+    return PreferenceLoss(loss, *torch.split_with_sizes(out, (T, 2 * P, P)), g)
 
 
 def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, clip_low: float = 0.2,
@@ -168,30 +180,32 @@ def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, cl
     the mean over the sequences of each one's mean.
     """
     dt = _matrix(logits, "logits")
-    device, (T, V) = logits.device, logits.shape
-    targets = _vector(targets, "targets", T, torch.int64, device)
-    old = _vector(old, "old", T, torch.float32, device)
-    advantages = _vector(advantages, "advantages", T, torch.float32, device)
+    device, index, (T, V), ld = logits.device, logits.get_device(), logits.shape, logits.stride(0)
+    targets = _vector(targets, "targets", T, torch.int64, index)
+    old = _vector(old, "old", T, torch.float32, index)
+    advantages = _vector(advantages, "advantages", T, torch.float32, index)
     if reference is not None:
-        reference = _vector(reference, "reference", T, torch.float32, device)
+        reference = _vector(reference, "reference", T, torch.float32, index)
     elif kl_coef != 0:
         _invalid("reference: wanted with a KL term")
     S = 0
     if offsets is not None:
-        offsets = _offsets(offsets, device)
-        S = offsets.shape[0] - 1
+        offsets = _offsets(offsets, index)
+        S = offsets.numel() - 1
         if S < 1:
             _invalid("offsets: S + 1 borders of S >= 1 sequences are wanted")
-    nbytes = _bytes("nmd_policy_workspace_bytes", T)
+    nbytes = _bytes_of_sizes("nmd_policy_workspace_bytes", T)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    out = torch.empty(3 + T, dtype=torch.float32, device=device)
-    g = _grad_like(logits) if grad else None
-    _call(device, "nmd_policy_loss", logits.data_ptr(), dt, T, V, logits.stride(0), targets.data_ptr(),
-          old.data_ptr(), None if reference is None else reference.data_ptr(), advantages.data_ptr(),
+    stats = torch.empty(3, dtype=torch.float32, device=device)
+    logps = torch.empty(T, dtype=torch.float32, device=device)
+    g = _grad_like(logits, T, V, ld) if grad else None
+    _call(index, "nmd_policy_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old.data_ptr(),
+          None if reference is None else reference.data_ptr(), advantages.data_ptr(),
           None if offsets is None else offsets.data_ptr(), S, clip_low, clip_high, kl_coef, temperature,
-          out.data_ptr(), out[3:].data_ptr() if T else None, g.data_ptr() if grad else None,
-          g.stride(0) if grad else 0, ws.data_ptr(), nbytes)
-    return PolicyLoss(out[0], out[3:], out[1], out[2], g)
+          stats.data_ptr(), logps.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0,
+          ws.data_ptr(), nbytes)
+    loss, kl, clipped = stats.unbind()
+    return PolicyLoss(loss, logps, kl, clipped, g)
 
 
 def _dense(x) -> bool:
@@ -209,28 +223,36 @@ def _dense(x) -> bool:
 def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
                    out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
     """Global 2-norm of ``grads`` (a scalar tensor), and the gradients scaled by min(1, max_norm / norm): in place, or
-    into ``out`` (tensors of the gradients' types, shapes and strides).  CUDA tensors of one device without gaps
+    into ``out`` (tensors of the gradients' types and sizes).  CUDA tensors of one device without gaps
     (contiguous, or contiguous after a permutation of the dimensions)."""
     grads = list(grads)
-    if not grads or not isinstance(grads[0], torch.Tensor):
-        _invalid("grads: at least one tensor is wanted")
-    device, count = grads[0].device, len(grads)
     outs = grads if out is None else list(out)
-    if len(outs) != count:
-        _invalid("out: %d tensors are wanted, got %d" % (count, len(outs)))
-    ptrs, sizes = (C.c_void_p * count)(), (C.c_int64 * count)()
-    optrs, kinds = (C.c_void_p * count)(), (C.c_int32 * count)()
-    for k, (x, o) in enumerate(zip(grads, outs)):
-        dt = _DTYPES.get(x.dtype)
-        if dt is None or not x.is_cuda or x.device != device or not _dense(x):
-            _invalid("grads[%d]: a float32, bfloat16 or float16 tensor without gaps on %s is wanted" % (k, device))
-        if o is not x and (o.dtype != x.dtype or o.device != device or o.shape != x.shape
-                           or o.stride() != x.stride()):
-            _invalid("out[%d]: a tensor of its gradient's type, shape, strides and device is wanted" % k)
-        ptrs[k], optrs[k], sizes[k], kinds[k] = x.data_ptr(), o.data_ptr(), x.numel(), dt
+    count, Tensor = len(grads), torch.Tensor
+    if count == 0 or len(outs) != count:
+        _invalid("grads, out: as many tensors as gradients are wanted, and at least one")
+    try:   # (maps over methods: a list of hundreds of tensors costs about half a microsecond each)
+        devices = set(map(Tensor.get_device, grads)) | set(map(Tensor.get_device, outs))
+        sizes = array.array("q", map(Tensor.numel, grads))
+        adjacent = all(map(Tensor.is_contiguous, grads)) and all(map(Tensor.is_contiguous, outs))
+    except TypeError:
+        _invalid("grads, out: tensors are wanted")
+    device = grads[0].device
+    if device.type != "cuda" or len(devices) != 1:
+        _invalid("grads, out: tensors of one CUDA device are wanted")
+    types = [x.dtype for x in grads]
+    if not _DTYPES.keys() >= set(types) or not (adjacent or all(map(_dense, grads))):
+        _invalid("grads: float32, bfloat16 or float16 tensors without gaps are wanted")
+    if outs is not grads and (types != [x.dtype for x in outs] or sizes != array.array("q", map(Tensor.numel, outs))
+                              or not (adjacent or all(x.shape == o.shape and x.stride() == o.stride()
+                                                      for x, o in zip(grads, outs)))):
+        _invalid("out: each tensor has its gradient's type and, unless all are contiguous, its shape and strides")
+    kinds = array.array("i", [_DTYPES[t] for t in types])
+    ptrs = array.array("Q", map(Tensor.data_ptr, grads))
+    optrs = None if out is None else array.array("Q", map(Tensor.data_ptr, outs))
     norm = torch.empty((), dtype=torch.float32, device=device)
-    nbytes = _bytes("nmd_clip_workspace_bytes", count)
+    nbytes = _bytes_of_sizes("nmd_clip_workspace_bytes", count)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _call(device, "nmd_clip_grad_norm", count, ptrs, sizes, kinds, max_norm, None if out is None else optrs,
-          norm.data_ptr(), ws.data_ptr(), nbytes)
+    _call(norm.get_device(), "nmd_clip_grad_norm", count, ptrs.buffer_info()[0], sizes.buffer_info()[0],
+          kinds.buffer_info()[0], max_norm, None if out is None else optrs.buffer_info()[0], norm.data_ptr(),
+          ws.data_ptr(), nbytes)
     return norm
