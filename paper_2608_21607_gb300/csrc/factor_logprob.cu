@@ -3,8 +3,8 @@
 //
 // The scores are formed tile by tile on the tcgen05 tensor cores (128 rows of A
 // against chunks of 128 rows of B) in TMEM, and the epilogue warps reduce each
-// row of a tile to a running maximum m and S = sum 2^(c (z - m)), c = log2(e) /
-// tau, as the row kernels of the logits do.  Nothing of the scores is written.
+// row of a tile to a running maximum and sum, as the row kernels of the logits
+// do.  Nothing of the scores is written.
 //
 // 16-bit factors are multiplied as they are.  fp32 factors are split into three
 // bf16 pieces each (x = hi + lo + lo2 to 2^-24 of x), and the six products of
@@ -17,9 +17,9 @@
 // partial results in the order of the chunks and takes the dot product a_t . b_y
 // in fp32 on the CUDA cores.
 //
-// Warp roles (320 threads): warps 0-7 epilogue (two warpgroups on alternate
-// chunks; thread t of each owns TMEM lane t = row t), warp 8 TMA and TMEM
-// allocation, warp 9 issues the MMAs.  Waits are bounded (2 s): a CTA whose wait
+// Warp roles: warps 0-15 epilogue (four warpgroups taking chunks in turn; thread
+// t of each owns TMEM lane t = row t), warp 16 TMA and TMEM allocation, and the
+// warps after it issue the MMAs.  Waits are bounded (2 s): a CTA whose wait
 // ran out flags its run, and the rows it would have counted become NaN.
 #include <cuda_fp16.h>
 
@@ -27,6 +27,7 @@
 #include <cmath>
 
 #include "nmd_internal.cuh"
+#include "softmax_sum.cuh"
 #include "tc_pipe.cuh"
 #include "tc_ptx.cuh"
 
@@ -36,8 +37,9 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128, BN = 128;
-constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kThreads = 320;
-constexpr int kPanel = BM * 128;            // bytes of 128 rows x 64 16-bit columns
+constexpr int kGroups = 4;                   // epilogue warpgroups
+constexpr int kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1;
+constexpr int kPanelA = BM * 128, kPanelB = BN * 128;   // bytes of a tile's or chunk's rows x 64 16-bit columns
 constexpr int kMaxCtas = 256;
 constexpr int kMaxRank = 256;
 
@@ -47,25 +49,28 @@ constexpr int kMaxRank = 256;
 template <int PIECES, bool ARES>
 struct Cfg {
   static constexpr int A_PANELS = ARES ? (PIECES == 1 ? 4 : 2) : 0;
-  static constexpr int A_BYTES = PIECES * A_PANELS * kPanel;
-  static constexpr int STAGE = PIECES * kPanel * (ARES ? 1 : 2);
-  static constexpr int NST = PIECES == 1 ? 8 : 2;
+  static constexpr int A_BYTES = PIECES * A_PANELS * kPanelA;
+  static constexpr int STAGE = PIECES * (kPanelB + (ARES ? 0 : kPanelA));   // the chunk's panels first
+  // Warps that issue MMAs, chunks in turn, each with a ring of stages of its own.
+  // (One issues a chunk of 16-bit factors in about 1100 cycles beside the
+  // epilogue's sixteen warps, more than the products take; the 24 MMAs and more
+  // of an fp32 chunk cover that.)
+  static constexpr int ISS = PIECES == 1 ? 2 : 1;
+  static constexpr int THREADS = 32 * (kMmaWarp + ISS);
+  static constexpr int RST = PIECES == 1 ? 8 / ISS : 2;   // stages of a ring: a power of two
+  static constexpr int NST = ISS * RST;
   static constexpr int NB = 512 / BN;       // TMEM buffers
-  static constexpr int NBAR = 2 * NST + 2 * NB + 3;
+  static constexpr int NBAR = 2 * NST + 2 * NB + 2 + ISS;
   static constexpr size_t SMEM = 1024 + A_BYTES + (size_t)NST * STAGE + NBAR * 8 + 64;
   static_assert(SMEM <= 227 * 1024, "shared memory per block");
   static_assert(SMEM > 114 * 1024, "one CTA (and its 512 TMEM columns) per SM");
 };
 
-struct Stat {
-  float m, S;
-};
-
 struct Params {
   int64_t T, n, C, W;        // rows, columns, chunks per tile, tiles x chunks
   int r, npan;               // rank, panels of 64
-  int slots;                 // partial results kept per tile (x 2 warpgroups)
-  float c;
+  int slots;                 // partial results kept per tile (x kGroups)
+  Scale c;
   uint32_t idesc;
   Stat* parts;               // [tile][slot][warpgroup][128]
   int* flags;                // 2 per CTA: nmd_status, detail
@@ -74,24 +79,91 @@ struct Params {
 // CTA that works on unit u of W dealt to G CTAs, CTA b taking [b W / G, (b + 1) W / G)
 __host__ __device__ __forceinline__ int64_t owner(int64_t u, int64_t W, int64_t G) { return ((u + 1) * G - 1) / W; }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ Stat merge(const Stat& a, const Stat& b, float c) {
-  const float m = fmaxf(a.m, b.m), z = base_of(m);
-  return {m, a.S * ex2((a.m - z) * c) + b.S * ex2((b.m - z) * c)};
+// 32 lanes x 32 columns of TMEM as 16 pairs of columns, waited for
+__device__ __forceinline__ void tmem_pairs(uint32_t taddr, pair_t (&x)[16]) {
+  asm volatile(
+      "{\n\t.reg .b32 t<32>;\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {t0, t1, t2, t3, t4, t5, t6, t7, t8, t9, t10, t11, t12, t13, t14, t15, t16, t17, t18, t19, t20, t21, t22, t23, t24, t25, t26, t27, t28, t29, t30, t31}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;\n\t"
+      "mov.b64 %0, {t0, t1};\n\t"
+      "mov.b64 %1, {t2, t3};\n\t"
+      "mov.b64 %2, {t4, t5};\n\t"
+      "mov.b64 %3, {t6, t7};\n\t"
+      "mov.b64 %4, {t8, t9};\n\t"
+      "mov.b64 %5, {t10, t11};\n\t"
+      "mov.b64 %6, {t12, t13};\n\t"
+      "mov.b64 %7, {t14, t15};\n\t"
+      "mov.b64 %8, {t16, t17};\n\t"
+      "mov.b64 %9, {t18, t19};\n\t"
+      "mov.b64 %10, {t20, t21};\n\t"
+      "mov.b64 %11, {t22, t23};\n\t"
+      "mov.b64 %12, {t24, t25};\n\t"
+      "mov.b64 %13, {t26, t27};\n\t"
+      "mov.b64 %14, {t28, t29};\n\t"
+      "mov.b64 %15, {t30, t31};\n\t"
+      "}"
+      : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]), "=l"(x[4]), "=l"(x[5]), "=l"(x[6]), "=l"(x[7]), "=l"(x[8]), "=l"(x[9]), "=l"(x[10]), "=l"(x[11]), "=l"(x[12]), "=l"(x[13]), "=l"(x[14]), "=l"(x[15])
+      : "r"(taddr)
+      : "memory");
 }
 
+// A row's running pair over its scores.
+struct RowSum : RunningSum {
+  float lost = 0.f;   // what the additions to S have rounded away: a row may have very many groups
+  __device__ __forceinline__ void put(float group) {
+    const float y = group - lost, sum = s.S + y;
+    lost = (sum - s.S) - y;
+    s.S = sum;
+  }
+  // 32 scores; get() gives them as pairs, again where the group is not a usual one
+  template <class G>
+  __device__ __forceinline__ void add(G get, Scale c) {
+    pair_t x[16];
+    if (__all_sync(0xffffffffu, usual)) {   // (TMEM is read by whole warps)
+      get(x);
+      const float group = group_sum(x, c);
+      const bool fine = group < kHigh;
+      if (fine) put(group);
+      if (__all_sync(0xffffffffu, fine)) return;
+      get(x);
+      if (!fine) slow(x, c);
+    } else {
+      get(x);
+      slow(x, c);
+    }
+  }
+
+ private:
+  // the first group, one with larger values, or one with NaN or infinities
+  __device__ __forceinline__ void slow(const pair_t (&x)[16], Scale c) {
+    float m = s.m;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 v = halves(x[i]);
+      m = max_nan(m, max_nan(v.x, v.y));
+    }
+    if (m != s.m) lost = 0.f;
+    raise(m, c);
+    // against the reference where it is an integer, against m itself otherwise
+    // (only -inf so far: the sum is 0 and stays 0)
+    const float z = s.m == -INFINITY ? 0.f : s.m;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 e = halves(power2(x[i], z, c));
+      sum += e.x + e.y;
+    }
+    put(sum * ex2(-above(s.m, c)));
+  }
+};
+
 template <int PIECES, bool ARES>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
     score_kernel(const __grid_constant__ CUtensorMap ta0, const __grid_constant__ CUtensorMap ta1,
                  const __grid_constant__ CUtensorMap ta2, const __grid_constant__ CUtensorMap tb0,
                  const __grid_constant__ CUtensorMap tb1, const __grid_constant__ CUtensorMap tb2, const Params p) {
   using C = Cfg<PIECES, ARES>;
-  constexpr int NST = C::NST, NB = C::NB;
+  constexpr int NST = C::NST, RST = C::RST, NB = C::NB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const uint32_t a_sm = smem_u32(smem), st_sm = a_sm + C::A_BYTES;
@@ -103,6 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                  b_drain = b_aempty + 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* status = p.flags + 2 * blockIdx.x;
+  asm volatile("griddepcontrol.launch_dependents;");
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
       mbar_init(b_full + 8 * i, 1);
@@ -113,8 +186,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(b_lfree + 8 * i, 4);
     }
     mbar_init(b_afull, 1);
-    mbar_init(b_aempty, 1);
-    mbar_init(b_drain, 1);
+    mbar_init(b_aempty, C::ISS);
+    for (int i = 0; i < C::ISS; ++i) mbar_init(b_drain + 8 * i, 1);
     *abort_flag = 0;
     status[0] = 0;
     status[1] = 0;
@@ -134,9 +207,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kTmaWarp) {
     if (lane == 0) {
-      int s = 0;
-      uint32_t ph = 1, aph = 1;
-      int64_t loads = 0, aloads = 0;
+      uint32_t aph = 1;
+      int64_t aloads = 0, done = 0;   // tiles of A, chunks asked for
       bool ok = true;
       int64_t tile = tile0, c = u0 - tile0 * p.C;
       bool first = true;
@@ -144,34 +216,33 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ARES && first) {
           if (!(ok = wait_bar(b_aempty, aph, abort_flag, status, 10))) break;
           aph ^= 1u;
-          mbar_expect_tx(b_afull, PIECES * p.npan * kPanel);
+          mbar_expect_tx(b_afull, PIECES * p.npan * kPanelA);
           for (int k = 0; k < p.npan; ++k) {
-            const uint32_t dst = a_sm + k * PIECES * kPanel;
+            const uint32_t dst = a_sm + k * PIECES * kPanelA;
             tma_load_2d(dst, &ta0, b_afull, 64 * k, (int)(tile * BM));
-            if (PIECES > 1) tma_load_2d(dst + kPanel, &ta1, b_afull, 64 * k, (int)(tile * BM));
-            if (PIECES > 1) tma_load_2d(dst + 2 * kPanel, &ta2, b_afull, 64 * k, (int)(tile * BM));
+            if (PIECES > 1) tma_load_2d(dst + kPanelA, &ta1, b_afull, 64 * k, (int)(tile * BM));
+            if (PIECES > 1) tma_load_2d(dst + 2 * kPanelA, &ta2, b_afull, 64 * k, (int)(tile * BM));
           }
           ++aloads;
           first = false;
         }
+        const uint32_t G = (uint32_t)(u - u0), use = G / C::ISS * p.npan;
         for (int k = 0; k < p.npan; ++k) {
-          if (!(ok = wait_bar(b_empty + 8 * s, ph, abort_flag, status, 1))) break;
+          const int s = (int)(G % C::ISS) * RST + (int)((use + k) % RST);
+          if (!(ok = wait_bar(b_empty + 8 * s, (((use + k) / RST) & 1u) ^ 1u, abort_flag, status, 1))) break;
           const uint32_t dst = st_sm + s * C::STAGE, bar = b_full + 8 * s;
           mbar_expect_tx(bar, C::STAGE);
           tma_load_2d(dst, &tb0, bar, 64 * k, (int)(c * BN));
-          if (PIECES > 1) tma_load_2d(dst + kPanel, &tb1, bar, 64 * k, (int)(c * BN));
-          if (PIECES > 1) tma_load_2d(dst + 2 * kPanel, &tb2, bar, 64 * k, (int)(c * BN));
+          if (PIECES > 1) tma_load_2d(dst + kPanelB, &tb1, bar, 64 * k, (int)(c * BN));
+          if (PIECES > 1) tma_load_2d(dst + 2 * kPanelB, &tb2, bar, 64 * k, (int)(c * BN));
           if (!ARES) {
-            tma_load_2d(dst + PIECES * kPanel, &ta0, bar, 64 * k, (int)(tile * BM));
-            if (PIECES > 1) tma_load_2d(dst + (PIECES + 1) * kPanel, &ta1, bar, 64 * k, (int)(tile * BM));
-            if (PIECES > 1) tma_load_2d(dst + (PIECES + 2) * kPanel, &ta2, bar, 64 * k, (int)(tile * BM));
-          }
-          ++loads;
-          if (++s == NST) {
-            s = 0;
-            ph ^= 1u;
+            const uint32_t da = dst + PIECES * kPanelB;
+            tma_load_2d(da, &ta0, bar, 64 * k, (int)(tile * BM));
+            if (PIECES > 1) tma_load_2d(da + kPanelA, &ta1, bar, 64 * k, (int)(tile * BM));
+            if (PIECES > 1) tma_load_2d(da + 2 * kPanelA, &ta2, bar, 64 * k, (int)(tile * BM));
           }
         }
+        ++done;
         if (++c == p.C) {
           c = 0;
           ++tile;
@@ -179,10 +250,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!ok) {   // wait for the copies in flight before shared memory goes away
-        for (int64_t k = loads > NST ? loads - NST : 0; k < loads; ++k) {
+        for (int i = 0; i < NST; ++i) {   // (a stage that never gets its phase is given up after 0.1 s)
+          const uint32_t ring = (uint32_t)(i / RST), chunks = (uint32_t)((done + C::ISS - 1 - ring) / C::ISS);
+          const uint32_t uses = chunks * p.npan;   // of this ring; the last use of its stage i % RST:
+          if (uses <= (uint32_t)(i % RST)) continue;
+          const uint32_t last = (uses - 1 - i % RST) / RST;
           const uint64_t t0 = globaltimer_ns();
-          while (!mbar_try_wait(b_full + 8 * (int)(k % NST), (uint32_t)((k / NST) & 1)) &&
-                 globaltimer_ns() - t0 < 100000000ull) {
+          while (!mbar_try_wait(b_full + 8 * i, last & 1u) && globaltimer_ns() - t0 < 100000000ull) {
           }
         }
         if (aloads > 0) {
@@ -192,76 +266,72 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-  } else if (warp == kMmaWarp) {
-    int s = 0, lb = 0;
-    uint32_t ph = 0, lph = 1, aph = 0;
+  } else if (warp >= kMmaWarp) {
+    const uint32_t me = warp - kMmaWarp;
+    uint32_t aph = 0;
     bool ok = true, first = true;
     int64_t c = u0 - tile0 * p.C;
     for (int64_t u = u0; u < u1 && ok; ++u) {
-      if (ARES && first) {
+      const uint32_t G = (uint32_t)(u - u0);
+      if (ARES && first) {   // by every issuer, so that none falls a phase behind
         if (!(ok = conv_wait(b_afull, aph, abort_flag, status, 2))) break;
-        aph ^= 1u;
         first = false;
       }
-      if (!(ok = conv_wait(b_lfree + 8 * lb, lph, abort_flag, status, 4))) break;
-      const uint32_t d = tmem + lb * BN;
-      for (int k = 0; k < p.npan; ++k) {
-        if (!(ok = conv_wait(b_full + 8 * s, ph, abort_flag, status, 3))) break;
-        fence_after();
-        const uint32_t bs = st_sm + s * C::STAGE;
-        const uint64_t db = sdesc(bs, 16, 1024, SWZ_128B);
-        const uint64_t da = sdesc(ARES ? a_sm + k * PIECES * kPanel : bs + PIECES * kPanel, 16, 1024, SWZ_128B);
-        const int steps = min(4, (p.r - 64 * k + 15) / 16);
-        for (int q = 0; q < steps; ++q) {
-          const uint32_t acc = (k | q) != 0;
-          if (PIECES == 1) {
-            mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, acc);
-          } else {
-            constexpr uint64_t P = kPanel >> 4;
-            mma_ss_elect(d, da + 2 * q + P, db + 2 * q + P, p.idesc, acc);          // lo lo
-            mma_ss_elect(d, da + 2 * q + 2 * P, db + 2 * q, p.idesc, 1);            // lo2 hi
-            mma_ss_elect(d, da + 2 * q, db + 2 * q + 2 * P, p.idesc, 1);            // hi lo2
-            mma_ss_elect(d, da + 2 * q + P, db + 2 * q, p.idesc, 1);                // lo hi
-            mma_ss_elect(d, da + 2 * q, db + 2 * q + P, p.idesc, 1);                // hi lo
-            mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, 1);                    // hi hi
+      if (G % C::ISS == me) {
+        const uint32_t lb = G % NB, use = G / C::ISS * p.npan;
+        if (!(ok = conv_wait(b_lfree + 8 * lb, ((G / NB) & 1u) ^ 1u, abort_flag, status, 4))) break;
+        const uint32_t d = tmem + lb * BN;
+        for (int k = 0; k < p.npan; ++k) {
+          const uint32_t s = me * RST + (use + k) % RST;
+          if (!(ok = conv_wait(b_full + 8 * s, ((use + k) / RST) & 1u, abort_flag, status, 3))) break;
+          fence_after();
+          const uint32_t bs = st_sm + s * C::STAGE;
+          const uint64_t db = sdesc(bs, 16, 1024, SWZ_128B);
+          const uint64_t da = sdesc(ARES ? a_sm + k * PIECES * kPanelA : bs + PIECES * kPanelB, 16, 1024, SWZ_128B);
+          const int steps = min(4, (p.r - 64 * k + 15) / 16);
+          for (int q = 0; q < steps; ++q) {
+            const uint32_t acc = (k | q) != 0;
+            if (PIECES == 1) {
+              mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, acc);
+            } else {
+              constexpr uint64_t A = kPanelA >> 4, B = kPanelB >> 4;
+              mma_ss_elect(d, da + 2 * q + A, db + 2 * q + B, p.idesc, acc);          // lo lo
+              mma_ss_elect(d, da + 2 * q + 2 * A, db + 2 * q, p.idesc, 1);            // lo2 hi
+              mma_ss_elect(d, da + 2 * q, db + 2 * q + 2 * B, p.idesc, 1);            // hi lo2
+              mma_ss_elect(d, da + 2 * q + A, db + 2 * q, p.idesc, 1);                // lo hi
+              mma_ss_elect(d, da + 2 * q, db + 2 * q + B, p.idesc, 1);                // hi lo
+              mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, 1);                    // hi hi
+            }
           }
+          commit_elect(b_empty + 8 * s);
         }
-        commit_elect(b_empty + 8 * s);
-        if (++s == NST) {
-          s = 0;
-          ph ^= 1u;
-        }
+        if (!ok) break;
+        commit_elect(b_lfull + 8 * lb);
       }
-      if (!ok) break;
-      commit_elect(b_lfull + 8 * lb);
-      if (++lb == NB) {
-        lb = 0;
-        lph ^= 1u;
-      }
-      if (++c == p.C) {
+      if (++c == p.C) {   // done with this tile of A
         c = 0;
         if (ARES) commit_elect(b_aempty);
+        aph ^= 1u;
         first = true;
       }
     }
-    commit_elect(b_drain);   // every MMA issued has to be over before TMEM is freed
+    commit_elect(b_drain + 8 * me);   // every MMA issued has to be over before TMEM is freed
     if (lane == 0) {
       const uint64_t t0 = globaltimer_ns();
-      while (!mbar_try_wait(b_drain, 0) && globaltimer_ns() - t0 < 200000000ull) {
+      while (!mbar_try_wait(b_drain + 8 * me, 0) && globaltimer_ns() - t0 < 200000000ull) {
       }
     }
     __syncwarp();
   } else {
     const int wg = warp >> 2, quarter = warp & 3;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    const float cc = p.c;
-    Stat st{-INFINITY, 0.f};
-    float lost = 0.f;   // what the additions to S have rounded away (compensated summation)
+    const Scale cc = p.c;
+    RowSum run;
     bool ok = true;
     int64_t tile = tile0, c = u0 - tile0 * p.C;
     for (int64_t u = u0; u < u1 && ok; ++u) {
       const int64_t G = u - u0;
-      if ((int)(G & 1) == wg) {
+      if ((int)(G % kGroups) == wg) {
         const int lb = (int)(G % NB);
         if (!(ok = warp_wait(b_lfull + 8 * lb, (uint32_t)((G / NB) & 1), abort_flag, status, 7))) break;
         fence_after();
@@ -269,33 +339,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int kv = (int)min((int64_t)BN, p.n - c * BN);
           const uint32_t col = tmem + lane_base + lb * BN;
 #pragma unroll 1
-          for (int j = 0; j < kv; j += 64) {
-            uint32_t v[2][32];
-            tmem_ld32(col + j, v[0]);
-            tmem_ld32(col + j + 32, v[1]);
-            tmem_wait_ld(v[0]);
-            tmem_wait_ld(v[1]);
-            if (kv < j + 64) {   // columns past the last count as -inf
+          for (int j = 0; j < kv; j += 32) {
+            if (kv >= j + 32) {
+              run.add([&](pair_t(&x)[16]) { tmem_pairs(col + j, x); }, cc);
+            } else {   // columns past the last count as -inf
+              run.add(
+                  [&](pair_t(&x)[16]) {
+                    tmem_pairs(col + j, x);
 #pragma unroll
-              for (int i = 0; i < 64; ++i)
-                if (j + i >= kv) v[i >> 5][i & 31] = 0xff800000u;
+                    for (int i = 0; i < 16; ++i) {
+                      const float2 v = halves(x[i]);
+                      x[i] = pair_of(j + 2 * i < kv ? v.x : -INFINITY, j + 2 * i + 1 < kv ? v.y : -INFINITY);
+                    }
+                  },
+                  cc);
             }
-            float m = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 64; ++i) m = fmaxf(m, __uint_as_float(v[i >> 5][i & 31]));
-            if (m > st.m) {
-              const float f = ex2((st.m - m) * cc);
-              st.S *= f;
-              lost *= f;
-              st.m = m;
-            }
-            const float z = base_of(st.m);
-            float t = 0.f;
-#pragma unroll
-            for (int i = 0; i < 64; ++i) t += ex2((__uint_as_float(v[i >> 5][i & 31]) - z) * cc);
-            const float y = t - lost, sum = st.S + y;
-            lost = (sum - st.S) - y;
-            st.S = sum;
           }
         }
         fence_before();
@@ -304,9 +362,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (++c == p.C || u + 1 == u1) {   // the end of a tile, or of the run: hand over the row's partial result
         const int64_t slot = blockIdx.x - owner(tile * p.C, p.W, gridDim.x);
-        p.parts[((tile * p.slots + slot) * 2 + wg) * BM + quarter * 32 + lane] = st;
-        st = Stat{-INFINITY, 0.f};
-        lost = 0.f;
+        p.parts[((tile * p.slots + slot) * kGroups + wg) * BM + quarter * 32 + lane] = run.s;
+        run = RowSum();
         c = 0;
         ++tile;
       }
@@ -327,68 +384,102 @@ __device__ __forceinline__ float value(bf16 x) { return __bfloat162float(x); }
 template <>
 __device__ __forceinline__ float value(__half x) { return __half2float(x); }
 
-// One warp per row: its partial results merged, the target's score, the difference.
-template <class T>
+// A row's partial results merged, the target's score, the difference: by one
+// warp, or by a CTA where few tiles spread over many CTAs leave many of them.
+template <class T, bool CTA>
 __global__ void __launch_bounds__(256)
     finish_kernel(const T* A, int64_t ar, int64_t ac, const T* B, int64_t br, int64_t bc, const int64_t* y,
                   float inv_temp, const Params p, int64_t G, float* logps) {
-  const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  __shared__ Stat red[8];
+  __shared__ int bad_any;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t t = CTA ? blockIdx.x : (int64_t)blockIdx.x * 8 + warp;
   if (t >= p.T) return;
+  if (CTA && threadIdx.x == 0) bad_any = 0;
   const int64_t yt = y[t];
+  float z = 0.f;
+  if (yt >= 0 && yt < p.n && (!CTA || warp == 0)) {   // before the scores are there
+    for (int k = lane; k < p.r; k += 32) z = fmaf(value(A[t * ar + k * ac]), value(B[yt * br + k * bc]), z);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (yt < 0 || yt >= p.n) {
-    if (lane == 0) logps[t] = yt < 0 ? 0.f : NAN;
+    if (CTA ? threadIdx.x == 0 : lane == 0) logps[t] = yt < 0 ? 0.f : NAN;
     return;
   }
   const int64_t tile = t / BM, b0 = owner(tile * p.C, p.W, G), b1 = owner(tile * p.C + p.C - 1, p.W, G);
-  Stat st{-INFINITY, 0.f};
+  const int count = (int)(kGroups * (b1 - b0 + 1)), first = CTA ? threadIdx.x : lane, step = CTA ? 256 : 32;
+  const Stat* parts = p.parts + tile * p.slots * kGroups * BM + t % BM;
+  float m = -INFINITY;
   int bad = 0;
-  for (int64_t k = lane; k < 2 * (b1 - b0 + 1); k += 32) {
-    st = merge(st, p.parts[(tile * p.slots * 2 + k) * BM + t % BM], p.c);
-    bad |= p.flags[2 * (b0 + k / 2)];
+#pragma unroll 4
+  for (int k = first; k < count; k += step) {
+    m = max_nan(m, parts[(int64_t)k * BM].m);
+    bad |= p.flags[2 * (b0 + k / kGroups)];
   }
-  float z = 0.f;
-  for (int k = lane; k < p.r; k += 32) z = fmaf(value(A[t * ar + k * ac]), value(B[yt * br + k * bc]), z);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Stat other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.S, o)};
-    st = merge(st, other, p.c);
-    z += __shfl_xor_sync(0xffffffffu, z, o);
-    bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+  Stat st{m, 0.f};
+#pragma unroll 4
+  for (int k = first; k < count; k += step) {
+    const Stat o = parts[(int64_t)k * BM];
+    st.S += o.S * rescale(o.m, m, p.c);
   }
-  if (lane == 0) logps[t] = bad ? NAN : (z - st.m) * inv_temp - logf(st.S);
+  st = merge_lanes<32>(st, p.c);
+  bad = __any_sync(0xffffffffu, bad);
+  if (CTA) {
+    __syncthreads();
+    if (lane == 0) {
+      red[warp] = st;
+      if (bad) bad_any = 1;
+    }
+    __syncthreads();
+    st = merge_lanes<8>(lane < 8 ? red[lane] : Stat{-INFINITY, 0.f}, p.c);
+    bad = bad_any;
+  }
+  if (CTA ? threadIdx.x == 0 : lane == 0)
+    logps[t] = bad || st.m == INFINITY ? NAN : (z - st.m) * inv_temp - (logf(st.S) + kLn2 * above(st.m, p.c));
 }
 
-// Rows x columns of any strides into row-major 16-bit pieces with row stride rp
-// (a multiple of 8 elements, as TMA asks), through tiles of 32 x 32 so that
-// both sides are read and written along their rows.
+// A factor of any strides and the row-major 16-bit pieces that it is packed
+// into, with row stride rp (a multiple of 8 elements, as TMA asks).
+template <class T, class D>
+struct PackJob {
+  const T* src;
+  int64_t sr, sc, rows;
+  int rp;
+  D* d[3];
+  int64_t blocks;   // of 32 rows; 0: this factor is read where it is
+};
+
+// Both factors in one launch, through tiles of 32 x 32 so that both sides are
+// read and written along their rows.
 template <class T, class D, int PIECES>
-__global__ void __launch_bounds__(256)
-    piece_kernel(const T* src, int64_t sr, int64_t sc, int64_t rows, int r, int rp, D* d0, D* d1, D* d2) {
+__global__ void __launch_bounds__(256) piece_kernel(const PackJob<T, D> ja, const PackJob<T, D> jb, int r) {
   __shared__ T tile[32][33];
-  const int64_t row0 = (int64_t)blockIdx.x * 32;
+  const bool first = blockIdx.x < ja.blocks;
+  const PackJob<T, D>& j = first ? ja : jb;
+  const int64_t row0 = ((int64_t)blockIdx.x - (first ? 0 : ja.blocks)) * 32;
   const int col0 = blockIdx.y * 32;
   const int a = threadIdx.x & 31, b = threadIdx.x >> 5;
   for (int i = b; i < 32; i += 8) {   // lanes along the dimension whose stride is the smaller
-    const int64_t row = row0 + (sc <= sr ? i : a);
-    const int col = col0 + (sc <= sr ? a : i);
-    if (row < rows && col < r) tile[row - row0][col - col0] = src[row * sr + col * sc];
+    const int64_t row = row0 + (j.sc <= j.sr ? i : a);
+    const int col = col0 + (j.sc <= j.sr ? a : i);
+    if (row < j.rows && col < r) tile[row - row0][col - col0] = j.src[row * j.sr + col * j.sc];
   }
   __syncthreads();
   for (int i = b; i < 32; i += 8) {
-    const int64_t row = row0 + i;
-    const int col = col0 + a;
-    if (row >= rows || col >= r) continue;
+    const int64_t row = row0 + i, at = row * j.rp + col0 + a;
+    if (row >= j.rows || col0 + a >= r) continue;
     if constexpr (PIECES == 1) {
-      d0[row * rp + col] = tile[i][a];
+      j.d[0][at] = tile[i][a];
     } else {
       const float x = tile[i][a];
       const bf16 h = __float2bfloat16_rn(x);
       const float e = x - __bfloat162float(h);
       const bf16 l = __float2bfloat16_rn(e);
-      d0[row * rp + col] = h;
-      d1[row * rp + col] = l;
-      d2[row * rp + col] = __float2bfloat16_rn(e - __bfloat162float(l));
+      j.d[0][at] = h;
+      j.d[1][at] = l;
+      j.d[2][at] = __float2bfloat16_rn(e - __bfloat162float(l));
     }
   }
 }
@@ -435,7 +526,7 @@ Layout layout(const void* A, int64_t ar, int64_t ac, const void* B, int64_t br, 
   // a tile's chunks are spread over at most (CTAs / tiles) + 2 CTAs
   L.slots = (int)std::min<int64_t>(kMaxCtas, kMaxCtas / std::max<int64_t>(1, L.tiles) + 2);
   L.parts = off;
-  off += ((size_t)L.tiles * L.slots * 2 * BM * sizeof(Stat) + 255) & ~size_t(255);
+  off += ((size_t)L.tiles * L.slots * kGroups * BM * sizeof(Stat) + 255) & ~size_t(255);
   L.flags = off;
   off += kMaxCtas * 2 * sizeof(int);
   L.total = off;
@@ -447,12 +538,12 @@ bool bad_sizes(int64_t ar, int64_t ac, int64_t br, int64_t bc, int dtype, int64_
          n >= (int64_t(1) << 31) || r < 1 || r > kMaxRank || ar < 0 || ac < 0 || br < 0 || bc < 0;
 }
 
-bool encode(const void* base, int64_t rows, int64_t r, int64_t stride, int dtype, CUtensorMap* m) {
+bool encode(const void* base, int64_t rows, int64_t r, int64_t stride, int dtype, int box_rows, CUtensorMap* m) {
   PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {(cuuint64_t)r, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-  cuuint32_t box[2] = {64, BM}, es[2] = {1, 1};
+  cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, es[2] = {1, 1};
   return fn(m, dtype == NMD_DT_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
             const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -469,21 +560,52 @@ nmd_status launch_scores(const CUtensorMap* ta, const CUtensorMap* tb, const Par
       }))
     return NMD_ERR_CUDA;
   constexpr int k1 = PIECES > 1 ? 1 : 0, k2 = PIECES > 1 ? 2 : 0;
-  score_kernel<PIECES, ARES><<<grid, kThreads, C::SMEM, s>>>(ta[0], ta[k1], ta[k2], tb[0], tb[k1], tb[k2], p);
+  score_kernel<PIECES, ARES><<<grid, C::THREADS, C::SMEM, s>>>(ta[0], ta[k1], ta[k2], tb[0], tb[k1], tb[k2], p);
   return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
-void pack(const void* src, int64_t sr, int64_t sc, int64_t rows, int64_t r, int dtype, const Operand& o, char* ws,
-          cudaStream_t s) {
-  const dim3 grid((unsigned)((rows + 31) / 32), (unsigned)((r + 31) / 32));
-  char* d = ws + o.at;
-  const int rp = (int)o.stride;
-  if (dtype == NMD_DT_FP32)
-    piece_kernel<float, bf16, 3><<<grid, 256, 0, s>>>((const float*)src, sr, sc, rows, (int)r, rp, (bf16*)d,
-                                                      (bf16*)(d + o.piece), (bf16*)(d + 2 * o.piece));
-  else   // 16-bit values are moved as they are
-    piece_kernel<uint16_t, uint16_t, 1><<<grid, 256, 0, s>>>((const uint16_t*)src, sr, sc, rows, (int)r, rp,
-                                                             (uint16_t*)d, nullptr, nullptr);
+// `overlap`: the kernel may start before the one ahead of it in the stream has
+// finished (it waits for that one itself).
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, size_t smem, bool overlap, cudaStream_t s,
+                   const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = overlap ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <class T>
+cudaError_t launch_finish(const void* const* f, const int64_t* st, const int64_t* y, float it, const Params& p,
+                          int64_t grid, int64_t tiles, float* logps, cudaStream_t s) {
+  // a CTA per row where a tile's partial results come from 32 CTAs or more
+  if (tiles * 32 <= grid)
+    return launch(finish_kernel<T, true>, p.T, 256, 0, true, s, (const T*)f[0], st[0], st[1], (const T*)f[1], st[2],
+                  st[3], y, it, p, grid, logps);
+  return launch(finish_kernel<T, false>, (p.T + 7) / 8, 256, 0, true, s, (const T*)f[0], st[0], st[1], (const T*)f[1],
+                st[2], st[3], y, it, p, grid, logps);
+}
+
+template <class T, class D, int PIECES>
+void pack(const void* A, const int64_t* sa, int64_t T_, const void* B, const int64_t* sb, int64_t n, int64_t r,
+          const Layout& L, char* ws, cudaStream_t s) {
+  auto job = [&](const void* src, const int64_t* st, int64_t rows, const Operand& o) {
+    D* d = (D*)(ws + o.at);
+    const size_t piece = o.piece / sizeof(D);
+    return PackJob<T, D>{(const T*)src, st[0], st[1], rows, (int)o.stride, {d, d + piece, d + 2 * piece},
+                         o.packed ? (rows + 31) / 32 : 0};
+  };
+  const PackJob<T, D> ja = job(A, sa, T_, L.a), jb = job(B, sb, n, L.b);
+  const int64_t blocks = ja.blocks + jb.blocks;
+  if (blocks > 0)
+    piece_kernel<T, D, PIECES><<<dim3((unsigned)blocks, (unsigned)((r + 31) / 32)), 256, 0, s>>>(ja, jb, (int)r);
 }
 
 }  // namespace
@@ -503,10 +625,9 @@ nmd_status nmd_factor_workspace_bytes(const void* d_A, int64_t a_row, int64_t a_
 nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, const void* d_B, int64_t b_row,
                                int64_t b_col, int32_t dtype, int64_t T, int64_t n, int64_t r, const int64_t* d_targets,
                                double temperature, float* d_logps, void* d_workspace, size_t ws_bytes, void* stream) {
-  if (bad_sizes(a_row, a_col, b_row, b_col, dtype, T, n, r) || !(temperature > 0.0) || !std::isfinite(temperature))
-    return NMD_ERR_INVALID;
-  const float c = (float)(1.4426950408889634074 / temperature), it = (float)(1.0 / temperature);
-  if (!(c > 0.f) || !std::isfinite(c) || !std::isfinite(it)) return NMD_ERR_INVALID;
+  Params p{};
+  if (bad_sizes(a_row, a_col, b_row, b_col, dtype, T, n, r) || !scale_of(temperature, &p.c)) return NMD_ERR_INVALID;
+  const float it = (float)(1.0 / temperature);
   if (T == 0) return NMD_OK;
   const int es = dtype == NMD_DT_FP32 ? 4 : 2;
   if (!d_A || !d_B || !d_targets || !d_logps || (((uintptr_t)d_A | (uintptr_t)d_B) & (uintptr_t)(es - 1)))
@@ -519,16 +640,16 @@ nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, co
     return NMD_ERR_CUDA;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)d_workspace;
-  if (L.a.packed) pack(d_A, a_row, a_col, T, r, dtype, L.a, ws, s);
-  if (L.b.packed) pack(d_B, b_row, b_col, n, r, dtype, L.b, ws, s);
+  const int64_t sa[2] = {a_row, a_col}, sb[2] = {b_row, b_col};
+  if (dtype == NMD_DT_FP32) pack<float, bf16, 3>(d_A, sa, T, d_B, sb, n, r, L, ws, s);
+  else pack<uint16_t, uint16_t, 1>(d_A, sa, T, d_B, sb, n, r, L, ws, s);   // 16-bit values are moved as they are
   CUtensorMap ta[3], tb[3];
   const int kind = dtype == NMD_DT_FP16 ? NMD_DT_FP16 : NMD_DT_BF16;
   for (int k = 0; k < L.pieces; ++k) {
-    if (!encode(L.a.packed ? ws + L.a.at + k * L.a.piece : d_A, T, r, L.a.stride, kind, &ta[k]) ||
-        !encode(L.b.packed ? ws + L.b.at + k * L.b.piece : d_B, n, r, L.b.stride, kind, &tb[k]))
+    if (!encode(L.a.packed ? ws + L.a.at + k * L.a.piece : d_A, T, r, L.a.stride, kind, BM, &ta[k]) ||
+        !encode(L.b.packed ? ws + L.b.at + k * L.b.piece : d_B, n, r, L.b.stride, kind, BN, &tb[k]))
       return NMD_ERR_CUDA;
   }
-  Params p{};
   p.T = T;
   p.n = n;
   p.C = L.C;
@@ -536,7 +657,6 @@ nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, co
   p.r = (int)r;
   p.npan = (int)((r + 63) / 64);
   p.slots = L.slots;
-  p.c = c;
   // kind::f16 with fp32 accumulation: A and B both bf16 (format 1) or both f16 (format 0)
   p.idesc = idesc_bf16(BM, BN, false) & (dtype == NMD_DT_FP16 ? ~((1u << 7) | (1u << 10)) : ~0u);
   p.parts = (Stat*)(ws + L.parts);
@@ -547,17 +667,13 @@ nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, co
   else if (r <= 128) st = launch_scores<3, true>(ta, tb, p, grid, s);
   else st = launch_scores<3, false>(ta, tb, p, grid, s);
   if (st != NMD_OK) return st;
-  const unsigned fg = (unsigned)((T + 7) / 8);
-  if (dtype == NMD_DT_FP32)
-    finish_kernel<<<fg, 256, 0, s>>>((const float*)d_A, a_row, a_col, (const float*)d_B, b_row, b_col, d_targets, it, p,
-                                     (int64_t)grid, d_logps);
-  else if (dtype == NMD_DT_BF16)
-    finish_kernel<<<fg, 256, 0, s>>>((const bf16*)d_A, a_row, a_col, (const bf16*)d_B, b_row, b_col, d_targets, it, p,
-                                     (int64_t)grid, d_logps);
-  else
-    finish_kernel<<<fg, 256, 0, s>>>((const __half*)d_A, a_row, a_col, (const __half*)d_B, b_row, b_col, d_targets, it,
-                                     p, (int64_t)grid, d_logps);
-  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  const void* f[2] = {d_A, d_B};
+  const int64_t strides[4] = {a_row, a_col, b_row, b_col};
+  cudaError_t e;
+  if (dtype == NMD_DT_FP32) e = launch_finish<float>(f, strides, d_targets, it, p, grid, L.tiles, d_logps, s);
+  else if (dtype == NMD_DT_BF16) e = launch_finish<bf16>(f, strides, d_targets, it, p, grid, L.tiles, d_logps, s);
+  else e = launch_finish<__half>(f, strides, d_targets, it, p, grid, L.tiles, d_logps, s);
+  return e == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
 }  // extern "C"

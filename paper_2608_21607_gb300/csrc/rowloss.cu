@@ -22,77 +22,12 @@
 #include <cmath>
 
 #include "nmd_internal.cuh"
+#include "softmax_sum.cuh"
 #include "tc_pipe.cuh"
 #include "tc_ptx.cuh"
 
 namespace nmd {
 namespace {
-
-constexpr float kLn2 = 0.693147180559945309f;
-constexpr double kLog2e = 1.4426950408889634074;
-
-// 2^x by the SFU (results below 2^-126 become 0, which no sum of
-// probabilities can tell from the exact value)
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// the larger value, NaN if one is
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-
-// Pairs of fp32 values (fp32x2 instructions: one issue slot for two)
-typedef unsigned long long pair_t;
-__device__ __forceinline__ pair_t pair_of(float a, float b) {
-  pair_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 halves(pair_t p) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
-  return r;
-}
-__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
-  pair_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
-  pair_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
-  pair_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-
-// c = log2(e) / tau as hi + lo, hi of 12 bits, so that a 16-bit x times hi less
-// an integer is exact and the exponent is rounded once, without a leaning that
-// the sum over a long sequence would show.  lo > 0: both products of -inf are
-// -inf.  `whole` is c in one fp32 value.
-struct Scale {
-  float hi, lo, whole;
-};
-// 2^(c (x - m))
-__device__ __forceinline__ float power(float x, float m, Scale c) {
-  const float d = x - m;
-  return ex2(fmaf(d, c.hi, d * c.lo));
-}
-__device__ __forceinline__ pair_t exponent2(pair_t x, float m, Scale c) {
-  const pair_t d = add2(x, pair_of(-m, -m));
-  return fma2(d, pair_of(c.hi, c.hi), mul2(d, pair_of(c.lo, c.lo)));
-}
-__device__ __forceinline__ pair_t power2(pair_t x, float m, Scale c) {
-  const float2 e = halves(exponent2(x, m, c));
-  return pair_of(ex2(e.x), ex2(e.y));
-}
 
 // 16-byte vectors of the three element types: N values, the largest of them (NaN
 // if one is), pairs of them
@@ -168,63 +103,15 @@ struct Vec<__half> {
   static __device__ __forceinline__ __half put(float x) { return __float2half_rn(x); }
 };
 
-// (m, S) of a set of elements: a value near their maximum (NaN if one is; -inf
-// of none) and the sum of 2^(c x - ref), where ref is the integer ceil(c m) if
-// that is within +-1024, and c m otherwise.  An integer reference makes every
-// rescaling exact.
-struct __align__(8) Stat {
-  float m, S;
-};
-__device__ __forceinline__ bool is_near(float m, Scale c) { return fabsf(m * c.hi) <= 1024.f; }
-__device__ __forceinline__ float ref_of(float m, Scale c) { return ceilf(m * c.hi); }
-// ref - c m: what the reference is above the maximum
-__device__ __forceinline__ float above(float m, Scale c) {
-  return is_near(m, c) ? fmaf(-m, c.lo, fmaf(-m, c.hi, ref_of(m, c))) : 0.f;
-}
-// 2^(reference of m - reference of to), m <= to
-__device__ __forceinline__ float rescale(float m, float to, Scale c) {
-  if (is_near(m, c) && is_near(to, c)) return ex2(ref_of(m, c) - ref_of(to, c));   // exact
-  if (m == to) return 1.f;
-  const float d = m - to;
-  return ex2(fmaf(d, c.hi, d * c.lo) + (above(m, c) - above(to, c)));
-}
-// Merges over groups of `width` lanes (a power of two); every lane of a group
-// gets the same result.
-template <int width>
-__device__ __forceinline__ Stat merge_lanes(Stat st, Scale c) {
-  float m = st.m;
-#pragma unroll
-  for (int o = width / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float S = st.S * rescale(st.m, m, c);
-#pragma unroll
-  for (int o = width / 2; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
-  return {m, S};
-}
-
-// A running pair.  The reference is the maximum of the first elements and stays
-// until a group of elements exceeds it by much (its sum passes kHigh), so that
-// the usual group costs a product, a correction, an exponential and an addition
-// per element and no comparison.  The SFU's exponential is low by 5e-8 on
-// average for negative arguments and high by 3.5e-8 for positive ones (measured
-// over many arguments), which the sum over a long sequence would show; every
-// second element is therefore taken 2^kLift larger, and its sum reduced by that,
-// exactly.
+// A running pair over a thread's vectors.
 template <class T>
-struct Running {
-  static constexpr float kHigh = 4096.f, kLift = 24.f, kDrop = 1.f / (1 << 24);
-  Stat s{-INFINITY, 0.f};
-  float r = 0.f;
-  bool usual = false;   // the reference is an integer
-
+struct Running : RunningSum {
   // four vectors: get(0) to get(3), asked for again where the group is not a usual one
   template <class G>
   __device__ __forceinline__ void add(G get, Scale c) {
     constexpr int P = Vec<T>::N / 2, H = 4 * P;
     for (;;) {
       if (usual) {
-        const pair_t hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo), k0 = pair_of(-r, kLift - r);
-        // all products, then all exponentials, then the sums: enough of each
-        // under way to cover their latencies
         pair_t x[H];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -232,19 +119,7 @@ struct Running {
 #pragma unroll
           for (int i = 0; i < P; ++i) x[k * P + i] = Vec<T>::pair(v, i);
         }
-#pragma unroll
-        for (int i = 0; i < H; ++i) x[i] = fma2(x[i], lo, fma2(x[i], hi, k0));
-#pragma unroll
-        for (int i = 0; i < H; ++i) {
-          const float2 e = halves(x[i]);
-          x[i] = pair_of(ex2(e.x), ex2(e.y));
-        }
-#pragma unroll
-        for (int d = H / 2; d > 0; d /= 2)
-#pragma unroll
-          for (int i = 0; i < d; ++i) x[i] = add2(x[i], x[i + d]);
-        const float2 t = halves(x[0]);
-        const float group = fmaf(t.y, kDrop, t.x);
+        const float group = group_sum(x, c);
         if (group < kHigh) {
           s.S += group;
           return;
@@ -275,15 +150,6 @@ struct Running {
     raise(max_nan(s.m, x), c);
     if (usual) s.S += ex2(fmaf(x, c.hi, -r) + x * c.lo);
     else s.S += power(x, s.m == -INFINITY ? 0.f : s.m, c);
-  }
-
- private:
-  __device__ __forceinline__ void raise(float m, Scale c) {
-    if (m == s.m) return;
-    s.S *= rescale(s.m, m, c);
-    s.m = m;
-    r = ref_of(m, c);
-    usual = is_near(m, c);
   }
 };
 
@@ -1205,16 +1071,10 @@ constexpr int64_t kMaxRows = int64_t(1) << 27;   // rows x 8 CTAs within a grid
 nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, const int64_t* y, double temperature,
                 float* logps, void* grad, int64_t gld, Rows* a) {
   if (dtype < NMD_DT_FP32 || dtype > NMD_DT_FP16 || T < 0 || T > kMaxRows || V < 1 || V >= (int64_t(1) << 31) ||
-      ld < 0 || !(temperature > 0.0) || !std::isfinite(temperature))
+      ld < 0)
     return NMD_ERR_INVALID;
-  const double c = kLog2e / temperature;
-  const float whole = (float)c, it = (float)(1.0 / temperature);
-  if (!(whole >= 1e-30f) || !(whole <= 1e30f)) return NMD_ERR_INVALID;
-  int e = 0;
-  const double f = std::frexp(c, &e);   // in [1/2, 1)
-  double head = std::floor(f * 4096.0);
-  if (head == f * 4096.0) head -= 1.0;   // hi is below c, so that lo > 0
-  const float hi = (float)std::ldexp(head, e - 12);
+  Scale scale;
+  if (!scale_of(temperature, &scale)) return NMD_ERR_INVALID;
   if (T > 0 && (!x || !y || !logps)) return NMD_ERR_INVALID;
   const int es = dtype_bytes(dtype);
   if (((uintptr_t)x | (uintptr_t)grad) & (uintptr_t)(es - 1)) return NMD_ERR_INVALID;
@@ -1224,8 +1084,8 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
   a->V = V;
   a->ld = ld;
   a->y = y;
-  a->c = Scale{hi, (float)(c - (double)hi), whole};
-  a->inv_temp = it;
+  a->c = scale;
+  a->inv_temp = (float)(1.0 / temperature);
   a->logps = logps;
   if (grad) {
     if (T > 0 && gld < V) return NMD_ERR_INVALID;
