@@ -157,9 +157,12 @@ struct Policy {
   const float* old;      // T: log-probabilities under the policy that produced the tokens
   const float* ref;      // T, or nullptr
   const float* adv;      // T
-  const float* weight;   // T: each row's share of the loss
+  const float* weight;   // T: each row's share of the loss; nullptr: the row kernel takes it itself
   float lo, hi, kl;      // 1 - clip_low, 1 + clip_high, KL coefficient
   float* terms;          // 3 T: weighted loss, KL, cut-off terms
+  const int64_t* offsets;   // S + 1, or nullptr
+  int64_t S;
+  float* stats;          // 3: the sums of the terms
 };
 
 struct Rows {
@@ -175,7 +178,7 @@ struct Rows {
   int64_t gld;
   int64_t each;          // vectors of a row that one CTA of its cluster takes
   int same_phase;        // rows of x and grad start at the same offset from a 16-byte boundary
-  unsigned* done;        // count of finished CTAs: zeroed by the kernel before the one that counts
+  unsigned* done;        // a count that starts at zero: finished CTAs, or rows
   Policy p;
 };
 
@@ -216,6 +219,46 @@ __device__ __forceinline__ bool last_cta(unsigned* done) {
   __syncthreads();
   if (last) __threadfence();
   return last != 0;
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// border k of the sequences, held within the rows whatever the array says
+__device__ __forceinline__ int64_t border(const int64_t* offsets, int64_t k, int64_t T) {
+  const int64_t o = offsets[k];
+  return o < 0 ? 0 : (o > T ? T : o);
+}
+
+// A row's share of the policy loss, by one warp: 1 / (live rows), or 1 /
+// (sequences x live rows of its sequence); 0 for a row outside every sequence.
+__device__ __forceinline__ float weight_of(const int64_t* y, const int64_t* offsets, int64_t T, int64_t S, int64_t t) {
+  const int lane = threadIdx.x & 31;
+  int64_t from = 0, to = T;
+  double sequences = 1.0;
+  if (offsets != nullptr) {
+    bool mine = false;
+    for (int64_t k = lane; k < S; k += 32) {
+      const int64_t a = border(offsets, k, T), b = border(offsets, k + 1, T);
+      if (a <= t && t < b) {
+        mine = true;
+        from = a;
+        to = b;
+      }
+    }
+    const unsigned m = __ballot_sync(0xffffffffu, mine);
+    if (m == 0) return 0.f;
+    from = __shfl_sync(0xffffffffu, from, __ffs(m) - 1);
+    to = __shfl_sync(0xffffffffu, to, __ffs(m) - 1);
+    sequences = (double)S;
+  }
+  int n = 0;
+#pragma unroll 8
+  for (int64_t i = from + lane; i < to; i += 32) n += y[i] >= 0;
+  n = __reduce_add_sync(0xffffffffu, n);
+  return (float)(1.0 / (sequences * (double)max(n, 1)));
 }
 
 // A row's gradient: d_v = down 2^(c (x_v - m)) + up [v = y].  16-bit gradients
@@ -378,6 +421,30 @@ __device__ __forceinline__ void write_row(const Rows& a, int64_t t, const RowOut
   }
 }
 
+// The sums of the rows' terms, in their order, by the warp (GROUP 32) or CTA that
+// finished the last row.
+template <int GROUP>
+__device__ __noinline__ void sum_terms(const Rows& a, double* red) {
+  __threadfence();
+  const int tid = GROUP == 32 ? threadIdx.x & 31 : threadIdx.x, step = GROUP == 32 ? 32 : blockDim.x;
+  double s[3] = {0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int64_t i = tid; i < a.T; i += step)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s[k] += (double)__ldcg(a.p.terms + k * a.T + i);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) s[k] = warp_sum(s[k]);
+  if (GROUP != 32) {   // red: 3 x 16 warps
+    if ((tid & 31) == 0)
+      for (int k = 0; k < 3; ++k) red[k * 16 + tid / 32] = s[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s[k] = warp_sum((tid & 31) < step / 32 ? red[k * 16 + (tid & 31)] : 0.0);
+  }
+  if (tid == 0)
+    for (int k = 0; k < 3; ++k) a.p.stats[k] = (float)s[k];
+}
+
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -396,6 +463,9 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
   extern __shared__ uint4 slots[];
   __shared__ Stat red[16], peers[8];
   __shared__ Slope shared_slope;
+  __shared__ int shared_last;
+  __shared__ double dred[MODE == kPolicy && !WARP ? 48 : 1];
+  __shared__ float shared_share;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (MODE == kStats) asm volatile("griddepcontrol.launch_dependents;");
   unsigned csize = 1, rank = 0;
@@ -425,6 +495,10 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
   // last column has no log-probability: NaN, so that the mistake shows
   float xy = NAN, adv = 0.f, old = 0.f, ref = 0.f;
   T xs = Vec<T>::put(0.f);
+  // a small policy batch: no kernel before this one has taken the weights, and
+  // none after it will add up the terms
+  const bool alone = MODE == kPolicy && a.p.weight == nullptr;
+  float share = 0.f;
   Stat st{-INFINITY, 0.f};
   if (live) {
     int ahead = tid;   // next vector to be loaded
@@ -442,6 +516,11 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
       adv = a.p.adv[t];
       old = a.p.old[t];
       if (a.p.ref != nullptr) ref = a.p.ref[t];
+      if (alone && WARP) share = weight_of(a.y, a.p.offsets, a.T, a.p.S, t);
+      if (alone && !WARP && warp == (int)blockDim.x / 32 - 1) {   // (the first warp has the rest to do)
+        share = weight_of(a.y, a.p.offsets, a.T, a.p.S, t);
+        if (lane == 0) shared_share = share;
+      }
     }
     Running<T> run;
     int d = 0;
@@ -462,14 +541,24 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     if (scalar >= 0) run.add(Vec<T>::get(xs), a.c);
     st = merge_lanes<32>(run.s, a.c);
   }
-  auto weight = [&] {   // the weights are the previous kernel's
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+  auto weight = [&] {
+    if (alone) return WARP ? share : shared_share;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the weights are the previous kernel's
     return a.p.weight[t];
   };
+  bool last = false;   // the batch's last row
   Slope d;
   if constexpr (WARP) {
     const RowOut o = row_out<MODE>(a, live, xy, adv, old, ref, weight, st);
-    if (lane == 0) write_row<MODE>(a, t, o, st);
+    if (lane == 0) {
+      write_row<MODE>(a, t, o, st);
+      if (alone) {
+        __threadfence();
+        last = atomicAdd(a.done, 1u) == (unsigned)a.T - 1;
+      }
+    }
+    last = __shfl_sync(0xffffffffu, last, 0);
+    if (last) sum_terms<32>(a, nullptr);
     if (MODE == kStats || a.grad == nullptr) return;
     d = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
   } else {
@@ -493,12 +582,21 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     if (warp == 0) {
       const RowOut o = row_out<MODE>(a, live, xy, adv, old, ref, weight, st);
       if (threadIdx.x == 0) {
-        if (rank == 0) write_row<MODE>(a, t, o, st);
+        shared_last = 0;
+        if (rank == 0) {
+          write_row<MODE>(a, t, o, st);
+          if (alone) {
+            __threadfence();
+            shared_last = atomicAdd(a.done, 1u) == (unsigned)a.T - 1;
+          }
+        }
         if (MODE == kPolicy) shared_slope = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
       }
     }
-    if (MODE == kStats || a.grad == nullptr) return;
+    if (MODE == kStats) return;
     __syncthreads();
+    if (shared_last) sum_terms<0>(a, dred);
+    if (a.grad == nullptr) return;
     d = shared_slope;
   }
   T* g = (T*)a.grad + t * a.gld;
@@ -779,17 +877,6 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ Rows 
   }
 }
 
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// border k of the sequences, held within the rows whatever the array says
-__device__ __forceinline__ int64_t border(const int64_t* offsets, int64_t k, int64_t T) {
-  const int64_t o = offsets[k];
-  return o < 0 ? 0 : (o > T ? T : o);
-}
-
 // One warp (GROUP 32) or one CTA (GROUP 256) per pair: the two sequences' sums
 // of log ratios, the margin, the pair's loss and the coefficient of each of its
 // rows.  Latency is all there is to it, so long sequences get a CTA.
@@ -938,7 +1025,7 @@ cudaError_t launch_row(void (*kernel)(P...), size_t smem, int64_t grid, int bloc
 // The statistics pass, or a policy batch without its gradient.
 template <class T, int MODE>
 cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
-  constexpr bool late = MODE == kPolicy;   // the weights' kernel is ahead of it
+  const bool late = MODE == kPolicy && a.p.weight != nullptr;   // the weights' kernel is ahead of it
   // A warp per row of up to 8192 16-bit columns where there are rows enough (at
   // V = 4096: 61 us against 113 us for 48,828 rows by CTAs of 128 threads).
   if (nvec <= 256 || (nvec <= 1024 && a.T >= 16 * sms))
@@ -955,23 +1042,30 @@ cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
   return launch_row(row_kernel<T, false, MODE, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, late, s, a);
 }
 
+// CTAs of a streaming cluster, and whether a batch with its gradient streams
+int64_t stream_cluster(int64_t nvec) { return std::min<int64_t>(8, ((nvec + kSlotVec - 1) / kSlotVec + 8) / 9); }
+bool streams(int64_t nvec, int64_t T, int sms) {
+  const int64_t cs = stream_cluster(nvec);
+  return nvec > 3072 && T * cs >= 4 * sms && (nvec + kSlotVec - 1) / kSlotVec <= cs * kSlots;
+}
+
 // A policy batch with its gradient.
 template <class T>
 cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
+  const bool late = a.p.weight != nullptr;   // the weights' kernel is ahead of it
   // a warp per row of up to 4096 16-bit columns (V = 4096, 48,828 rows: 195 us against 234 us by CTAs)
   if (nvec <= 256 || (nvec <= 513 && a.T >= 16 * sms)) {
     const int groups = (int)((nvec + 127) / 128);
     if (groups <= 2)
-      return launch_row(row_kernel<T, true, kPolicy, 2, true>, groups * 16384, (a.T + 7) / 8, 256, 1, true, s, a);
-    return launch_row(row_kernel<T, true, kPolicy, 8, true>, groups * 16384, (a.T + 7) / 8, 256, 1, true, s, a);
+      return launch_row(row_kernel<T, true, kPolicy, 2, true>, groups * 16384, (a.T + 7) / 8, 256, 1, late, s, a);
+    return launch_row(row_kernel<T, true, kPolicy, 8, true>, groups * 16384, (a.T + 7) / 8, 256, 1, late, s, a);
   }
   // Long rows in batches that fill the GPU: the streaming kernel, its clusters'
   // runs at most nine of the ring's thirteen slots (V = 32768, 6103 rows: 158 us
   // against 161 us by clusters of row_kernel; V = 139255: 163 us against 171 us;
   // V = 16384: 198 us against 153 us).
-  const int64_t slots = (nvec + kSlotVec - 1) / kSlotVec;
-  int64_t cs = std::min<int64_t>(8, (slots + 8) / 9);
-  if (nvec > 3072 && a.T * cs >= 4 * sms && slots <= cs * kSlots) {
+  int64_t cs = stream_cluster(nvec);
+  if (streams(nvec, a.T, sms)) {
     static std::atomic<int> ready[kMaxDevices], room[9][kMaxDevices];
     if (!per_device(ready, [] {
           return cudaFuncSetAttribute(policy_stream_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -996,7 +1090,7 @@ cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
     if (clusters == 0) return cudaErrorInvalidValue;
     a.each = (nvec + cs - 1) / cs;
     return launch(policy_stream_kernel<T>, std::min<int64_t>(a.T, clusters) * cs, kStreamThreads, kRingBytes,
-                  (unsigned)cs, true, s, a);
+                  (unsigned)cs, late, s, a);
   }
   // A CTA per row, or a cluster with runs of 32 KB, or where the rows are too few to fill the SMs
   cs = nvec * 16 <= 48 * 1024 ? 1 : std::min<int64_t>(8, (nvec * 16 + 32767) / 32768);
@@ -1011,11 +1105,11 @@ cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
   const int64_t groups = (a.each + 4 * block - 1) / (4 * block);
   const size_t smem = (size_t)block * 64 * groups;
   if (groups <= 2)
-    return launch_row(row_kernel<T, false, kPolicy, 2, true>, smem, a.T * cs, block, (unsigned)cs, true, s, a);
+    return launch_row(row_kernel<T, false, kPolicy, 2, true>, smem, a.T * cs, block, (unsigned)cs, late, s, a);
   if (groups <= 8 && smem <= kMaxKeep)
-    return launch_row(row_kernel<T, false, kPolicy, 8, true>, smem, a.T * cs, block, (unsigned)cs, true, s, a);
+    return launch_row(row_kernel<T, false, kPolicy, 8, true>, smem, a.T * cs, block, (unsigned)cs, late, s, a);
   // too long to be kept: read again
-  return launch_row(row_kernel<T, false, kPolicy, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, true,
+  return launch_row(row_kernel<T, false, kPolicy, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, late,
                     s, a);
 }
 
@@ -1101,6 +1195,10 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
   return NMD_OK;
 }
 
+bool policy_streams(int dtype, const Rows& a) {
+  return a.grad != nullptr && streams(a.V * dtype_bytes(dtype) / 16 + 1, a.T, num_sms());
+}
+
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
 }  // namespace
@@ -1163,7 +1261,7 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
 
 nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes) {
   if (T < 0 || T > kMaxRows || !bytes) return NMD_ERR_INVALID;
-  *bytes = align256((size_t)T * sizeof(float)) + align256((size_t)T * 3 * sizeof(float));
+  *bytes = align256((size_t)T * sizeof(float)) + align256((size_t)T * 3 * sizeof(float)) + 256;
   return NMD_OK;
 }
 
@@ -1187,8 +1285,15 @@ nmd_status nmd_policy_loss(const void* d_logits, int32_t dtype, int64_t T, int64
   char* w = (char*)d_workspace;
   float* weight = (float*)w;
   w += align256((size_t)T * sizeof(float));
-  a.p = Policy{d_old, d_reference, d_advantages, weight, (float)(1.0 - clip_low), (float)(1.0 + clip_high),
-               (float)kl_coef, (float*)w};
+  // up to 1024 rows one kernel does it all (and a cleared count): a launch costs more than the rows' counting
+  const bool alone = T <= 1024 && !policy_streams(dtype, a);
+  a.p = Policy{d_old, d_reference, d_advantages, alone ? nullptr : weight, (float)(1.0 - clip_low),
+               (float)(1.0 + clip_high), (float)kl_coef, (float*)w, d_offsets, S, d_stats};
+  a.done = (unsigned*)(w + align256((size_t)T * 3 * sizeof(float)));
+  if (alone) {
+    if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) return NMD_ERR_CUDA;
+    return launch_rows<kPolicy>(dtype, a, s);
+  }
   weight_kernel<<<1, 1024, 0, s>>>(d_targets, d_offsets, T, S, weight);
   if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
   if ((st = launch_rows<kPolicy>(dtype, a, s)) != NMD_OK) return st;

@@ -84,7 +84,7 @@ def _call(index: int, name: str, *args):
     f = _calls.get(name)
     if f is None:
         f = _calls[name] = getattr(nmd.lib(), name)
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         st = f(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(index):
@@ -204,8 +204,7 @@ def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, cl
           None if offsets is None else offsets.data_ptr(), S, clip_low, clip_high, kl_coef, temperature,
           stats.data_ptr(), logps.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0,
           ws.data_ptr(), nbytes)
-    loss, kl, clipped = stats.unbind()
-    return PolicyLoss(loss, logps, kl, clipped, g)
+    return PolicyLoss(stats[0], logps, stats[1], stats[2], g)
 
 
 def _dense(x) -> bool:
