@@ -106,7 +106,10 @@ __device__ __forceinline__ float above(float m, Scale c) {
 }
 // 2^(reference of m - reference of to), m <= to
 __device__ __forceinline__ float rescale(float m, float to, Scale c) {
-  if (is_near(m, c) && is_near(to, c)) return ex2(ref_of(m, c) - ref_of(to, c));   // exact
+  if (is_near(m, c) && is_near(to, c)) {   // a power of two, put together from its bits
+    const int e = (int)(ref_of(m, c) - ref_of(to, c));
+    return e < -126 ? 0.f : __int_as_float((e + 127) << 23);
+  }
   if (m == to) return 1.f;
   const float d = m - to;
   return ex2(fmaf(d, c.hi, d * c.lo) + (above(m, c) - above(to, c)));
@@ -128,12 +131,12 @@ __device__ __forceinline__ Stat merge_lanes(Stat st, Scale c) {
 // until a group of elements exceeds it by much (its sum passes kHigh), so that
 // the usual group costs a product, a correction, an exponential and an addition
 // per element and no comparison.  The SFU's exponential is low by 5e-8 on
-// average for negative arguments and high by 3.5e-8 for positive ones (measured
-// over many arguments), which the sum over a long sequence would show; every
-// second element is therefore taken 2^kLift larger, and its sum reduced by that,
-// exactly.
+// average for arguments below -1 and high by 3.5e-8 for those above 1 (measured
+// over many arguments), which the sum over a long sequence would show; so one
+// half of the elements is taken 2^kLift larger and the other half 2^kSink
+// smaller, and their sums are set right by these powers, exactly.
 struct RunningSum {
-  static constexpr float kHigh = 4096.f, kLift = 24.f, kDrop = 1.f / (1 << 24);
+  static constexpr float kHigh = 4096.f, kLift = 16.f, kSink = 2.f;
   Stat s{-INFINITY, 0.f};
   float r = 0.f;
   bool usual = false;   // the reference is an integer
@@ -143,7 +146,7 @@ struct RunningSum {
   // way to cover their latencies.
   template <int H>
   __device__ __forceinline__ float group_sum(pair_t (&x)[H], Scale c) const {
-    const pair_t hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo), k0 = pair_of(-r, kLift - r);
+    const pair_t hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo), k0 = pair_of(-r - kSink, kLift - r);
 #pragma unroll
     for (int i = 0; i < H; ++i) x[i] = fma2(x[i], lo, fma2(x[i], hi, k0));
 #pragma unroll
@@ -156,7 +159,7 @@ struct RunningSum {
 #pragma unroll
       for (int i = 0; i < d; ++i) x[i] = add2(x[i], x[i + d]);
     const float2 t = halves(x[0]);
-    return fmaf(t.y, kDrop, t.x);
+    return fmaf(t.y, 1.f / (1 << (int)kLift), t.x * (float)(1 << (int)kSink));
   }
   // takes m (at least s.m, or NaN) as the value near the maximum
   __device__ __forceinline__ void raise(float m, Scale c) {
