@@ -389,7 +389,7 @@ __device__ __forceinline__ float value(__half x) { return __half2float(x); }
 template <class T, bool CTA>
 __global__ void __launch_bounds__(256)
     finish_kernel(const T* A, int64_t ar, int64_t ac, const T* B, int64_t br, int64_t bc, const int64_t* y,
-                  float inv_temp, const Params p, int64_t G, float* logps) {
+                  float2 inv_temp, const Params p, int64_t G, float* logps) {
   __shared__ Stat red[8];
   __shared__ int bad_any;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(256)
     bad = bad_any;
   }
   if (CTA ? threadIdx.x == 0 : lane == 0)
-    logps[t] = bad || st.m == INFINITY ? NAN : (z - st.m) * inv_temp - (logf(st.S) + kLn2 * above(st.m, p.c));
+    logps[t] = bad || st.m == INFINITY ? NAN : log_prob(z, st, above(st.m, p.c), inv_temp).value();
 }
 
 // A factor of any strides and the row-major 16-bit pieces that it is packed
@@ -583,7 +583,7 @@ cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, size_t smem, b
 }
 
 template <class T>
-cudaError_t launch_finish(const void* const* f, const int64_t* st, const int64_t* y, float it, const Params& p,
+cudaError_t launch_finish(const void* const* f, const int64_t* st, const int64_t* y, float2 it, const Params& p,
                           int64_t grid, int64_t tiles, float* logps, cudaStream_t s) {
   // a CTA per row where a tile's partial results come from 32 CTAs or more
   if (tiles * 32 <= grid)
@@ -627,7 +627,7 @@ nmd_status nmd_factor_logprobs(const void* d_A, int64_t a_row, int64_t a_col, co
                                double temperature, float* d_logps, void* d_workspace, size_t ws_bytes, void* stream) {
   Params p{};
   if (bad_sizes(a_row, a_col, b_row, b_col, dtype, T, n, r) || !scale_of(temperature, &p.c)) return NMD_ERR_INVALID;
-  const float it = (float)(1.0 / temperature);
+  const float2 it = two_floats(1.0 / temperature);
   if (T == 0) return NMD_OK;
   const int es = dtype == NMD_DT_FP32 ? 4 : 2;
   if (!d_A || !d_B || !d_targets || !d_logps || (((uintptr_t)d_A | (uintptr_t)d_B) & (uintptr_t)(es - 1)))

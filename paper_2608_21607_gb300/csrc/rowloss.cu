@@ -155,7 +155,7 @@ struct Running : RunningSum {
 
 struct Policy {
   const float* old;      // T: log-probabilities under the policy that produced the tokens
-  const float* ref;      // T, or nullptr
+  const float* ref;      // T, or nullptr (the preference loss has it too)
   const float* adv;      // T
   const float* weight;   // T: each row's share of the loss; nullptr: the row kernel takes it itself
   float lo, hi, kl;      // 1 - clip_low, 1 + clip_high, KL coefficient
@@ -170,10 +170,11 @@ struct Rows {
   int64_t T, V, ld;
   const int64_t* y;
   Scale c;
-  float inv_temp;
+  float2 inv_temp;       // 1 / tau as the sum of two
   float* logps;          // T
   Stat* stats;           // T (the statistics pass writes, the gradient pass reads) or nullptr
   float* coef;           // T: g_t; zeroed by the statistics pass
+  float* gap;            // T: log-probability less the reference's
   void* grad;            // T x V with row stride gld, or nullptr
   int64_t gld;
   int64_t each;          // vectors of a row that one CTA of its cluster takes
@@ -269,11 +270,11 @@ struct Slope {
   bool zero, fold;
 };
 template <class T>
-__device__ __forceinline__ Slope slope_of(bool live, float coef, Stat st, float inv_temp, Scale c) {
+__device__ __forceinline__ Slope slope_of(bool live, float coef, Stat st, float2 inv_temp, Scale c) {
   Slope d;
   d.zero = !live || coef == 0.f;   // left out, cut off, in no sequence: the logits are not needed
   d.m = st.m;
-  d.up = coef * inv_temp;
+  d.up = coef * inv_temp.x;
   d.down = -d.up / st.S;
   const float l = log2f(fabsf(d.down));
   d.k = fmaf(-st.m, c.whole, l);
@@ -370,29 +371,30 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 // What a row's single values make of its statistics.
 struct RowOut {
-  float lp, term, kl, cut, coef;
+  float lp, term, kl, cut, coef, gap;   // gap: lp less the reference's
 };
 template <int MODE, class W>
 __device__ __forceinline__ RowOut row_out(const Rows& a, bool live, float xy, float adv, float old, float ref, W weight,
                                           Stat& st) {
-  RowOut o{0.f, 0.f, 0.f, 0.f, 0.f};
+  RowOut o{0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (!live) return o;
   if (st.m == INFINITY) st.m = NAN;   // no distribution
   const float over = above(st.m, a.c);
-  o.lp = (xy - st.m) * a.inv_temp - (logf(st.S) + kLn2 * over);
+  const LogProb lp = log_prob(xy, st, over, a.inv_temp);
+  o.lp = lp.value();
   st.S *= ex2(over);   // from here on against the maximum itself, as the gradient takes it
+  o.gap = lp.less(ref);
   if (MODE == kPolicy) {
     const Policy& p = a.p;
-    const float ratio = expf(o.lp - old);
+    const float ratio = expf(lp.less(old));
     const float bound = fminf(fmaxf(ratio, p.lo), p.hi);
     const bool off = (adv > 0.f && ratio > p.hi) || (adv < 0.f && ratio < p.lo);
     const float ra = ratio * adv, ba = bound * adv;
     o.term = -(ra < ba || ra != ra ? ra : ba);
     o.coef = off ? 0.f : -ra;
     if (p.ref != nullptr) {
-      const float gap = ref - o.lp;
-      const float q = expm1f(gap);
-      o.kl = q - gap;
+      const float q = expm1f(-o.gap);
+      o.kl = q + o.gap;
       if (p.kl != 0.f) {
         o.term += p.kl * o.kl;
         o.coef -= p.kl * q;
@@ -411,6 +413,7 @@ __device__ __forceinline__ void write_row(const Rows& a, int64_t t, const RowOut
   a.logps[t] = o.lp;
   if (MODE == kStats && a.stats != nullptr) {
     a.stats[t] = st;
+    a.gap[t] = o.gap;
     a.coef[t] = 0.f;
     if (t == 0) *a.done = 0;
   }
@@ -512,10 +515,10 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     for (int d = 0; d < DEPTH; ++d) load(d);
     if (scalar >= 0) xs = x[scalar];
     if (y < a.V) xy = Vec<T>::get(x[y]);
+    if (a.p.ref != nullptr) ref = a.p.ref[t];
     if (MODE == kPolicy) {
       adv = a.p.adv[t];
       old = a.p.old[t];
-      if (a.p.ref != nullptr) ref = a.p.ref[t];
       if (alone && WARP) share = weight_of(a.y, a.p.offsets, a.T, a.p.S, t);
       if (alone && !WARP && warp == (int)blockDim.x / 32 - 1) {   // (the first warp has the rest to do)
         share = weight_of(a.y, a.p.offsets, a.T, a.p.S, t);
@@ -882,7 +885,7 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ Rows 
 // rows.  Latency is all there is to it, so long sequences get a CTA.
 template <int GROUP>
 __global__ void __launch_bounds__(256)
-    pair_kernel(const int64_t* y, const float* logps, const float* ref, const int64_t* offsets, int64_t T, int64_t P,
+    pair_kernel(const int64_t* y, const float* gap, const int64_t* offsets, int64_t T, int64_t P,
                 double inv_pairs, double beta, double smoothing, int average, float* ratios, float* margins,
                 double* pair_loss, float* coef, unsigned* done, float* loss) {
   __shared__ double red[32];
@@ -901,7 +904,7 @@ __global__ void __launch_bounds__(256)
       int count = 0;
       for (int64_t t = at[k] + tid; t < at[k + 1]; t += GROUP) {
         const int64_t yt = y[t];
-        const float d = logps[t] - ref[t];
+        const float d = gap[t];
         if (yt >= 0) {
           sum += (double)d;
           ++count;
@@ -1179,7 +1182,7 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
   a->ld = ld;
   a->y = y;
   a->c = scale;
-  a->inv_temp = (float)(1.0 / temperature);
+  a->inv_temp = two_floats(1.0 / temperature);
   a->logps = logps;
   if (grad) {
     if (T > 0 && gld < V) return NMD_ERR_INVALID;
@@ -1218,8 +1221,8 @@ nmd_status nmd_token_logprobs(const void* d_logits, int32_t dtype, int64_t T, in
 
 nmd_status nmd_preference_workspace_bytes(int64_t T, int64_t P, size_t* bytes) {
   if (T < 0 || T > kMaxRows || P < 1 || P > kMaxRows || !bytes) return NMD_ERR_INVALID;
-  *bytes = align256((size_t)T * sizeof(Stat)) + align256((size_t)T * sizeof(float)) + align256((size_t)P * sizeof(double)) +
-           256;
+  *bytes = align256((size_t)T * sizeof(Stat)) + 2 * align256((size_t)T * sizeof(float)) +
+           align256((size_t)P * sizeof(double)) + 256;
   return NMD_OK;
 }
 
@@ -1243,6 +1246,9 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
   w += align256((size_t)T * sizeof(Stat));
   a.coef = (float*)w;
   w += align256((size_t)T * sizeof(float));
+  a.gap = (float*)w;
+  w += align256((size_t)T * sizeof(float));
+  a.p.ref = d_reference;
   double* pair_loss = (double*)w;
   a.done = (unsigned*)(w + align256((size_t)P * sizeof(double)));
   if (T > 0) {
@@ -1252,8 +1258,8 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
   }
   const bool large = T > 128 * P;   // long sequences
   const int64_t grid = std::min<int64_t>(large ? P : (P + 7) / 8, 1024);
-  if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, d_targets, (const float*)d_logps,
-             d_reference, d_offsets, T, P, 1.0 / (double)P, beta, smoothing, (int)average, d_ratios, d_margins, pair_loss,
+  if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, d_targets, (const float*)a.gap,
+             d_offsets, T, P, 1.0 / (double)P, beta, smoothing, (int)average, d_ratios, d_margins, pair_loss,
              d_grad ? a.coef : (float*)nullptr, a.done, d_loss) != cudaSuccess)
     return NMD_ERR_CUDA;
   return d_grad && T > 0 ? launch_grad(dtype, a, s) : NMD_OK;

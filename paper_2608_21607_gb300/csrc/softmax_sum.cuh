@@ -11,7 +11,7 @@
 
 namespace nmd {
 
-constexpr float kLn2 = 0.693147180559945309f;
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr double kLog2e = 1.4426950408889634074;
 
 // 2^x by the SFU (results below 2^-126 become 0, which no sum of
@@ -76,6 +76,12 @@ __device__ __forceinline__ pair_t power2(pair_t x, float m, Scale c) {
   const float2 e = halves(exponent2(x, m, c));
   return pair_of(ex2(e.x), ex2(e.y));
 }
+inline float2 two_floats(double v) {
+  float2 t;
+  t.x = (float)v;
+  t.y = (float)(v - (double)t.x);
+  return t;
+}
 // c of a temperature; false if it is not a positive number of ordinary size
 inline bool scale_of(double temperature, Scale* s) {
   if (!(temperature > 0.0)) return false;
@@ -113,6 +119,33 @@ __device__ __forceinline__ float rescale(float m, float to, Scale c) {
   if (m == to) return 1.f;
   const float d = m - to;
   return ex2(fmaf(d, c.hi, d * c.lo) + (above(m, c) - above(to, c)));
+}
+// log p = (x - m) / tau - ln S - ln2 above(m) as hi + lo, for 1 / tau = it.x + it.y:
+// its distance from a reference is much smaller than log p itself, and would show
+// the roundings of one fp32 value.  (In fp64 it cost the policy loss 3 %.)
+struct LogProb {
+  float hi, lo;
+  __device__ __forceinline__ float value() const { return hi + lo; }
+  __device__ __forceinline__ float less(float reference) const { return (hi - reference) + lo; }
+};
+__device__ __forceinline__ LogProb log_prob(float x, Stat st, float over, float2 it) {
+  int k = 0;
+  float f = frexpf(st.S, &k);   // S = f 2^k, f near 1
+  if (f < 0.7f) {
+    f *= 2.f;
+    --k;
+  }
+  constexpr float ln2_lo = (float)(kLn2 - (double)(float)kLn2);
+  const float d = x - st.m, t = d - x, kf = (float)k;
+  const float d_lo = (x - (d - t)) - (st.m + t);   // what the difference rounds away
+  const float p = d * it.x, p_lo = fmaf(d, it.x, -p) + fmaf(d, it.y, d_lo * it.x);
+  const float q = kf * (float)kLn2, q_lo = fmaf(kf, (float)kLn2, -q) + kf * ln2_lo;
+  LogProb o;
+  o.hi = p - q;
+  const float u = o.hi - p;
+  o.lo = (p - (o.hi - u)) - (q + u) + (p_lo - q_lo) - fmaf(over, (float)kLn2, log1pf(f - 1.f));
+  if (!(fabsf(o.hi) < INFINITY)) o.lo = st.S > 0.f ? 0.f : NAN;   // (no sum: no distribution)
+  return o;
 }
 // Merges over groups of `width` lanes (a power of two); every lane of a group
 // gets the same result.
