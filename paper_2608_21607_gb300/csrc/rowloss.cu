@@ -848,14 +848,37 @@ __global__ void __launch_bounds__(1024) terms_kernel(const float* terms, int64_t
   if (threadIdx.x == 0) stats[blockIdx.x] = (float)s;
 }
 
+struct Pairs {
+  const int64_t* offsets;   // 2 P + 1
+  int64_t P;
+  double inv_pairs, beta, smoothing;
+  int average;
+  float *ratios, *margins;  // 2 P, P
+  double* loss_of;          // P
+  float* loss;
+};
+
+// The mean of the pairs' losses, by one CTA.
+__device__ __forceinline__ void mean_loss(const Pairs& q, double* red) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < q.P; i += blockDim.x) s += __ldcg(q.loss_of + i);
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) *q.loss = (float)(s * q.inv_pairs);
+}
+
 // The gradient rows from the statistics and coefficients of earlier kernels:
 // one warp per row, or `pieces` CTAs per row of 4 vectors per thread.  The rows
 // are taken from the last to the first: the statistics pass read those last,
-// and part of them is still in L2.
+// and part of them is still in L2.  The first CTA takes the mean of the losses
+// along, which nothing has to wait for.
 template <class T, bool WARP>
-__global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ Rows a, unsigned pieces) {
+__global__ void __launch_bounds__(256)
+    grad_kernel(const __grid_constant__ Rows a, const __grid_constant__ Pairs q, unsigned pieces) {
   constexpr int N = Vec<T>::N, K = 4;
+  __shared__ double red[32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x == 0) mean_loss(q, red);
   const int64_t rows = WARP ? 8 : 1;
   const int64_t t = a.T - 1 - (WARP ? (int64_t)blockIdx.x * rows + (threadIdx.x >> 5) : blockIdx.x / pieces);
   if (t < 0) return;
@@ -882,63 +905,86 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ Rows 
 
 // One warp (GROUP 32) or one CTA (GROUP 256) per pair: the two sequences' sums
 // of log ratios, the margin, the pair's loss and the coefficient of each of its
-// rows.  Latency is all there is to it, so long sequences get a CTA.
+// rows.  Latency is all there is to it, so long sequences get a CTA.  Without a
+// gradient the CTA that finishes last takes the mean of the losses.
 template <int GROUP>
-__global__ void __launch_bounds__(256)
-    pair_kernel(const int64_t* y, const float* gap, const int64_t* offsets, int64_t T, int64_t P,
-                double inv_pairs, double beta, double smoothing, int average, float* ratios, float* margins,
-                double* pair_loss, float* coef, unsigned* done, float* loss) {
-  __shared__ double red[32];
+__global__ void __launch_bounds__(256) pair_kernel(const __grid_constant__ Rows a, const __grid_constant__ Pairs q) {
+  __shared__ double red[2][32];
+  __shared__ int count_of[2][8];
   constexpr int per = 256 / GROUP;   // pairs at a time per CTA
   const int tid = threadIdx.x % GROUP;
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int64_t p = (int64_t)blockIdx.x * per + threadIdx.x / GROUP; p < P; p += (int64_t)gridDim.x * per) {
+  for (int64_t p = (int64_t)blockIdx.x * per + threadIdx.x / GROUP; p < q.P; p += (int64_t)gridDim.x * per) {
     int64_t at[3];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) at[k] = border(offsets, 2 * p + k, T);
-    double ratio[2], share[2];
+    for (int k = 0; k < 3; ++k) at[k] = border(q.offsets, 2 * p + k, a.T);
+    // both sequences together, so that their loads and sums overlap
+    double sum[2] = {0.0, 0.0};
+    int n[2] = {0, 0};
+#pragma unroll 4
+    for (int64_t t = at[0] + tid; t < at[2]; t += GROUP) {
+      const int64_t yt = a.y[t];
+      const float d = a.gap[t];
+      const bool live = yt >= 0, second = t >= at[1];
+      sum[0] += live && !second ? (double)d : 0.0;
+      sum[1] += live && second ? (double)d : 0.0;
+      n[0] += live && !second;
+      n[1] += live && second;
+    }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      double sum = 0.0;
-      int count = 0;
-      for (int64_t t = at[k] + tid; t < at[k + 1]; t += GROUP) {
-        const int64_t yt = y[t];
-        const float d = gap[t];
-        if (yt >= 0) {
-          sum += (double)d;
-          ++count;
+    for (int o = 16; o > 0; o >>= 1) {
+      const double s0 = __shfl_xor_sync(0xffffffffu, sum[0], o), s1 = __shfl_xor_sync(0xffffffffu, sum[1], o);
+      sum[0] += s0;
+      sum[1] += s1;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) n[k] = __reduce_add_sync(0xffffffffu, n[k]);
+    if (GROUP != 32) {
+      const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+      __syncthreads();
+      if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          red[k][warp] = sum[k];
+          count_of[k][warp] = n[k];
         }
       }
-      double n = (double)count;
-      sum = GROUP == 32 ? warp_sum(sum) : block_sum(sum, red);
-      n = GROUP == 32 ? warp_sum(n) : block_sum(n, red);
-      share[k] = average && n > 1.0 ? 1.0 / n : 1.0;
-      ratio[k] = sum * share[k];
-    }
-    const double h = beta * (ratio[0] - ratio[1]);
-    // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|), in fp32 from here on
-    const float hf = (float)h, l = log1pf(expf(-fabsf(hf)));
-    const double down = (double)(fmaxf(-hf, 0.f) + l), up = (double)(fmaxf(hf, 0.f) + l);
-    if (tid == 0) {
-      ratios[2 * p] = (float)ratio[0];
-      ratios[2 * p + 1] = (float)ratio[1];
-      margins[p] = (float)h;
-      pair_loss[p] = smoothing > 0.0 ? (1.0 - smoothing) * down + smoothing * up : down;   // no 0 x inf
-    }
-    if (coef == nullptr) continue;
-    const double gain = beta * (smoothing - (double)(1.f / (1.f + expf(hf)))) * inv_pairs;
+      __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float g = (float)((k ? -gain : gain) * share[k]);
-      for (int64_t t = at[k] + tid; t < at[k + 1]; t += GROUP) coef[t] = y[t] >= 0 ? g : 0.f;
+      for (int k = 0; k < 2; ++k) {
+        sum[k] = 0.0;
+        n[k] = 0;
+        for (int w = 0; w < 8; ++w) {
+          sum[k] += red[k][w];
+          n[k] += count_of[k][w];
+        }
+      }
+    }
+    double share[2] = {1.0, 1.0};
+    if (q.average) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) share[k] = 1.0 / (double)max(n[k], 1);
+    }
+    const double ratio[2] = {sum[0] * share[0], sum[1] * share[1]};
+    const double h = q.beta * (ratio[0] - ratio[1]);
+    const float hf = (float)h;
+    if (a.grad != nullptr) {
+      const double gain = q.beta * (q.smoothing - (double)(1.f / (1.f + expf(hf)))) * q.inv_pairs;
+      const float g[2] = {(float)(gain * share[0]), (float)(-gain * share[1])};
+      for (int64_t t = at[0] + tid; t < at[2]; t += GROUP) a.coef[t] = a.y[t] >= 0 ? g[t >= at[1]] : 0.f;
+    }
+    if (tid == 0) {
+      // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|), in fp32 from here on
+      const float l = log1pf(expf(-fabsf(hf)));
+      const double down = (double)(fmaxf(-hf, 0.f) + l), up = (double)(fmaxf(hf, 0.f) + l);
+      q.ratios[2 * p] = (float)ratio[0];
+      q.ratios[2 * p + 1] = (float)ratio[1];
+      q.margins[p] = hf;
+      q.loss_of[p] = q.smoothing > 0.0 ? (1.0 - q.smoothing) * down + q.smoothing * up : down;   // no 0 x inf
     }
   }
-  if (!last_cta(done)) return;
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < P; i += blockDim.x) s += __ldcg(pair_loss + i);
-  s = block_sum(s, red);
-  if (threadIdx.x == 0) *loss = (float)(s * inv_pairs);
+  if (a.grad == nullptr && last_cta(a.done)) mean_loss(q, red[0]);
 }
 
 // Each row's share of the policy loss: 1 / (live rows), or 1 / (sequences x
@@ -1138,25 +1184,25 @@ nmd_status launch_rows(int dtype, const Rows& a, cudaStream_t s) {
 }
 
 template <class T>
-nmd_status launch_grad_t(const Rows& a, cudaStream_t s) {
+nmd_status launch_grad_t(const Rows& a, const Pairs& q, cudaStream_t s) {
   const int64_t nvec = a.V / Vec<T>::N;
   const int sms = num_sms();
   if (sms == 0) return NMD_ERR_CUDA;
   cudaError_t e;
   if (nvec <= 256 || (nvec <= 1024 && a.T >= 16 * sms)) {
-    e = launch(grad_kernel<T, true>, (a.T + 7) / 8, 256, 0, 1, true, s, a, 1u);
+    e = launch(grad_kernel<T, true>, (a.T + 7) / 8, 256, 0, 1, true, s, a, q, 1u);
   } else {
     const int64_t pieces = (nvec + 4 * 256 - 1) / (4 * 256);
-    e = launch(grad_kernel<T, false>, a.T * pieces, 256, 0, 1, true, s, a, (unsigned)pieces);
+    e = launch(grad_kernel<T, false>, a.T * pieces, 256, 0, 1, true, s, a, q, (unsigned)pieces);
   }
   return e == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
-nmd_status launch_grad(int dtype, const Rows& a, cudaStream_t s) {
+nmd_status launch_grad(int dtype, const Rows& a, const Pairs& q, cudaStream_t s) {
   switch (dtype) {
-    case NMD_DT_FP32: return launch_grad_t<float>(a, s);
-    case NMD_DT_BF16: return launch_grad_t<bf16>(a, s);
-    default: return launch_grad_t<__half>(a, s);
+    case NMD_DT_FP32: return launch_grad_t<float>(a, q, s);
+    case NMD_DT_BF16: return launch_grad_t<bf16>(a, q, s);
+    default: return launch_grad_t<__half>(a, q, s);
   }
 }
 
@@ -1249,20 +1295,19 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
   a.gap = (float*)w;
   w += align256((size_t)T * sizeof(float));
   a.p.ref = d_reference;
-  double* pair_loss = (double*)w;
+  const Pairs q{d_offsets, P, 1.0 / (double)P, beta, smoothing, (int)average, d_ratios, d_margins, (double*)w, d_loss};
   a.done = (unsigned*)(w + align256((size_t)P * sizeof(double)));
   if (T > 0) {
     if ((st = launch_rows<kStats>(dtype, a, s)) != NMD_OK) return st;   // zeroes the count too
-  } else if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) {
-    return NMD_ERR_CUDA;
+  } else {
+    a.grad = nullptr;   // no rows: no gradient pass
+    if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) return NMD_ERR_CUDA;
   }
   const bool large = T > 128 * P;   // long sequences
   const int64_t grid = std::min<int64_t>(large ? P : (P + 7) / 8, 1024);
-  if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, d_targets, (const float*)a.gap,
-             d_offsets, T, P, 1.0 / (double)P, beta, smoothing, (int)average, d_ratios, d_margins, pair_loss,
-             d_grad ? a.coef : (float*)nullptr, a.done, d_loss) != cudaSuccess)
+  if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, a, q) != cudaSuccess)
     return NMD_ERR_CUDA;
-  return d_grad && T > 0 ? launch_grad(dtype, a, s) : NMD_OK;
+  return a.grad ? launch_grad(dtype, a, q, s) : NMD_OK;
 }
 
 nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes) {

@@ -380,6 +380,53 @@ def test_large_batches(shape):
     check_grad(r.grad, x, y, lp, want["coef"], dcoef, want["grad"], dtype, 0.9)
 
 
+# many short pairs, some longer ones, empty ones, rows before the first and past the last
+SHORT = [  # P, rows per pair, V, pad, shift, dtype
+    (1230, 2, 2101, 0, 1, "bf16"), (310, 7, 2300, 0, 0, "fp32"), (160, 2, 30011, 0, 3, "fp16"),
+    (80, 2, 60001, 7, 0, "bf16"), (40, 2, 139255, 0, 0, "bf16"), (310, 3, 5000, 4, 2, "fp32"), (45, 1, 100003, 0, 1, "fp32"),
+]
+
+
+@pytest.mark.parametrize("even", [True, False], ids=["even", "ragged"])
+@pytest.mark.parametrize("shape", SHORT, ids=lambda s: "x".join(map(str, s)))
+def test_short_pairs(shape, even):
+    P, each, V, pad, shift, dtype = shape
+    T = P * each
+    rng = np.random.default_rng(P + V)
+    if even:
+        borders = np.minimum(np.arange(2 * P + 1) * each // 2 + (1 if each == 1 else 0), T)
+    else:
+        borders = np.sort(np.minimum(rng.integers(2, T, 2 * P + 1), T - 3))
+        borders[9:14] = borders[14] if borders[14] < T - 40 else borders[9]   # empty pairs, then one of 29 rows
+        borders[15:] = np.maximum(borders[15:], borders[14] + 29)
+    for average, smoothing, temperature, masked in ((False, 0.0, 1.0, 0.0), (True, 0.15, 1.4, 0.4)):
+        g, x, y = make_logits(T + V, T, V, dtype, pad=pad, shift=shift, masked=masked)
+        lp = O.tuning.token_logprobs(x, y, temperature)
+        ref = np.float32(lp + 0.4 * rng.standard_normal(T))
+        beta = 0.3
+        want = O.tuning.preference_loss(x, y, borders, ref, beta, smoothing, average, temperature)
+        given = np.where(y >= 0, ref, np.float32(np.nan))
+        runs = [tuning().preference_loss(g, cuda(y, torch.int64), cuda(borders, torch.int64), cuda(given), beta=beta,
+                                         label_smoothing=smoothing, average=average, temperature=temperature)
+                for _ in range(2)]
+        r = runs[0]
+        for a, b in zip(*runs):
+            assert torch.equal(a, b)
+        e = tol_lp(x, y, lp, temperature) + U * np.abs(lp)
+        check("logps", r.logps.cpu().numpy(), want["logps"], e)
+        K = 2 * P
+        n = [max(1, int((y[borders[k]:borders[k + 1]] >= 0).sum())) if average else 1 for k in range(K)]
+        er = np.array([e[borders[k]:borders[k + 1]].sum() / n[k] for k in range(K)])
+        check("ratios", r.ratios.cpu().numpy(), want["ratios"], er + 2 * U * np.abs(want["ratios"]) + 1e-12)
+        eh = beta * (er[0::2] + er[1::2])
+        check("margins", r.margins.cpu().numpy(), want["margins"], eh + 2 * U * np.abs(want["margins"]) + 1e-12)
+        check("loss", r.loss.cpu().numpy(), want["loss"], eh.mean() + 2 * U * abs(want["loss"]))
+        dcoef = np.zeros(T)
+        for k in range(K):
+            dcoef[borders[k]:borders[k + 1]] = beta / P * eh[k // 2] / 4 / n[k]
+        check_grad(r.grad, x, y, lp, want["coef"], dcoef, want["grad"], dtype, temperature)
+
+
 def test_all_rows_left_out():
     g, _, _ = make_logits(3, 20, 3000, "bf16")
     g.fill_(float("nan"))
