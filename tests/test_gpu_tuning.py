@@ -384,6 +384,7 @@ def test_large_batches(shape):
 SHORT = [  # P, rows per pair, V, pad, shift, dtype
     (1230, 2, 2101, 0, 1, "bf16"), (310, 7, 2300, 0, 0, "fp32"), (160, 2, 30011, 0, 3, "fp16"),
     (80, 2, 60001, 7, 0, "bf16"), (40, 2, 139255, 0, 0, "bf16"), (310, 3, 5000, 4, 2, "fp32"), (45, 1, 100003, 0, 1, "fp32"),
+    (610, 2, 25001, 0, 1, "bf16"), (305, 2, 60001, 7, 0, "fp16"), (610, 3, 12501, 0, 0, "fp32"), (152, 2, 139255, 0, 3, "bf16"),
 ]
 
 
