@@ -150,7 +150,7 @@ __device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e
   for (; i + (K - 1) * kThreads < p.nvec; i += K * kThreads) {
     uint4 v[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = xv[i + k * kThreads];
+    for (int k = 0; k < K; ++k) v[k] = __ldcs(xv + i + k * kThreads);   // read for the last time: room for what is written
 #pragma unroll
     for (int k = 0; k < K; ++k) put(v[k], i + k * kThreads);
   }
@@ -210,7 +210,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 }
 
 // The chunks are taken from the last to the first: the norm pass read those
-// last, and they are still in L2.
+// last, and they are still in L2.  They leave it as they are read (two tensors of
+// 8.9M fp32 elements: 39.3 us against 40.9 us where they stay; of 16M: 65.6
+// against 68.1).
 template <int K>
 __global__ void __launch_bounds__(kThreads, kScaleCtasPerSm)
     scale_kernel(const __grid_constant__ Table<K> tab, const double* parts, int nparts, double max_norm, int in_place,

@@ -1108,10 +1108,23 @@ cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
   return launch_row(row_kernel<T, false, MODE, 2, false>, (size_t)block * 128, a.T * cs, block, (unsigned)cs, late, s, a);
 }
 
-// CTAs of a streaming cluster, and whether a batch with its gradient streams
-int64_t stream_cluster(int64_t nvec) { return std::min<int64_t>(8, ((nvec + kSlotVec - 1) / kSlotVec + 8) / 9); }
-bool streams(int64_t nvec, int64_t T, int sms) {
-  const int64_t cs = stream_cluster(nvec);
+// CTAs of a streaming cluster of rows of `nvec` vectors: one or two where their
+// runs are at most nine of the ring's thirteen slots, else four or more, with
+// runs of at most nine slots, or six of fp32, which is written as fast as it comes
+// (V = 200,005, 2000 rows of bf16: 314 us by three CTAs, 286 by four; V =
+// 139,255, 2000 rows of fp32: 359 us by four, 335 by six).  Clusters of seven
+// and eight leave SMs idle (V = 120,000, 3000 rows of fp32: 421 us by six, 501
+// by eight) and are for rows that six cannot hold.
+int64_t stream_cluster(int64_t nvec, int es) {
+  for (int64_t cs = 1; cs <= 2; ++cs)
+    if (nvec <= cs * 9 * kSlotVec) return cs;
+  for (int64_t cs = 4; cs <= 6; ++cs)
+    if (nvec <= cs * (es == 4 ? 6 : 9) * kSlotVec) return cs;
+  return nvec <= 6 * 12 * kSlotVec ? 6 : 8;
+}
+// whether a policy batch with its gradient streams
+bool streams(int64_t nvec, int es, int64_t T, int sms) {
+  const int64_t cs = stream_cluster(nvec, es);
   return nvec > 3072 && T * cs >= 4 * sms && (nvec + kSlotVec - 1) / kSlotVec <= cs * kSlots;
 }
 
@@ -1126,12 +1139,11 @@ cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
       return launch_row(row_kernel<T, true, kPolicy, 2, true>, groups * 16384, (a.T + 7) / 8, 256, 1, late, s, a);
     return launch_row(row_kernel<T, true, kPolicy, 8, true>, groups * 16384, (a.T + 7) / 8, 256, 1, late, s, a);
   }
-  // Long rows in batches that fill the GPU: the streaming kernel, its clusters'
-  // runs at most nine of the ring's thirteen slots (V = 32768, 6103 rows: 158 us
-  // against 161 us by clusters of row_kernel; V = 139255: 163 us against 171 us;
-  // V = 16384: 198 us against 153 us).
-  int64_t cs = stream_cluster(nvec);
-  if (streams(nvec, a.T, sms)) {
+  // Long rows in batches that fill the GPU: the streaming kernel (V = 32768, 6103
+  // rows of bf16: 158 us against 161 us by clusters of row_kernel; V = 139255: 163
+  // us against 171 us; V = 16384: 198 us against 153 us).
+  int64_t cs = stream_cluster(nvec, sizeof(T));
+  if (streams(nvec, sizeof(T), a.T, sms)) {
     static std::atomic<int> ready[kMaxDevices], room[9][kMaxDevices];
     if (!per_device(ready, [] {
           return cudaFuncSetAttribute(policy_stream_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -1262,7 +1274,7 @@ nmd_status fill(const void* x, int32_t dtype, int64_t T, int64_t V, int64_t ld, 
 }
 
 bool policy_streams(int dtype, const Rows& a) {
-  return a.grad != nullptr && streams(a.V * dtype_bytes(dtype) / 16 + 1, a.T, num_sms());
+  return a.grad != nullptr && streams(a.V * dtype_bytes(dtype) / 16 + 1, dtype_bytes(dtype), a.T, num_sms());
 }
 
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
