@@ -158,17 +158,17 @@ def preference_loss(logits, targets, offsets, reference, *, beta: float = 0.1, l
     if offsets.numel() != 2 * P + 1 or P < 1:
         _invalid("offsets: 2 P + 1 borders of P >= 1 pairs are wanted, got %d" % offsets.numel())
     nbytes = _bytes_of_sizes("nmd_preference_workspace_bytes", T, P)
-    loss = torch.empty((), dtype=torch.float32, device=device)
-    # the workspace and the results in one tensor: an allocation costs more than a view
-    both = torch.empty(nbytes // 4 + T + 3 * P, dtype=torch.float32, device=device)
+    # the loss behind the workspace: an index costs less than an allocation (which costs less than a split)
+    both = torch.empty(nbytes // 4 + 1, dtype=torch.float32, device=device)
     ws = both.data_ptr()
-    at = ws + nbytes
+    logps = torch.empty(T, dtype=torch.float32, device=device)
+    ratios = torch.empty(2 * P, dtype=torch.float32, device=device)
+    margins = torch.empty(P, dtype=torch.float32, device=device)
     g = _grad_like(logits, T, V, ld) if grad else None
     _call(index, "nmd_preference_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), offsets.data_ptr(), P,
-          reference.data_ptr(), beta, label_smoothing, int(average), temperature, loss.data_ptr(), at, at + 4 * T,
-          at + 4 * (T + 2 * P), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
-    _, logps, ratios, margins = torch.split_with_sizes(both, (nbytes // 4, T, 2 * P, P))
-    return PreferenceLoss(loss, logps, ratios, margins, g)
+          reference.data_ptr(), beta, label_smoothing, int(average), temperature, ws + nbytes, logps.data_ptr(),
+          ratios.data_ptr(), margins.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
+    return PreferenceLoss(both[-1], logps, ratios, margins, g)
 
 
 def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, clip_low: float = 0.2,
@@ -197,17 +197,15 @@ def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, cl
         if S < 1:
             _invalid("offsets: S + 1 borders of S >= 1 sequences are wanted")
     nbytes = _bytes_of_sizes("nmd_policy_workspace_bytes", T)
-    both = torch.empty(nbytes // 4 + T + 3, dtype=torch.float32, device=device)   # the workspace and the results
+    both = torch.empty(nbytes // 4 + 3, dtype=torch.float32, device=device)   # the workspace, then three results
     ws = both.data_ptr()
-    at = ws + nbytes
+    logps = torch.empty(T, dtype=torch.float32, device=device)
     g = _grad_like(logits, T, V, ld) if grad else None
     _call(index, "nmd_policy_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old.data_ptr(),
           None if reference is None else reference.data_ptr(), advantages.data_ptr(),
           None if offsets is None else offsets.data_ptr(), S, clip_low, clip_high, kl_coef, temperature,
-          at + 4 * T, at, g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
-    _, logps, stats = torch.split_with_sizes(both, (nbytes // 4, T, 3))
-    loss, kl, clipped = stats.unbind()
-    return PolicyLoss(loss, logps, kl, clipped, g)
+          ws + nbytes, logps.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
+    return PolicyLoss(both[-3], logps, both[-2], both[-1], g)
 
 
 def _dense(x) -> bool:
