@@ -17,11 +17,12 @@
 // partial results in the order of the chunks and takes the dot product a_t . b_y
 // in fp32 on the CUDA cores.
 //
-// Bound by the epilogue: an element costs two packed products, an exponential
-// and half a packed addition, and its warps issue in 66 % of the cycles.  4096
-// rows of 139,255 columns at r = 64 in bf16: 134 us, 4.3e12 exponentials/s of the
-// 9.2e12 that the SFUs make, 545 TFLOP/s; 2047 rows of 20,000 columns at r = 32
-// in fp32: 29 us with packing and finish; 7 rows of 139,255 columns: 16 us.
+// Bound by the round trip of a TMEM buffer (products, commit, epilogue, release;
+// the SFUs work in half of the cycles): 4096 rows of 139,255 columns at r = 64 in
+// bf16 take 116 us with the finish, 4.9e12 exponentials/s of the 9.2e12 that the
+// SFUs make, 630 TFLOP/s; 2047 rows of 20,000 columns at r = 32 in fp32 27 us with
+// packing and finish; 7 rows of 139,255 columns 13 us.  Chunks of 64 columns
+// in eight buffers: 168 us, twice the products issued.
 //
 // Warp roles: warps 0-15 epilogue (four warpgroups taking chunks in turn; thread
 // t of each owns TMEM lane t = row t), warp 16 TMA and TMEM allocation, and the
@@ -60,7 +61,7 @@ struct Cfg {
   // Warps that issue MMAs, chunks in turn, each with a ring of stages of its own.
   // (One issues a chunk of 16-bit factors in about 1100 cycles beside the
   // epilogue's sixteen warps, more than the products take: 4096 rows of 139,255
-  // columns 169 us by one warp, 134 us by two.  The 24 MMAs and more of an fp32
+  // columns 169 us by one warp, 134 us by two at the time.  The 24 MMAs and more of an fp32
   // chunk cover that.)
   static constexpr int ISS = PIECES == 1 ? 2 : 1;
   static constexpr int THREADS = 32 * (kMmaWarp + ISS);
@@ -122,21 +123,35 @@ struct RowSum : RunningSum {
     lost = (sum - s.S) - y;
     s.S = sum;
   }
-  // 32 scores; get() gives them as pairs, again where the group is not a usual one
+  // `blocks` (at most four) times 32 scores; get(b, x) gives them as pairs, again
+  // where they are not usual ones.  One vote and one compensated addition for all
+  // (one for each 32 scores: 134 us instead of 119 for 4096 rows of 139,255
+  // columns); the loops are rolled, or the code of seven rows would take longer
+  // to arrive (16 us instead of 13) than it saves the 4096 (1.5 us).
   template <class G>
-  __device__ __forceinline__ void add(G get, Scale c) {
+  __device__ __forceinline__ void add(int blocks, G get, Scale c) {
     pair_t x[16];
     if (__all_sync(0xffffffffu, usual)) {   // (TMEM is read by whole warps)
-      get(x);
-      const float group = group_sum(x, c);
+      float group = 0.f;
+#pragma unroll 1
+      for (int b = 0; b < blocks; ++b) {
+        get(b, x);
+        group += group_sum(x, c);
+      }
       const bool fine = group < kHigh;
       if (fine) put(group);
       if (__all_sync(0xffffffffu, fine)) return;
-      get(x);
-      if (!fine) slow(x, c);
+#pragma unroll 1
+      for (int b = 0; b < blocks; ++b) {
+        get(b, x);
+        if (!fine) slow(x, c);
+      }
     } else {
-      get(x);
-      slow(x, c);
+#pragma unroll 1
+      for (int b = 0; b < blocks; ++b) {
+        get(b, x);
+        slow(x, c);
+      }
     }
   }
 
@@ -276,16 +291,14 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
   } else if (warp >= kMmaWarp) {
     const uint32_t me = warp - kMmaWarp;
     uint32_t aph = 0;
-    bool ok = true, first = true;
-    int64_t c = u0 - tile0 * p.C;
-    for (int64_t u = u0; u < u1 && ok; ++u) {
-      const uint32_t G = (uint32_t)(u - u0);
-      if (ARES && first) {   // by every issuer, so that none falls a phase behind
-        if (!(ok = conv_wait(b_afull, aph, abort_flag, status, 2))) break;
-        first = false;
-      }
-      if (G % C::ISS == me) {
-        const uint32_t lb = G % NB, use = G / C::ISS * p.npan;
+    bool ok = true;
+    int64_t c0 = u0 - tile0 * p.C;
+    for (int64_t u = u0; u < u1 && ok; c0 = 0) {   // the chunks of one tile of A after those of the other
+      const uint32_t G0 = (uint32_t)(u - u0), seg = (uint32_t)min(p.C - c0, u1 - u);
+      // by every issuer, so that none falls a phase behind
+      if (ARES && !(ok = conv_wait(b_afull, aph, abort_flag, status, 2))) break;
+      for (uint32_t i = (me - G0) % C::ISS; i < seg && ok; i += C::ISS) {
+        const uint32_t G = G0 + i, lb = G % NB, use = G / C::ISS * p.npan;
         if (!(ok = conv_wait(b_lfree + 8 * lb, ((G / NB) & 1u) ^ 1u, abort_flag, status, 4))) break;
         const uint32_t d = tmem + lb * BN;
         for (int k = 0; k < p.npan; ++k) {
@@ -315,12 +328,11 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
         if (!ok) break;
         commit_elect(b_lfull + 8 * lb);
       }
-      if (++c == p.C) {   // done with this tile of A
-        c = 0;
+      if (c0 + seg == p.C) {   // done with this tile of A
         if (ARES) commit_elect(b_aempty);
         aph ^= 1u;
-        first = true;
       }
+      u += seg;
     }
     commit_elect(b_drain + 8 * me);   // every MMA issued has to be over before TMEM is freed
     if (lane == 0) {
@@ -334,46 +346,46 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const Scale cc = p.c;
     RowSum run;
+    // a warpgroup has a TMEM buffer of its own, so that it sees every phase of its barrier
+    static_assert(NB == kGroups, "one TMEM buffer per epilogue warpgroup");
+    const uint32_t col = tmem + lane_base + wg * BN;
     bool ok = true;
-    int64_t tile = tile0, c = u0 - tile0 * p.C;
-    for (int64_t u = u0; u < u1 && ok; ++u) {
-      const int64_t G = u - u0;
-      if ((int)(G % kGroups) == wg) {
-        const int lb = (int)(G % NB);
-        if (!(ok = warp_wait(b_lfull + 8 * lb, (uint32_t)((G / NB) & 1), abort_flag, status, 7))) break;
+    int64_t tile = tile0, c0 = u0 - tile0 * p.C;
+    for (int64_t u = u0; u < u1; ++tile, c0 = 0) {
+      const uint32_t G0 = (uint32_t)(u - u0), seg = (uint32_t)min(p.C - c0, u1 - u);
+      const bool some = tile * BM + quarter * 32 < p.T;   // some row of this warp exists
+      for (uint32_t i = (wg - G0) % kGroups; i < seg; i += kGroups) {
+        if (!(ok = conv_wait(b_lfull + 8 * wg, ((G0 + i) / NB) & 1u, abort_flag, status, 7))) break;
         fence_after();
-        if (tile * BM + quarter * 32 < p.T) {   // some row of this warp exists
-          const int kv = (int)min((int64_t)BN, p.n - c * BN);
-          const uint32_t col = tmem + lane_base + lb * BN;
-#pragma unroll 1
-          for (int j = 0; j < kv; j += 32) {
-            if (kv >= j + 32) {
-              run.add([&](pair_t(&x)[16]) { tmem_pairs(col + j, x); }, cc);
-            } else {   // columns past the last count as -inf
-              run.add(
-                  [&](pair_t(&x)[16]) {
-                    tmem_pairs(col + j, x);
+        if (some) {
+          const int kv = (int)min((int64_t)BN, p.n - (c0 + i) * BN);
+          if (kv == BN) {
+            run.add(BN / 32, [&](int b, pair_t(&x)[16]) { tmem_pairs(col + 32 * b, x); }, cc);
+          } else {   // columns past the last count as -inf
+            run.add(
+                (kv + 31) / 32,
+                [&](int b, pair_t(&x)[16]) {
+                  tmem_pairs(col + 32 * b, x);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                      const float2 v = halves(x[i]);
-                      x[i] = pair_of(j + 2 * i < kv ? v.x : -INFINITY, j + 2 * i + 1 < kv ? v.y : -INFINITY);
-                    }
-                  },
-                  cc);
-            }
+                  for (int i = 0; i < 16; ++i) {
+                    const int k = 32 * b + 2 * i;
+                    const float2 v = halves(x[i]);
+                    x[i] = pair_of(k < kv ? v.x : -INFINITY, k + 1 < kv ? v.y : -INFINITY);
+                  }
+                },
+                cc);
           }
         }
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(b_lfree + 8 * lb);
+        if (lane == 0) mbar_arrive(b_lfree + 8 * wg);
       }
-      if (++c == p.C || u + 1 == u1) {   // the end of a tile, or of the run: hand over the row's partial result
-        const int64_t slot = blockIdx.x - owner(tile * p.C, p.W, gridDim.x);
-        p.parts[((tile * p.slots + slot) * kGroups + wg) * BM + quarter * 32 + lane] = run.s;
-        run = RowSum();
-        c = 0;
-        ++tile;
-      }
+      if (!ok) break;
+      // the end of a tile, or of the run: hand over the row's partial result
+      const int64_t slot = blockIdx.x - owner(tile * p.C, p.W, gridDim.x);
+      p.parts[((tile * p.slots + slot) * kGroups + wg) * BM + quarter * 32 + lane] = run.s;
+      run = RowSum();
+      u += seg;
     }
   }
   fence_before();
