@@ -93,15 +93,11 @@ def _call(index: int, name: str, *args):
         nmd._check(None, st, name)
 
 
-def _bytes(name: str, *args) -> int:
-    out = C.c_size_t(0)
-    nmd._check(None, getattr(nmd.lib(), name)(*args, C.byref(out)), name)
-    return out.value
-
-
 @functools.lru_cache(maxsize=256)
 def _bytes_of_sizes(name: str, *sizes) -> int:
-    return _bytes(name, *sizes)
+    out = C.c_size_t(0)
+    nmd._check(None, getattr(nmd.lib(), name)(*sizes, C.byref(out)), name)
+    return out.value
 
 
 def token_logprobs(logits, targets, *, temperature: float = 1.0) -> torch.Tensor:
@@ -132,10 +128,11 @@ def factor_logprobs(A, B, targets, *, temperature: float = 1.0) -> torch.Tensor:
         _invalid("A, B: 1 to 256 columns and at least one row of B are wanted")
     targets = _vector(targets, "targets", T, torch.int64, index)
     logps = torch.empty(T, dtype=torch.float32, device=device)
-    factors = (A.data_ptr(), *A.stride(), B.data_ptr(), *B.stride(), _DTYPES[A.dtype], T, n, r)
-    nbytes = _bytes("nmd_factor_workspace_bytes", *factors)
+    a, b, shape = A.data_ptr(), B.data_ptr(), (*B.stride(), _DTYPES[A.dtype], T, n, r)
+    # the size goes by the sizes, strides and alignments alone
+    nbytes = _bytes_of_sizes("nmd_factor_workspace_bytes", a & 15, *A.stride(), b & 15, *shape)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _call(index, "nmd_factor_logprobs", *factors, targets.data_ptr(), temperature, logps.data_ptr(), ws.data_ptr(),
+    _call(index, "nmd_factor_logprobs", a, *A.stride(), b, *shape, targets.data_ptr(), temperature, logps.data_ptr(), ws.data_ptr(),
           nbytes)
     return logps
 
