@@ -880,49 +880,85 @@ __device__ __forceinline__ void mean_loss(const Pairs& q, double* red) {
   if (threadIdx.x == 0) *q.loss = (float)(s * q.inv_pairs);
 }
 
-// The gradient rows from the statistics and coefficients of earlier kernels:
-// one warp per row, or `pieces` CTAs per row of 4 vectors per thread.  The rows
-// are taken from the last to the first: the statistics pass read those last,
-// and part of them is still in L2.  Bound by HBM: with the statistics pass and
-// the pairs between them 2048 rows of 139,255 bf16 columns take 269 us, 6.4 TB/s
-// over the three passes or 0.94 of a plain copy's rate.  The first CTA takes the mean of the losses
-// along, which nothing has to wait for.
-template <class T, bool WARP>
-__global__ void __launch_bounds__(256)
-    grad_kernel(const __grid_constant__ Rows a, const __grid_constant__ Pairs q, unsigned pieces) {
-  constexpr int N = Vec<T>::N, K = 4;
-  __shared__ double red[32];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (blockIdx.x == 0) mean_loss(q, red);
-  const int64_t rows = WARP ? 8 : 1;
-  const int64_t t = a.T - 1 - (WARP ? (int64_t)blockIdx.x * rows + (threadIdx.x >> 5) : blockIdx.x / pieces);
-  if (t < 0) return;
-  const int64_t y = a.y[t];
-  const float coef = y >= 0 ? a.coef[t] : 0.f;
-  const Stat st = a.stats[t];
-  const T* x = (const T*)a.x + t * a.ld;
-  T* g = (T*)a.grad + t * a.gld;
-  const Span sp = span_of(x, a.V);
-  const uint4* xv = (const uint4*)(x + sp.head);
-  const Slope d = slope_of<T>(y >= 0, coef, st, a.inv_temp, a.c);
-  const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, nthr = WARP ? 32 : blockDim.x;
-  const unsigned piece = WARP ? 0 : blockIdx.x % pieces;
-  const int64_t first = (int64_t)piece * K * nthr;
-  const int n = (int)(WARP ? sp.nvec : min((int64_t)K * nthr, sp.nvec - first));
-  const int64_t col = sp.head + first * N;
-  write_slope<T>(xv + first + tid, n, tid, nthr, g + col, d, a.c, y - col, a.same_phase, nthr);
-  if (piece == 0) {
-    const int64_t scalar = tid < sp.head ? tid
-                           : tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1;
-    if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(x[scalar], d, a.c, scalar == y));
+// The sums of the log ratios of pair rows [at0, at1) and [at1, at2) and their
+// numbers of live rows, by a warp or a CTA; every thread gets them.
+template <int GROUP>
+__device__ __forceinline__ void pair_sums(const Rows& a, const int64_t (&at)[3], double (&sum)[2], int (&n)[2],
+                                          double (*red)[32], int (*count_of)[8]) {
+  sum[0] = sum[1] = 0.0;
+  n[0] = n[1] = 0;
+  // both sequences together, so that their loads and sums overlap
+#pragma unroll 4
+  for (int64_t t = at[0] + threadIdx.x % GROUP; t < at[2]; t += GROUP) {
+    const int64_t yt = a.y[t];
+    const float d = a.gap[t];
+    const bool live = yt >= 0, second = t >= at[1];
+    sum[0] += live && !second ? (double)d : 0.0;
+    sum[1] += live && second ? (double)d : 0.0;
+    n[0] += live && !second;
+    n[1] += live && second;
   }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const double s0 = __shfl_xor_sync(0xffffffffu, sum[0], o), s1 = __shfl_xor_sync(0xffffffffu, sum[1], o);
+    sum[0] += s0;
+    sum[1] += s1;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) n[k] = __reduce_add_sync(0xffffffffu, n[k]);
+  if (GROUP != 32) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();
+    if (lane == 0) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        red[k][warp] = sum[k];
+        count_of[k][warp] = n[k];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      sum[k] = 0.0;
+      n[k] = 0;
+      for (int w = 0; w < 8; ++w) {
+        sum[k] += red[k][w];
+        n[k] += count_of[k][w];
+      }
+    }
+  }
+}
+
+// What a pair makes of them: with `write` its outputs; the coefficient of the
+// rows of each sequence.
+__device__ __forceinline__ float2 pair_out(const Pairs& q, int64_t p, const double (&sum)[2], const int (&n)[2],
+                                           bool write) {
+  double share[2] = {1.0, 1.0};
+  if (q.average) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) share[k] = 1.0 / (double)max(n[k], 1);
+  }
+  const double ratio[2] = {sum[0] * share[0], sum[1] * share[1]};
+  const double h = q.beta * (ratio[0] - ratio[1]);
+  const float hf = (float)h;
+  if (write) {
+    // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|), in fp32 from here on
+    const float l = log1pf(expf(-fabsf(hf)));
+    const double down = (double)(fmaxf(-hf, 0.f) + l), up = (double)(fmaxf(hf, 0.f) + l);
+    q.ratios[2 * p] = (float)ratio[0];
+    q.ratios[2 * p + 1] = (float)ratio[1];
+    q.margins[p] = hf;
+    q.loss_of[p] = q.smoothing > 0.0 ? (1.0 - q.smoothing) * down + q.smoothing * up : down;   // no 0 x inf
+  }
+  const double gain = q.beta * (q.smoothing - (double)(1.f / (1.f + expf(hf)))) * q.inv_pairs;
+  return {(float)(gain * share[0]), (float)(-gain * share[1])};
 }
 
 // One warp (GROUP 32) or one CTA (GROUP 256) per pair: the two sequences' sums
 // of log ratios, the margin, the pair's loss and the coefficient of each of its
 // rows.  Latency is all there is to it, so long sequences get a CTA (16 pairs of
-// 8191 rows: 216 us a call against 239 us by warps).  Without a
-// gradient the CTA that finishes last takes the mean of the losses.
+// 8191 rows: 216 us a call against 239 us by warps).  Without a gradient the CTA
+// that finishes last takes the mean of the losses.
 template <int GROUP>
 __global__ void __launch_bounds__(256) pair_kernel(const __grid_constant__ Rows a, const __grid_constant__ Pairs q) {
   __shared__ double red[2][32];
@@ -935,72 +971,98 @@ __global__ void __launch_bounds__(256) pair_kernel(const __grid_constant__ Rows 
     int64_t at[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) at[k] = border(q.offsets, 2 * p + k, a.T);
-    // both sequences together, so that their loads and sums overlap
-    double sum[2] = {0.0, 0.0};
-    int n[2] = {0, 0};
-#pragma unroll 4
-    for (int64_t t = at[0] + tid; t < at[2]; t += GROUP) {
-      const int64_t yt = a.y[t];
-      const float d = a.gap[t];
-      const bool live = yt >= 0, second = t >= at[1];
-      sum[0] += live && !second ? (double)d : 0.0;
-      sum[1] += live && second ? (double)d : 0.0;
-      n[0] += live && !second;
-      n[1] += live && second;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const double s0 = __shfl_xor_sync(0xffffffffu, sum[0], o), s1 = __shfl_xor_sync(0xffffffffu, sum[1], o);
-      sum[0] += s0;
-      sum[1] += s1;
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) n[k] = __reduce_add_sync(0xffffffffu, n[k]);
-    if (GROUP != 32) {
-      const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-      __syncthreads();
-      if (lane == 0) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          red[k][warp] = sum[k];
-          count_of[k][warp] = n[k];
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        sum[k] = 0.0;
-        n[k] = 0;
-        for (int w = 0; w < 8; ++w) {
-          sum[k] += red[k][w];
-          n[k] += count_of[k][w];
-        }
-      }
-    }
-    double share[2] = {1.0, 1.0};
-    if (q.average) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) share[k] = 1.0 / (double)max(n[k], 1);
-    }
-    const double ratio[2] = {sum[0] * share[0], sum[1] * share[1]};
-    const double h = q.beta * (ratio[0] - ratio[1]);
-    const float hf = (float)h;
-    if (a.grad != nullptr) {
-      const double gain = q.beta * (q.smoothing - (double)(1.f / (1.f + expf(hf)))) * q.inv_pairs;
-      const float g[2] = {(float)(gain * share[0]), (float)(-gain * share[1])};
-      for (int64_t t = at[0] + tid; t < at[2]; t += GROUP) a.coef[t] = a.y[t] >= 0 ? g[t >= at[1]] : 0.f;
-    }
-    if (tid == 0) {
-      // -log sigma(h) = max(-h, 0) + log(1 + e^-|h|), in fp32 from here on
-      const float l = log1pf(expf(-fabsf(hf)));
-      const double down = (double)(fmaxf(-hf, 0.f) + l), up = (double)(fmaxf(hf, 0.f) + l);
-      q.ratios[2 * p] = (float)ratio[0];
-      q.ratios[2 * p + 1] = (float)ratio[1];
-      q.margins[p] = hf;
-      q.loss_of[p] = q.smoothing > 0.0 ? (1.0 - q.smoothing) * down + q.smoothing * up : down;   // no 0 x inf
-    }
+    double sum[2];
+    int n[2];
+    pair_sums<GROUP>(a, at, sum, n, red, count_of);
+    const float2 g = pair_out(q, p, sum, n, tid == 0);
+    if (a.grad != nullptr)
+      for (int64_t t = at[0] + tid; t < at[2]; t += GROUP) a.coef[t] = a.y[t] < 0 ? 0.f : t < at[1] ? g.x : g.y;
   }
   if (a.grad == nullptr && last_cta(a.done)) mean_loss(q, red[0]);
+}
+
+// The coefficient of row t by one warp, and with `write`, where t is the first
+// row of its pair, the pair's outputs.
+__device__ __noinline__ float coef_of(const Rows& a, const Pairs& q, int64_t t, bool write) {
+  const int lane = threadIdx.x & 31;
+  unsigned in = 0;
+  int64_t p0 = 0;
+  for (; p0 < q.P; p0 += 32) {
+    const int64_t p = p0 + lane;
+    in = __ballot_sync(0xffffffffu, p < q.P && border(q.offsets, 2 * p, a.T) <= t && t < border(q.offsets, 2 * p + 2, a.T));
+    if (in) break;
+  }
+  if (!in) return 0.f;   // outside of the sequences
+  const int64_t p = p0 + __ffs(in) - 1;
+  int64_t at[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) at[k] = border(q.offsets, 2 * p + k, a.T);
+  double sum[2];
+  int n[2];
+  pair_sums<32>(a, at, sum, n, nullptr, nullptr);
+  const float2 g = pair_out(q, p, sum, n, write && t == at[0] && lane == 0);
+  return t < at[1] ? g.x : g.y;
+}
+
+// The gradient rows from the statistics and coefficients of earlier kernels:
+// one warp per row, or `pieces` CTAs per row of 4 vectors per thread.  The rows
+// are taken from the last to the first: the statistics pass read those last,
+// and part of them is still in L2.  Bound by HBM: with the statistics pass and
+// the pairs between them 2048 rows of 139,255 bf16 columns take 269 us, 6.4 TB/s
+// over the three passes or 0.94 of a plain copy's rate.  The first CTA takes the
+// mean of the losses along, which nothing has to wait for.  ALONE (small
+// batches): no kernel has dealt with the pairs; each row takes its coefficient
+// from its pair's log ratios itself, and the last CTA takes the mean.
+template <class T, bool WARP, bool ALONE>
+__global__ void __launch_bounds__(256)
+    grad_kernel(const __grid_constant__ Rows a, const __grid_constant__ Pairs q, unsigned pieces) {
+  constexpr int N = Vec<T>::N, K = 4;
+  __shared__ double red[32];
+  __shared__ float row_coef;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!ALONE && blockIdx.x == 0) mean_loss(q, red);
+  const int64_t rows = WARP ? 8 : 1;
+  const int64_t t = a.T - 1 - (WARP ? (int64_t)blockIdx.x * rows + (threadIdx.x >> 5) : blockIdx.x / pieces);
+  const unsigned piece = WARP ? 0 : blockIdx.x % pieces;
+  float coef = 0.f;
+  if (ALONE) {
+    if (blockIdx.x == 0) {   // pairs without rows
+      const double sum[2] = {0.0, 0.0};
+      const int n[2] = {0, 0};
+      for (int64_t p = threadIdx.x; p < q.P; p += blockDim.x)
+        if (border(q.offsets, 2 * p + 2, a.T) <= border(q.offsets, 2 * p, a.T)) pair_out(q, p, sum, n, true);
+    }
+    if (t >= 0 && (WARP || threadIdx.x < 32)) coef = coef_of(a, q, t, piece == 0);
+    if (!WARP) {
+      if (threadIdx.x == 0) row_coef = coef;
+      __syncthreads();
+      coef = row_coef;
+    }
+  } else if (t >= 0) {
+    coef = a.coef[t];
+  }
+  if (t >= 0) {
+    const int64_t y = a.y[t];
+    const Stat st = a.stats[t];
+    const T* x = (const T*)a.x + t * a.ld;
+    T* g = (T*)a.grad + t * a.gld;
+    const Span sp = span_of(x, a.V);
+    const uint4* xv = (const uint4*)(x + sp.head);
+    const Slope d = slope_of<T>(y >= 0, coef, st, a.inv_temp, a.c);
+    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, nthr = WARP ? 32 : blockDim.x;
+    const int64_t first = (int64_t)piece * K * nthr;
+    const int n = (int)(WARP ? sp.nvec : min((int64_t)K * nthr, sp.nvec - first));
+    const int64_t col = sp.head + first * N;
+    write_slope<T>(xv + first + tid, n, tid, nthr, g + col, d, a.c, y - col, a.same_phase, nthr);
+    if (piece == 0) {
+      const int64_t scalar = tid < sp.head ? tid
+                             : tid - sp.head < sp.tail ? sp.head + sp.nvec * N + tid - sp.head : -1;
+      if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(x[scalar], d, a.c, scalar == y));
+    }
+  }
+  if (ALONE) {
+    if (last_cta(a.done)) mean_loss(q, red);
+  }
 }
 
 // Each row's share of the policy loss: 1 / (live rows), or 1 / (sequences x
@@ -1212,26 +1274,41 @@ nmd_status launch_rows(int dtype, const Rows& a, cudaStream_t s) {
   }
 }
 
+// CTAs of the gradient pass: `pieces` per row, or one for 8 rows (0 pieces)
+unsigned grad_pieces(int64_t nvec, int64_t T, int sms) {
+  return nvec <= 256 || (nvec <= 1024 && T >= 16 * sms) ? 0 : (unsigned)((nvec + 4 * 256 - 1) / (4 * 256));
+}
+// Whether the gradient pass deals with the pairs too: in small batches of short
+// sequences, where all its CTAs run at the same time and each looks through few
+// pairs and rows.  Such calls wait for the host, and a launch less is worth more
+// than the row's own search (4 pairs, 160 rows of 4096 fp32 columns: 29 us a call
+// against 36, of which the device works 12.0 against 10.6).
+bool grad_alone(int64_t nvec, int64_t T, int64_t P, int sms) {
+  const int64_t pieces = grad_pieces(nvec, T, sms);
+  return T <= 1024 && P <= 128 && T <= 128 * P && (pieces ? T * pieces : (T + 7) / 8) <= 8 * sms;
+}
+
 template <class T>
-nmd_status launch_grad_t(const Rows& a, const Pairs& q, cudaStream_t s) {
+nmd_status launch_grad_t(const Rows& a, const Pairs& q, bool alone, cudaStream_t s) {
   const int64_t nvec = a.V / Vec<T>::N;
   const int sms = num_sms();
   if (sms == 0) return NMD_ERR_CUDA;
+  const unsigned pieces = grad_pieces(nvec, a.T, sms);
   cudaError_t e;
-  if (nvec <= 256 || (nvec <= 1024 && a.T >= 16 * sms)) {
-    e = launch(grad_kernel<T, true>, (a.T + 7) / 8, 256, 0, 1, true, s, a, q, 1u);
-  } else {
-    const int64_t pieces = (nvec + 4 * 256 - 1) / (4 * 256);
-    e = launch(grad_kernel<T, false>, a.T * pieces, 256, 0, 1, true, s, a, q, (unsigned)pieces);
-  }
+  if (pieces == 0)
+    e = launch(alone ? grad_kernel<T, true, true> : grad_kernel<T, true, false>, (a.T + 7) / 8, 256, 0, 1, true, s, a, q,
+               1u);
+  else
+    e = launch(alone ? grad_kernel<T, false, true> : grad_kernel<T, false, false>, a.T * pieces, 256, 0, 1, true, s, a, q,
+               pieces);
   return e == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
-nmd_status launch_grad(int dtype, const Rows& a, const Pairs& q, cudaStream_t s) {
+nmd_status launch_grad(int dtype, const Rows& a, const Pairs& q, bool alone, cudaStream_t s) {
   switch (dtype) {
-    case NMD_DT_FP32: return launch_grad_t<float>(a, q, s);
-    case NMD_DT_BF16: return launch_grad_t<bf16>(a, q, s);
-    default: return launch_grad_t<__half>(a, q, s);
+    case NMD_DT_FP32: return launch_grad_t<float>(a, q, alone, s);
+    case NMD_DT_BF16: return launch_grad_t<bf16>(a, q, alone, s);
+    default: return launch_grad_t<__half>(a, q, alone, s);
   }
 }
 
@@ -1332,11 +1409,13 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
     a.grad = nullptr;   // no rows: no gradient pass
     if (cudaMemsetAsync(a.done, 0, sizeof(unsigned), s) != cudaSuccess) return NMD_ERR_CUDA;
   }
+  const bool alone = a.grad && grad_alone(V * dtype_bytes(dtype) / 16, T, P, num_sms());
+  if (alone) return launch_grad(dtype, a, q, true, s);
   const bool large = T > 128 * P;   // long sequences
   const int64_t grid = std::min<int64_t>(large ? P : (P + 7) / 8, 1024);
   if (launch(large ? pair_kernel<256> : pair_kernel<32>, grid, 256, 0, 1, true, s, a, q) != cudaSuccess)
     return NMD_ERR_CUDA;
-  return a.grad ? launch_grad(dtype, a, q, s) : NMD_OK;
+  return a.grad ? launch_grad(dtype, a, q, false, s) : NMD_OK;
 }
 
 nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes) {
