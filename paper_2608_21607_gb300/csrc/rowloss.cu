@@ -1008,7 +1008,7 @@ __device__ __noinline__ float coef_of(const Rows& a, const Pairs& q, int64_t t, 
 // one warp per row, or `pieces` CTAs per row of 4 vectors per thread.  The rows
 // are taken from the last to the first: the statistics pass read those last,
 // and part of them is still in L2.  Bound by HBM: with the statistics pass and
-// the pairs between them 2048 rows of 139,255 bf16 columns take 269 us, 6.4 TB/s
+// the pairs between them 2048 rows of 139,255 bf16 columns take 267 us, 6.4 TB/s
 // over the three passes or 0.94 of a plain copy's rate.  The first CTA takes the
 // mean of the losses along, which nothing has to wait for.  ALONE (small
 // batches): no kernel has dealt with the pairs; each row takes its coefficient
