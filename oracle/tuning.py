@@ -32,9 +32,9 @@ def factor_logprobs(A, B, y, temperature=1.0):
 
 
 def logits_gradient(x, y, g, temperature=1.0):
-    """d[t, v] = g_t (1[v = y_t] - p_tv) / temperature, zero rows where y[t] < 0."""
+    """d[t, v] = g_t (1[v = y_t] - p_tv) / temperature, zero rows where y[t] < 0 or g_t = 0."""
     d = np.zeros(np.shape(x))
-    live = np.flatnonzero(np.asarray(y) >= 0)
+    live = np.flatnonzero((np.asarray(y) >= 0) & (np.asarray(g) != 0))
     if len(live):
         z = np.asarray(x, np.float64)[live] / temperature
         p = np.exp(z - _lse(z)[:, None])
@@ -95,7 +95,7 @@ def policy_loss(x, y, old, reference, advantages, offsets=None, clip_low=0.2, cl
     lp = token_logprobs(x, y, temperature)
     w = policy_weights(y, offsets)
     coef, loss, kl_sum, cut_sum = np.zeros(len(y)), 0.0, 0.0, 0.0
-    for t in np.flatnonzero(y >= 0):
+    for t in np.flatnonzero(w):                         # neither left out nor outside every sequence
         rho, A = np.exp(lp[t] - np.float64(old[t])), np.float64(advantages[t])
         cut = (A > 0 and rho > 1.0 + clip_high) or (A < 0 and rho < 1.0 - clip_low)
         term = -min(rho * A, min(max(rho, 1.0 - clip_low), 1.0 + clip_high) * A)

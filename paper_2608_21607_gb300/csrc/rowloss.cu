@@ -401,9 +401,10 @@ __device__ __forceinline__ RowOut row_out(const Rows& a, bool live, float xy, fl
       }
     }
     const float w = weight();
-    o.term *= w;
-    o.kl *= w;
-    o.coef *= w;
+    // a row outside every sequence takes no part, whatever it holds (0 x inf is no number)
+    o.term = w != 0.f ? o.term * w : 0.f;
+    o.kl = w != 0.f ? o.kl * w : 0.f;
+    o.coef = w != 0.f ? o.coef * w : 0.f;
     o.cut = off ? w : 0.f;
   }
   return o;

@@ -1,0 +1,81 @@
+"""The fine-tuning operators at their edges, against the fp64 oracle (oracle/tuning.py) or a property of the definition.
+
+Tolerances are those of test_gpu_tuning.py (counted from the formulas there) unless a test says otherwise.
+"""
+import numpy as np
+import pytest
+
+import oracle as O
+from gpu_common import require_gpu
+from test_gpu_tuning import DTYPES, HALF, NORM_TOL, U, check, check_grad, cuda, make_grads, make_logits, tol_lp, tuning
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    return require_gpu()
+
+
+def check_policy(r, x, y, lp, old, ref, adv, want, dtype, kl, temperature, borders=None):
+    """Loss, terms and gradient of a policy batch against the oracle's, with the tolerances of test_policy_loss."""
+    live = y >= 0
+    e = tol_lp(x, y, lp, temperature) + U * np.abs(lp)
+    w = O.tuning.policy_weights(y, borders)
+    rho = np.where(live, np.exp(np.where(adv != 0, lp - old, 0.0)), 0.0)
+    erho = rho * (e + U * (np.abs(lp) + np.abs(old) + 8))
+    gap = np.where(live, ref - lp, 0.0)
+    egap = e + U * (np.abs(gap) + np.abs(lp))
+    ek = np.abs(np.expm1(gap)) * egap + 8 * U * (np.exp(gap) + np.abs(gap))
+    eterm = w * (erho * np.abs(adv) + 4 * U * np.abs(rho * adv) + kl * ek)
+    check("loss", r.loss.cpu().numpy(), want["loss"], eterm.sum() + 2 * U * np.sum(w * (np.abs(rho * adv) + 1)))
+    check("kl", r.kl.cpu().numpy(), want["kl"], (w * ek).sum() + 4 * U * abs(want["kl"]))
+    check("clipped", r.clipped.cpu().numpy(), want["clipped"], 4 * U)
+    if r.grad is not None:
+        dcoef = w * (erho * np.abs(adv) + 4 * U * np.abs(rho * adv) + kl * (np.exp(gap) * egap + 8 * U * np.exp(gap)))
+        check_grad(r.grad, x, y, lp, want["coef"], dcoef, want["grad"], dtype, temperature)
+
+
+def policy_values(lp, rng):
+    """old, reference, advantages: ratios well away from the borders of the clipped range 0.8 to 1.3."""
+    T = len(lp)
+    return (np.float32(lp - rng.choice([-0.7, -0.1, 0.05, 0.6], T)), np.float32(lp + 0.4 * rng.standard_normal(T)),
+            np.float32(rng.standard_normal(T)))
+
+
+# a warp per row and a CTA per row, with and without a kernel of their own for the weights, and streamed rows
+OUTSIDE = [(50, 200, "fp32"), (40, 5000, "bf16"), (1100, 60, "fp16"), (1030, 3000, "fp32"), (620, 25000, "bf16")]
+
+
+@pytest.mark.parametrize("shape", OUTSIDE, ids=lambda s: "x".join(map(str, s)))
+def test_policy_rows_outside_every_sequence(shape):
+    """Live rows before the first border and past the last take no part, whatever they hold."""
+    T, V, dtype = shape
+    borders = [3, 3, T // 3, T - 4]
+    g, x, y = make_logits(T + V, T, V, dtype, masked=0.2)
+    rng = np.random.default_rng(T)
+    out = np.r_[0:3, T - 4:T]
+    y[out] = 1
+    x[out] = rng.standard_normal((len(out), V))
+    x[1, 1] = -200.0                       # log-probability -200 against a reference of 0: past fp32's range
+    x[T - 2] = np.nan
+    x[T - 1, 0] = np.inf
+    g.copy_(torch.from_numpy(np.float32(x)))
+    x = g.double().cpu().numpy()
+    inside = y.copy()
+    inside[out] = -1
+    lp = O.tuning.token_logprobs(x, inside, 0.9)
+    old, ref, adv = policy_values(lp, rng)
+    given = [np.where(inside >= 0, v, np.float32(np.nan)) for v in (old, ref, adv)]
+    for v, inf in zip(given, (-np.inf, np.inf, -np.inf)):
+        v[0], v[1], v[T - 4] = 0.0, 0.0, inf
+    given[2][1] = -1.0
+    given[0][2], given[2][2] = -1e9, -1.0  # a ratio past fp32's range
+    off = cuda(borders, torch.int64)
+    args = dict(clip_low=0.2, clip_high=0.3, kl_coef=0.2, temperature=0.9)
+    want = O.tuning.policy_loss(x, inside, old, ref, adv, borders, **args)
+    for grad in (True, False):
+        r = tuning().policy_loss(g, cuda(y, torch.int64), *map(cuda, given), offsets=off, grad=grad, **args)
+        check_policy(r, x, inside, lp, old, ref, adv, want, dtype, 0.2, 0.9, borders)

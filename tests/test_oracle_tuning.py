@@ -106,3 +106,19 @@ def test_clip_grad_norm():
     np.testing.assert_allclose(norm, 5e200)
     norm, _ = T.clip_grad_norm([np.array([3e-200, 4e-200])], 1.0)
     np.testing.assert_allclose(norm, 5e-200)
+
+
+def test_policy_rows_outside_every_sequence():
+    rng, x, y = _problem(6)
+    y[[0, 1, 21, 22]] = 2
+    lp = T.token_logprobs(x, y)
+    old, ref, adv = lp - 0.1, lp + 0.3, rng.standard_normal(23)
+    out, offsets = np.array([0, 1, 21, 22]), np.array([2, 9, 9, 21])
+    inside = y.copy()
+    inside[out] = -1
+    want = T.policy_loss(x, inside, old, ref, adv, offsets, kl_coef=0.1)
+    old[0], ref[1], adv[21], x[22] = np.nan, np.inf, -np.inf, np.nan
+    got = T.policy_loss(x, y, old, ref, adv, offsets, kl_coef=0.1)
+    for name in ("loss", "kl", "clipped", "coef"):
+        np.testing.assert_array_equal(got[name], want[name])
+    np.testing.assert_array_equal(got["grad"], want["grad"])
