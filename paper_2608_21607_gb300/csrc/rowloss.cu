@@ -386,10 +386,11 @@ __device__ __forceinline__ RowOut row_out(const Rows& a, bool live, float xy, fl
   o.gap = lp.less(ref);
   if (MODE == kPolicy) {
     const Policy& p = a.p;
-    const float ratio = expf(lp.less(old));
+    const float d = lp.less(old), ratio = expf(d);
     const float bound = fminf(fmaxf(ratio, p.lo), p.hi);
     const bool off = (adv > 0.f && ratio > p.hi) || (adv < 0.f && ratio < p.lo);
-    const float ra = ratio * adv, ba = bound * adv;
+    // without an advantage there is no term, also where exp(d) passes fp32's range
+    const float ra = adv == 0.f && d < INFINITY ? 0.f : ratio * adv, ba = bound * adv;
     o.term = -(ra < ba || ra != ra ? ra : ba);
     o.coef = off ? 0.f : -ra;
     if (p.ref != nullptr) {

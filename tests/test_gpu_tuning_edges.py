@@ -79,3 +79,22 @@ def test_policy_rows_outside_every_sequence(shape):
     for grad in (True, False):
         r = tuning().policy_loss(g, cuda(y, torch.int64), *map(cuda, given), offsets=off, grad=grad, **args)
         check_policy(r, x, inside, lp, old, ref, adv, want, dtype, 0.2, 0.9, borders)
+
+
+@pytest.mark.parametrize("shape", [(50, 200, "fp32"), (40, 5000, "bf16"), (1100, 60, "fp16"), (620, 25000, "bf16")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_policy_advantage_of_zero(shape):
+    """A row without an advantage has no first term, also where its ratio is past fp32's range."""
+    T, V, dtype = shape
+    g, x, y = make_logits(T + V, T, V, dtype, masked=0.2)
+    rng = np.random.default_rng(V)
+    lp = O.tuning.token_logprobs(x, y, 0.9)
+    old, ref, adv = policy_values(lp, rng)
+    none = rng.random(T) < 0.3
+    adv[none] = 0.0
+    old[none] = np.float32(lp[none] - 120.0)
+    args = dict(clip_low=0.2, clip_high=0.3, kl_coef=0.2, temperature=0.9)
+    want = O.tuning.policy_loss(x, y, old, ref, adv, **args)
+    # such a row's ratio still counts as it is: nothing of it is cut off
+    r = tuning().policy_loss(g, cuda(y, torch.int64), cuda(old), cuda(ref), cuda(adv), **args)
+    check_policy(r, x, y, lp, old, ref, adv, want, dtype, 0.2, 0.9)
