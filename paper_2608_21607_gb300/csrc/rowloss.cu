@@ -554,6 +554,9 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the weights are the previous kernel's
     return a.p.weight[t];
   };
+  // Rows left out have not waited.  Where all are, the grid would be over before the
+  // weights' kernel, which still writes to a workspace that the caller may reuse.
+  auto finish = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
   bool last = false;   // the batch's last row
   Slope d;
   if constexpr (WARP) {
@@ -567,7 +570,11 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     }
     last = __shfl_sync(0xffffffffu, last, 0);
     if (last) sum_terms<32>(a, nullptr);
-    if (MODE == kStats || a.grad == nullptr) return;
+    if (MODE == kStats) return;
+    if (a.grad == nullptr) {
+      finish();
+      return;
+    }
     d = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
   } else {
     if (lane == 0) red[warp] = st;
@@ -604,7 +611,10 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
     if (MODE == kStats) return;
     __syncthreads();
     if (shared_last) sum_terms<0>(a, dred);
-    if (a.grad == nullptr) return;
+    if (a.grad == nullptr) {
+      finish();
+      return;
+    }
     d = shared_slope;
   }
   T* g = (T*)a.grad + t * a.gld;
@@ -614,7 +624,7 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
   else
     write_slope<T>(xv + tid, n, tid, nthr, g + sp.head + v0 * N, d, a.c, target, a.same_phase, nthr);
   if (scalar >= 0) g[scalar] = Vec<T>::put(d.zero ? 0.f : slope_at(xs, d, a.c, scalar == y));
-  if (MODE == kPolicy) asm volatile("griddepcontrol.wait;" ::: "memory");   // rows left out have not waited
+  if (MODE == kPolicy) finish();
 }
 
 // The policy loss with its gradient for batches that fill the GPU: one

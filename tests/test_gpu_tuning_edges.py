@@ -98,3 +98,23 @@ def test_policy_advantage_of_zero(shape):
     # such a row's ratio still counts as it is: nothing of it is cut off
     r = tuning().policy_loss(g, cuda(y, torch.int64), cuda(old), cuda(ref), cuda(adv), **args)
     check_policy(r, x, y, lp, old, ref, adv, want, dtype, 0.2, 0.9)
+
+
+@pytest.mark.parametrize("shape", [(200_000, 2), (1500, 300), (1030, 9000)], ids=lambda s: "%dx%d" % s)
+def test_policy_without_gradient_of_rows_all_left_out(shape):
+    """Once the call's work on the stream is done, its workspace is free: what the caller writes there next stays."""
+    T, V = shape
+    x = torch.full((T, V), float("nan"), device="cuda", dtype=torch.bfloat16)
+    y = torch.full((T,), -1, device="cuda", dtype=torch.int64)
+    nan = torch.full((T,), float("nan"), device="cuda")
+    ends = torch.tensor([0, T // 3, T], device="cuda")
+    for off in (None, ends):
+        for _ in range(5):
+            p = tuning().policy_loss(x, y, nan, nan, nan, offsets=off, kl_coef=0.1, grad=False)
+            assert p.grad is None
+            kept = [float(v) for v in (p.loss, p.kl, p.clipped)], p.logps.any()
+            del p
+            tuning().policy_loss(x, y, nan, nan, nan, offsets=off, kl_coef=0.1, grad=False)
+            reused = [torch.full((n,), 5.0, device="cuda") for n in (T, 2 * T, 4 * T, 4 * T + 64, 4 * T + 131)]
+            assert all(bool((r == 5.0).all()) for r in reused)
+            assert kept[0] == [0.0, 0.0, 0.0] and not kept[1]
