@@ -767,7 +767,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(b_slopefree + 8 * (k % kSlopes));
         for (int c = 0; c < n; c += kSlotVec) {
-          if (!(ok = ring_wait(b_full + 8 * slot, phase, stop))) break;
+          // the whole warp goes on or gives up: it meets again below
+          if (!(ok = __all_sync(0xffffffffu, ring_wait(b_full + 8 * slot, phase, stop)))) break;
           const int64_t col = sp.head + (v0 + c) * N;
           write_slope<T>(ring + slot * kSlotVec + tid, min(kSlotVec, n - c), tid, kGroup, g + col, d, a.c, y - col,
                          a.same_phase, kGroup);
@@ -775,7 +776,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
           if (lane == 0) tc::mbar_arrive(b_empty + 8 * slot);
           advance();
         }
-        if (!__all_sync(0xffffffffu, ok)) break;
+        if (!ok) break;
       } else {
         write_slope<T>(nullptr, n, tid, kGroup, g + sp.head + v0 * N, d, a.c, -1, a.same_phase, kGroup);
       }
@@ -783,13 +784,14 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
     } else if (warp == kScalarWarp) {
       float xy = NAN, adv = 0.f, old = 0.f, ref = 0.f, w = 0.f;
       Stat st{0.f, 1.f};
+      bool room = true;   // for this row's slope
       if (live) {
         if (y < a.V) xy = Vec<T>::get(x[y]);
         adv = a.p.adv[t];
         old = a.p.old[t];
         w = a.p.weight[t];
         if (a.p.ref != nullptr) ref = a.p.ref[t];
-        ok = ring_wait(b_sum + 8 * (k & 1), (k >> 1) & 1u, stop);
+        ok = __all_sync(0xffffffffu, ring_wait(b_sum + 8 * (k & 1), (k >> 1) & 1u, stop));
         st = merge_lanes<8>(lane < kGroupWarps ? red[k & 1][lane] : Stat{-INFINITY, 0.f}, a.c);
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(b_sumfree + 8 * (k & 1));
@@ -808,17 +810,16 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
                          "f"(st.m), "f"(st.S), "r"(tobar)
                          : "memory");
           }
-          ok = ring_wait(bar, (k >> 1) & 1u, stop) && ok;
+          ok = __all_sync(0xffffffffu, ring_wait(bar, (k >> 1) & 1u, stop)) && ok;
           st = merge_lanes<8>(lane < (int)csize ? peers[k & 1][lane] : Stat{-INFINITY, 0.f}, a.c);
           if (!ok) st.m = st.S = NAN;
         }
-        if (lane < kGroupWarps) ok = ok && ring_wait(b_slopefree + 8 * (k % kSlopes), ((k / kSlopes) & 1u) ^ 1u, stop);
-        ok = __all_sync(0xffffffffu, ok);
+        room = __all_sync(0xffffffffu, ring_wait(b_slopefree + 8 * (k % kSlopes), ((k / kSlopes) & 1u) ^ 1u, stop));
       }
       const RowOut o = row_out<kPolicy>(a, live, xy, adv, old, ref, [&] { return w; }, st);
       if (lane == 0) {
         if (rank == 0) write_row<kPolicy>(a, t, o, st);
-        if (live) {
+        if (live && room) {
           slopes[k % kSlopes] = slope_of<T>(live, o.coef, st, a.inv_temp, a.c);
           tc::mbar_arrive(b_slope + 8 * (k % kSlopes));
         }
