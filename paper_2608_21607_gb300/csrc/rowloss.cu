@@ -1187,20 +1187,19 @@ cudaError_t launch_sums(Rows a, int64_t nvec, int sms, cudaStream_t s) {
 // runs are at most nine of the ring's thirteen slots, else four or more, with
 // runs of at most nine slots, or six of fp32, which is written as fast as it comes
 // (V = 200,005, 2000 rows of bf16: 314 us by three CTAs, 286 by four; V =
-// 139,255, 2000 rows of fp32: 359 us by four, 335 by six).  Clusters of seven
-// and eight leave SMs idle (V = 120,000, 3000 rows of fp32: 421 us by six, 501
-// by eight) and are for rows that six cannot hold.
+// 139,255, 2000 rows of fp32: 359 us by four, 335 by six).
+constexpr int64_t kMostCluster = 6;
 int64_t stream_cluster(int64_t nvec, int es) {
   for (int64_t cs = 1; cs <= 2; ++cs)
     if (nvec <= cs * 9 * kSlotVec) return cs;
-  for (int64_t cs = 4; cs <= 6; ++cs)
+  for (int64_t cs = 4; cs < kMostCluster; ++cs)
     if (nvec <= cs * (es == 4 ? 6 : 9) * kSlotVec) return cs;
-  return nvec <= 6 * 12 * kSlotVec ? 6 : 8;
+  return kMostCluster;
 }
-// whether a policy batch with its gradient streams
+// whether a policy batch with its gradient streams: long rows, which six CTAs hold
+// in twelve slots each, in batches that fill the GPU
 bool streams(int64_t nvec, int es, int64_t T, int sms) {
-  const int64_t cs = stream_cluster(nvec, es);
-  return nvec > 3072 && T * cs >= 4 * sms && (nvec + kSlotVec - 1) / kSlotVec <= cs * kSlots;
+  return nvec > 3072 && nvec <= kMostCluster * (kSlots - 1) * kSlotVec && T * stream_cluster(nvec, es) >= 4 * sms;
 }
 
 // A policy batch with its gradient.
@@ -1219,7 +1218,7 @@ cudaError_t launch_policy(Rows a, int64_t nvec, int sms, cudaStream_t s) {
   // us against 171 us; V = 16384: 198 us against 153 us).
   int64_t cs = stream_cluster(nvec, sizeof(T));
   if (streams(nvec, sizeof(T), a.T, sms)) {
-    static std::atomic<int> ready[kMaxDevices], room[9][kMaxDevices];
+    static std::atomic<int> ready[kMaxDevices], room[kMostCluster + 1][kMaxDevices];
     if (!per_device(ready, [] {
           return cudaFuncSetAttribute(policy_stream_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       (int)kRingBytes) == cudaSuccess ? 1 : 0;

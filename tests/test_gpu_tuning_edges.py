@@ -118,3 +118,31 @@ def test_policy_without_gradient_of_rows_all_left_out(shape):
             reused = [torch.full((n,), 5.0, device="cuda") for n in (T, 2 * T, 4 * T, 4 * T + 64, 4 * T + 131)]
             assert all(bool((r == 5.0).all()) for r in reused)
             assert kept[0] == [0.0, 0.0, 0.0] and not kept[1]
+
+
+# The streaming kernel's clusters: two, four, five and six CTAs a row in fp32 (from 36,864, 73,728, 98,304 and 122,880
+# columns on), five and six in 16 bits (from 294,912 and 368,640); rows that six CTAs cannot hold are kept by a cluster
+# of the row kernel (fp32 from 294,912 columns on) and, past what that holds, read twice
+CLUSTERS = [(310, 40001, 0, 1, "fp32", True), (160, 90001, 7, 0, "fp32", False), (125, 100003, 0, 3, "fp32", True),
+            (110, 139255, 9, 0, "fp32", True), (125, 300001, 0, 0, "bf16", True), (104, 370001, 0, 5, "fp16", False),
+            (80, 300001, 3, 0, "fp32", True), (2, 400001, 0, 1, "fp32", False), (2, 400000, 0, 0, "fp32", True),
+            (2, 900001, 0, 0, "bf16", True), (40, 400001, 0, 0, "fp32", False)]
+
+
+@pytest.mark.parametrize("shape", CLUSTERS, ids=lambda s: "x".join(map(str, s)))
+def test_policy_of_long_rows(shape):
+    T, V, pad, shift, dtype, sequences = shape
+    g, x, y = make_logits(V, T, V, dtype, pad=pad, shift=shift, banned=0.05, masked=0.3 if T > 2 else 0.0)
+    rng = np.random.default_rng(T)
+    lp = O.tuning.token_logprobs(x, y, 0.9)
+    old, ref, adv = policy_values(lp, rng)
+    borders = [0, T // 2, T // 2, T] if sequences else None
+    args = dict(clip_low=0.2, clip_high=0.3, kl_coef=0.2, temperature=0.9)
+    want = O.tuning.policy_loss(x, y, old, ref, adv, borders, **args)
+    off = cuda(borders, torch.int64) if sequences else None
+    given = [cuda(np.where(y >= 0, v, np.float32(np.nan))) for v in (old, ref, adv)]
+    runs = [tuning().policy_loss(g, cuda(y, torch.int64), *given, offsets=off, **args) for _ in range(2)]
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    check("logps", runs[0].logps.cpu().numpy(), lp, tol_lp(x, y, lp, 0.9) + U * np.abs(lp))
+    check_policy(runs[0], x, y, lp, old, ref, adv, want, dtype, 0.2, 0.9, borders)
