@@ -146,3 +146,24 @@ def test_policy_of_long_rows(shape):
         assert torch.equal(a, b)
     check("logps", runs[0].logps.cpu().numpy(), lp, tol_lp(x, y, lp, 0.9) + U * np.abs(lp))
     check_policy(runs[0], x, y, lp, old, ref, adv, want, dtype, 0.2, 0.9, borders)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_gradient_of_a_slice_takes_its_own_size(dtype):
+    """The gradient's rows are less than a 128-byte line longer than the logits', however far apart those lie."""
+    T, S, V = 6, 50, 1003
+    g, x, y = make_logits(5, T, V, dtype)
+    lp = O.tuning.token_logprobs(x, y)
+    es = g.element_size()
+    big = torch.zeros(T, S, V, dtype=g.dtype, device="cuda")
+    wide = torch.zeros(T, 40 * V, dtype=g.dtype, device="cuda")
+    for given in (big[:, -1, :], wide[:, :V], wide[:, 8:8 + V], wide.view(40 * T, V)[::40]):
+        given.copy_(g)
+        z = cuda(np.zeros(T))
+        want = O.tuning.preference_loss(x, y, [0, 2, 6], np.zeros(T), 0.1)
+        e = tol_lp(x, y, lp, 1.0) + U * np.abs(lp)
+        r = tuning().preference_loss(given, cuda(y, torch.int64), cuda([0, 2, 6], torch.int64), z, beta=0.1)
+        check_grad(r.grad, x, y, lp, want["coef"], np.full(T, 0.1 * 0.1 * e.sum()), want["grad"], dtype, 1.0)
+        p = tuning().policy_loss(given, cuda(y, torch.int64), z, None, z + 1)
+        for grad in (r.grad, p.grad):
+            assert grad.untyped_storage().nbytes() < T * (V * es + 128)
