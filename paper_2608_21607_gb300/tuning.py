@@ -159,17 +159,17 @@ def preference_loss(logits, targets, offsets, reference, *, beta: float = 0.1, l
     if offsets.numel() != 2 * P + 1 or P < 1:
         _invalid("offsets: 2 P + 1 borders of P >= 1 pairs are wanted, got %d" % offsets.numel())
     nbytes = _bytes_of_sizes("nmd_preference_workspace_bytes", T, P)
-    # the loss behind the workspace: an index costs less than an allocation (which costs less than a split)
-    both = torch.empty(nbytes // 4 + 1, dtype=torch.float32, device=device)
-    ws = both.data_ptr()
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    loss = torch.empty((), dtype=torch.float32, device=device)   # its own: a loss that is kept keeps nothing else
     logps = torch.empty(T, dtype=torch.float32, device=device)
     ratios = torch.empty(2 * P, dtype=torch.float32, device=device)
     margins = torch.empty(P, dtype=torch.float32, device=device)
     g = _grad_like(logits, T, V, ld) if grad else None
     _call(index, "nmd_preference_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), offsets.data_ptr(), P,
-          reference.data_ptr(), beta, label_smoothing, int(average), temperature, ws + nbytes, logps.data_ptr(),
-          ratios.data_ptr(), margins.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
-    return PreferenceLoss(both[-1], logps, ratios, margins, g)
+          reference.data_ptr(), beta, label_smoothing, int(average), temperature, loss.data_ptr(), logps.data_ptr(),
+          ratios.data_ptr(), margins.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0,
+          ws.data_ptr(), nbytes)
+    return PreferenceLoss(loss, logps, ratios, margins, g)
 
 
 def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, clip_low: float = 0.2,
@@ -198,15 +198,16 @@ def policy_loss(logits, targets, old, reference, advantages, *, offsets=None, cl
         if S < 1:
             _invalid("offsets: S + 1 borders of S >= 1 sequences are wanted")
     nbytes = _bytes_of_sizes("nmd_policy_workspace_bytes", T)
-    both = torch.empty(nbytes // 4 + 3, dtype=torch.float32, device=device)   # the workspace, then three results
-    ws = both.data_ptr()
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    stats = torch.empty(3, dtype=torch.float32, device=device)   # their own: results that are kept keep nothing else
     logps = torch.empty(T, dtype=torch.float32, device=device)
     g = _grad_like(logits, T, V, ld) if grad else None
     _call(index, "nmd_policy_loss", logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old.data_ptr(),
           None if reference is None else reference.data_ptr(), advantages.data_ptr(),
           None if offsets is None else offsets.data_ptr(), S, clip_low, clip_high, kl_coef, temperature,
-          ws + nbytes, logps.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0, ws, nbytes)
-    return PolicyLoss(both[-3], logps, both[-2], both[-1], g)
+          stats.data_ptr(), logps.data_ptr(), g.data_ptr() if grad else None, g.stride(0) if grad else 0,
+          ws.data_ptr(), nbytes)
+    return PolicyLoss(stats[0], logps, stats[1], stats[2], g)
 
 
 def _dense(x) -> bool:

@@ -167,3 +167,13 @@ def test_gradient_of_a_slice_takes_its_own_size(dtype):
         p = tuning().policy_loss(given, cuda(y, torch.int64), z, None, z + 1)
         for grad in (r.grad, p.grad):
             assert grad.untyped_storage().nbytes() < T * (V * es + 128)
+
+
+def test_small_results_hold_nothing_else():
+    """A scalar that is kept for a log does not keep the call's workspace."""
+    g, _, y = make_logits(2, 3000, 40, "bf16")
+    z, yt = cuda(np.zeros(3000)), cuda(y, torch.int64)
+    r = tuning().preference_loss(g, yt, cuda(np.arange(3001) - np.arange(3001) % 3000, torch.int64), z)
+    p = tuning().policy_loss(g, yt, z, z, z + 1, kl_coef=0.1)
+    for scalar in (r.loss, p.loss, p.kl, p.clipped):
+        assert scalar.dim() == 0 and scalar.untyped_storage().nbytes() <= 64
