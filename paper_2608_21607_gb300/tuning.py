@@ -257,4 +257,5 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
     _call(norm.get_device(), "nmd_clip_grad_norm", count, ptrs.buffer_info()[0], sizes.buffer_info()[0],
           kinds.buffer_info()[0], max_norm, None if out is None else optrs.buffer_info()[0], norm.data_ptr(),
           ws.data_ptr(), nbytes)
+    torch.autograd.graph.increment_version(outs)   # autograd has to know that a tensor it may have saved has changed
     return norm

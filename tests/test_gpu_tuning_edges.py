@@ -177,3 +177,25 @@ def test_small_results_hold_nothing_else():
     p = tuning().policy_loss(g, yt, z, z, z + 1, kl_coef=0.1)
     for scalar in (r.loss, p.loss, p.kl, p.clipped):
         assert scalar.dim() == 0 and scalar.untyped_storage().nbytes() <= 64
+
+
+def test_written_gradients_count_as_changed():
+    """Autograd finds that a tensor which it has saved was overwritten."""
+    x, y = torch.randn(300, device="cuda"), torch.randn(7, 5, device="cuda").t()
+    seen = [x._version, y._version]
+    tuning().clip_grad_norm([x, y], 0.1)
+    assert x._version > seen[0] and y._version > seen[1]
+    out, seen = torch.empty_like(x), x._version
+    was = out._version
+    tuning().clip_grad_norm([x], 0.1, out=[out])
+    assert out._version > was and x._version == seen
+    w = torch.randn(300, device="cuda", requires_grad=True)
+    saved = w * 1.0
+    loss = (saved * saved).sum()
+    tuning().clip_grad_norm([saved.detach()], 0.1)
+    with pytest.raises(RuntimeError):
+        loss.backward()
+    with torch.inference_mode():
+        z = torch.randn(300, device="cuda")
+        tuning().clip_grad_norm([z], 0.1)
+    assert abs(float(z.norm()) - 0.1) < 1e-5
