@@ -145,6 +145,9 @@ __device__ __forceinline__ LogProb log_prob(float x, Stat st, float over, float2
   const float u = o.hi - p;
   o.lo = (p - (o.hi - u)) - (q + u) + (p_lo - q_lo) - fmaf(over, (float)kLn2, log1pf(f - 1.f));
   if (!(fabsf(o.hi) < INFINITY)) o.lo = st.S > 0.f ? 0.f : NAN;   // (no sum: no distribution)
+  // No probability is above 1: roundings that say so, above all of a target's score
+  // that was not formed like those in the sum, would make log(1 - p) no number.
+  if (o.hi + o.lo > 0.f) o.hi = o.lo = 0.f;
   return o;
 }
 // Merges over groups of `width` lanes (a power of two); every lane of a group

@@ -199,3 +199,25 @@ def test_written_gradients_count_as_changed():
         z = torch.randn(300, device="cuda")
         tuning().clip_grad_norm([z], 0.1)
     assert abs(float(z.norm()) - 0.1) < 1e-5
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_log_probabilities_are_not_positive(dtype):
+    """Rows whose target has all of the probability: log(1 - p) of a log-probability above 0 would be no number."""
+    T, n, r = 400, 500, 64
+    rng = np.random.default_rng(3)
+    A = cuda(4.0 * rng.standard_normal((T, r))).to(DTYPES[dtype])
+    B = cuda(4.0 * rng.standard_normal((n, r))).to(DTYPES[dtype])
+    z = A.double() @ B.double().t()
+    y = z.argmax(1)
+    got = tuning().factor_logprobs(A, B, y)
+    assert (got <= 0).all() and (got > -50).any()
+    x = z.to(DTYPES[dtype])
+    y = x.double().argmax(1)
+    got = tuning().token_logprobs(x, y)
+    assert (got <= 0).all()
+    for V in (1, 3000):
+        x = torch.full((T, V), -60.0, device="cuda", dtype=DTYPES[dtype])
+        x[:, 0] = cuda(20.0 * rng.standard_normal(T)).to(x.dtype)
+        got = tuning().token_logprobs(x, torch.zeros_like(y), temperature=0.3)
+        assert (got <= 0).all()
