@@ -130,7 +130,7 @@ __device__ __noinline__ void chunk_squares(const T* x, int64_t e0, int64_t e1, S
 }
 
 template <class T, bool SAME>
-__device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e1, float scale) {
+__device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e1, float2 scale) {
   constexpr int N = 16 / sizeof(T), K = 8;
   const Piece p = piece_of(x, e0, e1);
   const uint4* xv = (const uint4*)(x + e0 + p.head);
@@ -138,7 +138,7 @@ __device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e
   auto put = [&](const uint4& v, int i) {
     uint4 w;
 #pragma unroll
-    for (int k = 0; k < N; ++k) from_float(as_float(((const T*)&v)[k]) * scale, (T*)&w + k);
+    for (int k = 0; k < N; ++k) from_float(as_float(((const T*)&v)[k]) * scale.x * scale.y, (T*)&w + k);
     if (SAME) {
       __stcs((uint4*)to + i, w);
     } else {
@@ -156,10 +156,10 @@ __device__ __noinline__ void chunk_scale(const T* x, T* o, int64_t e0, int64_t e
   }
   for (; i < p.nvec; i += kThreads) put(xv[i], i);
   const int s = single_of<T>(p);
-  if (s >= 0) from_float(as_float(x[e0 + s]) * scale, o + e0 + s);
+  if (s >= 0) from_float(as_float(x[e0 + s]) * scale.x * scale.y, o + e0 + s);
 }
 template <class T>
-__device__ __forceinline__ void scale_piece(const void* in, void* out, int64_t e0, int64_t e1, float scale) {
+__device__ __forceinline__ void scale_piece(const void* in, void* out, int64_t e0, int64_t e1, float2 scale) {
   // vectors on both sides where they start at the same offset from a 16-byte boundary
   if ((((uintptr_t)in ^ (uintptr_t)out) & 15) == 0) chunk_scale<T, true>((const T*)in, (T*)out, e0, e1, scale);
   else chunk_scale<T, false>((const T*)in, (T*)out, e0, e1, scale);
@@ -224,8 +224,11 @@ __global__ void __launch_bounds__(kThreads, kScaleCtasPerSm)
   const double norm = sqrt(cta_sum(sum, red));
   if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   // a norm that is not a number makes every gradient so
-  const float scale = norm <= max_norm ? 1.f : (float)(max_norm / norm);
-  if (in_place && scale == 1.f) return;
+  const double ratio = norm <= max_norm ? 1.0 : max_norm / norm;
+  // A ratio below fp32's normal numbers would lose bits: as the product of two.  (The
+  // first leaves every element normal whose scaled value is, and its own product exact.)
+  const float2 scale = ratio < 0x1p-126 ? make_float2(0x1p-100f, (float)(ratio * 0x1p100)) : make_float2(1.f, (float)ratio);
+  if (in_place && scale.y == 1.f) return;
   for (int64_t c = tab.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
     const int e = entry_of(tab, c);
     const int es = tab.dtype[e] == NMD_DT_FP32 ? 4 : 2;

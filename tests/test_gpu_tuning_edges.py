@@ -221,3 +221,19 @@ def test_log_probabilities_are_not_positive(dtype):
         x[:, 0] = cuda(20.0 * rng.standard_normal(T)).to(x.dtype)
         got = tuning().token_logprobs(x, torch.zeros_like(y), temperature=0.3)
         assert (got <= 0).all()
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1e-2, 1e-5, 1e-8])
+def test_scales_below_the_normal_range(kind, max_norm):
+    """max_norm / norm below fp32's smallest normal number: the scaled gradients keep their 24 bits."""
+    grads = make_grads(6, [1000, 77, 8193], [kind], 1e37)
+    old = [g.double().cpu().numpy() for g in grads]
+    norm, want = O.tuning.clip_grad_norm(old, max_norm)
+    assert max_norm / norm < 2.0 ** -126
+    out = [torch.empty_like(g) for g in grads]
+    tuning().clip_grad_norm(grads, max_norm, out=out)
+    tuning().clip_grad_norm(grads, max_norm)
+    for g, o, w in zip(grads, out, want):
+        assert torch.equal(g, o)
+        check("out", g.double().cpu().numpy(), w, (NORM_TOL + 4 * U + HALF[kind][0]) * np.abs(w) + 2.0 ** -126)
