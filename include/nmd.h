@@ -461,8 +461,9 @@ nmd_status nmd_policy_loss(const void* d_logits, int32_t dtype, int64_t T, int64
  * arrays of `count` entries, read before the call returns; the tensors are
  * contiguous, of any alignment of an element.  d_out NULL: in place (nothing
  * is written when the norm is within max_norm); otherwise each out[k] has its
- * gradient's type and is either the gradient itself or apart from every other
- * tensor.  d_norm: 1 fp32.  A norm that is NaN makes every gradient NaN; an
+ * gradient's type and is either the gradient itself or apart from it.  A
+ * tensor that is written overlaps no other one (NMD_ERR_INVALID).  d_norm: 1
+ * fp32.  A norm that is NaN makes every gradient NaN; an
  * infinite one makes its infinite entries NaN and the others 0.  The squares
  * neither overflow nor vanish over the whole range of fp32. */
 nmd_status nmd_clip_workspace_bytes(int64_t count, size_t* bytes);

@@ -22,6 +22,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "nmd_internal.cuh"
 
@@ -305,6 +307,33 @@ nmd_status run(int64_t count, const void* const* in, const int64_t* n, const int
   return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
 }
 
+// Whether each tensor that is written lies apart from every other one, read or
+// written: CTAs take the pieces of tensors in no order.
+struct Range {
+  uintptr_t from, to;
+};
+nmd_status apart(int64_t count, const void* const* in, const int64_t* n, const int32_t* dtype, void* const* out) {
+  const std::unique_ptr<Range[]> to(new (std::nothrow) Range[(size_t)count]);
+  if (!to) return NMD_ERR_CUDA;
+  auto range = [&](const void* x, int64_t k) {
+    return Range{(uintptr_t)x, (uintptr_t)x + (uintptr_t)n[k] * (dtype[k] == NMD_DT_FP32 ? 4 : 2)};
+  };
+  Range* end = to.get();
+  for (int64_t k = 0; k < count; ++k)
+    if (n[k] > 0) *end++ = range(out ? out[k] : in[k], k);
+  std::sort(to.get(), end, [](const Range& a, const Range& b) { return a.from < b.from; });
+  for (const Range* r = to.get() + 1; r < end; ++r)
+    if (r->from < r[-1].to) return NMD_ERR_INVALID;
+  if (out)
+    for (int64_t k = 0; k < count; ++k) {
+      if (n[k] == 0 || in[k] == out[k]) continue;
+      const Range r = range(in[k], k);   // against the first range that ends past its start
+      const Range* at = std::upper_bound(to.get(), end, r.from, [](uintptr_t v, const Range& a) { return v < a.to; });
+      if (at != end && at->from < r.to) return NMD_ERR_INVALID;
+    }
+  return NMD_OK;
+}
+
 // tensors per launch: the table is copied with every launch, so short lists take a small one
 constexpr int kSmallTable = 16, kTable = 512;
 
@@ -336,6 +365,7 @@ nmd_status nmd_clip_grad_norm(int64_t count, const void* const* d_grads, const i
     const uintptr_t in = (uintptr_t)d_grads[k], out = d_out ? (uintptr_t)d_out[k] : in;
     if (!in || !out || ((in | out) & mis)) return NMD_ERR_INVALID;
   }
+  if ((count > 1 || d_out) && (st = apart(count, d_grads, sizes, dtypes, d_out)) != NMD_OK) return st;
   if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
   double* parts = (double*)d_workspace;

@@ -226,7 +226,7 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
                    out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
     """Global 2-norm of ``grads`` (a scalar tensor), and the gradients scaled by min(1, max_norm / norm): in place, or
     into ``out`` (tensors of the gradients' types and sizes).  CUDA tensors of one device without gaps
-    (contiguous, or contiguous after a permutation of the dimensions)."""
+    (contiguous, or contiguous after a permutation of the dimensions); one that is written overlaps no other."""
     grads = list(grads)
     outs = grads if out is None else list(out)
     count, Tensor = len(grads), torch.Tensor

@@ -7,6 +7,7 @@ import pytest
 
 import oracle as O
 from gpu_common import require_gpu
+from paper_2608_21607_gb300 import nmd as N
 from test_gpu_tuning import DTYPES, HALF, NORM_TOL, U, check, check_grad, cuda, make_grads, make_logits, tol_lp, tuning
 
 pytestmark = pytest.mark.gpu
@@ -237,3 +238,25 @@ def test_scales_below_the_normal_range(kind, max_norm):
     for g, o, w in zip(grads, out, want):
         assert torch.equal(g, o)
         check("out", g.double().cpu().numpy(), w, (NORM_TOL + 4 * U + HALF[kind][0]) * np.abs(w) + 2.0 ** -126)
+
+
+def test_written_tensors_that_overlap_are_refused():
+    """A tensor that is written twice, or written while another is read from it, has no defined result."""
+    clip = tuning().clip_grad_norm
+    buf, other = torch.randn(4000, device="cuda"), torch.empty(4000, device="cuda")
+    was = buf.clone()
+    for grads, out in (([buf, buf], None), ([buf[:100], other, buf[99:200]], None),
+                       ([buf[:10], buf[20:30]], [other[:10], other[9:19]]),
+                       ([buf[:10], buf[10:20]], [buf[10:20], buf[:10]]),
+                       ([buf[:100]], [buf[1:101]]), ([buf[100:200], buf[300:400]], [other[:100], buf[150:250]])):
+        with pytest.raises(N.NmdError) as e:
+            clip(grads, 0.1, out=out)
+        assert e.value.status == N.NMD_ERR_INVALID
+    assert torch.equal(buf, was)
+    # neighbours, empty tensors anywhere, a gradient that is its own output, one that is read twice
+    clip([buf[:100], buf[50:50], buf[100:201], buf[201:]], 0.1)
+    assert abs(float(buf.norm()) - 0.1) < 1e-5
+    clip([buf[:100], buf[100:200]], 1e-3, out=[buf[:100], other[:100]])
+    assert abs(float((buf[:100].square().sum() + other[:100].square().sum()).sqrt()) - 1e-3) < 1e-7
+    clip([was, was], 1.0, out=[other[:4000], torch.empty_like(was)])
+    assert abs(float(other.norm()) - 0.5 ** 0.5) < 1e-5
