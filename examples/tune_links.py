@@ -7,7 +7,9 @@
    columns' log-probabilities with those of the fitted model (factor_logprobs,
    which stores no scores) and gives the scores' gradient, the factors'
    gradients are two matrix products, clip_grad_norm bounds them, and a plain
-   gradient step is taken.
+   gradient step is taken.  (Both rows of a pair are one cell's here, so that
+   their log-sum-exps cancel in the margin; pairs of different cells, or of
+   sequences over several, take the same calls.)
 3. Rewards: columns drawn from the model earn a reward where they are links;
    policy_loss with a KL term against the fitted model does the rest.
 
@@ -75,7 +77,7 @@ def tune(S, solver, steps: int, pairs: int, rate: float = 20.0, seed: int = 0) -
     rng = np.random.default_rng(seed)
     torch.manual_seed(seed)
     put = lambda v: torch.as_tensor(v, dtype=torch.int64, device="cuda")  # noqa: E731
-    report = {}
+    report = {"loss_before": solver.loss()["obj"]}
 
     # two sequences of one column per pair: present, absent
     offsets = torch.arange(2 * pairs + 1, device="cuda")

@@ -23,3 +23,13 @@ def test_tune_links():
     assert r["preference_loss"] < 0.69            # below that of the unchanged model, log 2
     assert r["reward_after"] > r["reward_before"]
     assert r["kl"] >= 0.0 and r["loss_after"] < 100.0
+
+
+def test_tuned_factors_still_complete_the_matrix():
+    """The steps are bounded (clipped to a norm of 1, rates 20 and 80, far below the factors' own norm) and the rewards
+    held to the fitted model by the KL term: the completion's objective rises by less than a tenth."""
+    require_gpu()
+    import tune_links
+
+    r = tune_links.main(["--cells", "2048", "--steps", "40", "--pairs", "256"])
+    assert r["loss_before"] > 0.0 and r["loss_after"] < 1.1 * r["loss_before"]
