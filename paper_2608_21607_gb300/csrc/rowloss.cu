@@ -653,11 +653,26 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
+// The test of a phase that other CTAs of the cluster complete: what they sent is seen
+// after an acquire of the cluster's scope (the plain test acquires within the CTA).
+__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait (2 s); false once any wait of this CTA has run out.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
-  if (tc::mbar_try_wait(bar, parity)) return true;
+  auto done = [&] { return CLUSTER ? try_wait_cluster(bar, parity) : tc::mbar_try_wait(bar, parity); };
+  if (done()) return true;
   const uint64_t t0 = tc::globaltimer_ns();
-  while (!tc::mbar_try_wait(bar, parity)) {
+  while (!done()) {
     if (*stop) return false;
     if (tc::globaltimer_ns() - t0 > tc::kTimeoutNs) {
       *stop = 1;
@@ -810,7 +825,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
                          "f"(st.m), "f"(st.S), "r"(tobar)
                          : "memory");
           }
-          ok = __all_sync(0xffffffffu, ring_wait(bar, (k >> 1) & 1u, stop)) && ok;
+          ok = __all_sync(0xffffffffu, ring_wait<true>(bar, (k >> 1) & 1u, stop)) && ok;
           st = merge_lanes<8>(lane < (int)csize ? peers[k & 1][lane] : Stat{-INFINITY, 0.f}, a.c);
           if (!ok) st.m = st.S = NAN;
         }
