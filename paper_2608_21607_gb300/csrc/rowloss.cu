@@ -782,8 +782,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(b_slopefree + 8 * (k % kSlopes));
         for (int c = 0; c < n; c += kSlotVec) {
-          // the whole warp goes on or gives up: it meets again below
-          if (!(ok = __all_sync(0xffffffffu, ring_wait(b_full + 8 * slot, phase, stop)))) break;
+          // A lane whose wait ran out stays with its warp, which meets below, to the row's end;
+          // what it writes there counts for nothing.  A vote instead: 398.5
+          // us for the case above, 395.9 without.
+          ok = ring_wait(b_full + 8 * slot, phase, stop) && ok;
           const int64_t col = sp.head + (v0 + c) * N;
           write_slope<T>(ring + slot * kSlotVec + tid, min(kSlotVec, n - c), tid, kGroup, g + col, d, a.c, y - col,
                          a.same_phase, kGroup);
@@ -791,7 +793,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
           if (lane == 0) tc::mbar_arrive(b_empty + 8 * slot);
           advance();
         }
-        if (!ok) break;
+        if (!__all_sync(0xffffffffu, ok)) break;
       } else {
         write_slope<T>(nullptr, n, tid, kGroup, g + sp.head + v0 * N, d, a.c, -1, a.same_phase, kGroup);
       }
