@@ -447,7 +447,8 @@ nmd_status nmd_preference_loss(const void* d_logits, int32_t dtype, int64_t T, i
  *   and rho_t < lo.
  * d_stats: 3 fp32: loss, sum w_t k_t, sum of w_t over the rows cut off.
  * d_reference may be NULL if kl_coef is 0 (k_t then counts as 0).  clip_low in
- * [0, 1], clip_high >= 0, kl_coef >= 0.  d_logps: T; d_grad may be NULL. */
+ * [0, 1], clip_high >= 0, kl_coef >= 0.  d_logps: T; d_grad may be NULL.  A
+ * wait in the kernel that runs out (2 s) makes all of d_stats NaN. */
 nmd_status nmd_policy_workspace_bytes(int64_t T, size_t* bytes);
 nmd_status nmd_policy_loss(const void* d_logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                            const int64_t* d_targets, const float* d_old, const float* d_reference,

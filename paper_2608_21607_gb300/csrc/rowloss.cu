@@ -870,7 +870,12 @@ __global__ void __launch_bounds__(kStreamThreads, 1) policy_stream_kernel(const 
   if (csize > 1) {   // no CTA's shared memory goes away while a peer may write to it
     cluster_arrive();
     cluster_wait();
-    if (*stop) {     // (a CTA whose wait ran out has not waited for what peers had sent it)
+  } else {
+    __syncthreads();
+  }
+  if (*stop) {   // some rows have no gradient, whatever their terms: the loss says so
+    if (threadIdx.x < 3) a.p.terms[threadIdx.x * a.T + t0] = NAN;
+    if (csize > 1) {   // (a CTA whose wait ran out has not waited for what peers had sent it)
       const uint64_t from = tc::globaltimer_ns();
       while (tc::globaltimer_ns() - from < 100000ull) {
       }
