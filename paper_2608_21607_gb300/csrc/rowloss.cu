@@ -11,8 +11,9 @@
 // range where a row is masked with the type's lowest value.)  m and S come
 // from one pass with a running maximum: a thread keeps its own (m, S),
 // rescales S when a group of vectors raises m, and the threads' pairs are
-// merged in a fixed order.  All sums are fp32; the only rounding to fewer bits is that of
-// the gradient to the logits' type, once, when it is stored.
+// merged in a fixed order.  A row's sum of powers is fp32, sums over the rows of a
+// sequence or batch are fp64; the only rounding to fewer bits is that of the gradient
+// to the logits' type, once, when it is stored.
 //
 // Everything here is bound by HBM: a row is read once (twice where the
 // gradient's coefficient depends on other rows) and its gradient written once.
