@@ -8,8 +8,13 @@
 //
 // 16-bit factors are multiplied as they are.  fp32 factors are split into three
 // bf16 pieces each (x = hi + lo + lo2 to 2^-24 of x), and the six products of
-// pieces above 2^-24 are accumulated in fp32: hi hi, hi lo, lo hi, lo lo,
-// hi lo2, lo2 hi.
+// pieces above 2^-24 are accumulated in fp32: lo lo, lo2 hi, hi lo2, lo hi and
+// hi lo of all columns, and only then hi hi.  The tensor cores round every
+// accumulation towards zero by up to a unit of the sum so far, so the five small
+// products are taken while that is small (scores of 100 at r = 256 come out
+// 1.25e-4 low on average in the order of the columns, 9e-6 in this one).  Past
+// one panel of 64 columns the hi pieces are loaded again for it: 2047 rows of
+// 20,000 columns at r = 128 take 60.5 us instead of 53.5, at r = 64 35.1 and 34.5.
 //
 // The tiles x chunks are dealt to one CTA per SM in equal contiguous runs, so
 // that any T and n fill the GPU; a run that crosses into the next tile of rows
@@ -68,6 +73,9 @@ struct Cfg {
   static constexpr int RST = PIECES == 1 ? 8 / ISS : 2;   // stages of a ring: a power of two
   static constexpr int NST = ISS * RST;
   static constexpr int NB = 512 / BN;       // TMEM buffers
+  // Stages that a chunk of `npan` panels passes through: of fp32 factors the hi pieces of
+  // all panels but the last come again together, once the small products are there.
+  static __device__ __forceinline__ int uses(int npan) { return PIECES > 1 && npan > 1 ? npan + 1 : npan; }
   static constexpr int NBAR = 2 * NST + 2 * NB + 2 + ISS;
   static constexpr size_t SMEM = 1024 + A_BYTES + (size_t)NST * STAGE + NBAR * 8 + 64;
   static_assert(SMEM <= 227 * 1024, "shared memory per block");
@@ -226,6 +234,7 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
 
   const int64_t u0 = blockIdx.x * p.W / gridDim.x, u1 = (blockIdx.x + 1) * p.W / gridDim.x;
   const int64_t tile0 = u0 / p.C;
+  const int uses = C::uses(p.npan);
 
   if (warp == kTmaWarp) {
     if (lane == 0) {
@@ -248,17 +257,24 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
           ++aloads;
           first = false;
         }
-        const uint32_t G = (uint32_t)(u - u0), use = G / C::ISS * p.npan;
-        for (int k = 0; k < p.npan; ++k) {
+        const uint32_t G = (uint32_t)(u - u0), use = G / C::ISS * uses;
+        for (int k = 0; k < uses; ++k) {
           const int s = (int)(G % C::ISS) * RST + (int)((use + k) % RST);
           if (!(ok = wait_bar(b_empty + 8 * s, (((use + k) / RST) & 1u) ^ 1u, abort_flag, status, 1))) break;
-          const uint32_t dst = st_sm + s * C::STAGE, bar = b_full + 8 * s;
+          const uint32_t dst = st_sm + s * C::STAGE, da = dst + PIECES * kPanelB, bar = b_full + 8 * s;
+          if (PIECES > 1 && k == p.npan) {
+            mbar_expect_tx(bar, (p.npan - 1) * (kPanelB + (ARES ? 0 : kPanelA)));
+            for (int h = 0; h < p.npan - 1; ++h) {
+              tma_load_2d(dst + h * kPanelB, &tb0, bar, 64 * h, (int)(c * BN));
+              if (!ARES) tma_load_2d(da + h * kPanelA, &ta0, bar, 64 * h, (int)(tile * BM));
+            }
+            break;
+          }
           mbar_expect_tx(bar, C::STAGE);
           tma_load_2d(dst, &tb0, bar, 64 * k, (int)(c * BN));
           if (PIECES > 1) tma_load_2d(dst + kPanelB, &tb1, bar, 64 * k, (int)(c * BN));
           if (PIECES > 1) tma_load_2d(dst + 2 * kPanelB, &tb2, bar, 64 * k, (int)(c * BN));
           if (!ARES) {
-            const uint32_t da = dst + PIECES * kPanelB;
             tma_load_2d(da, &ta0, bar, 64 * k, (int)(tile * BM));
             if (PIECES > 1) tma_load_2d(da + kPanelA, &ta1, bar, 64 * k, (int)(tile * BM));
             if (PIECES > 1) tma_load_2d(da + 2 * kPanelA, &ta2, bar, 64 * k, (int)(tile * BM));
@@ -274,9 +290,9 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
       if (!ok) {   // wait for the copies in flight before shared memory goes away
         for (int i = 0; i < NST; ++i) {   // (a stage that never gets its phase is given up after 0.1 s)
           const uint32_t ring = (uint32_t)(i / RST), chunks = (uint32_t)((done + C::ISS - 1 - ring) / C::ISS);
-          const uint32_t uses = chunks * p.npan;   // of this ring; the last use of its stage i % RST:
-          if (uses <= (uint32_t)(i % RST)) continue;
-          const uint32_t last = (uses - 1 - i % RST) / RST;
+          const uint32_t total = chunks * uses;   // of this ring; the last use of its stage i % RST:
+          if (total <= (uint32_t)(i % RST)) continue;
+          const uint32_t last = (total - 1 - i % RST) / RST;
           const uint64_t t0 = globaltimer_ns();
           while (!mbar_try_wait(b_full + 8 * i, last & 1u) && globaltimer_ns() - t0 < 100000000ull) {
           }
@@ -298,29 +314,36 @@ __global__ void __launch_bounds__((Cfg<PIECES, ARES>::THREADS), 1)
       // by every issuer, so that none falls a phase behind
       if (ARES && !(ok = conv_wait(b_afull, aph, abort_flag, status, 2))) break;
       for (uint32_t i = (me - G0) % C::ISS; i < seg && ok; i += C::ISS) {
-        const uint32_t G = G0 + i, lb = G % NB, use = G / C::ISS * p.npan;
+        const uint32_t G = G0 + i, lb = G % NB, use = G / C::ISS * uses;
         if (!(ok = conv_wait(b_lfree + 8 * lb, ((G / NB) & 1u) ^ 1u, abort_flag, status, 4))) break;
         const uint32_t d = tmem + lb * BN;
-        for (int k = 0; k < p.npan; ++k) {
+        for (int k = 0; k < uses; ++k) {
           const uint32_t s = me * RST + (use + k) % RST;
           if (!(ok = conv_wait(b_full + 8 * s, ((use + k) / RST) & 1u, abort_flag, status, 3))) break;
           fence_after();
-          const uint32_t bs = st_sm + s * C::STAGE;
-          const uint64_t db = sdesc(bs, 16, 1024, SWZ_128B);
-          const uint64_t da = sdesc(ARES ? a_sm + k * PIECES * kPanelA : bs + PIECES * kPanelB, 16, 1024, SWZ_128B);
-          const int steps = min(4, (p.r - 64 * k + 15) / 16);
-          for (int q = 0; q < steps; ++q) {
-            const uint32_t acc = (k | q) != 0;
-            if (PIECES == 1) {
-              mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, acc);
-            } else {
+          const uint32_t bs = st_sm + s * C::STAGE, as = bs + PIECES * kPanelB;
+          const bool again = PIECES > 1 && k == p.npan;   // the hi pieces of the panels before the last
+          if (!again) {
+            const uint64_t db = sdesc(bs, 16, 1024, SWZ_128B);
+            const uint64_t da = sdesc(ARES ? a_sm + k * PIECES * kPanelA : as, 16, 1024, SWZ_128B);
+            const int steps = min(4, (p.r - 64 * k + 15) / 16);
+            if (PIECES > 1) {
               constexpr uint64_t A = kPanelA >> 4, B = kPanelB >> 4;
-              mma_ss_elect(d, da + 2 * q + A, db + 2 * q + B, p.idesc, acc);          // lo lo
-              mma_ss_elect(d, da + 2 * q + 2 * A, db + 2 * q, p.idesc, 1);            // lo2 hi
-              mma_ss_elect(d, da + 2 * q, db + 2 * q + 2 * B, p.idesc, 1);            // hi lo2
-              mma_ss_elect(d, da + 2 * q + A, db + 2 * q, p.idesc, 1);                // lo hi
-              mma_ss_elect(d, da + 2 * q, db + 2 * q + B, p.idesc, 1);                // hi lo
-              mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, 1);                    // hi hi
+              for (int q = 0; q < steps; ++q) {
+                mma_ss_elect(d, da + 2 * q + A, db + 2 * q + B, p.idesc, (k | q) != 0);   // lo lo
+                mma_ss_elect(d, da + 2 * q + 2 * A, db + 2 * q, p.idesc, 1);              // lo2 hi
+                mma_ss_elect(d, da + 2 * q, db + 2 * q + 2 * B, p.idesc, 1);              // hi lo2
+                mma_ss_elect(d, da + 2 * q + A, db + 2 * q, p.idesc, 1);                  // lo hi
+                mma_ss_elect(d, da + 2 * q, db + 2 * q + B, p.idesc, 1);                  // hi lo
+              }
+            }
+            if (PIECES == 1 || k == p.npan - 1)
+              for (int q = 0; q < steps; ++q) mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, PIECES > 1 || (k | q) != 0);
+          } else {
+            for (int h = 0; h < p.npan - 1; ++h) {
+              const uint64_t db = sdesc(bs + h * kPanelB, 16, 1024, SWZ_128B);
+              const uint64_t da = sdesc(ARES ? a_sm + h * PIECES * kPanelA : as + h * kPanelA, 16, 1024, SWZ_128B);
+              for (int q = 0; q < 4; ++q) mma_ss_elect(d, da + 2 * q, db + 2 * q, p.idesc, 1);
             }
           }
           commit_elect(b_empty + 8 * s);

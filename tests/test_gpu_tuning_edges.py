@@ -260,3 +260,23 @@ def test_written_tensors_that_overlap_are_refused():
     assert abs(float((buf[:100].square().sum() + other[:100].square().sum()).sqrt()) - 1e-3) < 1e-7
     clip([was, was], 1.0, out=[other[:4000], torch.empty_like(was)])
     assert abs(float(other.norm()) - 0.5 ** 0.5) < 1e-5
+
+
+@pytest.mark.parametrize("r", [100, 128, 192, 256])
+def test_fp32_factor_scores_have_little_leaning(r):
+    """Scores z near 100 made of positive products only, whose roundings towards zero all lean the same way.
+
+    The r / 16 accumulations of the leading products lose half a unit of the sum so far on average, which grows evenly:
+    2^-23 z (r / 16 + 1) / 4 in all.  The others are below 2^-7 of z together and there are five for each: 2^-23 z 5 (r /
+    16) / 2 2^-7.  The target's own score (fp32, r / 32 additions in each lane) and the logarithm lean by u z at most.
+    """
+    rng = np.random.default_rng(r)
+    A = cuda(np.sqrt(100 / r) * (0.5 + rng.random((600, r))))
+    B = cuda(np.sqrt(100 / r) * (0.5 + rng.random((400, r))))
+    y = rng.integers(0, 400, 600)
+    a, b = A.double().cpu().numpy(), B.double().cpu().numpy()
+    z = (a @ b.T).max()
+    want = O.tuning.factor_logprobs(a, b, y)
+    got = tuning().factor_logprobs(A, B, cuda(y, torch.int64)).cpu().numpy()
+    leaning = abs(np.mean(got - want))
+    assert leaning <= 2.0 ** -23 * z * ((r / 16 + 1) / 4 + 5 * (r / 16) / 2 * 2.0 ** -7) + U * z
