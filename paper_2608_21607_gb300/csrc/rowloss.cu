@@ -105,7 +105,7 @@ struct Vec<__half> {
 };
 
 // A running pair over a thread's vectors.
-template <class T>
+template <class T, int LIFT = 16>
 struct Running : RunningSum {
   // four vectors: get(0) to get(3), asked for again where the group is not a usual one
   template <class G>
@@ -120,7 +120,7 @@ struct Running : RunningSum {
 #pragma unroll
           for (int i = 0; i < P; ++i) x[k * P + i] = Vec<T>::pair(v, i);
         }
-        const float group = group_sum(x, c);
+        const float group = this->template group_sum<H, LIFT>(x, c);
         if (group < kHigh) {
           s.S += group;
           return;
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(512, 2) row_kernel(const __grid_constant__ Row
         if (lane == 0) shared_share = share;
       }
     }
-    Running<T> run;
+    Running<T, WARP ? 4 : 16> run;
     int d = 0;
     for (int i = tid; i < n; i += 4 * nthr) {
       copy_wait<DEPTH - 1>();

@@ -280,3 +280,26 @@ def test_fp32_factor_scores_have_little_leaning(r):
     got = tuning().factor_logprobs(A, B, cuda(y, torch.int64)).cpu().numpy()
     leaning = abs(np.mean(got - want))
     assert leaning <= 2.0 ** -23 * z * ((r / 16 + 1) / 4 + 5 * (r / 16) / 2 * 2.0 ** -7) + U * z
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [16, 64, 500])
+def test_short_rows_of_one_large_probability(V, dtype):
+    """Rows in which one column has most of the probability, so that nothing averages its roundings.
+
+    An exponent in (2, 4] is rounded to 2^-22, the exponential to about as much: 2^-22 / sqrt(12) (ln 2 and 1) each, of
+    three quarters of the sum; the logarithm's and the result's roundings at 1.2 are 2^-23 / sqrt(12) each.  Together
+    7.5e-8 in the root mean square; half as much again is allowed.
+    """
+    T = 4000
+    rng = np.random.default_rng(V)
+    x = rng.normal(3.0, 4.0, (T, 1)) - 30.0 - 5.0 * rng.random((T, V))
+    for top in (1, 2):
+        x[:, top] = x[:, 0] + 40.0 + rng.random(T)
+        x[:, 5] = x[:, top] - 1.1
+        g = cuda(x).to(DTYPES[dtype])
+        y = np.full(T, 5)
+        want = O.tuning.token_logprobs(g.double().cpu().numpy(), y)
+        got = tuning().token_logprobs(g, cuda(y, torch.int64)).double().cpu().numpy()
+        assert np.sqrt(np.mean((got - want) ** 2)) <= 1.1e-7
+        x[:, top] = x[:, 0]
