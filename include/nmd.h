@@ -472,6 +472,88 @@ nmd_status nmd_clip_grad_norm(int64_t count, const void* const* d_grads, const i
                               double max_norm, void* const* d_out, float* d_norm, void* d_workspace, size_t ws_bytes,
                               void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Sequences from the model itself, for the losses above: beam search keeps the
+ * K best continuations of each of B groups.  Rows, logits and temperature as
+ * above, row b K + k being beam k of group b. */
+
+/* One step of beam search.  Beam (b, k) has the log-probability d_scores[b K + k]
+ * so far, and each column v offers to go on with
+ *   s_bkv = d_scores[b K + k] + x_v / tau - log sum_u exp(x_u / tau).
+ * A beam with d_finished (bytes, or NULL: none) set offers itself as it is, as
+ * column `end` at its score; a score of -inf marks a beam that is not in use.
+ * Neither's logits are read.  Only finite s are offered: a banned column
+ * (-inf), a row of nothing else and one that holds NaN or +inf offer nothing.
+ * Of each group the `width` largest offers are taken, compared as they are
+ * before rounding to fp32 (to about 1e-7), of equal ones the lowest beam, then
+ * the lowest column, in descending order:
+ *   d_out_scores, d_parents (the beam k), d_tokens (the column), B x width each;
+ *   d_out_finished (bytes, or NULL) is 1 where the column is `end`.
+ * Places that nothing is offered for: score -inf, parent 0, column -1 and not
+ * finished.  0 <= B <= 2^20, 1 <= K <= 64, 1 <= width <= 128, B K <= 2^27.  end
+ * in [0, V), or -1 without d_finished (nothing finishes).  The results may not
+ * overlap the inputs. */
+nmd_status nmd_beam_select(const void* d_logits, int32_t dtype, int64_t B, int64_t K, int64_t V, int64_t ld,
+                           const float* d_scores, const uint8_t* d_finished, int64_t end, int64_t width,
+                           double temperature, float* d_out_scores, int64_t* d_parents, int64_t* d_tokens,
+                           uint8_t* d_out_finished, void* stream);
+
+/* The beams' states in the order of their parents.  A state holds `outer` x
+ * B K rows of `bytes` bytes, row (o, i) at in + o in_outer + i in_row (strides
+ * in bytes); afterwards row (o, b width + k) of out is what row
+ * (o, b K + d_parents[b width + k]) of in was.  A parent outside [0, K) leaves
+ * its row of out as it is.  in == out (with equal strides and width == K): in
+ * place.  Otherwise no memory of any out lies between the first and the last byte
+ * of any other in or out of the call.  In place, states that lie between each
+ * other's bytes are dealt with one after another, in the order of the array.
+ * Rows of one state lie apart.  `states` is a host array, read before the call
+ * returns.  B, K, width as above. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t outer, in_outer, out_outer, in_row, out_row, bytes;
+} nmd_beam_state;
+nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t B, int64_t K, int64_t width,
+                            const int64_t* d_parents, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The training step on the gradients of the factors, or of other matrices.
+ * Matrices are rows x cols (at most 2^31 - 1 each, 0 allowed), element (i, j) at
+ * i row_stride + j col_stride (elements; >= 0), of any of the three types.  The
+ * smaller side is at most 16384.  The elements of a matrix that is written lie
+ * apart (NMD_ERR_INVALID), and it overlaps no other one, except that d_out may be
+ * d_update itself with its strides.
+ *
+ * An update replaced by a matrix near its orthogonal factor U V^T (G = U S V^T):
+ * with X = G / (|G|_F + eps), `steps` (1 to 16) times
+ *   A = X X^T,  X <- a X + (b A + c A^2) X      (A of the smaller side),
+ * (a, b, c) = coefficients, which maps every singular value s to
+ * a s + b s^3 + c s^5 and leaves the singular vectors.  X is held to 22 bits or
+ * more, sums to fp32; the result is rounded once to its own type.  Singular
+ * values on the way and |a| + |b| s^2 + |c| s^4 have to stay below 15, or the result is not
+ * finite; so is that of a G with NaN or infinities.  G = 0 gives 0.  eps > 0.
+ * Equal calls give equal bits. */
+nmd_status nmd_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+nmd_status nmd_orthogonalize(const void* d_update, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                             int64_t col_stride, int32_t steps, const double* coefficients, double eps, void* d_out,
+                             int64_t out_row_stride, int64_t out_col_stride, void* d_workspace, size_t ws_bytes,
+                             void* stream);
+
+/* The training step with it, in place:
+ *   M <- beta M + (1 - beta) G,
+ *   U  = nesterov ? beta M + (1 - beta) G : M,
+ *   W <- (1 - lr weight_decay) W - lr scale O(U),   O as above, in fp32 until W is
+ * rounded.  U is formed of M as it is stored, after its rounding. */
+typedef struct {
+  void* data;
+  int32_t dtype;
+  int64_t row_stride, col_stride;
+} nmd_matrix;
+nmd_status nmd_muon_step(const nmd_matrix* weight, const nmd_matrix* grad, const nmd_matrix* momentum, int64_t rows,
+                         int64_t cols, double lr, double beta, int32_t nesterov, double weight_decay, double scale,
+                         int32_t steps, const double* coefficients, double eps, void* d_workspace, size_t ws_bytes,
+                         void* stream);
+
 const char* nmd_status_string(nmd_status s);
 const char* nmd_last_error(const nmd_handle* h);
 void nmd_destroy(nmd_handle* h);

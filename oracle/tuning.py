@@ -121,3 +121,67 @@ def clip_grad_norm(grads, max_norm):
         np.sqrt(sum(np.sum(g ** 2) for g in flat))
     scale = 1.0 if norm <= max_norm else max_norm / norm
     return norm, [g * scale for g in flat]
+
+
+def beam_select(x, scores, width, finished=None, end=None, temperature=1.0):
+    """(scores, parents, tokens, finished), each (B, width): the largest of scores[b, k] + log softmax(x / temperature),
+    of equal ones the lowest (k, column); -inf, 0, -1 and False where nothing finite is left."""
+    scores = np.asarray(scores, np.float64)
+    B, K = scores.shape
+    V = np.shape(x)[1]
+    finished = None if finished is None else np.asarray(finished)
+    value = np.full((B, K, V), -np.inf)
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        for b in range(B):
+            for k in range(K):
+                if not np.isfinite(scores[b, k]):
+                    continue
+                if finished is not None and finished[b, k]:
+                    value[b, k, end] = scores[b, k]
+                    continue
+                z = np.asarray(x[b * K + k], np.float64)
+                z = (z - z.max()) / temperature   # (huge values would swallow the logarithm of the sum)
+                value[b, k] = scores[b, k] + (z - np.log(np.exp(z).sum()))
+    value[~np.isfinite(value)] = -np.inf
+    value = value.reshape(B, K * V)
+    value = np.concatenate([value, np.full((B, max(0, width - K * V)), -np.inf)], axis=1)
+    order = np.argsort(-value, axis=1, kind="stable")[:, :width]
+    best = np.take_along_axis(value, order, 1)
+    some = best > -np.inf
+    tokens = np.where(some, order % V, -1)
+    return best, np.where(some, order // V, 0), tokens, some & (tokens == (-2 if end is None else end))
+
+
+def beam_reorder(x, parents, dim=0, out=None):
+    """Along ``dim``, row b K + k of what parents (B, width) take; a parent outside [0, K) leaves the row of ``out``."""
+    B, w = np.shape(parents)
+    K = np.shape(x)[dim] // B if B else 0
+    y = np.moveaxis(np.array(x if out is None else out), dim, 0)
+    x = np.moveaxis(np.array(x), dim, 0)
+    for b in range(B):
+        for k in range(w):
+            if 0 <= parents[b, k] < K:
+                y[b * w + k] = x[b * K + parents[b, k]]
+    return np.moveaxis(y, 0, dim)
+
+
+def orthogonalize(G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    """U f(S) V^T of the update's singular value decomposition, f the map of the steps on S / (|G|_F + eps)."""
+    G = np.asarray(G, np.float64)
+    a, b, c = coefficients
+    if G.size == 0:
+        return G.copy()
+    U, s, Vt = np.linalg.svd(G / (np.linalg.norm(G) + eps), full_matrices=False)
+    for _ in range(steps):
+        s = a * s + b * s ** 3 + c * s ** 5
+    return (U * s) @ Vt
+
+
+def muon_step(W, G, M, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None, round_momentum=lambda m: m, **kw):
+    """(weights, momentum) after one step; ``round_momentum`` rounds the momentum to its type."""
+    W, G, M = (np.asarray(v, np.float64) for v in (W, G, M))
+    M = round_momentum(beta * M + (1 - beta) * G)
+    U = beta * M + (1 - beta) * G if nesterov else M
+    if scale is None:
+        scale = max(1.0, W.shape[0] / max(1, W.shape[1])) ** 0.5
+    return (1 - lr * weight_decay) * W - lr * scale * orthogonalize(U, **kw), M

@@ -37,7 +37,8 @@ EXPORTS = [
     "nmd_embed", "nmd_nn_workspace_bytes", "nmd_nearest_neighbors",
     "nmd_token_logprobs", "nmd_preference_workspace_bytes", "nmd_preference_loss", "nmd_policy_workspace_bytes",
     "nmd_policy_loss", "nmd_clip_workspace_bytes", "nmd_clip_grad_norm", "nmd_factor_workspace_bytes",
-    "nmd_factor_logprobs",
+    "nmd_factor_logprobs", "nmd_beam_select", "nmd_beam_reorder", "nmd_orthogonalize_workspace_bytes",
+    "nmd_orthogonalize", "nmd_muon_step",
 ]
 
 
@@ -51,6 +52,15 @@ class nmd_options(C.Structure):
 class nmd_loss_out(C.Structure):
     _fields_ = [("obj", C.c_double), ("rmse", C.c_double), ("wjd", C.c_double),
                 ("s_fro", C.c_double), ("sum_relu2", C.c_double), ("sum_relu", C.c_double)]
+
+
+class nmd_beam_state(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("outer", C.c_int64), ("in_outer", C.c_int64),
+                ("out_outer", C.c_int64), ("in_row", C.c_int64), ("out_row", C.c_int64), ("bytes", C.c_int64)]
+
+
+class nmd_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("row_stride", C.c_int64), ("col_stride", C.c_int64)]
 
 
 class NmdError(RuntimeError):
@@ -125,6 +135,14 @@ def lib() -> C.CDLL:
                                           C.c_int64, _P, C.c_size_t, _P]),
             "nmd_clip_workspace_bytes": (C.c_int, [C.c_int64, C.POINTER(C.c_size_t)]),
             "nmd_clip_grad_norm": (C.c_int, [C.c_int64, _P, _P, _P, C.c_double, _P, _P, _P, C.c_size_t, _P]),
+            "nmd_beam_select": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _P, _P, C.c_int64,
+                                          C.c_int64, C.c_double, _P, _P, _P, _P, _P]),
+            "nmd_beam_reorder": (C.c_int, [C.c_int64, _P, C.c_int64, C.c_int64, C.c_int64, _P, _P]),
+            "nmd_orthogonalize_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+            "nmd_orthogonalize": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _P,
+                                            C.c_double, _P, C.c_int64, C.c_int64, _P, C.c_size_t, _P]),
+            "nmd_muon_step": (C.c_int, [_P, _P, _P, C.c_int64, C.c_int64, C.c_double, C.c_double, C.c_int32, C.c_double,
+                                        C.c_double, C.c_int32, _P, C.c_double, _P, C.c_size_t, _P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)

@@ -1,4 +1,5 @@
-"""Fine-tuning a fitted model on preferences or rewards (include/nmd.h).
+"""Fine-tuning a fitted model on preferences or rewards (include/nmd.h): sequences from the model by beam search,
+log-probabilities and losses with the logits' gradient, and the step on the factors' gradients.
 
 Row i of the model L = W H scores the n columns, and softmax(L_i) is its
 distribution over them.  The functions below take the scores of T rows
@@ -37,6 +38,16 @@ class PolicyLoss(NamedTuple):
     kl: torch.Tensor                 # scalar: mean estimate of the KL divergence from the reference
     clipped: torch.Tensor            # scalar: share of the loss's weight on rows that were cut off
     grad: Optional[torch.Tensor]     # T x V, the logits' type
+
+
+class Beams(NamedTuple):
+    scores: torch.Tensor             # B x width: log-probability of each selected sequence, descending
+    parents: torch.Tensor            # B x width: the beam that it goes on from
+    tokens: torch.Tensor             # B x width: the column that it goes on with, -1 where nothing was offered
+    finished: Optional[torch.Tensor]   # B x width: whether that column is the end
+
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)   # steep at 0: singular values from 1e-3 to 1 come near 1 in five steps
 
 
 def _invalid(what: str):
@@ -259,3 +270,169 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
           ws.data_ptr(), nbytes)
     torch.autograd.graph.increment_version(outs)   # autograd has to know that a tensor it may have saved has changed
     return norm
+
+
+def beam_select(logits, scores, *, width: Optional[int] = None, finished=None, end: Optional[int] = None,
+                temperature: float = 1.0) -> Beams:
+    """One step of beam search: of each group the ``width`` best continuations of its beams.
+
+    ``scores`` (B x K fp32) are the beams' log-probabilities so far, -inf for a beam that is not in use, and row
+    b K + k of ``logits`` scores the columns that beam (b, k) may go on with.  A beam marked in ``finished`` (B x K
+    bool; ``end`` is wanted with it) offers itself alone, unchanged, as column ``end``.  ``width`` is K if not given.
+    """
+    dt = _matrix(logits, "logits")
+    device, index, (rows, V) = logits.device, logits.get_device(), logits.shape
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or scores.numel() != rows \
+            or scores.dtype != torch.float32 or scores.device != device or scores.shape[1] < 1:
+        _invalid("scores: a float32 matrix of B groups of K beams, %d in all, on cuda:%d is wanted" % (rows, index))
+    B, K = scores.shape
+    scores = scores if scores.is_contiguous() else scores.contiguous()
+    if finished is not None:
+        if not isinstance(finished, torch.Tensor) or finished.dtype != torch.bool or finished.shape != scores.shape \
+                or finished.device != device:
+            _invalid("finished: a bool matrix of the scores' shape on cuda:%d is wanted" % index)
+        if end is None:
+            _invalid("end: wanted with finished")
+        finished = finished if finished.is_contiguous() else finished.contiguous()
+    if end is not None and not 0 <= end < V:
+        _invalid("end: a column is wanted")
+    w = K if width is None else width
+    if not 1 <= K <= 64 or not 1 <= w <= 128:
+        _invalid("scores, width: 1 to 64 beams and a width of 1 to 128 are wanted")
+    out = torch.empty((B, w), dtype=torch.float32, device=device)
+    parents = torch.empty((B, w), dtype=torch.int64, device=device)
+    tokens = torch.empty((B, w), dtype=torch.int64, device=device)
+    done = None if end is None else torch.empty((B, w), dtype=torch.bool, device=device)
+    _call(index, "nmd_beam_select", logits.data_ptr(), dt, B, K, V, logits.stride(0), scores.data_ptr(),
+          None if finished is None else finished.data_ptr(), -1 if end is None else end, w, temperature, out.data_ptr(),
+          parents.data_ptr(), tokens.data_ptr(), None if done is None else done.data_ptr())
+    return Beams(out, parents, tokens, done)
+
+
+def _rows_of(x, dim: int, name: str):
+    """(outer count, outer stride, row stride, bytes of a row) of a tensor whose dimension ``dim`` counts the rows."""
+    shape, strides, size = x.shape, x.stride(), x.element_size()
+    want = 1
+    for n, s in zip(reversed(shape[dim + 1:]), reversed(strides[dim + 1:])):
+        if n > 1 and s != want:
+            _invalid("%s: the elements of a row have to be adjacent" % name)
+        want *= n
+    outer, stride = 1, 0
+    for n, s in zip(reversed(shape[:dim]), reversed(strides[:dim])):
+        if n > 1:
+            if outer > 1 and s != stride * outer:
+                _invalid("%s: the dimensions before the rows have to lie at one distance" % name)
+            if outer == 1:
+                stride = s
+        outer *= n
+    return outer, stride * size, strides[dim] * size, want * size
+
+
+def beam_reorder(states, parents, *, dim: int = 0, out=None):
+    """The beams' states (a tensor, or several) in the order of ``parents``: along dimension ``dim``, which counts
+    B x K rows, row b K + k becomes what row b K + parents[b, k] was.
+
+    In place, or into ``out``: tensors apart from the states with B x width rows for ``parents`` of B x width.  Types
+    are any; the elements of a row are adjacent, rows and what lies before them at any distance.  A parent outside
+    the group leaves its row as it is.  Returns what was written, as it was given.
+    """
+    xs = list(states) if isinstance(states, (list, tuple)) else [states]
+    ys = xs if out is None else list(out) if isinstance(out, (list, tuple)) else [out]
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or parents.dtype != torch.int64 \
+            or not parents.is_cuda or not all(isinstance(x, torch.Tensor) for x in xs + ys) or len(xs) != len(ys):
+        _invalid("states, parents, out: tensors, an int64 CUDA matrix and as many tensors are wanted")
+    B, w = parents.shape
+    device, index = parents.device, parents.get_device()
+    if not xs:
+        return states if out is None else out
+    K, table = None, (nmd.nmd_beam_state * len(xs))()
+    for t, x, y in zip(table, xs, ys):
+        if x.device != device or y.device != device or y.dtype != x.dtype:
+            _invalid("states, out: tensors on %s, of one type each, are wanted" % device)
+        if not 0 <= dim < x.dim() or y.dim() != x.dim() or x.shape[:dim] != y.shape[:dim] \
+                or x.shape[dim + 1:] != y.shape[dim + 1:]:
+            _invalid("states, out: tensors with a dimension %d of rows, alike apart from it, are wanted" % dim)
+        rows = x.shape[dim]
+        k = rows // B if B else w
+        if rows != B * k or y.shape[dim] != B * w or (K is not None and k != K):
+            _invalid("states, out: B x K rows and B x width rows for parents of %d x %d are wanted" % (B, w))
+        K = k
+        t.outer, t.in_outer, t.in_row, t.bytes = _rows_of(x, dim, "states")
+        t.in_, t.out = x.data_ptr(), y.data_ptr()
+        if y is x:
+            t.out_outer, t.out_row = t.in_outer, t.in_row
+        else:
+            _, t.out_outer, t.out_row, _ = _rows_of(y, dim, "out")
+    if not 1 <= K <= 64 or not 1 <= w <= 128 or (out is None and K != w):
+        _invalid("states, parents: 1 to 64 beams and a width of 1 to 128, the same in place, are wanted")
+    parents = parents if parents.is_contiguous() else parents.contiguous()
+    _call(index, "nmd_beam_reorder", len(xs), C.addressof(table), B, K, w, parents.data_ptr())
+    torch.autograd.graph.increment_version(ys)
+    return states if out is None else out
+
+
+def _update_matrix(x, name: str, shape=None, device=None) -> int:
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda or x.dtype not in _DTYPES:
+        _invalid("%s: a two-dimensional float32, bfloat16 or float16 CUDA tensor is wanted" % name)
+    if shape is not None and (x.shape != shape or x.device != device):
+        _invalid("%s: %d x %d on %s is wanted" % (name, *shape, device))
+    return _DTYPES[x.dtype]
+
+
+def _map(steps: int, coefficients):
+    if len(coefficients) != 3:
+        _invalid("coefficients: three are wanted")
+    if not 1 <= steps <= 16:
+        _invalid("steps: 1 to 16 are wanted")
+    return (C.c_double * 3)(*coefficients)
+
+
+def orthogonalize(update, *, steps: int = 5, coefficients: Sequence[float] = COEFFICIENTS, eps: float = 1e-7,
+                  out=None) -> torch.Tensor:
+    """``update`` replaced by a matrix near its orthogonal factor U V^T, of the update's type: ``steps`` times
+    X <- a X + (b X X^T + c (X X^T)^2) X from X = update / (|update|_F + eps).
+
+    Any strides; the smaller side is at most 16384.  Into ``out`` if it is given (``update`` itself, or apart from it).
+    """
+    dt = _update_matrix(update, "update")
+    rows, cols = update.shape
+    if out is None:
+        out = torch.empty_like(update)
+    elif _update_matrix(out, "out", update.shape, update.device) != dt:
+        _invalid("out: the update's type is wanted")
+    k = _map(steps, coefficients)
+    nbytes = _bytes_of_sizes("nmd_orthogonalize_workspace_bytes", rows, cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=update.device)
+    _call(update.get_device(), "nmd_orthogonalize", update.data_ptr(), dt, rows, cols, *update.stride(), steps,
+          C.addressof(k), eps, out.data_ptr(), *out.stride(), ws.data_ptr(), nbytes)
+    torch.autograd.graph.increment_version([out])
+    return out
+
+
+def muon_step(weight, grad, momentum, *, lr: float, beta: float = 0.95, nesterov: bool = True,
+              weight_decay: float = 0.0, scale: Optional[float] = None, steps: int = 5,
+              coefficients: Sequence[float] = COEFFICIENTS, eps: float = 1e-7) -> None:
+    """One training step of a matrix with an orthogonalised update (Muon), in place:
+    momentum <- beta momentum + (1 - beta) grad, and
+    weight <- (1 - lr weight_decay) weight - lr scale orthogonalize(update), where the update is the momentum or, with
+    ``nesterov``, beta momentum + (1 - beta) grad.
+
+    ``scale`` is sqrt(max(1, rows / columns)) if not given.  The three tensors have one shape, types and strides of
+    their own, and lie apart.
+    """
+    shape, device = getattr(weight, "shape", None), getattr(weight, "device", None)
+    table = (nmd.nmd_matrix * 3)()
+    for t, x, name in zip(table, (weight, grad, momentum), ("weight", "grad", "momentum")):
+        t.dtype = _update_matrix(x, name, shape, device)
+        t.data = x.data_ptr()
+        t.row_stride, t.col_stride = x.stride()
+    rows, cols = shape
+    if scale is None:
+        scale = max(1.0, rows / max(1, cols)) ** 0.5
+    k = _map(steps, coefficients)
+    nbytes = _bytes_of_sizes("nmd_orthogonalize_workspace_bytes", rows, cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    at, size = C.addressof(table), C.sizeof(nmd.nmd_matrix)
+    _call(weight.get_device(), "nmd_muon_step", at, at + size, at + 2 * size, rows, cols, lr, beta, int(nesterov),
+          weight_decay, scale, steps, C.addressof(k), eps, ws.data_ptr(), nbytes)
+    torch.autograd.graph.increment_version([weight, momentum])
