@@ -1,20 +1,39 @@
 // An update replaced by a matrix near its orthogonal factor, by Newton-Schulz
 // products, and the training step with it (formulas in include/nmd.h).
+//
+// The products run on the tcgen05 tensor cores.  Every matrix on the way (X, A =
+// X X^T, P = a I + b A + c A^2) is kept as two fp16 pieces of 2^12 x, hi =
+// fp16(v), lo = fp16(v - hi): 22 bits, and an absolute error below 2^-37 however
+// small the element (|X|_F starts at 1).  (Where eps is most of the divisor, X starts
+// much smaller and is kept 2^t larger, t falling to 0 as the steps raise it.)  A product is hi hi + hi lo + lo hi, three
+// MMAs; what lo lo would add is below 2^-22.  In fp32 throughout the errors of
+// early steps grow by up to a per step just the same, and the two come out
+// equally far from the definition (within a third, over decaying, flat and low-rank
+// spectra); with one piece (11 bits) the result would be off by parts in a hundred.
+// The tensor cores add in fp32 but round towards zero, which leans by up to a
+// unit per addition of a sum of squares; so a tile's sum leaves TMEM every 128
+// products and goes on in the epilogue's registers, rounded to nearest.
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <cmath>
 
 #include "nmd_internal.cuh"
+#include "tc_pipe.cuh"
+#include "tc_ptx.cuh"
 
 namespace nmd {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kParts = 608;          // CTAs of the norm's pass
-constexpr int64_t kMostSide = 16384;
+using namespace tc;
 
-struct Matrix {
+constexpr int64_t kMostSide = 16384;
+constexpr int kThreads = 256;
+constexpr int kParts = 608;          // CTAs of the norm's pass: four per SM
+constexpr int kSms = 152;            // the splitting of sums goes by this number, not by the device, for equal bits
+constexpr float kUnit = 4096.f;      // pieces hold 2^12 x
+
+struct Matrix {   // elements at i rs + j cs
   void* x;
   int dtype;
   int64_t rs, cs;
@@ -31,9 +50,10 @@ struct Matrix {
   }
 };
 
-// What becomes of the update: rows x cols of it are G, or a momentum that G goes into.
+// What becomes of the update: an R x C matrix, C the side whose elements are
+// adjacent in memory (or nearer).
 struct Job {
-  int64_t rows, cols;
+  int64_t R, C;
   Matrix grad, momentum, out;   // out: the result, or the weights
   int step;                     // 1: a training step (momentum and weights)
   float beta, rest;             // rest = 1 - beta
@@ -42,22 +62,60 @@ struct Job {
   double eps;
 };
 
-// U = M or beta M + (1 - beta) G after M <- beta M + (1 - beta) G, and its sum of squares
-__global__ void __launch_bounds__(kThreads) update_kernel(Job j, float* X, double* parts) {
+// Two fp16 pieces of an R x C matrix: plane 0 hi, plane 1 lo, rows of ld elements
+struct Pieces {
+  __half* hi;
+  int64_t rows, cols, ld;
+  __host__ __device__ int64_t plane() const { return rows * ld; }
+};
+__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  lo = __float2half_rn(v - __half2float(hi));   // an overflow leaves infinities of both signs: NaN in the next product
+}
+
+// ------------------------------------------------------------------ the update and its norm
+
+// fp32 squares of a few values, in fp64 where they leave fp32's range or come near its ends
+template <int N>
+__device__ __forceinline__ double squares(const float (&f)[N]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s = fmaf(f[i], f[i], s);
+  if (s >= 0x1p-60f && s <= 0x1p96f) return (double)s;
+  double d = 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) d += (double)f[i] * (double)f[i];
+  return d;
+}
+__device__ __forceinline__ float update_of(const Job& j, float m, float g) { return j.nesterov ? fmaf(j.beta, m, j.rest * g) : m; }
+
+constexpr int kEach = 8;   // elements of a thread at a time
+
+// M <- beta M + (1 - beta) G, and the sum of squares of the update
+__global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, int* status) {
   __shared__ double red[kThreads / 32];
+  if (blockIdx.x == 0 && threadIdx.x < 2) status[threadIdx.x] = 0;
   double sum = 0.0;
-  const int64_t n = j.rows * j.cols;
-  for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < n; e += (int64_t)gridDim.x * kThreads) {
-    const int64_t r = e / j.cols, c = e % j.cols;
-    float u = j.grad.get(r, c);
+  const int64_t across = (j.C + kThreads * kEach - 1) / (kThreads * kEach), work = across * j.R;
+  for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+    const int64_t r = w / across, c0 = (w - r * across) * (kThreads * kEach) + threadIdx.x;
+    float u[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) u[i] = c0 + i * kThreads < j.C ? j.grad.get(r, c0 + i * kThreads) : 0.f;
     if (j.step) {
-      const float g = u, m = j.beta * j.momentum.get(r, c) + j.rest * g;
-      j.momentum.put(r, c, m);
-      u = j.momentum.get(r, c);
-      if (j.nesterov) u = j.beta * u + j.rest * g;
+      float m[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) m[i] = c0 + i * kThreads < j.C ? j.momentum.get(r, c0 + i * kThreads) : 0.f;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int64_t c = c0 + i * kThreads;
+        if (c < j.C) {
+          j.momentum.put(r, c, fmaf(j.beta, m[i], j.rest * u[i]));
+          u[i] = update_of(j, j.momentum.get(r, c), u[i]);   // of the momentum as it is stored
+        }
+      }
     }
-    X[e] = u;
-    sum += (double)u * (double)u;
+    sum += squares(u);
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -69,86 +127,592 @@ __global__ void __launch_bounds__(kThreads) update_kernel(Job j, float* X, doubl
     parts[blockIdx.x] = sum;
   }
 }
-__global__ void __launch_bounds__(kThreads) normalise_kernel(float* X, int64_t n, const double* parts, int count, double eps) {
-  __shared__ double inv;
-  if (threadIdx.x == 0) {
-    double sum = 0.0;
-    for (int i = 0; i < count; ++i) sum += parts[i];
-    inv = 1.0 / (sqrt(sum) + eps);
-  }
+
+// X = update / (norm + eps) in pieces
+// shift: t of X before each step and after the last
+__global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
+                                                          int grows) {
+  __shared__ double red[kThreads / 32];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < count; i += kThreads) sum += parts[i];
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
   __syncthreads();
-  for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < n; e += (int64_t)gridDim.x * kThreads)
-    X[e] = (float)((double)X[e] * inv);
-}
-
-// C = alpha A B + beta D, elements at i * row + j * col
-struct View {
-  float* x;
-  int64_t row, col;
-  __device__ __forceinline__ float& at(int64_t i, int64_t j) const { return x[i * row + j * col]; }
-};
-constexpr int kTile = 32;
-__global__ void __launch_bounds__(kThreads) product_kernel(View A, View B, View C, View D, int64_t m, int64_t n, int64_t k,
-                                                           float alpha, float beta) {
-  __shared__ float a[kTile][kTile + 1], b[kTile][kTile + 1];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t k0 = 0; k0 < k; k0 += kTile) {
-    for (int q = 0; q < 4; ++q) {
-      const int r = ty + 8 * q;
-      a[r][tx] = i0 + r < m && k0 + tx < k ? A.at(i0 + r, k0 + tx) : 0.f;
-      b[r][tx] = k0 + r < k && j0 + tx < n ? B.at(k0 + r, j0 + tx) : 0.f;
+  sum = 0.0;
+  for (int i = 0; i < kThreads / 32; ++i) sum += red[i];
+  // |X| = 2^-t at most; `grows`: a step takes a small X to 2^grows times itself at most
+  const double norm = sqrt(sum), size = norm / (norm + j.eps);
+  const int small = size > 0.0 && size < 0x1p-8 ? min(100, -ilogb(size) - 1) : 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    int t = small;
+    for (int i = 0; i <= steps; ++i) {
+      shift[i] = t;
+      t = t < 8 ? 0 : max(0, t - grows);
     }
-    __syncthreads();
-    for (int e = 0; e < kTile; ++e)
-      for (int q = 0; q < 4; ++q) sum[q] = fmaf(a[ty + 8 * q][e], b[e][tx], sum[q]);
-    __syncthreads();
   }
-  for (int q = 0; q < 4; ++q) {
-    const int64_t i = i0 + ty + 8 * q, j = j0 + tx;
-    if (i < m && j < n) C.at(i, j) = alpha * sum[q] + (D.x ? beta * D.at(i, j) : 0.f);
+  // 2^(12 + t) / (norm + eps) as a number near 1 and a power of two in two halves, so that norms of 1e-40 and 1e38 do
+  int e = 0;
+  const float f = (float)frexp((double)kUnit / (norm + j.eps), &e);
+  e = max(-280, min(280, e + small));
+  const float p = ldexpf(1.f, e / 2), q = ldexpf(1.f, e - e / 2);
+  const int64_t across = (j.C + kThreads * kEach - 1) / (kThreads * kEach), work = across * j.R;
+  for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+    const int64_t r = w / across, c0 = (w - r * across) * (kThreads * kEach) + threadIdx.x;
+    float u[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) u[i] = c0 + i * kThreads < j.C ? j.grad.get(r, c0 + i * kThreads) : 0.f;
+    if (j.step) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (c0 + i * kThreads < j.C) u[i] = update_of(j, j.momentum.get(r, c0 + i * kThreads), u[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int64_t c = c0 + i * kThreads;
+      if (c >= j.C) continue;
+      __half hi, lo;
+      split(u[i] * p * q * f, hi, lo);
+      X.hi[r * X.ld + c] = hi;
+      X.hi[X.plane() + r * X.ld + c] = lo;
+    }
   }
-}
-void product(View A, View B, View C, View D, int64_t m, int64_t n, int64_t k, float alpha, float beta, cudaStream_t s) {
-  product_kernel<<<dim3((unsigned)((n + 31) / 32), (unsigned)((m + 31) / 32)), kThreads, 0, s>>>(A, B, C, D, m, n, k, alpha, beta);
 }
 
-__global__ void __launch_bounds__(kThreads) finish_kernel(Job j, const float* X) {
-  const int64_t n = j.rows * j.cols;
-  for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < n; e += (int64_t)gridDim.x * kThreads) {
-    const int64_t r = e / j.cols, c = e % j.cols;
-    j.out.put(r, c, j.step ? j.keep * j.out.get(r, c) - j.lr * X[e] : X[e]);
+// ---------------------------------------------------------------------------- products
+
+enum Mode { kSymmetric, kPartial, kMatrix, kResult };
+
+struct Gemm {
+  int64_t M, N;             // D is M x N
+  int kblocks, splits;      // blocks of 64 of the sum; parts of it that are tiles of their own
+  int tiles_n, items;       // tiles across; tiles x splits
+  int lower;                // 1: D is symmetric, tiles below and on the diagonal only
+  int mode;
+  float alpha, beta, diag;  // D = alpha 2^(*up - times *down) (sum) + beta C + diag I, in pieces
+  const int *up, *down;     // or nullptr
+  int times;
+  Pieces c, d;
+  float* part;              // items x 128 x BN
+  Job out;
+  int* status;
+};
+
+constexpr int kBM = 128, kBK = 64, kChunk = 2;   // rows of a tile, products of a stage, stages of a sum in TMEM
+constexpr int kEpilogue = 256, kProducer = 8, kIssuer = 9, kGemmThreads = 320;
+template <int BN>
+struct Cfg {
+  static constexpr int A_BYTES = 2 * kBM * kBK * 2, B_BYTES = 2 * BN * kBK * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr int NS = 196608 / STAGE;
+  static constexpr int TMEM = 2 * BN;
+  static constexpr size_t OFF_TURN = (size_t)NS * STAGE;                // a 32 x 32 square per epilogue warp
+  static constexpr size_t OFF_BARS = OFF_TURN + 8 * 4096;
+  static constexpr int NBAR = 2 * NS + 5;
+  static constexpr size_t SMEM = 1024 + OFF_BARS + NBAR * 8 + 16;
+  static_assert(SMEM <= 227 * 1024, "shared memory");
+};
+
+__device__ __forceinline__ float scale_of_sum(const Gemm& p) {
+  return ldexpf(p.alpha, (p.up ? *p.up : 0) - (p.down ? p.times * *p.down : 0));
+}
+
+// tile (i, j) and the part of the sum of a work item
+struct Item {
+  int i, j, k0, k1;
+};
+__device__ __forceinline__ Item item_of(const Gemm& p, int w, int BN) {
+  Item t;
+  const int tile = w / p.splits, part = w - tile * p.splits;
+  if (p.lower) {
+    int left = tile;
+    t.i = 0;
+    for (;;) {
+      const int n = min((kBM * (t.i + 1) - 1) / BN + 1, p.tiles_n);
+      if (left < n) break;
+      left -= n;
+      ++t.i;
+    }
+    t.j = left;
+  } else {
+    t.i = tile / p.tiles_n;
+    t.j = tile - t.i * p.tiles_n;
+  }
+  t.k0 = (int)((int64_t)p.kblocks * part / p.splits);
+  t.k1 = (int)((int64_t)p.kblocks * (part + 1) / p.splits);
+  return t;
+}
+
+__device__ __forceinline__ uint32_t halves_of(__half a, __half b) {
+  return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16;
+}
+
+// 32 columns of one row of D by a thread, in pieces; a symmetric D also as 32 rows of a column
+__device__ __forceinline__ void put_pieces(const Gemm& p, float alpha, float (&v)[32], int64_t row, int64_t col) {
+  if (row >= p.M || col >= p.d.ld) return;
+  __half* at = p.d.hi + row * p.d.ld + col;
+  const int64_t plane = p.d.plane();
+  if (p.mode == kSymmetric) {
+    if (col > row) return;
+    if (p.beta != 0.f) {
+      const uint4* h = (const uint4*)(p.c.hi + row * p.c.ld + col);
+      const uint4* l = (const uint4*)(p.c.hi + p.c.plane() + row * p.c.ld + col);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4 a = h[q], b = l[q];
+        const __half2* x = (const __half2*)&a;
+        const __half2* y = (const __half2*)&b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = __half22float2(x[i]), g = __half22float2(y[i]);
+          v[q * 8 + 2 * i] = fmaf(p.beta, f.x + g.x, v[q * 8 + 2 * i] * alpha);
+          v[q * 8 + 2 * i + 1] = fmaf(p.beta, f.y + g.y, v[q * 8 + 2 * i + 1] * alpha);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] *= alpha;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= alpha;
+  }
+  if (p.mode == kSymmetric && col + 31 >= row) {   // across the diagonal
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (col + i > row) continue;
+      __half hi, lo;
+      split(col + i == row ? v[i] + p.diag : v[i], hi, lo);
+      at[i] = hi;
+      at[plane + i] = lo;
+      if (col + i < row) {
+        p.d.hi[(col + i) * p.d.ld + row] = hi;
+        p.d.hi[plane + (col + i) * p.d.ld + row] = lo;
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __half a[2], b[2];
+      split(v[q * 8 + 2 * i], a[0], b[0]);
+      split(v[q * 8 + 2 * i + 1], a[1], b[1]);
+      h[i] = halves_of(a[0], a[1]);
+      l[i] = halves_of(b[0], b[1]);
+      if (p.mode == kSymmetric) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int64_t t = (col + q * 8 + 2 * i + k) * p.d.ld + row;
+          p.d.hi[t] = a[k];
+          p.d.hi[plane + t] = b[k];
+        }
+      }
+    }
+    ((uint4*)at)[q] = make_uint4(h[0], h[1], h[2], h[3]);
+    ((uint4*)(at + plane))[q] = make_uint4(l[0], l[1], l[2], l[3]);
   }
 }
+
+// 32 rows x 32 columns of the result by a warp: turned in shared memory, so that lanes write adjacent elements
+__device__ __forceinline__ void put_result(const Gemm& p, float alpha, const float (&v)[32], int64_t row0, int64_t col0, float* square) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 32; ++i) square[lane * 32 + (i ^ lane)] = v[i] * alpha;
+  __syncwarp();
+  if (col0 + lane >= p.N) return;
+  const Matrix& o = p.out.out;
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    if (row0 + r >= p.M) break;
+    float x = square[r * 32 + (lane ^ r)];
+    if (p.out.step) x = fmaf(-p.out.lr, x, p.out.keep * o.get(row0 + r, col0 + lane));
+    o.put(row0 + r, col0 + lane, x);
+  }
+}
+
+// D = A B^T in tiles of 128 x BN.  An operand whose sum runs along its rows in memory
+// (AMN = false: A[m][k]) comes in tiles of 64 adjacent k; one whose sum runs
+// across them (AMN: A[k][m]) in panels of 64 adjacent m, and the tensor cores take
+// it as MN-major.  Hi and lo pieces are the two planes of one tensor map.
+//   warps 0-7   epilogue: a sum's chunks from TMEM (lane = row, two halves of the
+//               columns), added up in registers, then written
+//   warp 8      loads, one elected lane
+//   warp 9      issues the products
+// Work items (tile, part of the sum) are dealt to one CTA per SM in turn; two TMEM
+// buffers and the ring of stages run on from one item to the next.
+template <int BN, bool AMN, bool BMN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Gemm p) {
+  using C = Cfg<BN>;
+  extern __shared__ char smem_raw[];
+  char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  const uint32_t stage0 = smem_u32(smem);
+  const uint32_t bars = smem_u32(smem + C::OFF_BARS);
+  const uint32_t b_full = bars, b_empty = bars + 8 * C::NS, b_tfull = bars + 16 * C::NS, b_tempty = b_tfull + 16, b_drain = b_tempty + 16;
+  uint32_t* slot = (uint32_t*)(smem + C::OFF_BARS + C::NBAR * 8);
+  volatile int* abort_flag = (volatile int*)(slot + 1);
+  int* dead_word = (int*)(slot + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::NS; ++s) {
+      mbar_init(b_full + 8 * s, 1);
+      mbar_init(b_empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(b_tfull + 8 * b, 1);
+      mbar_init(b_tempty + 8 * b, kEpilogue / 32);
+    }
+    mbar_init(b_drain, 1);
+    fence_mbar_init();
+    *abort_flag = 0;
+    *dead_word = *(volatile int*)p.status;   // an earlier product's wait ran out: what follows has no input
+  }
+  if (warp == kIssuer) {
+    tmem_alloc(smem_u32(slot), C::TMEM);
+    tmem_relinquish();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)slot;
+  const bool dead = *dead_word != 0;
+
+  if (warp == kProducer) {
+    if (lane == 0 && !dead) {
+      int64_t n = 0;
+      bool ok = true;
+      for (int w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
+        const Item t = item_of(p, w, BN);
+        for (int k = t.k0; k < t.k1; ++k, ++n) {
+          const int s = (int)(n % C::NS);
+          if (!(ok = wait_bar(b_empty + 8 * s, (uint32_t)((n / C::NS) & 1) ^ 1u, abort_flag, p.status, 1))) break;
+          const uint32_t full = b_full + 8 * s, dst = stage0 + s * C::STAGE;
+          mbar_expect_tx(full, C::STAGE);
+          if (AMN) {
+#pragma unroll
+            for (int q = 0; q < kBM / 64; ++q) tma_load_3d(dst + q * 2 * kBK * 128, &ta, full, t.i * kBM + q * 64, k * kBK, 0);
+          } else {
+            tma_load_3d(dst, &ta, full, k * kBK, t.i * kBM, 0);
+          }
+          if (BMN) {
+#pragma unroll
+            for (int q = 0; q < BN / 64; ++q)
+              tma_load_3d(dst + C::A_BYTES + q * 2 * kBK * 128, &tb, full, t.j * BN + q * 64, k * kBK, 0);
+          } else {
+            tma_load_3d(dst + C::A_BYTES, &tb, full, k * kBK, t.j * BN, 0);
+          }
+        }
+      }
+      if (!ok)   // copies still under way land before shared memory goes away
+        for (int64_t k = n > C::NS ? n - C::NS : 0; k < n; ++k) {
+          const uint64_t t0 = globaltimer_ns();
+          while (!mbar_try_wait(b_full + 8 * (int)(k % C::NS), (uint32_t)((k / C::NS) & 1)) && globaltimer_ns() - t0 < 100000000ull) {
+          }
+        }
+    }
+    __syncwarp();
+  } else if (warp == kIssuer) {
+    if (!dead) {
+      constexpr uint32_t idesc = idesc_fp16(kBM, BN, AMN, BMN);
+      // between the hi and the lo tile of a stage, and between steps of 16 products
+      constexpr uint32_t A_LO = AMN ? kBK * 128 : kBM * 128, B_LO = BMN ? kBK * 128 : BN * 128;
+      constexpr uint32_t A_STEP = AMN ? 16 * 128 : 32, B_STEP = BMN ? 16 * 128 : 32;
+      int64_t n = 0, ch = 0;
+      bool ok = true;
+      for (int w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
+        const Item t = item_of(p, w, BN);
+        for (int k = t.k0; k < t.k1; ++k, ++n) {
+          const int s = (int)(n % C::NS), buf = (int)(ch & 1);
+          const bool first = (k - t.k0) % kChunk == 0, last = (k - t.k0) % kChunk == kChunk - 1 || k + 1 == t.k1;
+          if (first && !(ok = conv_wait(b_tempty + 8 * buf, (uint32_t)((ch >> 1) & 1) ^ 1u, abort_flag, p.status, 2))) break;
+          if (!(ok = conv_wait(b_full + 8 * s, (uint32_t)((n / C::NS) & 1), abort_flag, p.status, 3))) break;
+          fence_after();
+          const uint32_t a0 = stage0 + s * C::STAGE, b0 = a0 + C::A_BYTES, d = tmem + buf * BN;
+          const uint64_t ah = AMN ? sdesc(a0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(a0, 16, 1024, SWZ_128B);
+          const uint64_t bh = BMN ? sdesc(b0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(b0, 16, 1024, SWZ_128B);
+#pragma unroll
+          for (int q = 0; q < kBK / 16; ++q) {
+            const uint64_t a = ah + ((q * A_STEP) >> 4), b = bh + ((q * B_STEP) >> 4);
+            mma_ss_elect(d, a + (A_LO >> 4), b, idesc, !(first && q == 0));
+            mma_ss_elect(d, a, b + (B_LO >> 4), idesc, 1);
+            mma_ss_elect(d, a, b, idesc, 1);
+          }
+          commit_elect(b_empty + 8 * s);
+          if (last) {
+            commit_elect(b_tfull + 8 * buf);
+            ++ch;
+          }
+        }
+      }
+      commit_elect(b_drain);   // every product issued has ended before TMEM is given back
+      if (lane == 0) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(b_drain, 0) && globaltimer_ns() - t0 < 200000000ull) {
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    constexpr int G = BN / 64;   // groups of 32 columns of a warpgroup
+    const int part = warp >> 2, row = (warp & 3) * 32;
+    const uint32_t lanes = (uint32_t)row << 16;
+    float* square = (float*)(smem + C::OFF_TURN) + warp * 1024;
+    const float alpha = scale_of_sum(p);
+    int64_t ch = 0;
+    bool ok = !dead;
+    for (int w = blockIdx.x; w < p.items; w += gridDim.x) {
+      const Item t = item_of(p, w, BN);
+      const int chunks = (t.k1 - t.k0 + kChunk - 1) / kChunk;
+      float acc[G][32];
+      for (int c = 0; c < chunks && ok; ++c, ++ch) {
+        const int buf = (int)(ch & 1);
+        if (!(ok = warp_wait(b_tfull + 8 * buf, (uint32_t)((ch >> 1) & 1), abort_flag, p.status, 4))) break;
+        fence_after();
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          uint32_t v[32];
+          tmem_ld32(tmem + lanes + buf * BN + (part * G + g) * 32, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[g][i] = c == 0 ? __uint_as_float(v[i]) : acc[g][i] + __uint_as_float(v[i]);
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_tempty + 8 * buf);
+      }
+      if (!ok && p.mode != kResult) break;
+      const int64_t r = (int64_t)t.i * kBM + row;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int64_t col = (int64_t)t.j * BN + (part * G + g) * 32;
+        if (!ok) {   // the result of a wait that ran out shows
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[g][i] = NAN;
+        }
+        if (p.mode == kPartial) {
+          float4* at = (float4*)(p.part + ((int64_t)w * kBM + row + lane) * BN + (part * G + g) * 32);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) at[q] = make_float4(acc[g][4 * q], acc[g][4 * q + 1], acc[g][4 * q + 2], acc[g][4 * q + 3]);
+        } else if (p.mode == kResult) {
+          put_result(p, alpha, acc[g], r, col, square);
+        } else {
+          put_pieces(p, alpha, acc[g], r + lane, col);
+        }
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kIssuer) {
+    fence_after();
+    tmem_dealloc(tmem, C::TMEM);
+  }
+}
+
+// The parts of a symmetric D added up in order, in pieces.  A CTA takes 32 columns of
+// one row of a tile; eight groups of lanes take every eighth part.
+__global__ void __launch_bounds__(kThreads) join_kernel(Gemm p, int BN) {
+  __shared__ float sums[8][32];
+  const int per = kBM * (BN / 32), lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int tile = blockIdx.x / per, at = blockIdx.x - tile * per, r = at / (BN / 32), c = at % (BN / 32) * 32 + lane;
+  const Item t = item_of(p, tile * p.splits, BN);
+  const int64_t row = (int64_t)t.i * kBM + r, col = (int64_t)t.j * BN + c;
+  if (row >= p.M || col - lane > row) return;
+  const float* x = p.part + ((int64_t)tile * p.splits * kBM + r) * BN + c;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int s = g; s < p.splits; s += 8) sum += x[(int64_t)s * kBM * BN];
+  sums[g][lane] = sum;
+  __syncthreads();
+  if (g != 0 || col > row) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) sum += sums[i][lane];
+  __half hi, lo;
+  split(sum * scale_of_sum(p), hi, lo);
+  p.d.hi[row * p.d.ld + col] = hi;
+  p.d.hi[p.d.plane() + row * p.d.ld + col] = lo;
+  p.d.hi[col * p.d.ld + row] = hi;
+  p.d.hi[p.d.plane() + col * p.d.ld + row] = lo;
+}
+
+// ------------------------------------------------------------------------------- host
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// boxes of 64 columns x `rows` rows x both pieces
+bool map_of(const Pieces& x, int rows, CUtensorMap* m) {
+  const auto encode = encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2};
+  const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane() * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)rows, 2}, one[3] = {1, 1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.hi, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count() {
+  static std::atomic<int> sms[kMaxDevices];
+  return per_device(sms, [] {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return 0;
+    return n;
+  });
+}
+
+template <int BN, bool AMN, bool BMN>
+nmd_status launch_bn(const Pieces& a, const Pieces& b, const Gemm& g, cudaStream_t s) {
+  static std::atomic<int> ready[kMaxDevices];
+  auto kernel = gemm_kernel<BN, AMN, BMN>;
+  if (!per_device(ready, [&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<BN>::SMEM) == cudaSuccess;
+      }))
+    return NMD_ERR_CUDA;
+  CUtensorMap ta, tb;
+  if (!map_of(a, AMN ? 64 : kBM, &ta) || !map_of(b, BMN ? 64 : BN, &tb)) return NMD_ERR_CUDA;
+  const int sms = sm_count();
+  if (sms == 0) return NMD_ERR_CUDA;
+  kernel<<<std::min(g.items, sms), kGemmThreads, Cfg<BN>::SMEM, s>>>(ta, tb, g);
+  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+}
+template <bool AMN, bool BMN>
+nmd_status launch(int BN, const Pieces& a, const Pieces& b, const Gemm& g, cudaStream_t s) {
+  if (BN == 256) return launch_bn<256, AMN, BMN>(a, b, g, s);
+  if (BN == 128) return launch_bn<128, AMN, BMN>(a, b, g, s);
+  return launch_bn<64, AMN, BMN>(a, b, g, s);
+}
+
+int64_t tiles_of(int64_t M, int64_t N, int BN, bool lower) {
+  const int64_t tm = (M + kBM - 1) / kBM, tn = (N + BN - 1) / BN;
+  if (!lower) return tm * tn;
+  int64_t n = 0;
+  for (int64_t i = 0; i < tm; ++i) n += std::min<int64_t>((kBM * (i + 1) - 1) / BN + 1, tn);
+  return n;
+}
+// The widest tiles that still give every SM one; 64 columns where none do.
+int columns_of(int64_t M, int64_t N, bool lower) {
+  for (int BN : {256, 128})
+    if (N > BN / 2 && tiles_of(M, N, BN, lower) >= kSms) return BN;
+  return 64;
+}
+
+// The sums of a Gram matrix run over the long side: tiles, and parts of the sum where there are few of them
+struct GramPlan {
+  int BN;
+  int64_t tiles, splits;
+};
+GramPlan gram_plan(int64_t r, int64_t M) {
+  GramPlan g;
+  const int64_t blocks = (M + kBK - 1) / kBK;
+  g.BN = r <= 64 ? 64 : tiles_of(r, r, 256, true) >= kSms ? 256 : 128;
+  g.tiles = tiles_of(r, r, g.BN, true);
+  g.splits = std::max<int64_t>(1, std::min<int64_t>(kSms / g.tiles, blocks / kChunk));
+  return g;
+}
+
+// What a call keeps in its workspace
+struct Layout {
+  size_t status, parts, X[2], A, P, part, bytes;
+  int64_t R, C, ldx, r, ldr;
+};
+Layout layout_of(int64_t R, int64_t C) {
+  Layout l;
+  l.R = R;
+  l.C = C;
+  l.ldx = (C + 63) / 64 * 64;
+  l.r = std::min(R, C);
+  l.ldr = (l.r + 63) / 64 * 64;
+  const GramPlan g = gram_plan(l.r, std::max(R, C));
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t here = at;
+    at += align256(n);
+    return here;
+  };
+  l.status = take(256);
+  l.parts = take(kParts * sizeof(double));
+  for (size_t& x : l.X) x = take((size_t)R * l.ldx * 4);
+  l.A = take((size_t)l.r * l.ldr * 4);
+  l.P = take((size_t)l.r * l.ldr * 4);
+  l.part = take(g.splits > 1 ? (size_t)(g.tiles * g.splits) * kBM * g.BN * 4 : 0);
+  l.bytes = at;
+  return l;
+}
+
 nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t s) {
-  const int64_t n = j.rows * j.cols, r = std::min(j.rows, j.cols), M = std::max(j.rows, j.cols);
+  const Layout l = layout_of(j.R, j.C);
   char* w = (char*)ws;
-  double* parts = (double*)w;
-  w += align256(kParts * sizeof(double));
-  float* X = (float*)w;
-  w += align256((size_t)n * 4);
-  float* Y = (float*)w;
-  w += align256((size_t)n * 4);
-  float* A = (float*)w;
-  w += align256((size_t)(r * r) * 4);
-  float* P = (float*)w;
-  update_kernel<<<kParts, kThreads, 0, s>>>(j, X, parts);
-  normalise_kernel<<<kParts, kThreads, 0, s>>>(X, n, parts, kParts, j.eps);
-  const bool tall = j.rows > j.cols;
-  const View none{nullptr, 0, 0}, VA{A, r, 1}, VP{P, r, 1};
+  int* status = (int*)(w + l.status);
+  int* shift = status + 4;   // steps + 1 of them
+  double* parts = (double*)(w + l.parts);
+  Pieces X{(__half*)(w + l.X[0]), j.R, j.C, l.ldx}, Y{(__half*)(w + l.X[1]), j.R, j.C, l.ldx};
+  const Pieces A{(__half*)(w + l.A), l.r, l.r, l.ldr}, P{(__half*)(w + l.P), l.r, l.r, l.ldr};
+  const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
+  const int64_t r = l.r, M = std::max(j.R, j.C);
+  const int64_t work = (j.C + kThreads * kEach - 1) / (kThreads * kEach) * j.R;
+  const int grid = (int)std::min<int64_t>(work, kParts);
+  norm_kernel<<<grid, kThreads, 0, s>>>(j, parts, status);
+  const int grows = (int)std::ceil(std::log2(std::max(1.0, 1.001 * std::fabs(k[0]))));
+  pieces_kernel<<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
+  if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
+  const GramPlan plan = gram_plan(r, M);
+  const int bn_r = columns_of(r, r, true), bn_x = columns_of(j.R, j.C, false);
+  auto product = [&](int64_t m, int64_t n, int64_t depth, int BN, bool lower, Mode mode) {
+    Gemm g{};
+    g.M = m;
+    g.N = n;
+    g.kblocks = (int)((depth + kBK - 1) / kBK);
+    g.splits = 1;
+    g.tiles_n = (int)((n + BN - 1) / BN);
+    g.items = (int)tiles_of(m, n, BN, lower);
+    g.lower = lower;
+    g.mode = mode;
+    g.status = status;
+    return g;
+  };
+  nmd_status st;
   for (int i = 0; i < steps; ++i) {
-    const View x{X, tall ? 1 : j.cols, tall ? j.cols : 1}, xt{X, x.col, x.row}, y{Y, x.row, x.col};   // r x M
-    product(x, xt, VA, none, r, r, M, 1.f, 0.f, s);
-    product(VA, VA, VP, VA, r, r, r, (float)k[2], (float)k[1], s);
-    product(VP, x, y, x, r, M, r, 1.f, (float)k[0], s);
+    // A = X X^T: 2^24 a in the sums, 2^12 a in the pieces
+    Gemm g = product(r, r, M, plan.BN, true, plan.splits > 1 ? kPartial : kSymmetric);
+    g.alpha = 1.f / kUnit;
+    g.d = A;
+    g.down = shift + i;
+    g.times = 2;
+    g.splits = (int)plan.splits;
+    g.items *= g.splits;
+    g.part = (float*)(w + l.part);
+    st = wide ? launch<false, false>(plan.BN, X, X, g, s) : launch<true, true>(plan.BN, X, X, g, s);
+    if (st != NMD_OK) return st;
+    if (plan.splits > 1) {
+      join_kernel<<<(unsigned)(plan.tiles * kBM * (plan.BN / 32)), kThreads, 0, s>>>(g, plan.BN);
+      if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
+    }
+    // P = a I + b A + c A A
+    g = product(r, r, r, bn_r, true, kSymmetric);
+    g.alpha = (float)(k[2] / kUnit);
+    g.beta = (float)k[1];
+    g.diag = (float)(k[0] * kUnit);
+    g.c = A;
+    g.d = P;
+    if ((st = launch<false, false>(bn_r, A, A, g, s)) != NMD_OK) return st;
+    // X <- P X, or X P: P is symmetric
+    const bool last = i + 1 == steps;
+    g = product(j.R, j.C, r, bn_x, false, last ? kResult : kMatrix);
+    g.alpha = last ? 1.f / (kUnit * kUnit) : 1.f / kUnit;
+    g.up = last ? nullptr : shift + i + 1;
+    g.down = shift + i;
+    g.times = 1;
+    g.d = Y;
+    g.out = j;
+    st = wide ? launch<false, true>(bn_x, P, X, g, s) : launch<false, false>(bn_x, X, P, g, s);
+    if (st != NMD_OK) return st;
     std::swap(X, Y);
   }
-  finish_kernel<<<kParts, kThreads, 0, s>>>(j, X);
-  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  return NMD_OK;
 }
 
 // Whether the elements of a matrix lie apart, and the bytes from its first to its last
@@ -181,6 +745,14 @@ bool check(const void* x, int dtype, int64_t rows, int64_t cols, int64_t rs, int
   *at = Range{(uintptr_t)x, (uintptr_t)x + (uintptr_t)reach};
   return true;
 }
+// whether the rows' elements lie further apart than the columns'
+bool columns_apart(int64_t rows, int64_t cols, int64_t rs, int64_t cs) {
+  return rows > 1 && (cols <= 1 || rs < cs);
+}
+void turn(Job* j) {   // the transpose of every matrix: the steps are the same
+  std::swap(j->R, j->C);
+  for (Matrix* m : {&j->grad, &j->momentum, &j->out}) std::swap(m->rs, m->cs);
+}
 bool sizes_ok(int64_t rows, int64_t cols) {
   return rows >= 0 && cols >= 0 && rows < ((int64_t)1 << 31) && cols < ((int64_t)1 << 31) && std::min(rows, cols) <= kMostSide &&
          (rows == 0 || cols <= ((int64_t)1 << 36) / rows);
@@ -199,8 +771,8 @@ extern "C" {
 
 nmd_status nmd_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes) {
   if (!sizes_ok(rows, cols) || !bytes) return NMD_ERR_INVALID;
-  const size_t n = (size_t)rows * (size_t)cols, r = (size_t)std::min(rows, cols);
-  *bytes = align256(kParts * sizeof(double)) + 2 * align256(n * 4) + 2 * align256(r * r * 4);
+  // either side may be the adjacent one
+  *bytes = rows == 0 || cols == 0 ? 256 : std::max(layout_of(rows, cols).bytes, layout_of(cols, rows).bytes);
   return NMD_OK;
 }
 
@@ -220,11 +792,12 @@ nmd_status nmd_orthogonalize(const void* d_update, int32_t dtype, int64_t rows, 
     return NMD_ERR_INVALID;
   if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   Job j{};
-  j.rows = rows;
-  j.cols = cols;
+  j.R = rows;
+  j.C = cols;
   j.grad = Matrix{(void*)d_update, dtype, row_stride, col_stride};
   j.out = Matrix{d_out, dtype, out_row_stride, out_col_stride};
   j.eps = eps;
+  if (columns_apart(rows, cols, row_stride, col_stride)) turn(&j);
   return run(j, steps, coefficients, d_workspace, (cudaStream_t)stream);
 }
 
@@ -247,8 +820,8 @@ nmd_status nmd_muon_step(const nmd_matrix* weight, const nmd_matrix* grad, const
     return NMD_ERR_INVALID;
   if (!d_workspace || ws_bytes < need || ((uintptr_t)d_workspace & 255u)) return NMD_ERR_WORKSPACE;
   Job j{};
-  j.rows = rows;
-  j.cols = cols;
+  j.R = rows;
+  j.C = cols;
   j.grad = Matrix{grad->data, grad->dtype, grad->row_stride, grad->col_stride};
   j.momentum = Matrix{momentum->data, momentum->dtype, momentum->row_stride, momentum->col_stride};
   j.out = Matrix{weight->data, weight->dtype, weight->row_stride, weight->col_stride};
@@ -259,6 +832,7 @@ nmd_status nmd_muon_step(const nmd_matrix* weight, const nmd_matrix* grad, const
   j.keep = (float)(1.0 - lr * weight_decay);
   j.lr = (float)(lr * scale);
   j.eps = eps;
+  if (columns_apart(rows, cols, weight->row_stride, weight->col_stride)) turn(&j);
   return run(j, steps, coefficients, d_workspace, (cudaStream_t)stream);
 }
 
