@@ -33,20 +33,28 @@ constexpr int kParts = 608;          // CTAs of the norm's pass: four per SM
 constexpr int kSms = 152;            // the splitting of sums goes by this number, not by the device, for equal bits
 constexpr float kUnit = 4096.f;      // pieces hold 2^12 x
 
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(bf16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ void from_float(float v, float* x) { *x = v; }
+__device__ __forceinline__ void from_float(float v, bf16* x) { *x = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void from_float(float v, __half* x) { *x = __float2half_rn(v); }
+
 struct Matrix {   // elements at i rs + j cs
   void* x;
   int dtype;
   int64_t rs, cs;
+  template <class T>
+  __device__ __forceinline__ T& at(int64_t i, int64_t j) const {
+    return ((T*)x)[i * rs + j * cs];
+  }
   __device__ __forceinline__ float get(int64_t i, int64_t j) const {
-    const int64_t e = i * rs + j * cs;
-    return dtype == NMD_DT_FP32 ? ((const float*)x)[e]
-                                : dtype == NMD_DT_BF16 ? __bfloat162float(((const bf16*)x)[e]) : __half2float(((const __half*)x)[e]);
+    return dtype == NMD_DT_FP32 ? at<float>(i, j) : dtype == NMD_DT_BF16 ? as_float(at<bf16>(i, j)) : as_float(at<__half>(i, j));
   }
   __device__ __forceinline__ void put(int64_t i, int64_t j, float v) const {
-    const int64_t e = i * rs + j * cs;
-    if (dtype == NMD_DT_FP32) ((float*)x)[e] = v;
-    else if (dtype == NMD_DT_BF16) ((bf16*)x)[e] = __float2bfloat16_rn(v);
-    else ((__half*)x)[e] = __float2half_rn(v);
+    if (dtype == NMD_DT_FP32) from_float(v, &at<float>(i, j));
+    else if (dtype == NMD_DT_BF16) from_float(v, &at<bf16>(i, j));
+    else from_float(v, &at<__half>(i, j));
   }
 };
 
@@ -89,32 +97,55 @@ __device__ __forceinline__ double squares(const float (&f)[N]) {
 }
 __device__ __forceinline__ float update_of(const Job& j, float m, float g) { return j.nesterov ? fmaf(j.beta, m, j.rest * g) : m; }
 
-constexpr int kEach = 8;   // elements of a thread at a time
+// A warp takes kEach groups of 32 adjacent elements at a time: of as many rows, or of
+// one row where there are fewer.
+constexpr int kEach = 8;
+struct Walk {
+  int64_t across, work;   // pieces of work of a row (of rows), and in all
+  int down, step;         // rows and columns from one group to the next
+};
+__host__ __device__ __forceinline__ Walk walk_of(int64_t R, int64_t C) {
+  Walk w;
+  const bool rows = R >= kEach;
+  w.down = rows ? 1 : 0;
+  w.step = rows ? 0 : 32;
+  const int wide = rows ? 32 : 32 * kEach;
+  w.across = (C + wide - 1) / wide;
+  w.work = w.across * (rows ? (R + kEach - 1) / kEach : R);
+  return w;
+}
+// the elements of one piece of work: f(i, row, column) for those that there are
+template <class F>
+__device__ __forceinline__ void each(const Walk& w, const Job& j, int64_t at, F f) {
+  const int64_t q = at / w.across, r0 = q * (w.down ? kEach : 1), c0 = (at - q * w.across) * (w.down ? 32 : 32 * kEach) + (threadIdx.x & 31);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (r0 + i * w.down < j.R && c0 + i * w.step < j.C) f(i, r0 + i * w.down, c0 + i * w.step);
+}
 
 // M <- beta M + (1 - beta) G, and the sum of squares of the update
+template <class G, class M, bool STEP>
 __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, int* status) {
   __shared__ double red[kThreads / 32];
   if (blockIdx.x == 0 && threadIdx.x < 2) status[threadIdx.x] = 0;
   double sum = 0.0;
-  const int64_t across = (j.C + kThreads * kEach - 1) / (kThreads * kEach), work = across * j.R;
-  for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-    const int64_t r = w / across, c0 = (w - r * across) * (kThreads * kEach) + threadIdx.x;
+  const Walk w = walk_of(j.R, j.C);
+  for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
+    G g[kEach];
+    M m[kEach];
     float u[kEach];
+    each(w, j, at, [&](int i, int64_t r, int64_t c) { g[i] = j.grad.at<G>(r, c); });
+    if (STEP) each(w, j, at, [&](int i, int64_t r, int64_t c) { m[i] = j.momentum.at<M>(r, c); });
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) u[i] = c0 + i * kThreads < j.C ? j.grad.get(r, c0 + i * kThreads) : 0.f;
-    if (j.step) {
-      float m[kEach];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) m[i] = c0 + i * kThreads < j.C ? j.momentum.get(r, c0 + i * kThreads) : 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int64_t c = c0 + i * kThreads;
-        if (c < j.C) {
-          j.momentum.put(r, c, fmaf(j.beta, m[i], j.rest * u[i]));
-          u[i] = update_of(j, j.momentum.get(r, c), u[i]);   // of the momentum as it is stored
-        }
+    for (int i = 0; i < kEach; ++i) u[i] = 0.f;
+    each(w, j, at, [&](int i, int64_t r, int64_t c) {
+      u[i] = as_float(g[i]);
+      if (STEP) {
+        from_float(fmaf(j.beta, as_float(m[i]), j.rest * u[i]), &m[i]);
+        j.momentum.at<M>(r, c) = m[i];
+        u[i] = update_of(j, as_float(m[i]), u[i]);   // of the momentum as it is stored
       }
-    }
+    });
     sum += squares(u);
   }
 #pragma unroll
@@ -130,6 +161,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, in
 
 // X = update / (norm + eps) in pieces
 // shift: t of X before each step and after the last
+template <class G, class M, bool STEP>
 __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
                                                           int grows) {
   __shared__ double red[kThreads / 32];
@@ -156,26 +188,19 @@ __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const
   const float f = (float)frexp((double)kUnit / (norm + j.eps), &e);
   e = max(-280, min(280, e + small));
   const float p = ldexpf(1.f, e / 2), q = ldexpf(1.f, e - e / 2);
-  const int64_t across = (j.C + kThreads * kEach - 1) / (kThreads * kEach), work = across * j.R;
-  for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-    const int64_t r = w / across, c0 = (w - r * across) * (kThreads * kEach) + threadIdx.x;
-    float u[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) u[i] = c0 + i * kThreads < j.C ? j.grad.get(r, c0 + i * kThreads) : 0.f;
-    if (j.step) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if (c0 + i * kThreads < j.C) u[i] = update_of(j, j.momentum.get(r, c0 + i * kThreads), u[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int64_t c = c0 + i * kThreads;
-      if (c >= j.C) continue;
+  const Walk w = walk_of(j.R, j.C);
+  for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
+    G g[kEach];
+    M m[kEach];
+    each(w, j, at, [&](int i, int64_t r, int64_t c) { g[i] = j.grad.at<G>(r, c); });
+    if (STEP) each(w, j, at, [&](int i, int64_t r, int64_t c) { m[i] = j.momentum.at<M>(r, c); });
+    each(w, j, at, [&](int i, int64_t r, int64_t c) {
+      const float u = STEP ? update_of(j, as_float(m[i]), as_float(g[i])) : as_float(g[i]);
       __half hi, lo;
-      split(u[i] * p * q * f, hi, lo);
+      split(u * p * q * f, hi, lo);
       X.hi[r * X.ld + c] = hi;
       X.hi[X.plane() + r * X.ld + c] = lo;
-    }
+    });
   }
 }
 
@@ -643,6 +668,13 @@ Layout layout_of(int64_t R, int64_t C) {
   return l;
 }
 
+template <class F>
+void with_type(int dtype, F f) {
+  if (dtype == NMD_DT_FP32) f(0.f);
+  else if (dtype == NMD_DT_BF16) f(bf16{});
+  else f(__half{});
+}
+
 nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t s) {
   const Layout l = layout_of(j.R, j.C);
   char* w = (char*)ws;
@@ -653,11 +685,21 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
   const Pieces A{(__half*)(w + l.A), l.r, l.r, l.ldr}, P{(__half*)(w + l.P), l.r, l.r, l.ldr};
   const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
   const int64_t r = l.r, M = std::max(j.R, j.C);
-  const int64_t work = (j.C + kThreads * kEach - 1) / (kThreads * kEach) * j.R;
-  const int grid = (int)std::min<int64_t>(work, kParts);
-  norm_kernel<<<grid, kThreads, 0, s>>>(j, parts, status);
+  const int grid = (int)std::min<int64_t>((walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
   const int grows = (int)std::ceil(std::log2(std::max(1.0, 1.001 * std::fabs(k[0]))));
-  pieces_kernel<<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
+  with_type(j.grad.dtype, [&](auto g) {
+    with_type(j.step ? j.momentum.dtype : j.grad.dtype, [&](auto m) {
+      typedef decltype(g) G;
+      typedef decltype(m) M;
+      if (j.step) {
+        norm_kernel<G, M, true><<<grid, kThreads, 0, s>>>(j, parts, status);
+        pieces_kernel<G, M, true><<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
+      } else {
+        norm_kernel<G, G, false><<<grid, kThreads, 0, s>>>(j, parts, status);
+        pieces_kernel<G, G, false><<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
+      }
+    });
+  });
   if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
   const GramPlan plan = gram_plan(r, M);
   const int bn_r = columns_of(r, r, true), bn_x = columns_of(j.R, j.C, false);
