@@ -1,30 +1,39 @@
 // One step of beam search over the rows of a logits matrix, and the beams'
 // states in the order of their parents (formulas in include/nmd.h).
-#include <cuda_fp16.h>
-
+//
+// A cluster of CTAs per group reads the rows of the beams that are in use once.  The
+// rows' columns are dealt to its CTAs in equal contiguous runs, whatever the number
+// of beams; a run that ends one row and begins the next is two segments.  Of a
+// segment a CTA keeps the running sum of the softmax and the `width` largest logits:
+// within a row the logits' order is that of the offers, so that nothing has to wait
+// for the row's sum.  The segments' lists go to the cluster's first CTA, which adds up
+// the sums and merges the lists by the offers' values in fp64.
+//
+// What is largest is found on the way at the cost of one comparison per four vectors:
+// a group of elements whose sum of powers is below the power of the width-th largest
+// so far holds nothing that could displace it.  (The elements themselves are looked at
+// in the few groups that pass.)
 #include <algorithm>
 #include <cmath>
 #include <memory>
 #include <new>
 
-#include "nmd_internal.cuh"
-#include "softmax_sum.cuh"
+#include "row_vec.cuh"
+#include "tc_ptx.cuh"
 
 namespace nmd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostBeams = 64, kMostWidth = 128;
-
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ float as_float(bf16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
+constexpr int kMostBeams = 64, kMostWidth = 128, kMostCluster = 8;
+constexpr int kDepth = 3;   // groups of four vectors under way
 
 struct Select {
   const void* x;
   int64_t V, ld;
   int K, width;
-  double inv_temp;
+  Scale c;
+  double log2_scale, inv_temp;   // c in fp64, 1 / tau
   const float* scores;
   const uint8_t* finished;
   int64_t end;
@@ -34,101 +43,360 @@ struct Select {
   uint8_t* out_finished;
 };
 
-// an offer: its value and its place among the group's (beam, column) pairs
-struct Offer {
-  double value;
-  int64_t at;
-  __device__ __forceinline__ bool before(const Offer& o) const { return value > o.value || (value == o.value && at < o.at); }
-};
-__device__ __forceinline__ Offer better(Offer a, Offer b) { return b.before(a) ? b : a; }
+// A logit and its column as one number: larger logits first, of equal ones (0 and -0
+// are equal) the lower column.
+typedef unsigned long long entry_t;
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return (int)b < 0 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ entry_t entry_of(float x, int64_t col) { return (entry_t)order_of(x) << 32 | (0xffffffffu - (uint32_t)col); }
+__device__ __forceinline__ float value_of(entry_t e) {
+  const uint32_t o = (uint32_t)(e >> 32);
+  return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint32_t column_of(entry_t e) { return 0xffffffffu - (uint32_t)e; }
 
-__device__ __forceinline__ Offer cta_best(Offer o, Offer* red) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    Offer p;
-    p.value = __shfl_xor_sync(0xffffffffu, o.value, d);
-    p.at = __shfl_xor_sync(0xffffffffu, o.at, d);
-    o = better(o, p);
+// The largest entries so far: up to `limit` of them between rounds, the width largest
+// after a cut.  A round adds at most 36 width.
+struct Best {
+  entry_t* list;       // limit + 36 width
+  entry_t* sorted;     // width
+  int* count;
+  entry_t* least;      // what an entry has to be above
+  int width, limit, room;
+
+  // the width largest of the list, in order; what is not among them cannot come back.
+  // The whole CTA; ends with a barrier.
+  __device__ __noinline__ void cut() {
+    const int n = min(*count, room);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const entry_t e = list[i];
+      int rank = 0;
+      for (int k = 0; k < n; ++k) rank += list[k] > e;
+      if (rank < width) sorted[rank] = e;
+    }
+    __syncthreads();
+    const int kept = min(n, width);
+    for (int i = threadIdx.x; i < kept; i += kThreads) list[i] = sorted[i];
+    if (threadIdx.x == 0) {
+      *count = kept;
+      if (kept == width) *least = sorted[width - 1];
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = o;
-  __syncthreads();
-  for (int i = 0; i < kThreads / 32; ++i) o = better(o, red[i]);
-  return o;
+};
+
+// Dynamic shared memory: slots, then the lists
+struct Shape {
+  int cluster, limit, room;
+  size_t off_list, off_sorted, off_all, bytes;
+};
+Shape shape_of(int64_t K, int width, int cluster) {
+  Shape s;
+  s.cluster = cluster;
+  s.limit = std::max(4 * width, 64);
+  s.room = s.limit + 36 * width;
+  s.off_list = (size_t)kDepth * 4 * kThreads * 16;
+  s.off_sorted = s.off_list + (size_t)s.room * 8;
+  s.off_all = s.off_sorted + (size_t)width * 8;
+  s.bytes = s.off_all + (size_t)(K + cluster) * width * 8;   // the segments' lists, in the first CTA
+  return s;
 }
 
-// A CTA per group: every row's maximum and sum, then the offers one by one, each the
-// best of those that come after the last one taken.
+__device__ __forceinline__ uint32_t first_cta(const void* p) {   // the address in the cluster's first CTA
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(tc::smem_u32(p)));
+  return a;
+}
+__device__ __forceinline__ void put_remote(uint32_t at, entry_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
+}
+
+// Bound by HBM; one group by the launch, two barriers of the cluster and the merge.
 template <class T>
-__global__ void __launch_bounds__(kThreads) select_kernel(Select a) {
-  __shared__ Offer red[kThreads / 32];
-  __shared__ double base[kMostBeams], top[kMostBeams], sums[kThreads / 32];
-  __shared__ int kind[kMostBeams];   // 0: offers nothing, 1: a row, 2: finished
-  const int64_t b = blockIdx.x;
-  const int64_t none = (int64_t)1 << 62;
-  for (int k = 0; k < a.K; ++k) {
-    const float s = a.scores[b * a.K + k];
-    const bool used = fabsf(s) < INFINITY;
-    const bool done = a.finished != nullptr && a.finished[b * a.K + k] != 0;
-    if (!used || done) {
-      if (threadIdx.x == 0) {
-        kind[k] = used ? 2 : 0;
-        base[k] = s;
+__global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_constant__ Select a, const __grid_constant__ Shape shape) {
+  constexpr int N = Vec<T>::N;
+  constexpr int kSegments = kMostBeams + kMostCluster;
+  extern __shared__ uint4 slots[];
+  __shared__ Stat red[kThreads / 32], stats[kSegments];
+  __shared__ int counts[kSegments], row_beam[kMostBeams], done_beam[kMostBeams], count, rows_in_use, finished_in_use;
+  __shared__ float row_score[kMostBeams], done_score[kMostBeams];
+  __shared__ double base[kMostBeams];
+  __shared__ float top[kMostBeams];
+  __shared__ entry_t least, bests[kThreads];
+  char* raw = (char*)slots;
+  Best best{(entry_t*)(raw + shape.off_list), (entry_t*)(raw + shape.off_sorted), &count, &least, a.width, shape.limit, shape.room};
+  entry_t* all = (entry_t*)(raw + shape.off_all);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  unsigned csize, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  if (csize > 1) cluster_arrive();   // waited for before the first CTA's shared memory is written
+  const int64_t b = blockIdx.x / csize;
+
+  // the beams whose rows are read, and the finished ones
+  if (warp == 0) {
+    int rows = 0, done = 0;
+    for (int k0 = 0; k0 < a.K; k0 += 32) {
+      const int k = k0 + lane;
+      const float s = k < a.K ? a.scores[b * a.K + k] : -INFINITY;
+      const bool used = fabsf(s) < INFINITY;
+      const bool fin = used && a.finished != nullptr && a.finished[b * a.K + k] != 0;
+      const unsigned m = __ballot_sync(0xffffffffu, used && !fin), f = __ballot_sync(0xffffffffu, fin);
+      const int before = __popc(m & ((1u << lane) - 1)), fbefore = __popc(f & ((1u << lane) - 1));
+      if (used && !fin) {
+        row_beam[rows + before] = k;
+        row_score[rows + before] = s;
       }
-      continue;
+      if (fin) {
+        done_beam[done + fbefore] = k;
+        done_score[done + fbefore] = s;
+      }
+      rows += __popc(m);
+      done += __popc(f);
     }
-    const T* row = (const T*)a.x + (b * a.K + k) * a.ld;
-    Offer m{-INFINITY, 0};
-    bool bad = false;
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-      const float x = as_float(row[v]);
-      bad |= !(x < INFINITY);
-      m.value = fmax(m.value, (double)x);
-    }
-    bad = __syncthreads_or(bad);
-    m = cta_best(m, red);
-    double sum = 0.0;
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads)
-      sum += m.value > -INFINITY ? exp(((double)as_float(row[v]) - m.value) * a.inv_temp) : 0.0;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      sum = 0.0;
-      for (int i = 0; i < kThreads / 32; ++i) sum += sums[i];
-      kind[k] = !bad && m.value > -INFINITY;
-      base[k] = s - log(sum);
-      top[k] = m.value;
+    if (lane == 0) {
+      rows_in_use = rows;
+      finished_in_use = done;
     }
   }
   __syncthreads();
-  Offer last{INFINITY, -1};
+  const int R = rows_in_use;
+  const int64_t total = R * a.V, from = total * rank / csize, to = total * (rank + 1) / csize;
+  const uint4* mine = slots + tid;
+  bool waited = csize == 1;
+
+  for (int64_t at = from; at < to;) {
+    const int row = (int)(at / a.V);
+    const int64_t e0 = at - row * a.V, e1 = min(a.V, to - row * a.V);
+    at = row * a.V + e1;
+    const T* x = (const T*)a.x + (b * a.K + row_beam[row]) * a.ld;
+    const Span sp = span_of(x, a.V);
+    // this segment's vectors; the cut between two CTAs falls on the same vector for both
+    auto vector_at = [&](int64_t e) { return e == 0 ? (int64_t)0 : e == a.V ? sp.nvec : min(sp.nvec, max((int64_t)0, (e - sp.head) / N)); };
+    const int64_t v0 = vector_at(e0);
+    const int n = (int)(vector_at(e1) - v0);
+    const uint4* xv = (const uint4*)(x + sp.head) + v0;
+    // elements before and after the row's vectors
+    int64_t scalar = -1;
+    if (e0 == 0 && tid < sp.head) scalar = tid;
+    if (e1 == a.V && tid >= 32 && tid - 32 < sp.tail) scalar = sp.head + sp.nvec * N + tid - 32;
+
+    int ahead = tid;
+    auto load = [&](int slot) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q, ahead += kThreads)
+        if (ahead < n) copy_async(tc::smem_u32(mine + (slot * 4 + q) * kThreads), xv + ahead);
+      copy_commit();
+    };
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) load(d);
+    const T xs = scalar >= 0 ? x[scalar] : Vec<T>::put(0.f);
+    if (tid == 0) {
+      count = 0;
+      least = entry_of(-INFINITY, 0);   // a banned column is not among them
+    }
+    __syncthreads();
+
+    Running<T> run;
+    const int rounds = (n + 4 * kThreads - 1) / (4 * kThreads);
+    int d = 0;
+    for (int i = 0; i <= rounds; ++i) {   // the last one: the single elements
+      const int v = i * 4 * kThreads + tid;
+      auto get = [&](int q) { return v + q * kThreads < n ? mine[(d * 4 + q) * kThreads] : Vec<T>::none(); };
+      const entry_t bar = least;   // it only rises, and between barriers
+      entry_t mybest = 0;
+      if (i < rounds) {
+        copy_wait<kDepth - 1>();
+        float group;
+        if (v + 3 * kThreads < n) group = run.add([&](int q) { return mine[(d * 4 + q) * kThreads]; }, a.c);
+        else group = run.add(get, a.c);
+        const float bar_x = value_of(bar);
+        // (0.99 is far more than the sum's rounding)
+        if (!(group < 0.99f * ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo))) {
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            const uint4 w = get(q);
+            const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
+#pragma unroll
+            for (int e = 0; e < N; ++e) mybest = max(mybest, entry_of(Vec<T>::get(((const T*)&w)[e]), col + e));
+          }
+        }
+      } else if (scalar >= 0) {
+        run.add(Vec<T>::get(xs), a.c);
+        mybest = entry_of(Vec<T>::get(xs), scalar);
+      }
+      const int some = __syncthreads_count(mybest > bar);
+      if (some > 0) {   // the same for the whole CTA, as is all that follows
+        entry_t over = bar;
+        if (some > a.width) {
+          // the width-th of the threads' largest: nothing at or below it is among the width largest but itself
+          bests[tid] = mybest > bar ? mybest : 0;
+          __syncthreads();
+          if (mybest > bar) {
+            int r = 0;
+            for (int k = 0; k < kThreads; ++k) r += bests[k] > mybest;
+            if (r == a.width - 1) least = mybest - 1;
+          }
+          __syncthreads();
+          over = least;
+        }
+        if (mybest > over) {
+          if (i < rounds) {
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const uint4 w = get(q);
+              const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
+#pragma unroll
+              for (int e = 0; e < N; ++e) {
+                const entry_t k = entry_of(Vec<T>::get(((const T*)&w)[e]), col + e);
+                if (k > over) {
+                  const int p = atomicAdd(&count, 1);
+                  if (p < shape.room) best.list[p] = k;
+                }
+              }
+            }
+          } else {
+            const int p = atomicAdd(&count, 1);
+            if (p < shape.room) best.list[p] = mybest;
+          }
+        }
+        __syncthreads();
+        if (count >= shape.limit) best.cut();
+      }
+      if (i < rounds) {
+        load(d);
+        if (++d == kDepth) d = 0;
+      }
+    }
+    copy_wait<0>();
+    // the segment's sum and list
+    const Stat st = merge_lanes<32>(run.s, a.c);
+    if (lane == 0) red[warp] = st;
+    best.cut();
+    if (!waited) {
+      cluster_wait();
+      waited = true;
+    }
+    const int seg = row + (int)rank, kept = count;
+    const uint32_t to_list = first_cta(all + (int64_t)seg * a.width);
+    for (int i = tid; i < kept; i += kThreads) put_remote(to_list + i * 8, best.sorted[i]);
+    if (warp == 0) {
+      const Stat s = merge_lanes<32>(lane < kThreads / 32 ? red[lane] : Stat{-INFINITY, 0.f}, a.c);
+      if (lane == 0) {
+        put_remote(first_cta(stats + seg), (entry_t)__float_as_uint(s.m) | (entry_t)__float_as_uint(s.S) << 32);
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(first_cta(counts + seg)), "r"(kept) : "memory");
+      }
+    }
+    __syncthreads();
+  }
+  if (csize > 1) {
+    if (!waited) cluster_wait();
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
+
+  // A row's segments are row + q for the CTAs q that hold part of it
+  auto first_of = [&](int row) {   // the CTA that holds the row's first column
+    int q = 0;
+    while (q + 1 < (int)csize && total * (q + 1) / csize <= row * a.V) ++q;
+    return q;
+  };
+  auto last_of = [&](int row) {
+    int q = first_of(row);
+    while (q + 1 < (int)csize && total * (q + 1) / csize < (row + 1) * a.V) ++q;
+    return q;
+  };
+  for (int row = tid; row < R; row += kThreads) {
+    const int q0 = first_of(row), q1 = last_of(row);
+    float m = -INFINITY;
+    for (int q = q0; q <= q1; ++q) m = max_nan(m, stats[row + q].m);
+    float S = 0.f;
+    for (int q = q0; q <= q1; ++q) S += stats[row + q].S * rescale(stats[row + q].m, m, a.c);
+    // the sum is S 2^reference; offers are score + (x - m) / tau - (ln S + ln 2 (reference - c m))
+    const double cm = a.log2_scale * (double)m;
+    const double over = is_near(m, a.c) ? (double)ref_of(m, a.c) - cm : 0.0;
+    base[row] = m < INFINITY && S > 0.f ? (double)row_score[row] - (log((double)S) + kLn2 * over) : NAN;
+    top[row] = m;
+  }
+  __syncthreads();
+  if (warp != 0) return;
+
+  // Lists are in order: of their heads the best is the next offer.  Lane l has lists l,
+  // l + 32, ...: the segments', then the finished beams.
+  const int segments = R + (int)csize - 1, lists = segments + finished_in_use;
+  constexpr int kLists = (kMostBeams + kMostCluster + kMostBeams + 31) / 32;
+  int next[kLists];
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) next[i] = 0;
+  const int64_t none = (int64_t)1 << 62;
+  double value = -INFINITY;   // of this lane's best head
+  int64_t place = none;       // beam V + column
+  int from_list = 0;
+  auto row_of = [&](int seg) {   // the row of segment row + q: there is one q with both borders right
+    for (int row = max(0, seg - (int)csize + 1); row <= min(R - 1, seg); ++row)
+      if (first_of(row) <= seg - row && seg - row <= last_of(row)) return row;
+    return -1;
+  };
+  int rows[kLists];
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) rows[i] = lane + 32 * i < segments ? row_of(lane + 32 * i) : -1;
+  auto look = [&] {
+    value = -INFINITY;
+    place = none;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+      const int l = lane + 32 * i;
+      double v = -INFINITY;
+      int64_t p = none;
+      if (l < segments) {
+        if (rows[i] >= 0 && next[i] < counts[l]) {
+          const entry_t e = all[(int64_t)l * a.width + next[i]];
+          v = base[rows[i]] + ((double)value_of(e) - (double)top[rows[i]]) * a.inv_temp;
+          p = row_beam[rows[i]] * a.V + column_of(e);
+        }
+      } else if (l < lists && next[i] == 0) {
+        v = done_score[l - segments];
+        p = done_beam[l - segments] * a.V + a.end;
+      }
+      if (v > value || (v == value && v > -INFINITY && p < place)) {
+        value = v;
+        place = p;
+        from_list = i;
+      }
+    }
+  };
+  look();
   for (int i = 0; i < a.width; ++i) {
-    Offer best{-INFINITY, none};
-    for (int k = 0; k < a.K; ++k) {
-      if (kind[k] == 2) {
-        const Offer o{base[k], k * a.V + a.end};
-        if (last.before(o)) best = better(best, o);
-      }
-      if (kind[k] != 1) continue;
-      const T* row = (const T*)a.x + (b * a.K + k) * a.ld;
-      for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-        const Offer o{base[k] + ((double)as_float(row[v]) - top[k]) * a.inv_temp, k * a.V + v};
-        if (last.before(o)) best = better(best, o);
+    double v = value;
+    int64_t p = place;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const double w = __shfl_xor_sync(0xffffffffu, v, o);
+      const int64_t q = __shfl_xor_sync(0xffffffffu, p, o);
+      if (w > v || (w == v && q < p)) {
+        v = w;
+        p = q;
       }
     }
-    last = cta_best(best, red);
-    if (threadIdx.x == 0) {
-      const bool offered = last.value > -INFINITY;
-      const int64_t token = offered ? last.at % a.V : -1;
-      a.out_scores[b * a.width + i] = offered ? (float)last.value : -INFINITY;
-      a.parents[b * a.width + i] = offered ? last.at / a.V : 0;
-      a.tokens[b * a.width + i] = token;
-      if (a.out_finished != nullptr) a.out_finished[b * a.width + i] = offered && token == a.end;
+    const bool offered = v > -INFINITY;
+    if (lane == 0) {
+      const int64_t beam = p / a.V, token = offered ? p - beam * a.V : -1, at = b * a.width + i;
+      a.out_scores[at] = offered ? (float)v : -INFINITY;
+      a.parents[at] = offered ? beam : 0;
+      a.tokens[at] = token;
+      if (a.out_finished != nullptr) a.out_finished[at] = offered && token == a.end;
     }
-    if (!(last.value > -INFINITY)) last.value = -INFINITY, last.at = none;
+    if (offered && p == place) {   // places are unique
+#pragma unroll
+      for (int k = 0; k < kLists; ++k) next[k] += k == from_list;
+      look();
+    }
   }
 }
 
@@ -198,6 +466,34 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
   }
 }
 
+// CTAs of a group: enough that the groups give every SM three, and none with less than
+// a round of its own.
+template <class T>
+nmd_status launch_select(const Select& a, int64_t B, cudaStream_t s) {
+  int cluster = 1;
+  while (cluster < kMostCluster && B * cluster < 456 && a.K * a.V > (int64_t)cluster * 4 * kThreads * Vec<T>::N) cluster *= 2;
+  const Shape shape = shape_of(a.K, a.width, cluster);
+  static std::atomic<int> ready[kMaxDevices];
+  auto kernel = select_kernel<T>;
+  if (!per_device(ready, [&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)shape_of(kMostBeams, kMostWidth, kMostCluster).bytes) == cudaSuccess;
+      }))
+    return NMD_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(B * cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = shape.bytes;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, shape) == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+}
+
 bool beams_ok(int64_t B, int64_t K, int64_t width) {
   return B >= 0 && B <= (1 << 20) && K >= 1 && K <= kMostBeams && width >= 1 && width <= kMostWidth &&
          B * K <= ((int64_t)1 << 27);
@@ -243,13 +539,11 @@ nmd_status nmd_beam_select(const void* d_logits, int32_t dtype, int64_t B, int64
   const uintptr_t mis = dtype == NMD_DT_FP32 ? 3 : 1;
   if (!d_logits || ((uintptr_t)d_logits & mis) || !d_scores || !d_out_scores || !d_parents || !d_tokens)
     return NMD_ERR_INVALID;
-  const Select a{d_logits, V, ld, (int)K, (int)width, 1.0 / temperature, d_scores, d_finished, end,
+  const Select a{d_logits, V, ld, (int)K, (int)width, c, kLog2e / temperature, 1.0 / temperature, d_scores, d_finished, end,
                  d_out_scores, d_parents, d_tokens, d_out_finished};
   cudaStream_t s = (cudaStream_t)stream;
-  if (dtype == NMD_DT_FP32) select_kernel<float><<<(unsigned)B, kThreads, 0, s>>>(a);
-  else if (dtype == NMD_DT_BF16) select_kernel<bf16><<<(unsigned)B, kThreads, 0, s>>>(a);
-  else select_kernel<__half><<<(unsigned)B, kThreads, 0, s>>>(a);
-  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  if (dtype == NMD_DT_FP32) return launch_select<float>(a, B, s);
+  return dtype == NMD_DT_BF16 ? launch_select<bf16>(a, B, s) : launch_select<__half>(a, B, s);
 }
 
 nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t B, int64_t K, int64_t width,

@@ -67,6 +67,8 @@ def check(rows, scores, done, width, end=None, temperature=1.0, got=None):
     for z in live:
         if len(z):
             spread = max(spread, z.max() - z.min())
+    alike = np.unique(np.concatenate([np.nan_to_num(x, nan=7e77), scores.reshape(-1, 1)], 1), axis=0, return_inverse=True)[1]
+    alike = alike.reshape(B, K)
     s, p, t = (v.cpu().numpy() for v in (got.scores, got.parents, got.tokens))
     assert s.shape == p.shape == t.shape == (B, width) and got.scores.dtype == torch.float32
     for b in range(B):
