@@ -55,21 +55,39 @@ __device__ __forceinline__ float value_of(entry_t e) {
   const uint32_t o = (uint32_t)(e >> 32);
   return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
 }
+// a finite number, above 0; zeros of either sign are equal
+__device__ __forceinline__ entry_t order_of(double v) {
+  const entry_t b = (entry_t)__double_as_longlong(v + 0.0);
+  return (long long)b < 0 ? ~b : b | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double number_of(entry_t o) {
+  return __longlong_as_double((long long)((long long)o < 0 ? o & 0x7fffffffffffffffull : ~o));
+}
 __device__ __forceinline__ uint32_t column_of(entry_t e) { return 0xffffffffu - (uint32_t)e; }
 
-// The largest entries so far: up to `limit` of them between rounds, the width largest
-// after a cut.  A round adds at most 36 width.
+// The largest entries so far, by a CTA.
 struct Best {
-  entry_t* list;       // limit + 36 width
+  entry_t* list;       // room
   entry_t* sorted;     // width
-  int* count;
-  entry_t* least;      // what an entry has to be above
+  int* count;          // offered; those past the room are lost
+  int* lost;
+  entry_t* least;      // what an entry has to be above; at least `width` entries are at or above it
   int width, limit, room;
 
-  // the width largest of the list, in order; what is not among them cannot come back.
-  // The whole CTA; ends with a barrier.
+  __device__ __forceinline__ void clear() {   // by one thread
+    *count = 0;
+    *lost = 0;
+    *least = entry_of(-INFINITY, 0);   // a banned column is not among them
+  }
+  __device__ __forceinline__ void offer(entry_t e, entry_t bar) {
+    if (e <= bar) return;
+    const int p = atomicAdd(count, 1);
+    if (p < room) list[p] = e;
+  }
+  // The width largest of the list, in order.  By the whole CTA, between barriers.
   __device__ __noinline__ void cut() {
     const int n = min(*count, room);
+    if (threadIdx.x == 0 && *count > room) *lost = 1;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const entry_t e = list[i];
@@ -82,16 +100,101 @@ struct Best {
     for (int i = threadIdx.x; i < kept; i += kThreads) list[i] = sorted[i];
     if (threadIdx.x == 0) {
       *count = kept;
-      if (kept == width) *least = sorted[width - 1];
+      if (kept == width) *least = max(*least, sorted[width - 1]);
     }
     __syncthreads();
   }
 };
 
+// A first bar: the width-th largest of the maxima of groups of elements that threads
+// have in hand, as at least that many elements are not below it.  Up to 32 wide the
+// groups are those of eight threads, and every warp ranks all 32 of them; beyond,
+// those of single threads.
+template <class T, class G>
+__device__ __forceinline__ entry_t first_bar(G get, const Best& best, entry_t* bests) {
+  float m = Vec<T>::top(get(0));
+#pragma unroll
+  for (int q = 1; q < 4; ++q) m = max_nan(m, Vec<T>::top(get(q)));
+  uint32_t o = order_of(m);
+  const int lane = threadIdx.x & 31;
+  entry_t bar = *best.least;
+  if (best.width <= 32) {
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
+    uint32_t* all = (uint32_t*)bests;
+    if ((lane & 7) == 0) all[threadIdx.x >> 3] = o;
+    __syncthreads();
+    o = all[lane];
+    int rank = 0;
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) rank += all[k] > o || (all[k] == o && k < lane);
+    o = __shfl_sync(0xffffffffu, o, __ffs(__ballot_sync(0xffffffffu, rank == best.width - 1)) - 1);
+    bar = max(bar, (entry_t)o << 32);
+    if (lane == 0) *best.least = bar;   // every warp the same
+    __syncwarp();
+  } else {
+    const entry_t mine = (entry_t)o << 32 | threadIdx.x;
+    bests[threadIdx.x] = mine;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 8
+    for (int k = 0; k < kThreads; ++k) rank += bests[k] > mine;
+    if (rank == best.width - 1) *best.least = max(bar, (entry_t)o << 32);
+    __syncthreads();
+    bar = *best.least;
+  }
+  return bar;
+}
+
+// A segment's largest entries again, where there were more offers than room: one
+// vector of a thread at a time, and where more than `width` threads have something to
+// offer, the width-th of their largest entries is the bar first.  A round adds at most
+// 8 width entries.  Rows that rise from column to column, and rows of few values.
+template <class T>
+__device__ __noinline__ void again(Best best, entry_t* bests, const uint4* xv, int n, int64_t col0, T xs, int64_t scalar) {
+  constexpr int N = Vec<T>::N;
+  if (threadIdx.x == 0) best.clear();
+  __syncthreads();
+  const int rounds = (n + kThreads - 1) / kThreads;
+  for (int i = 0; i <= rounds; ++i) {
+    const int v = i * kThreads + threadIdx.x;
+    const entry_t bar = *best.least;
+    entry_t mine[N], top = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) mine[e] = 0;
+    if (i == rounds) {
+      if (scalar >= 0) mine[0] = entry_of(Vec<T>::get(xs), scalar);
+    } else if (v < n) {
+      const uint4 w = xv[v];
+#pragma unroll
+      for (int e = 0; e < N; ++e) mine[e] = entry_of(Vec<T>::get(((const T*)&w)[e]), col0 + (int64_t)v * N + e);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = max(top, mine[e]);
+    const int some = __syncthreads_count(top > bar);
+    if (some == 0) continue;
+    entry_t over = bar;
+    if (some > best.width) {
+      bests[threadIdx.x] = top;
+      __syncthreads();
+      int rank = 0;
+      for (int k = 0; k < kThreads; ++k) rank += bests[k] > top;
+      if (top > bar && rank == best.width - 1) *best.least = top - 1;
+      __syncthreads();
+      over = *best.least;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) best.offer(mine[e], over);
+    __syncthreads();
+    if (*(volatile int*)best.count >= best.limit) best.cut();
+    else __syncthreads();
+  }
+}
+
 // Dynamic shared memory: slots, then the lists
 struct Shape {
   int cluster, limit, room;
-  size_t off_list, off_sorted, off_all, bytes;
+  size_t off_list, off_sorted, off_all, off_places, bytes;
 };
 Shape shape_of(int64_t K, int width, int cluster) {
   Shape s;
@@ -101,7 +204,8 @@ Shape shape_of(int64_t K, int width, int cluster) {
   s.off_list = (size_t)kDepth * 4 * kThreads * 16;
   s.off_sorted = s.off_list + (size_t)s.room * 8;
   s.off_all = s.off_sorted + (size_t)width * 8;
-  s.bytes = s.off_all + (size_t)(K + cluster) * width * 8;   // the segments' lists, in the first CTA
+  s.off_places = s.off_all + (size_t)(K + cluster) * width * 8;   // the segments' lists, in the first CTA
+  s.bytes = s.off_places + (size_t)(K + cluster) * width * 4;
   return s;
 }
 
@@ -121,18 +225,23 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
   constexpr int kSegments = kMostBeams + kMostCluster;
   extern __shared__ uint4 slots[];
   __shared__ Stat red[kThreads / 32], stats[kSegments];
-  __shared__ int counts[kSegments], row_beam[kMostBeams], done_beam[kMostBeams], count, rows_in_use, finished_in_use;
+  __shared__ int counts[kSegments], row_beam[kMostBeams], done_beam[kMostBeams], count, lost, rows_in_use, finished_in_use;
   __shared__ float row_score[kMostBeams], done_score[kMostBeams];
   __shared__ double base[kMostBeams];
   __shared__ float top[kMostBeams];
-  __shared__ entry_t least, bests[kThreads];
+  __shared__ int row_first[kMostBeams], row_last[kMostBeams], seg_row[kSegments];   // CTAs of a row, row of a segment
+  __shared__ entry_t least;
+  __shared__ entry_t bests[kThreads];
   char* raw = (char*)slots;
-  Best best{(entry_t*)(raw + shape.off_list), (entry_t*)(raw + shape.off_sorted), &count, &least, a.width, shape.limit, shape.room};
+  Best best{(entry_t*)(raw + shape.off_list), (entry_t*)(raw + shape.off_sorted), &count, &lost, &least, a.width, shape.limit,
+            shape.room};
   entry_t* all = (entry_t*)(raw + shape.off_all);
+  uint32_t* places = (uint32_t*)(raw + shape.off_places);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned csize, rank;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int log_cluster = __ffs(csize) - 1;
   if (csize > 1) cluster_arrive();   // waited for before the first CTA's shared memory is written
   const int64_t b = blockIdx.x / csize;
 
@@ -164,12 +273,28 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
   }
   __syncthreads();
   const int R = rows_in_use;
-  const int64_t total = R * a.V, from = total * rank / csize, to = total * (rank + 1) / csize;
+  // The rows' columns one after another, cut into as many runs as there are CTAs.
+  // Segment row + q is what CTA q has of the row: no two have one number, as each step
+  // along the runs raises the row, the CTA or both.
+  const int64_t total = R * a.V;
+  auto border = [&](unsigned q) { return (int64_t)((unsigned long long)(total * q) >> log_cluster); };   // (csize is a power of two)
+  const int64_t from = border(rank), to = border(rank + 1);
+  if (rank == 0) {
+    for (int row = tid; row < R; row += kThreads) {
+      unsigned q = 0;
+      while (q + 1 < csize && border(q + 1) <= row * a.V) ++q;
+      row_first[row] = q;
+      while (q + 1 < csize && border(q + 1) < (row + 1) * a.V) ++q;
+      row_last[row] = q;
+    }
+    for (int i = tid; i < kSegments; i += kThreads) seg_row[i] = -1;
+  }
   const uint4* mine = slots + tid;
   bool waited = csize == 1;
 
+  int row = 0;
   for (int64_t at = from; at < to;) {
-    const int row = (int)(at / a.V);
+    while (at >= (row + 1) * a.V) ++row;
     const int64_t e0 = at - row * a.V, e1 = min(a.V, to - row * a.V);
     at = row * a.V + e1;
     const T* x = (const T*)a.x + (b * a.K + row_beam[row]) * a.ld;
@@ -194,87 +319,54 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) load(d);
     const T xs = scalar >= 0 ? x[scalar] : Vec<T>::put(0.f);
-    if (tid == 0) {
-      count = 0;
-      least = entry_of(-INFINITY, 0);   // a banned column is not among them
-    }
+    if (tid == 0) best.clear();
     __syncthreads();
 
     Running<T> run;
     const int rounds = (n + 4 * kThreads - 1) / (4 * kThreads);
     int d = 0;
-    for (int i = 0; i <= rounds; ++i) {   // the last one: the single elements
+    for (int i = 0; i < rounds; ++i) {
       const int v = i * 4 * kThreads + tid;
       auto get = [&](int q) { return v + q * kThreads < n ? mine[(d * 4 + q) * kThreads] : Vec<T>::none(); };
-      const entry_t bar = least;   // it only rises, and between barriers
-      entry_t mybest = 0;
-      if (i < rounds) {
-        copy_wait<kDepth - 1>();
-        float group;
-        if (v + 3 * kThreads < n) group = run.add([&](int q) { return mine[(d * 4 + q) * kThreads]; }, a.c);
-        else group = run.add(get, a.c);
-        const float bar_x = value_of(bar);
-        // (0.99 is far more than the sum's rounding)
-        if (!(group < 0.99f * ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo))) {
+      copy_wait<kDepth - 1>();
+      float group;
+      if (v + 3 * kThreads < n) group = run.add([&](int q) { return mine[(d * 4 + q) * kThreads]; }, a.c);
+      else group = run.add(get, a.c);
+      // What has to be passed only rises; an older value lets more through, not less
+      const entry_t bar = i == 0 ? first_bar<T>(get, best, bests) : *(volatile entry_t*)&least;
+      const float bar_x = value_of(bar);
+      if (!(group < 0.99f * ex2(   // (far more than the sum's rounding)
+                        fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo))) {
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            const uint4 w = get(q);
-            const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
+        for (int q = 0; q < 4; ++q) {
+          const uint4 w = get(q);
+          if (Vec<T>::top(w) < bar_x) continue;
+          const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
 #pragma unroll
-            for (int e = 0; e < N; ++e) mybest = max(mybest, entry_of(Vec<T>::get(((const T*)&w)[e]), col + e));
-          }
+          for (int e = 0; e < N; ++e) best.offer(entry_of(Vec<T>::get(((const T*)&w)[e]), col + e), bar);
         }
-      } else if (scalar >= 0) {
-        run.add(Vec<T>::get(xs), a.c);
-        mybest = entry_of(Vec<T>::get(xs), scalar);
       }
-      const int some = __syncthreads_count(mybest > bar);
-      if (some > 0) {   // the same for the whole CTA, as is all that follows
-        entry_t over = bar;
-        if (some > a.width) {
-          // the width-th of the threads' largest: nothing at or below it is among the width largest but itself
-          bests[tid] = mybest > bar ? mybest : 0;
-          __syncthreads();
-          if (mybest > bar) {
-            int r = 0;
-            for (int k = 0; k < kThreads; ++k) r += bests[k] > mybest;
-            if (r == a.width - 1) least = mybest - 1;
-          }
-          __syncthreads();
-          over = least;
-        }
-        if (mybest > over) {
-          if (i < rounds) {
-#pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-              const uint4 w = get(q);
-              const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
-#pragma unroll
-              for (int e = 0; e < N; ++e) {
-                const entry_t k = entry_of(Vec<T>::get(((const T*)&w)[e]), col + e);
-                if (k > over) {
-                  const int p = atomicAdd(&count, 1);
-                  if (p < shape.room) best.list[p] = k;
-                }
-              }
-            }
-          } else {
-            const int p = atomicAdd(&count, 1);
-            if (p < shape.room) best.list[p] = mybest;
-          }
-        }
+      load(d);
+      if (++d == kDepth) d = 0;
+      if ((i & 3) == 3) {
         __syncthreads();
-        if (count >= shape.limit) best.cut();
+        if (*(volatile int*)&count >= shape.limit) best.cut();   // the same for all: the next offers come after a barrier
+        else __syncthreads();
       }
-      if (i < rounds) {
-        load(d);
-        if (++d == kDepth) d = 0;
-      }
+    }
+    if (scalar >= 0) {
+      run.add(Vec<T>::get(xs), a.c);
+      best.offer(entry_of(Vec<T>::get(xs), scalar), *(volatile entry_t*)&least);
     }
     copy_wait<0>();
     // the segment's sum and list
     const Stat st = merge_lanes<32>(run.s, a.c);
     if (lane == 0) red[warp] = st;
+    __syncthreads();
+    if (*(volatile int*)&count > shape.room || lost) {   // more offers than there is room for (rising rows, many equal values)
+      __syncthreads();
+      again<T>(best, bests, xv, n, sp.head + v0 * N, xs, scalar);
+    }
     best.cut();
     if (!waited) {
       cluster_wait();
@@ -301,102 +393,97 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
     __syncthreads();
   }
 
-  // A row's segments are row + q for the CTAs q that hold part of it
-  auto first_of = [&](int row) {   // the CTA that holds the row's first column
-    int q = 0;
-    while (q + 1 < (int)csize && total * (q + 1) / csize <= row * a.V) ++q;
-    return q;
-  };
-  auto last_of = [&](int row) {
-    int q = first_of(row);
-    while (q + 1 < (int)csize && total * (q + 1) / csize < (row + 1) * a.V) ++q;
-    return q;
-  };
+  // The values of all offers, as whole numbers in their order
   for (int row = tid; row < R; row += kThreads) {
-    const int q0 = first_of(row), q1 = last_of(row);
+    const int q0 = row_first[row], q1 = row_last[row];
     float m = -INFINITY;
     for (int q = q0; q <= q1; ++q) m = max_nan(m, stats[row + q].m);
     float S = 0.f;
     for (int q = q0; q <= q1; ++q) S += stats[row + q].S * rescale(stats[row + q].m, m, a.c);
     // the sum is S 2^reference; offers are score + (x - m) / tau - (ln S + ln 2 (reference - c m))
-    const double cm = a.log2_scale * (double)m;
-    const double over = is_near(m, a.c) ? (double)ref_of(m, a.c) - cm : 0.0;
+    const double over = is_near(m, a.c) ? (double)ref_of(m, a.c) - a.log2_scale * (double)m : 0.0;
     base[row] = m < INFINITY && S > 0.f ? (double)row_score[row] - (log((double)S) + kLn2 * over) : NAN;
     top[row] = m;
+    for (int q = q0; q <= q1; ++q) seg_row[row + q] = row;
+  }
+  const int segments = R == 0 ? 0 : R + (int)csize - 1, lists = segments + finished_in_use;
+  __syncthreads();
+  for (int i = tid; i < segments * a.width; i += kThreads) {
+    const int seg = i / a.width, row = seg_row[seg];
+    if (row < 0 || i - seg * a.width >= counts[seg]) continue;
+    const entry_t e = all[i];
+    places[i] = column_of(e);
+    const double v = base[row] + ((double)value_of(e) - (double)top[row]) * a.inv_temp;
+    all[i] = fabs(v) < INFINITY ? order_of(v) : 0;
   }
   __syncthreads();
   if (warp != 0) return;
 
-  // Lists are in order: of their heads the best is the next offer.  Lane l has lists l,
+  // Lists are in order: the best of their heads is the next offer.  Lane l has lists l,
   // l + 32, ...: the segments', then the finished beams.
-  const int segments = R + (int)csize - 1, lists = segments + finished_in_use;
   constexpr int kLists = (kMostBeams + kMostCluster + kMostBeams + 31) / 32;
   int next[kLists];
 #pragma unroll
   for (int i = 0; i < kLists; ++i) next[i] = 0;
-  const int64_t none = (int64_t)1 << 62;
-  double value = -INFINITY;   // of this lane's best head
-  int64_t place = none;       // beam V + column
+  entry_t value = 0;      // of this lane's best head
+  uint32_t beam = 0, column = 0;
   int from_list = 0;
-  auto row_of = [&](int seg) {   // the row of segment row + q: there is one q with both borders right
-    for (int row = max(0, seg - (int)csize + 1); row <= min(R - 1, seg); ++row)
-      if (first_of(row) <= seg - row && seg - row <= last_of(row)) return row;
-    return -1;
-  };
-  int rows[kLists];
-#pragma unroll
-  for (int i = 0; i < kLists; ++i) rows[i] = lane + 32 * i < segments ? row_of(lane + 32 * i) : -1;
   auto look = [&] {
-    value = -INFINITY;
-    place = none;
+    value = 0;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
       const int l = lane + 32 * i;
-      double v = -INFINITY;
-      int64_t p = none;
+      entry_t v = 0;
+      uint32_t k = 0, col = 0;
       if (l < segments) {
-        if (rows[i] >= 0 && next[i] < counts[l]) {
-          const entry_t e = all[(int64_t)l * a.width + next[i]];
-          v = base[rows[i]] + ((double)value_of(e) - (double)top[rows[i]]) * a.inv_temp;
-          p = row_beam[rows[i]] * a.V + column_of(e);
+        if (seg_row[l] >= 0 && next[i] < counts[l]) {
+          v = all[l * a.width + next[i]];
+          col = places[l * a.width + next[i]];
+          k = row_beam[seg_row[l]];
         }
       } else if (l < lists && next[i] == 0) {
-        v = done_score[l - segments];
-        p = done_beam[l - segments] * a.V + a.end;
+        v = order_of((double)done_score[l - segments]);
+        k = done_beam[l - segments];
+        col = (uint32_t)a.end;
       }
-      if (v > value || (v == value && v > -INFINITY && p < place)) {
+      if (v > value || (v == value && (k < beam || (k == beam && col < column)))) {
         value = v;
-        place = p;
+        beam = k;
+        column = col;
         from_list = i;
       }
     }
   };
   look();
   for (int i = 0; i < a.width; ++i) {
-    double v = value;
-    int64_t p = place;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const double w = __shfl_xor_sync(0xffffffffu, v, o);
-      const int64_t q = __shfl_xor_sync(0xffffffffu, p, o);
-      if (w > v || (w == v && q < p)) {
-        v = w;
-        p = q;
+    // the largest value, then the lowest beam, then its lowest column; the warp's reductions take 32 bits
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(value >> 32));
+    bool mine_is = (uint32_t)(value >> 32) == hi;
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, mine_is ? (uint32_t)value : 0u);
+    mine_is = mine_is && (uint32_t)value == lo;
+    const bool offered = hi != 0;   // (the order of a number starts above 0)
+    const uint32_t k = __reduce_min_sync(0xffffffffu, mine_is ? beam : 0xffffffffu);
+    mine_is = mine_is && beam == k;
+    const uint32_t col = __reduce_min_sync(0xffffffffu, mine_is ? column : 0xffffffffu);
+    mine_is = mine_is && column == col;
+    const int64_t at = b * a.width + i;
+    if (!offered) {
+      if (lane == 0) {
+        a.out_scores[at] = -INFINITY;
+        a.parents[at] = 0;
+        a.tokens[at] = -1;
+        if (a.out_finished != nullptr) a.out_finished[at] = 0;
       }
-    }
-    const bool offered = v > -INFINITY;
-    if (lane == 0) {
-      const int64_t beam = p / a.V, token = offered ? p - beam * a.V : -1, at = b * a.width + i;
-      a.out_scores[at] = offered ? (float)v : -INFINITY;
-      a.parents[at] = offered ? beam : 0;
-      a.tokens[at] = token;
-      if (a.out_finished != nullptr) a.out_finished[at] = offered && token == a.end;
-    }
-    if (offered && p == place) {   // places are unique
+    } else if (mine_is) {   // one lane: no two offers have one place
+      a.out_scores[at] = (float)number_of(value);
+      a.parents[at] = k;
+      a.tokens[at] = col;
+      if (a.out_finished != nullptr) a.out_finished[at] = col == a.end;
 #pragma unroll
-      for (int k = 0; k < kLists; ++k) next[k] += k == from_list;
+      for (int n = 0; n < kLists; ++n) next[n] += n == from_list;
       look();
     }
+    __syncwarp();
   }
 }
 
