@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostBeams = 64, kMostWidth = 128, kMostCluster = 8;
-constexpr int kDepth = 3;   // groups of four vectors under way
+constexpr int kDepth = 2;   // groups of four vectors under way
 
 struct Select {
   const void* x;
@@ -83,6 +83,15 @@ struct Best {
     if (e <= bar) return;
     const int p = atomicAdd(count, 1);
     if (p < room) list[p] = e;
+  }
+  __device__ __forceinline__ void offer_warp(entry_t e, entry_t bar) {
+    const unsigned some = __ballot_sync(0xffffffffu, e > bar);
+    if (some == 0) return;
+    const int lane = threadIdx.x & 31;
+    int p = 0;
+    if (lane == 0) p = atomicAdd(count, __popc(some));
+    p = __shfl_sync(0xffffffffu, p, 0) + __popc(some & ((1u << lane) - 1));
+    if (e > bar && p < room) list[p] = e;
   }
   // The width largest of the list, in order.  By the whole CTA, between barriers.
   __device__ __noinline__ void cut() {
@@ -199,7 +208,7 @@ struct Shape {
 Shape shape_of(int64_t K, int width, int cluster) {
   Shape s;
   s.cluster = cluster;
-  s.limit = std::max(4 * width, 64);
+  s.limit = 2 * width;
   s.room = s.limit + 36 * width;
   s.off_list = (size_t)kDepth * 4 * kThreads * 16;
   s.off_sorted = s.off_list + (size_t)s.room * 8;
@@ -220,7 +229,7 @@ __device__ __forceinline__ void put_remote(uint32_t at, entry_t v) {
 
 // Bound by HBM; one group by the launch, two barriers of the cluster and the merge.
 template <class T>
-__global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_constant__ Select a, const __grid_constant__ Shape shape) {
+__global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_constant__ Select a, const __grid_constant__ Shape shape) {
   constexpr int N = Vec<T>::N;
   constexpr int kSegments = kMostBeams + kMostCluster;
   extern __shared__ uint4 slots[];
@@ -335,20 +344,29 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
       // What has to be passed only rises; an older value lets more through, not less
       const entry_t bar = i == 0 ? first_bar<T>(get, best, bests) : *(volatile entry_t*)&least;
       const float bar_x = value_of(bar);
-      if (!(group < 0.99f * ex2(   // (far more than the sum's rounding)
-                        fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo))) {
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          const uint4 w = get(q);
-          if (Vec<T>::top(w) < bar_x) continue;
-          const int64_t col = sp.head + (v0 + v + q * kThreads) * N;
-#pragma unroll
-          for (int e = 0; e < N; ++e) best.offer(entry_of(Vec<T>::get(((const T*)&w)[e]), col + e), bar);
-        }
+      const float power = ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo);
+      // (0.99: far more than the sum's rounding.)  The warp looks at a thread's elements
+      // together, one or none a lane.
+      unsigned look = __ballot_sync(0xffffffffu, !(group < 0.99f * power));
+      if (look != 0) {
+        __syncwarp();   // the copies of all lanes have landed
+        do {
+          const int from = __ffs(look) - 1;
+          look &= look - 1;
+          const int q = lane / N, vec = i * 4 * kThreads + warp * 32 + from + q * kThreads;
+          entry_t e = 0;
+          if (q < 4 && vec < n) {
+            const T* its = (const T*)(slots + (d * 4 + q) * kThreads + warp * 32 + from);
+            e = entry_of(Vec<T>::get(its[lane % N]), sp.head + (v0 + vec) * N + lane % N);
+          }
+          best.offer_warp(e, bar);
+        } while (look != 0);
+        __syncwarp();   // before the slots are filled again
       }
       load(d);
       if (++d == kDepth) d = 0;
-      if ((i & 3) == 3) {
+      // a higher bar after 2, 4, 8 and every 16 rounds
+      if ((i & 15) == 15 || i == 1 || i == 3 || i == 7) {
         __syncthreads();
         if (*(volatile int*)&count >= shape.limit) best.cut();   // the same for all: the next offers come after a barrier
         else __syncthreads();
@@ -402,7 +420,13 @@ __global__ void __launch_bounds__(kThreads, 3) select_kernel(const __grid_consta
     for (int q = q0; q <= q1; ++q) S += stats[row + q].S * rescale(stats[row + q].m, m, a.c);
     // the sum is S 2^reference; offers are score + (x - m) / tau - (ln S + ln 2 (reference - c m))
     const double over = is_near(m, a.c) ? (double)ref_of(m, a.c) - a.log2_scale * (double)m : 0.0;
-    base[row] = m < INFINITY && S > 0.f ? (double)row_score[row] - (log((double)S) + kLn2 * over) : NAN;
+    int k = 0;   // S = f 2^k, f near 1
+    float f = frexpf(S, &k);
+    if (f < 0.7f) {
+      f *= 2.f;
+      --k;
+    }
+    base[row] = m < INFINITY && S > 0.f ? (double)row_score[row] - kLn2 * (over + k) - (double)log1pf(f - 1.f) : NAN;
     top[row] = m;
     for (int q = q0; q <= q1; ++q) seg_row[row + q] = row;
   }
