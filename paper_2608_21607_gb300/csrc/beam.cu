@@ -98,11 +98,23 @@ struct Best {
     const int n = min(*count, room);
     if (threadIdx.x == 0 && *count > room) *lost = 1;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const entry_t e = list[i];
-      int rank = 0;
-      for (int k = 0; k < n; ++k) rank += list[k] > e;
-      if (rank < width) sorted[rank] = e;
+    // a warp per entry: its rank among the others by a vote on 32 of them at a time
+    const int lane = threadIdx.x & 31;
+    if (n <= 32) {
+      const entry_t mine = lane < n ? list[lane] : 0;
+      for (int i = threadIdx.x >> 5; i < n; i += kThreads / 32) {
+        const entry_t e = list[i];
+        const int rank = __popc(__ballot_sync(0xffffffffu, mine > e));
+        if (lane == 0 && rank < width) sorted[rank] = e;
+      }
+    } else {
+      for (int i = threadIdx.x >> 5; i < n; i += kThreads / 32) {
+        const entry_t e = list[i];
+        int rank = 0;
+        for (int k = lane; k < n; k += 32) rank += list[k] > e;
+        rank = __reduce_add_sync(0xffffffffu, rank);
+        if (lane == 0 && rank < width) sorted[rank] = e;
+      }
     }
     __syncthreads();
     const int kept = min(n, width);
@@ -135,8 +147,12 @@ __device__ __forceinline__ entry_t first_bar(G get, const Best& best, entry_t* b
     __syncthreads();
     o = all[lane];
     int rank = 0;
-#pragma unroll 8
-    for (int k = 0; k < 32; ++k) rank += all[k] > o || (all[k] == o && k < lane);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint4 u = ((const uint4*)all)[k];
+      rank += (u.x > o) + (u.y > o) + (u.z > o) + (u.w > o);
+    }
+    rank += __popc(__match_any_sync(0xffffffffu, o) & ((1u << lane) - 1));   // equal ones in the order of the lanes
     o = __shfl_sync(0xffffffffu, o, __ffs(__ballot_sync(0xffffffffu, rank == best.width - 1)) - 1);
     bar = max(bar, (entry_t)o << 32);
     if (lane == 0) *best.least = bar;   // every warp the same
@@ -238,9 +254,9 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
   __shared__ float row_score[kMostBeams], done_score[kMostBeams];
   __shared__ double base[kMostBeams];
   __shared__ float top[kMostBeams];
-  __shared__ int row_first[kMostBeams], row_last[kMostBeams], seg_row[kSegments];   // CTAs of a row, row of a segment
+  __shared__ int row_first[kMostBeams], row_last[kMostBeams], seg_row[kSegments], next[kSegments + kMostBeams];   // CTAs of a row, row of a segment
   __shared__ entry_t least;
-  __shared__ entry_t bests[kThreads];
+  __shared__ __align__(16) entry_t bests[kThreads];
   char* raw = (char*)slots;
   Best best{(entry_t*)(raw + shape.off_list), (entry_t*)(raw + shape.off_sorted), &count, &lost, &least, a.width, shape.limit,
             shape.room};
@@ -260,8 +276,8 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     for (int k0 = 0; k0 < a.K; k0 += 32) {
       const int k = k0 + lane;
       const float s = k < a.K ? a.scores[b * a.K + k] : -INFINITY;
-      const bool used = fabsf(s) < INFINITY;
-      const bool fin = used && a.finished != nullptr && a.finished[b * a.K + k] != 0;
+      const uint8_t ended = k < a.K && a.finished != nullptr ? a.finished[b * a.K + k] : 0;
+      const bool used = fabsf(s) < INFINITY, fin = used && ended != 0;
       const unsigned m = __ballot_sync(0xffffffffu, used && !fin), f = __ballot_sync(0xffffffffu, fin);
       const int before = __popc(m & ((1u << lane) - 1)), fbefore = __popc(f & ((1u << lane) - 1));
       if (used && !fin) {
@@ -323,6 +339,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
 #pragma unroll
       for (int q = 0; q < 4; ++q, ahead += kThreads)
         if (ahead < n) copy_async(tc::smem_u32(mine + (slot * 4 + q) * kThreads), xv + ahead);
+        else slots[(slot * 4 + q) * kThreads + tid] = Vec<T>::none();   // -inf past the segment's end
       copy_commit();
     };
 #pragma unroll
@@ -335,12 +352,9 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     const int rounds = (n + 4 * kThreads - 1) / (4 * kThreads);
     int d = 0;
     for (int i = 0; i < rounds; ++i) {
-      const int v = i * 4 * kThreads + tid;
-      auto get = [&](int q) { return v + q * kThreads < n ? mine[(d * 4 + q) * kThreads] : Vec<T>::none(); };
+      auto get = [&](int q) { return mine[(d * 4 + q) * kThreads]; };
       copy_wait<kDepth - 1>();
-      float group;
-      if (v + 3 * kThreads < n) group = run.add([&](int q) { return mine[(d * 4 + q) * kThreads]; }, a.c);
-      else group = run.add(get, a.c);
+      const float group = run.add(get, a.c);
       // What has to be passed only rises; an older value lets more through, not less
       const entry_t bar = i == 0 ? first_bar<T>(get, best, bests) : *(volatile entry_t*)&least;
       const float bar_x = value_of(bar);
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
           look &= look - 1;
           const int q = lane / N, vec = i * 4 * kThreads + warp * 32 + from + q * kThreads;
           entry_t e = 0;
-          if (q < 4 && vec < n) {
+          if (q < 4) {   // (-inf past the segment's end is below every bar)
             const T* its = (const T*)(slots + (d * 4 + q) * kThreads + warp * 32 + from);
             e = entry_of(Vec<T>::get(its[lane % N]), sp.head + (v0 + vec) * N + lane % N);
           }
@@ -431,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     for (int q = q0; q <= q1; ++q) seg_row[row + q] = row;
   }
   const int segments = R == 0 ? 0 : R + (int)csize - 1, lists = segments + finished_in_use;
+  for (int i = tid; i < lists; i += kThreads) next[i] = 0;
   __syncthreads();
   for (int i = tid; i < segments * a.width; i += kThreads) {
     const int seg = i / a.width, row = seg_row[seg];
@@ -445,27 +460,24 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
 
   // Lists are in order: the best of their heads is the next offer.  Lane l has lists l,
   // l + 32, ...: the segments', then the finished beams.
-  constexpr int kLists = (kMostBeams + kMostCluster + kMostBeams + 31) / 32;
-  int next[kLists];
-#pragma unroll
-  for (int i = 0; i < kLists; ++i) next[i] = 0;
   entry_t value = 0;      // of this lane's best head
   uint32_t beam = 0, column = 0;
   int from_list = 0;
   auto look = [&] {
     value = 0;
-#pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-      const int l = lane + 32 * i;
+#pragma unroll 1
+    for (int l = lane; l < lists; l += 32) {
       entry_t v = 0;
       uint32_t k = 0, col = 0;
+      const int at = next[l];
       if (l < segments) {
-        if (seg_row[l] >= 0 && next[i] < counts[l]) {
-          v = all[l * a.width + next[i]];
-          col = places[l * a.width + next[i]];
-          k = row_beam[seg_row[l]];
+        const int row = seg_row[l];
+        if (row >= 0 && at < counts[l]) {
+          v = all[l * a.width + at];
+          col = places[l * a.width + at];
+          k = row_beam[row];
         }
-      } else if (l < lists && next[i] == 0) {
+      } else if (at == 0) {
         v = order_of((double)done_score[l - segments]);
         k = done_beam[l - segments];
         col = (uint32_t)a.end;
@@ -474,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
         value = v;
         beam = k;
         column = col;
-        from_list = i;
+        from_list = l;
       }
     }
   };
@@ -503,8 +515,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       a.parents[at] = k;
       a.tokens[at] = col;
       if (a.out_finished != nullptr) a.out_finished[at] = col == a.end;
-#pragma unroll
-      for (int n = 0; n < kLists; ++n) next[n] += n == from_list;
+      ++next[from_list];   // this lane's own
       look();
     }
     __syncwarp();
