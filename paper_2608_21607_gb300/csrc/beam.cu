@@ -94,7 +94,7 @@ struct Best {
     if (e > bar && p < room) list[p] = e;
   }
   // The width largest of the list, in order.  By the whole CTA, between barriers.
-  __device__ __noinline__ void cut() {
+  __device__ __forceinline__ void cut() {
     const int n = min(*count, room);
     if (threadIdx.x == 0 && *count > room) *lost = 1;
     __syncthreads();
