@@ -7,7 +7,7 @@
 // segment a CTA keeps the running sum of the softmax and the `width` largest logits:
 // within a row the logits' order is that of the offers, so that nothing has to wait
 // for the row's sum.  The segments' lists go to the cluster's first CTA, which adds up
-// the sums and merges the lists by the offers' values in fp64.
+// the sums and merges the lists by the offers' values, each kept as two fp32 values.
 //
 // What is largest is found on the way at the cost of one comparison per four vectors:
 // a group of elements whose sum of powers is below the power of the width-th largest
@@ -33,7 +33,7 @@ struct Select {
   int64_t V, ld;
   int K, width;
   Scale c;
-  double log2_scale, inv_temp;   // c in fp64, 1 / tau
+  float2 inv_temp;   // 1 / tau as the sum of two
   const float* scores;
   const uint8_t* finished;
   int64_t end;
@@ -55,13 +55,18 @@ __device__ __forceinline__ float value_of(entry_t e) {
   const uint32_t o = (uint32_t)(e >> 32);
   return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
 }
-// a finite number, above 0; zeros of either sign are equal
-__device__ __forceinline__ entry_t order_of(double v) {
-  const entry_t b = (entry_t)__double_as_longlong(v + 0.0);
-  return (long long)b < 0 ? ~b : b | 0x8000000000000000ull;
+// A value hi + lo, hi rounded to nearest, as one number above 0 (finite hi)
+__device__ __forceinline__ entry_t order_of(float hi, float lo) { return (entry_t)order_of(hi) << 32 | order_of(lo); }
+__device__ __forceinline__ float score_of(entry_t o) {
+  const uint32_t h = (uint32_t)(o >> 32);
+  return __uint_as_float((int)h < 0 ? h & 0x7fffffffu : ~h);
 }
-__device__ __forceinline__ double number_of(entry_t o) {
-  return __longlong_as_double((long long)((long long)o < 0 ? o & 0x7fffffffffffffffull : ~o));
+// score + lp in two fp32 values: offers are compared to 2^-40 of them, not as the rounded
+// sums; 0 if it is not finite
+__device__ __forceinline__ entry_t sum_of(float score, LogProb lp) {
+  const float s = score + lp.hi, t = s - score, rest = (score - (s - t)) + (lp.hi - t) + lp.lo;
+  const float hi = s + rest;
+  return fabsf(hi) < INFINITY ? order_of(hi, rest - (hi - s)) : 0;
 }
 __device__ __forceinline__ uint32_t column_of(entry_t e) { return 0xffffffffu - (uint32_t)e; }
 
@@ -229,8 +234,9 @@ Shape shape_of(int64_t K, int width, int cluster) {
   s.off_list = (size_t)kDepth * 4 * kThreads * 16;
   s.off_sorted = s.off_list + (size_t)s.room * 8;
   s.off_all = s.off_sorted + (size_t)width * 8;
-  s.off_places = s.off_all + (size_t)(K + cluster) * width * 8;   // the segments' lists, in the first CTA
-  s.bytes = s.off_places + (size_t)(K + cluster) * width * 4;
+  const size_t offers = ((size_t)(K + cluster) * width + K) * 8;   // the segments' lists and finished beams, in the first CTA
+  s.off_places = s.off_all + offers;
+  s.bytes = s.off_places + offers;
   return s;
 }
 
@@ -252,8 +258,8 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
   __shared__ Stat red[kThreads / 32], stats[kSegments];
   __shared__ int counts[kSegments], row_beam[kMostBeams], done_beam[kMostBeams], count, lost, rows_in_use, finished_in_use;
   __shared__ float row_score[kMostBeams], done_score[kMostBeams];
-  __shared__ double base[kMostBeams];
-  __shared__ float top[kMostBeams];
+  __shared__ Stat row_stat[kMostBeams];
+  __shared__ float row_over[kMostBeams];
   __shared__ int row_first[kMostBeams], row_last[kMostBeams], seg_row[kSegments], next[kSegments + kMostBeams];   // CTAs of a row, row of a segment
   __shared__ entry_t least;
   __shared__ __align__(16) entry_t bests[kThreads];
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
   Best best{(entry_t*)(raw + shape.off_list), (entry_t*)(raw + shape.off_sorted), &count, &lost, &least, a.width, shape.limit,
             shape.room};
   entry_t* all = (entry_t*)(raw + shape.off_all);
-  uint32_t* places = (uint32_t*)(raw + shape.off_places);
+  entry_t* places = (entry_t*)(raw + shape.off_places);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned csize, rank;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
@@ -425,96 +431,100 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     __syncthreads();
   }
 
-  // The values of all offers, as whole numbers in their order
+  // The values of all offers, as whole numbers in their order.  Places: beam, column.
+#pragma unroll 1
   for (int row = tid; row < R; row += kThreads) {
     const int q0 = row_first[row], q1 = row_last[row];
-    float m = -INFINITY;
+    float m = -INFINITY, S = 0.f;
     for (int q = q0; q <= q1; ++q) m = max_nan(m, stats[row + q].m);
-    float S = 0.f;
     for (int q = q0; q <= q1; ++q) S += stats[row + q].S * rescale(stats[row + q].m, m, a.c);
-    // the sum is S 2^reference; offers are score + (x - m) / tau - (ln S + ln 2 (reference - c m))
-    const double over = is_near(m, a.c) ? (double)ref_of(m, a.c) - a.log2_scale * (double)m : 0.0;
-    int k = 0;   // S = f 2^k, f near 1
-    float f = frexpf(S, &k);
-    if (f < 0.7f) {
-      f *= 2.f;
-      --k;
-    }
-    base[row] = m < INFINITY && S > 0.f ? (double)row_score[row] - kLn2 * (over + k) - (double)log1pf(f - 1.f) : NAN;
-    top[row] = m;
+    row_stat[row] = Stat{m < INFINITY ? m : NAN, S};   // +inf: no distribution
+    row_over[row] = above(m, a.c);
     for (int q = q0; q <= q1; ++q) seg_row[row + q] = row;
   }
-  const int segments = R == 0 ? 0 : R + (int)csize - 1, lists = segments + finished_in_use;
-  for (int i = tid; i < lists; i += kThreads) next[i] = 0;
-  __syncthreads();
-  for (int i = tid; i < segments * a.width; i += kThreads) {
-    const int seg = i / a.width, row = seg_row[seg];
-    if (row < 0 || i - seg * a.width >= counts[seg]) continue;
-    const entry_t e = all[i];
-    places[i] = column_of(e);
-    const double v = base[row] + ((double)value_of(e) - (double)top[row]) * a.inv_temp;
-    all[i] = fabs(v) < INFINITY ? order_of(v) : 0;
+  const int segments = R == 0 ? 0 : R + (int)csize - 1, listed = segments * a.width, offers = listed + finished_in_use;
+  for (int i = tid; i < finished_in_use; i += kThreads) {
+    all[listed + i] = order_of(done_score[i], 0.f);
+    places[listed + i] = (entry_t)done_beam[i] << 32 | (uint32_t)a.end;
   }
   __syncthreads();
+#pragma unroll 1
+  for (int i = tid; i < listed; i += kThreads) {
+    const int seg = i / a.width, row = seg_row[seg];
+    entry_t v = 0;
+    if (row >= 0 && i - seg * a.width < counts[seg]) {
+      const entry_t e = all[i];
+      places[i] = (entry_t)row_beam[row] << 32 | column_of(e);
+      const LogProb lp = log_prob(value_of(e), row_stat[row], row_over[row], a.inv_temp);
+      v = sum_of(row_score[row], lp);
+    }
+    all[i] = v;
+  }
+  __syncthreads();
+
+  // The order of two offers: the larger value, then the lower beam, then its lower column
+  auto put = [&](int i, entry_t value, entry_t place) {
+    const int64_t at = b * a.width + i;
+    const bool offered = value != 0;
+    const int64_t column = offered ? (int64_t)(uint32_t)place : -1;
+    a.out_scores[at] = offered ? score_of(value) : -INFINITY;
+    a.parents[at] = offered ? (int64_t)(place >> 32) : 0;
+    a.tokens[at] = column;
+    if (a.out_finished != nullptr) a.out_finished[at] = offered && column == a.end;
+  };
+  if (offers <= kThreads) {   // a thread per offer: its rank among all
+    const entry_t v = tid < offers ? all[tid] : 0, place = v != 0 ? places[tid] : 0;
+    const int there = __syncthreads_count(v != 0);
+    if (v != 0) {
+      int rank = 0;
+#pragma unroll 8
+      for (int k = 0; k < offers; ++k) {
+        const entry_t u = all[k];
+        rank += u > v;
+        if (u == v && k != tid) rank += places[k] < place;
+      }
+      if (rank < a.width) put(rank, v, place);
+    }
+    if (tid >= there && tid < a.width) put(tid, 0, 0);
+    return;
+  }
   if (warp != 0) return;
 
   // Lists are in order: the best of their heads is the next offer.  Lane l has lists l,
   // l + 32, ...: the segments', then the finished beams.
-  entry_t value = 0;      // of this lane's best head
-  uint32_t beam = 0, column = 0;
+  const int lists = segments + finished_in_use;
+  for (int l = lane; l < lists; l += 32) next[l] = 0;
+  entry_t value = 0, place = 0;   // of this lane's best head
   int from_list = 0;
   auto look = [&] {
     value = 0;
 #pragma unroll 1
     for (int l = lane; l < lists; l += 32) {
-      entry_t v = 0;
-      uint32_t k = 0, col = 0;
-      const int at = next[l];
-      if (l < segments) {
-        const int row = seg_row[l];
-        if (row >= 0 && at < counts[l]) {
-          v = all[l * a.width + at];
-          col = places[l * a.width + at];
-          k = row_beam[row];
-        }
-      } else if (at == 0) {
-        v = order_of((double)done_score[l - segments]);
-        k = done_beam[l - segments];
-        col = (uint32_t)a.end;
-      }
-      if (v > value || (v == value && (k < beam || (k == beam && col < column)))) {
+      const int at = next[l], i = l < segments ? l * a.width + at : listed + l - segments;
+      const entry_t v = at < (l < segments ? a.width : 1) ? all[i] : 0;
+      if (v == 0) continue;
+      if (v > value || (v == value && places[i] < place)) {
         value = v;
-        beam = k;
-        column = col;
+        place = places[i];
         from_list = l;
       }
     }
   };
   look();
   for (int i = 0; i < a.width; ++i) {
-    // the largest value, then the lowest beam, then its lowest column; the warp's reductions take 32 bits
+    // the warp's reductions take 32 bits
     const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(value >> 32));
-    bool mine_is = (uint32_t)(value >> 32) == hi;
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, mine_is ? (uint32_t)value : 0u);
-    mine_is = mine_is && (uint32_t)value == lo;
-    const bool offered = hi != 0;   // (the order of a number starts above 0)
-    const uint32_t k = __reduce_min_sync(0xffffffffu, mine_is ? beam : 0xffffffffu);
-    mine_is = mine_is && beam == k;
-    const uint32_t col = __reduce_min_sync(0xffffffffu, mine_is ? column : 0xffffffffu);
-    mine_is = mine_is && column == col;
-    const int64_t at = b * a.width + i;
-    if (!offered) {
-      if (lane == 0) {
-        a.out_scores[at] = -INFINITY;
-        a.parents[at] = 0;
-        a.tokens[at] = -1;
-        if (a.out_finished != nullptr) a.out_finished[at] = 0;
-      }
-    } else if (mine_is) {   // one lane: no two offers have one place
-      a.out_scores[at] = (float)number_of(value);
-      a.parents[at] = k;
-      a.tokens[at] = col;
-      if (a.out_finished != nullptr) a.out_finished[at] = col == a.end;
+    bool best_is = (uint32_t)(value >> 32) == hi;
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, best_is ? (uint32_t)value : 0u);
+    best_is = best_is && (uint32_t)value == lo;
+    const uint32_t k = __reduce_min_sync(0xffffffffu, best_is ? (uint32_t)(place >> 32) : 0xffffffffu);
+    best_is = best_is && (uint32_t)(place >> 32) == k;
+    const uint32_t col = __reduce_min_sync(0xffffffffu, best_is ? (uint32_t)place : 0xffffffffu);
+    best_is = best_is && (uint32_t)place == col;
+    if (hi == 0) {   // (the order of a number starts above 0)
+      if (lane == 0) put(i, 0, 0);
+    } else if (best_is) {   // one lane: no two offers have one place
+      put(i, value, place);
       ++next[from_list];   // this lane's own
       look();
     }
@@ -661,7 +671,7 @@ nmd_status nmd_beam_select(const void* d_logits, int32_t dtype, int64_t B, int64
   const uintptr_t mis = dtype == NMD_DT_FP32 ? 3 : 1;
   if (!d_logits || ((uintptr_t)d_logits & mis) || !d_scores || !d_out_scores || !d_parents || !d_tokens)
     return NMD_ERR_INVALID;
-  const Select a{d_logits, V, ld, (int)K, (int)width, c, kLog2e / temperature, 1.0 / temperature, d_scores, d_finished, end,
+  const Select a{d_logits, V, ld, (int)K, (int)width, c, two_floats(1.0 / temperature), d_scores, d_finished, end,
                  d_out_scores, d_parents, d_tokens, d_out_finished};
   cudaStream_t s = (cudaStream_t)stream;
   if (dtype == NMD_DT_FP32) return launch_select<float>(a, B, s);
