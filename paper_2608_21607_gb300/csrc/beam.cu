@@ -547,53 +547,72 @@ constexpr int kStates = 32;
 struct States {
   State s[kStates];
   int count;
-  int K, width, per;      // per: bytes of a row in a CTA's memory
+  int K, width, per;      // per: bytes of a row in a CTA's memory, a power of two
   int64_t B, work;
   const int64_t* parents;
 };
 
+// A piece of all K rows of a group: `rows` of them at a time, `across` threads to a row.
 template <class U>
-__device__ __forceinline__ void move(const State& s, int64_t w, const States& a, char* smem, const int* parent) {
-  const int64_t slice = w % s.slices, g = w / s.slices, b = g % a.B, o = g / a.B;
-  const int per = a.per / (int)sizeof(U);
-  const int64_t u0 = slice * per;
-  const int n = (int)min((int64_t)per, s.units - u0);
+__device__ __forceinline__ void move(const State& s, int64_t slice, int64_t b, int64_t o, const States& a, char* smem,
+                                     const int* parent, unsigned long long needed) {
+  const int per = a.per / (int)sizeof(U), across = min(per, kThreads), rows = kThreads / across;
+  const int u0 = threadIdx.x & (across - 1), k0 = threadIdx.x / across;
+  const int n = (int)min((int64_t)per, s.units - slice * per);
+  const char* in = s.in + o * s.in_outer + b * a.K * s.in_row + slice * a.per;
+  char* out = s.out + o * s.out_outer + b * a.width * s.out_row + slice * a.per;
   U* buf = (U*)smem;
-  const char* in = s.in + o * s.in_outer + b * a.K * s.in_row;
-  char* out = s.out + o * s.out_outer + b * a.width * s.out_row;
-  for (int i = threadIdx.x; i < a.K * n; i += kThreads) {
-    const int k = i / n, u = i - k * n;
-    buf[k * per + u] = ((const U*)(in + k * s.in_row))[u0 + u];
+  for (int u = u0; u < n; u += across) {
+#pragma unroll 4
+    for (int k = k0; k < a.K; k += rows)
+      if (needed >> k & 1) {
+        const U* from = (const U*)(in + k * s.in_row) + u;
+        if (sizeof(U) == 16) copy_async(tc::smem_u32(buf + k * per + u), from);
+        else buf[k * per + u] = *from;
+      }
+  }
+  if (sizeof(U) == 16) {
+    copy_commit();
+    copy_wait<0>();
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.width * n; i += kThreads) {
-    const int k = i / n, u = i - k * n, p = parent[k];
-    if (p >= 0) ((U*)(out + k * s.out_row))[u0 + u] = buf[p * per + u];
+  for (int u = u0; u < n; u += across) {
+#pragma unroll 4
+    for (int k = k0; k < a.width; k += rows) {
+      const int p = parent[k];
+      if (p >= 0) ((U*)(out + k * s.out_row))[u] = buf[p * per + u];
+    }
   }
 }
 
-// A CTA takes a piece of all K rows of a group at a time: it is in shared memory before
-// any row is written, so that rows may change places.
+// A CTA takes a piece of all K rows of a group at a time: what is needed of it is in
+// shared memory before any row is written, so that rows may change places.  In place,
+// rows that stay are not written, and those that nothing goes on from not read.
 __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant__ States a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ int parent[kMostWidth];
+  __shared__ unsigned long long needed;
   for (int64_t w = blockIdx.x; w < a.work; w += gridDim.x) {
     int e = 0;
     while (e + 1 < a.count && a.s[e + 1].first <= w) ++e;
     const State& s = a.s[e];
-    const int64_t mine = w - s.first, b = mine / s.slices % a.B;
+    const int64_t mine = w - s.first, g = mine / s.slices, slice = mine - g * s.slices, o = g / a.B, b = g - o * a.B;
+    __syncthreads();
+    if (threadIdx.x == 0) needed = 0;
     __syncthreads();
     for (int k = threadIdx.x; k < a.width; k += kThreads) {
       const int64_t p = a.parents[b * a.width + k];
-      parent[k] = p >= 0 && p < a.K ? (int)p : -1;
+      const bool moves = p >= 0 && p < a.K && !(s.in == s.out && p == k);
+      parent[k] = moves ? (int)p : -1;
+      if (moves) atomicOr(&needed, 1ull << p);
     }
     __syncthreads();
     switch (s.unit) {
-      case 16: move<uint4>(s, mine, a, smem, parent); break;
-      case 8: move<uint2>(s, mine, a, smem, parent); break;
-      case 4: move<uint32_t>(s, mine, a, smem, parent); break;
-      case 2: move<uint16_t>(s, mine, a, smem, parent); break;
-      default: move<uint8_t>(s, mine, a, smem, parent);
+      case 16: move<uint4>(s, slice, b, o, a, smem, parent, needed); break;
+      case 8: move<uint2>(s, slice, b, o, a, smem, parent, needed); break;
+      case 4: move<uint32_t>(s, slice, b, o, a, smem, parent, needed); break;
+      case 2: move<uint16_t>(s, slice, b, o, a, smem, parent, needed); break;
+      default: move<uint8_t>(s, slice, b, o, a, smem, parent, needed);
     }
   }
 }
@@ -716,16 +735,27 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
   int64_t k = 0;
   while (k < count) {
     States a{};
+    Range taken[kStates];
     a.B = B;
     a.K = (int)K;
     a.width = (int)width;
     a.parents = d_parents;
-    a.per = (int)std::max<int64_t>(16, std::min<int64_t>(4096, 32768 / K / 16 * 16));
-    for (; k < count && a.count < 1; ++k) {
+    a.per = 4096;
+    while (a.per * K > 32768) a.per /= 2;
+    for (; k < count && a.count < kStates; ++k) {
       const nmd_beam_state& s = states[k];
       if (s.outer == 0 || s.bytes == 0 || B == 0) continue;
+      // in place, states between each other's bytes go one after another
+      int64_t reach = 0;
+      rows_apart(s.outer, s.out_outer, B * width, s.out_row, s.bytes, &reach);
+      const Range r{(uintptr_t)s.out, (uintptr_t)s.out + (uintptr_t)reach, kPlace};
+      bool meets = false;
+      for (int i = 0; i < a.count; ++i) meets |= r.from < taken[i].to && taken[i].from < r.to;
+      if (meets) break;
+      taken[a.count] = r;
       uintptr_t all = (uintptr_t)s.in | (uintptr_t)s.out | (uintptr_t)s.bytes | 16;
-      all |= (uintptr_t)s.in_row | (uintptr_t)s.out_row;
+      if (B * K > 1) all |= (uintptr_t)s.in_row;
+      if (B * width > 1) all |= (uintptr_t)s.out_row;
       if (s.outer > 1) all |= (uintptr_t)s.in_outer | (uintptr_t)s.out_outer;
       State& t = a.s[a.count++];
       t = State{(const char*)s.in, (char*)s.out, s.in_outer, s.out_outer, s.in_row, s.out_row, 0, 0, a.work,
