@@ -10,9 +10,10 @@
 // early steps grow by up to a per step just the same, and the two come out
 // equally far from the definition (within a third, over decaying, flat and low-rank
 // spectra); with one piece (11 bits) the result would be off by parts in a hundred.
-// The tensor cores add in fp32 but round towards zero, which leans by up to a
-// unit per addition of a sum of squares; so a tile's sum leaves TMEM every 128
-// products and goes on in the epilogue's registers, rounded to nearest.
+// The tensor cores add in fp32 but round towards zero, which leans by up to a unit of
+// the sum so far per addition; so the two small products of 64 columns come first,
+// and after each 64 columns the sum leaves TMEM and goes on in the epilogue's
+// registers, rounded to nearest.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -48,14 +49,6 @@ struct Matrix {   // elements at i rs + j cs
   __device__ __forceinline__ T& at(int64_t i, int64_t j) const {
     return ((T*)x)[i * rs + j * cs];
   }
-  __device__ __forceinline__ float get(int64_t i, int64_t j) const {
-    return dtype == NMD_DT_FP32 ? at<float>(i, j) : dtype == NMD_DT_BF16 ? as_float(at<bf16>(i, j)) : as_float(at<__half>(i, j));
-  }
-  __device__ __forceinline__ void put(int64_t i, int64_t j, float v) const {
-    if (dtype == NMD_DT_FP32) from_float(v, &at<float>(i, j));
-    else if (dtype == NMD_DT_BF16) from_float(v, &at<bf16>(i, j));
-    else from_float(v, &at<__half>(i, j));
-  }
 };
 
 // What becomes of the update: an R x C matrix, C the side whose elements are
@@ -76,12 +69,24 @@ struct Pieces {
   int64_t rows, cols, ld;
   __host__ __device__ int64_t plane() const { return rows * ld; }
 };
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+  hi = *(const uint32_t*)&h;
+  lo = *(const uint32_t*)&l;
+}
 __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
   lo = __float2half_rn(v - __half2float(hi));   // an overflow leaves infinities of both signs: NaN in the next product
 }
 
 // ------------------------------------------------------------------ the update and its norm
+
+// Every kernel here lets the next one start and waits for the one before to have ended
+// before it touches memory, so that launches and set-up overlap.
+__device__ __forceinline__ void ready_for_next() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // fp32 squares of a few values, in fp64 where they leave fp32's range or come near its ends
 template <int N>
@@ -127,6 +132,8 @@ __device__ __forceinline__ void each(const Walk& w, const Job& j, int64_t at, F 
 template <class G, class M, bool STEP>
 __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, int* status) {
   __shared__ double red[kThreads / 32];
+  ready_for_next();
+  after_previous();   // the kernels of an earlier call have done with the workspace
   if (blockIdx.x == 0 && threadIdx.x < 2) status[threadIdx.x] = 0;
   double sum = 0.0;
   const Walk w = walk_of(j.R, j.C);
@@ -165,6 +172,8 @@ template <class G, class M, bool STEP>
 __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
                                                           int grows) {
   __shared__ double red[kThreads / 32];
+  ready_for_next();
+  after_previous();
   double sum = 0.0;
   for (int i = threadIdx.x; i < count; i += kThreads) sum += parts[i];
 #pragma unroll
@@ -223,7 +232,7 @@ struct Gemm {
   int* status;
 };
 
-constexpr int kBM = 128, kBK = 64, kChunk = 2;   // rows of a tile, products of a stage, stages of a sum in TMEM
+constexpr int kBM = 128, kBK = 64;   // rows of a tile, products of a stage
 constexpr int kEpilogue = 256, kProducer = 8, kIssuer = 9, kGemmThreads = 320;
 template <int BN>
 struct Cfg {
@@ -267,94 +276,122 @@ __device__ __forceinline__ Item item_of(const Gemm& p, int w, int BN) {
   return t;
 }
 
-__device__ __forceinline__ uint32_t halves_of(__half a, __half b) {
-  return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16;
+// What a warp writes goes through a 32 x 32 square of its own in shared memory, element
+// (r, c) at r 32 + (c ^ r), so that adjacent lanes write adjacent elements.  (A row per
+// lane, 16 bytes at a time, are as many requests to L2 as there are half sectors.)  The
+// code is one copy for all columns of a tile: most tiles are few per CTA, and fetching
+// instructions counted for more than executing them.
+__device__ __forceinline__ float& in_square(float* sq, int r, int c) { return sq[r * 32 + (c ^ r)]; }
+
+// 32 rows x 32 columns of D in pieces, from row0 and col0 on: alpha (the square, or with
+// `turned` its transpose) + beta C + diag I.  Four lanes write 64 adjacent bytes of a row.
+// Rows past the last are not written; columns up to the row's stride are.
+__device__ __forceinline__ void put_block(const Gemm& p, float alpha, float* sq, int64_t row0, int64_t col0, bool turned, bool lower) {
+  const int lane = threadIdx.x & 31, c = (lane & 3) * 8;
+#pragma unroll 2
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2);
+    const int64_t row = row0 + r, col = col0 + c;
+    if (row >= p.M) return;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // on the diagonal what is above it is what is below it, in every bit
+      const bool swap = turned || (lower && c + e > r);
+      v[e] = alpha * (swap ? in_square(sq, c + e, r) : in_square(sq, r, c + e));
+    }
+    if (p.beta != 0.f) {
+      const __half* at = p.c.hi + row * p.c.ld + col;
+      const uint4 a = *(const uint4*)at, b = *(const uint4*)(at + p.c.plane());
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, __half2float(((const __half*)&a)[e]) + __half2float(((const __half*)&b)[e]), v[e]);
+    }
+    if (lower) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e == r) v[e] += p.diag;
+    }
+    uint4 h, l;
+    split2(v[0], v[1], h.x, l.x);
+    split2(v[2], v[3], h.y, l.y);
+    split2(v[4], v[5], h.z, l.z);
+    split2(v[6], v[7], h.w, l.w);
+    __half* to = p.d.hi + row * p.d.ld + col;
+    *(uint4*)to = h;
+    *(uint4*)(to + p.d.plane()) = l;
+  }
 }
 
-// 32 columns of one row of D by a thread, in pieces; a symmetric D also as 32 rows of a column
-__device__ __forceinline__ void put_pieces(const Gemm& p, float alpha, float (&v)[32], int64_t row, int64_t col) {
-  if (row >= p.M || col >= p.d.ld) return;
-  __half* at = p.d.hi + row * p.d.ld + col;
-  const int64_t plane = p.d.plane();
-  if (p.mode == kSymmetric) {
-    if (col > row) return;
-    if (p.beta != 0.f) {
-      const uint4* h = (const uint4*)(p.c.hi + row * p.c.ld + col);
-      const uint4* l = (const uint4*)(p.c.hi + p.c.plane() + row * p.c.ld + col);
+template <class T>
+__device__ __forceinline__ void put_rows(const Gemm& p, float alpha, int64_t row0, int rows, int64_t col, float* sq) {
+  const int lane = threadIdx.x & 31;
+  T* at = &p.out.out.at<T>(row0, col);
+  const int64_t rs = p.out.out.rs;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 8) {
+    T w[8];
+    if (p.out.step) {   // all loads, then all stores
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint4 a = h[q], b = l[q];
-        const __half2* x = (const __half2*)&a;
-        const __half2* y = (const __half2*)&b;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 f = __half22float2(x[i]), g = __half22float2(y[i]);
-          v[q * 8 + 2 * i] = fmaf(p.beta, f.x + g.x, v[q * 8 + 2 * i] * alpha);
-          v[q * 8 + 2 * i + 1] = fmaf(p.beta, f.y + g.y, v[q * 8 + 2 * i + 1] * alpha);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] *= alpha;
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < rows) w[i] = at[(r0 + i) * rs];
     }
-  } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] *= alpha;
-  }
-  if (p.mode == kSymmetric && col + 31 >= row) {   // across the diagonal
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (col + i > row) continue;
-      __half hi, lo;
-      split(col + i == row ? v[i] + p.diag : v[i], hi, lo);
-      at[i] = hi;
-      at[plane + i] = lo;
-      if (col + i < row) {
-        p.d.hi[(col + i) * p.d.ld + row] = hi;
-        p.d.hi[plane + (col + i) * p.d.ld + row] = lo;
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + i;
+      if (r >= rows) break;
+      float x = alpha * in_square(sq, r, lane);
+      if (p.out.step) x = fmaf(-p.out.lr, x, p.out.keep * as_float(w[i]));
+      from_float(x, &at[r * rs]);
     }
-    return;
   }
+}
+// 32 x 32 of D in pieces from a row per lane, without C: each lane's vectors of pieces go
+// through shared memory instead (a fifth of the instructions)
+__device__ __forceinline__ void put_rows_of(const Gemm& p, float alpha, const float (&v)[32], float* sq, int64_t row0, int64_t col0) {
+  const int lane = threadIdx.x & 31;
+  uint4* s = (uint4*)sq;   // [piece][row][four vectors], a row's in an order that spreads over the banks
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    uint32_t h[4], l[4];
+    uint4 h, l;
+    split2(v[8 * q] * alpha, v[8 * q + 1] * alpha, h.x, l.x);
+    split2(v[8 * q + 2] * alpha, v[8 * q + 3] * alpha, h.y, l.y);
+    split2(v[8 * q + 4] * alpha, v[8 * q + 5] * alpha, h.z, l.z);
+    split2(v[8 * q + 6] * alpha, v[8 * q + 7] * alpha, h.w, l.w);
+    s[lane * 4 + (q ^ (lane >> 1 & 3))] = h;
+    s[128 + lane * 4 + (q ^ (lane >> 1 & 3))] = l;
+  }
+  __syncwarp();
+  if (col0 >= p.d.ld) return;
+  __half* to = p.d.hi + (row0 + (lane >> 2)) * p.d.ld + col0 + (lane & 3) * 8;
+  const int64_t plane = p.d.plane(), step = 8 * p.d.ld;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __half a[2], b[2];
-      split(v[q * 8 + 2 * i], a[0], b[0]);
-      split(v[q * 8 + 2 * i + 1], a[1], b[1]);
-      h[i] = halves_of(a[0], a[1]);
-      l[i] = halves_of(b[0], b[1]);
-      if (p.mode == kSymmetric) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int64_t t = (col + q * 8 + 2 * i + k) * p.d.ld + row;
-          p.d.hi[t] = a[k];
-          p.d.hi[plane + t] = b[k];
-        }
-      }
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2), at = r * 4 + ((lane & 3) ^ (r >> 1 & 3));
+    if (row0 + r < p.M) {
+      *(uint4*)(to + i * step) = s[at];
+      *(uint4*)(to + i * step + plane) = s[128 + at];
     }
-    ((uint4*)at)[q] = make_uint4(h[0], h[1], h[2], h[3]);
-    ((uint4*)(at + plane))[q] = make_uint4(l[0], l[1], l[2], l[3]);
   }
 }
-
-// 32 rows x 32 columns of the result by a warp: turned in shared memory, so that lanes write adjacent elements
-__device__ __forceinline__ void put_result(const Gemm& p, float alpha, const float (&v)[32], int64_t row0, int64_t col0, float* square) {
+// the square of rows from row0 and columns from col0 on, by the kernel's mode
+__device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq, int64_t row0, int64_t col0, float* part, int BN) {
   const int lane = threadIdx.x & 31;
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 32; ++i) square[lane * 32 + (i ^ lane)] = v[i] * alpha;
-  __syncwarp();
-  if (col0 + lane >= p.N) return;
-  const Matrix& o = p.out.out;
-#pragma unroll 8
-  for (int r = 0; r < 32; ++r) {
-    if (row0 + r >= p.M) break;
-    float x = square[r * 32 + (lane ^ r)];
-    if (p.out.step) x = fmaf(-p.out.lr, x, p.out.keep * o.get(row0 + r, col0 + lane));
-    o.put(row0 + r, col0 + lane, x);
+  if (p.mode == kPartial) {
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) part[r * BN + lane] = in_square(sq, r, lane);
+  } else if (p.mode == kResult) {
+    if (col0 + lane >= p.N) return;
+    const Matrix& o = p.out.out;
+    const int rows = (int)min((int64_t)32, p.M - row0);
+    if (o.dtype == NMD_DT_FP32) put_rows<float>(p, alpha, row0, rows, col0 + lane, sq);
+    else if (o.dtype == NMD_DT_BF16) put_rows<bf16>(p, alpha, row0, rows, col0 + lane, sq);
+    else put_rows<__half>(p, alpha, row0, rows, col0 + lane, sq);
+  } else if (col0 < p.d.ld) {
+    if (p.mode == kSymmetric && col0 > row0) return;   // above the diagonal
+    put_block(p, alpha, sq, row0, col0, false, p.mode == kSymmetric && col0 == row0);
+    if (p.mode == kSymmetric && col0 < row0 && row0 < p.M) {
+      put_block(p, alpha, sq, col0, row0, true, false);
+    }
   }
 }
 
@@ -382,7 +419,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   int* dead_word = (int*)(slot + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  ready_for_next();
   if (threadIdx.x == 0) {
+    prefetch_tmap(&ta);
+    prefetch_tmap(&tb);
     for (int s = 0; s < C::NS; ++s) {
       mbar_init(b_full + 8 * s, 1);
       mbar_init(b_empty + 8 * s, 1);
@@ -394,18 +434,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     mbar_init(b_drain, 1);
     fence_mbar_init();
     *abort_flag = 0;
-    *dead_word = *(volatile int*)p.status;   // an earlier product's wait ran out: what follows has no input
   }
   if (warp == kIssuer) {
     tmem_alloc(smem_u32(slot), C::TMEM);
     tmem_relinquish();
   }
+  after_previous();
+  if (threadIdx.x == 0) *dead_word = *(volatile int*)p.status;   // an earlier product's wait ran out: what follows has no input
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = *(volatile uint32_t*)slot;
   const bool dead = *dead_word != 0;
-
   if (warp == kProducer) {
     if (lane == 0 && !dead) {
       int64_t n = 0;
@@ -452,25 +492,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const Item t = item_of(p, w, BN);
         for (int k = t.k0; k < t.k1; ++k, ++n) {
           const int s = (int)(n % C::NS), buf = (int)(ch & 1);
-          const bool first = (k - t.k0) % kChunk == 0, last = (k - t.k0) % kChunk == kChunk - 1 || k + 1 == t.k1;
-          if (first && !(ok = conv_wait(b_tempty + 8 * buf, (uint32_t)((ch >> 1) & 1) ^ 1u, abort_flag, p.status, 2))) break;
+          if (!(ok = conv_wait(b_tempty + 8 * buf, (uint32_t)((ch >> 1) & 1) ^ 1u, abort_flag, p.status, 2))) break;
           if (!(ok = conv_wait(b_full + 8 * s, (uint32_t)((n / C::NS) & 1), abort_flag, p.status, 3))) break;
           fence_after();
           const uint32_t a0 = stage0 + s * C::STAGE, b0 = a0 + C::A_BYTES, d = tmem + buf * BN;
           const uint64_t ah = AMN ? sdesc(a0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(a0, 16, 1024, SWZ_128B);
           const uint64_t bh = BMN ? sdesc(b0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(b0, 16, 1024, SWZ_128B);
+          // the small products first: what an addition loses is a part of the sum so far
 #pragma unroll
           for (int q = 0; q < kBK / 16; ++q) {
             const uint64_t a = ah + ((q * A_STEP) >> 4), b = bh + ((q * B_STEP) >> 4);
-            mma_ss_elect(d, a + (A_LO >> 4), b, idesc, !(first && q == 0));
+            mma_ss_elect(d, a + (A_LO >> 4), b, idesc, q > 0);
             mma_ss_elect(d, a, b + (B_LO >> 4), idesc, 1);
-            mma_ss_elect(d, a, b, idesc, 1);
           }
+#pragma unroll
+          for (int q = 0; q < kBK / 16; ++q) mma_ss_elect(d, ah + ((q * A_STEP) >> 4), bh + ((q * B_STEP) >> 4), idesc, 1);
           commit_elect(b_empty + 8 * s);
-          if (last) {
-            commit_elect(b_tfull + 8 * buf);
-            ++ch;
-          }
+          commit_elect(b_tfull + 8 * buf);
+          ++ch;
         }
       }
       commit_elect(b_drain);   // every product issued has ended before TMEM is given back
@@ -481,7 +520,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       __syncwarp();
     }
-  } else {
+  } else if (warp < kEpilogue / 32) {
     constexpr int G = BN / 64;   // groups of 32 columns of a warpgroup
     const int part = warp >> 2, row = (warp & 3) * 32;
     const uint32_t lanes = (uint32_t)row << 16;
@@ -491,42 +530,51 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     bool ok = !dead;
     for (int w = blockIdx.x; w < p.items; w += gridDim.x) {
       const Item t = item_of(p, w, BN);
-      const int chunks = (t.k1 - t.k0 + kChunk - 1) / kChunk;
+      const int chunks = t.k1 - t.k0;
       float acc[G][32];
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[g][i] = 0.f;
       for (int c = 0; c < chunks && ok; ++c, ++ch) {
         const int buf = (int)(ch & 1);
         if (!(ok = warp_wait(b_tfull + 8 * buf, (uint32_t)((ch >> 1) & 1), abort_flag, p.status, 4))) break;
         fence_after();
+        uint32_t v[G][32];   // all loads, and the buffer is free again
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          uint32_t v[32];
-          tmem_ld32(tmem + lanes + buf * BN + (part * G + g) * 32, v);
-          tmem_wait_ld(v);
+        for (int g = 0; g < G; ++g) tmem_ld32(tmem + lanes + buf * BN + (part * G + g) * 32, v[g]);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[g][i] = c == 0 ? __uint_as_float(v[i]) : acc[g][i] + __uint_as_float(v[i]);
-        }
+        for (int g = 0; g < G; ++g) tmem_wait_ld(v[g]);
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(b_tempty + 8 * buf);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[g][i] += __uint_as_float(v[g][i]);
       }
       if (!ok && p.mode != kResult) break;
       const int64_t r = (int64_t)t.i * kBM + row;
-#pragma unroll
+      if (r >= p.M && p.mode != kPartial) continue;
+#pragma unroll 1
       for (int g = 0; g < G; ++g) {
-        const int64_t col = (int64_t)t.j * BN + (part * G + g) * 32;
-        if (!ok) {   // the result of a wait that ran out shows
+        const int col = (part * G + g) * 32;
+        __syncwarp();
+        float v[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[g][i] = NAN;
-        }
-        if (p.mode == kPartial) {
-          float4* at = (float4*)(p.part + ((int64_t)w * kBM + row + lane) * BN + (part * G + g) * 32);
+        for (int k = 0; k < G; ++k)
+          if (k == g) {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) at[q] = make_float4(acc[g][4 * q], acc[g][4 * q + 1], acc[g][4 * q + 2], acc[g][4 * q + 3]);
-        } else if (p.mode == kResult) {
-          put_result(p, alpha, acc[g], r, col, square);
-        } else {
-          put_pieces(p, alpha, acc[g], r + lane, col);
+            for (int i = 0; i < 32; ++i) v[i] = acc[k][i];
+          }
+        if (p.mode == kMatrix) {
+          put_rows_of(p, alpha, v, square, r, (int64_t)t.j * BN + col);
+          continue;
         }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) in_square(square, lane, i) = ok ? v[i] : NAN;   // the result of a wait that ran out shows
+        __syncwarp();
+        put_square(p, alpha, square, r, (int64_t)t.j * BN + col, p.part + ((int64_t)w * kBM + row) * BN + col, BN);
       }
     }
   }
@@ -538,30 +586,59 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
 }
 
-// The parts of a symmetric D added up in order, in pieces.  A CTA takes 32 columns of
-// one row of a tile; eight groups of lanes take every eighth part.
+// The parts of a symmetric D added up in order, in pieces.  MANY: a CTA takes 32 columns
+// of one row of a tile, eight groups of lanes every eighth part each; otherwise 32 rows
+// and columns, which it turns in shared memory for the copy above the diagonal.
+template <bool MANY>
 __global__ void __launch_bounds__(kThreads) join_kernel(Gemm p, int BN) {
-  __shared__ float sums[8][32];
-  const int per = kBM * (BN / 32), lane = threadIdx.x & 31, g = threadIdx.x >> 5;
-  const int tile = blockIdx.x / per, at = blockIdx.x - tile * per, r = at / (BN / 32), c = at % (BN / 32) * 32 + lane;
+  __shared__ float sums[32][33];
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int down = MANY ? kBM : kBM / 32, per = down * (BN / 32);
+  ready_for_next();
+  after_previous();
+  const int tile = blockIdx.x / per, at = blockIdx.x - tile * per, r0 = at / (BN / 32) * (MANY ? 1 : 32), c0 = at % (BN / 32) * 32;
   const Item t = item_of(p, tile * p.splits, BN);
-  const int64_t row = (int64_t)t.i * kBM + r, col = (int64_t)t.j * BN + c;
-  if (row >= p.M || col - lane > row) return;
-  const float* x = p.part + ((int64_t)tile * p.splits * kBM + r) * BN + c;
-  float sum = 0.f;
-#pragma unroll 4
-  for (int s = g; s < p.splits; s += 8) sum += x[(int64_t)s * kBM * BN];
-  sums[g][lane] = sum;
-  __syncthreads();
-  if (g != 0 || col > row) return;
+  const int64_t row0 = (int64_t)t.i * kBM + r0, col0 = (int64_t)t.j * BN + c0;
+  if (row0 >= p.M || col0 > row0 + (MANY ? 0 : 31)) return;
+  const float* x = p.part + ((int64_t)tile * p.splits * kBM + r0) * BN + c0 + lane;
+  const int64_t apart = (int64_t)kBM * BN, plane = p.d.plane();
+  const float scale = scale_of_sum(p);
+  auto put = [&](int64_t row, int64_t col, float v) {
+    __half hi, lo;
+    split(v * scale, hi, lo);
+    p.d.hi[row * p.d.ld + col] = hi;
+    p.d.hi[plane + row * p.d.ld + col] = lo;
+  };
+  if (MANY) {
+    float sum = 0.f;
+#pragma unroll 8
+    for (int s = g; s < p.splits; s += 8) sum += x[s * apart];
+    sums[g][lane] = sum;
+    __syncthreads();
+    if (g != 0 || col0 + lane > row0) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) sum += sums[i][lane];
-  __half hi, lo;
-  split(sum * scale_of_sum(p), hi, lo);
-  p.d.hi[row * p.d.ld + col] = hi;
-  p.d.hi[p.d.plane() + row * p.d.ld + col] = lo;
-  p.d.hi[col * p.d.ld + row] = hi;
-  p.d.hi[p.d.plane() + col * p.d.ld + row] = lo;
+    for (int i = 1; i < 8; ++i) sum += sums[i][lane];
+    put(row0, col0 + lane, sum);
+    if (col0 + lane < row0) put(col0 + lane, row0, sum);
+    return;
+  }
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += x[s * apart + (int64_t)(g + 8 * i) * BN];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = g + 8 * i;
+    sums[r][lane] = sum[i];
+    if (row0 + r < p.M && col0 + lane <= row0 + r) put(row0 + r, col0 + lane, sum[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = g + 8 * i;
+    if (row0 + lane < p.M && col0 + c < row0 + lane) put(col0 + c, row0 + lane, sums[lane][c]);
+  }
 }
 
 // ------------------------------------------------------------------------------- host
@@ -589,6 +666,21 @@ int sm_count() {
   });
 }
 
+template <class... P, class... A>
+nmd_status start(void (*kernel)(P...), int64_t grid, int threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+}
+
 template <int BN, bool AMN, bool BMN>
 nmd_status launch_bn(const Pieces& a, const Pieces& b, const Gemm& g, cudaStream_t s) {
   static std::atomic<int> ready[kMaxDevices];
@@ -601,12 +693,10 @@ nmd_status launch_bn(const Pieces& a, const Pieces& b, const Gemm& g, cudaStream
   if (!map_of(a, AMN ? 64 : kBM, &ta) || !map_of(b, BMN ? 64 : BN, &tb)) return NMD_ERR_CUDA;
   const int sms = sm_count();
   if (sms == 0) return NMD_ERR_CUDA;
-  kernel<<<std::min(g.items, sms), kGemmThreads, Cfg<BN>::SMEM, s>>>(ta, tb, g);
-  return cudaGetLastError() == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+  return start(kernel, std::min(g.items, sms), kGemmThreads, Cfg<BN>::SMEM, s, ta, tb, g);
 }
 template <bool AMN, bool BMN>
 nmd_status launch(int BN, const Pieces& a, const Pieces& b, const Gemm& g, cudaStream_t s) {
-  if (BN == 256) return launch_bn<256, AMN, BMN>(a, b, g, s);
   if (BN == 128) return launch_bn<128, AMN, BMN>(a, b, g, s);
   return launch_bn<64, AMN, BMN>(a, b, g, s);
 }
@@ -618,12 +708,9 @@ int64_t tiles_of(int64_t M, int64_t N, int BN, bool lower) {
   for (int64_t i = 0; i < tm; ++i) n += std::min<int64_t>((kBM * (i + 1) - 1) / BN + 1, tn);
   return n;
 }
-// The widest tiles that still give every SM one; 64 columns where none do.
-int columns_of(int64_t M, int64_t N, bool lower) {
-  for (int BN : {256, 128})
-    if (N > BN / 2 && tiles_of(M, N, BN, lower) >= kSms) return BN;
-  return 64;
-}
+// Tiles of 128 columns where they give every SM one, of 64 otherwise.  (Of 256, half
+// the operand traffic per product, do not leave the epilogue's threads the registers.)
+int columns_of(int64_t M, int64_t N, bool lower) { return N > 64 && tiles_of(M, N, 128, lower) >= kSms ? 128 : 64; }
 
 // The sums of a Gram matrix run over the long side: tiles, and parts of the sum where there are few of them
 struct GramPlan {
@@ -633,9 +720,9 @@ struct GramPlan {
 GramPlan gram_plan(int64_t r, int64_t M) {
   GramPlan g;
   const int64_t blocks = (M + kBK - 1) / kBK;
-  g.BN = r <= 64 ? 64 : tiles_of(r, r, 256, true) >= kSms ? 256 : 128;
+  g.BN = r <= 64 ? 64 : 128;
   g.tiles = tiles_of(r, r, g.BN, true);
-  g.splits = std::max<int64_t>(1, std::min<int64_t>(kSms / g.tiles, blocks / kChunk));
+  g.splits = std::max<int64_t>(1, std::min<int64_t>(kSms / g.tiles, blocks / 2));
   return g;
 }
 
@@ -687,20 +774,20 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
   const int64_t r = l.r, M = std::max(j.R, j.C);
   const int grid = (int)std::min<int64_t>((walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
   const int grows = (int)std::ceil(std::log2(std::max(1.0, 1.001 * std::fabs(k[0]))));
+  nmd_status st = NMD_OK;
   with_type(j.grad.dtype, [&](auto g) {
     with_type(j.step ? j.momentum.dtype : j.grad.dtype, [&](auto m) {
       typedef decltype(g) G;
       typedef decltype(m) M;
-      if (j.step) {
-        norm_kernel<G, M, true><<<grid, kThreads, 0, s>>>(j, parts, status);
-        pieces_kernel<G, M, true><<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
-      } else {
-        norm_kernel<G, G, false><<<grid, kThreads, 0, s>>>(j, parts, status);
-        pieces_kernel<G, G, false><<<grid, kThreads, 0, s>>>(j, X, parts, grid, shift, steps, grows);
-      }
+      auto both = [&](auto norm, auto pieces) {
+        st = start(norm, grid, kThreads, 0, s, j, parts, status);
+        if (st == NMD_OK) st = start(pieces, grid, kThreads, 0, s, j, X, (const double*)parts, grid, shift, steps, grows);
+      };
+      if (j.step) both(norm_kernel<G, M, true>, pieces_kernel<G, M, true>);
+      else both(norm_kernel<G, G, false>, pieces_kernel<G, G, false>);
     });
   });
-  if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
+  if (st != NMD_OK) return st;
   const GramPlan plan = gram_plan(r, M);
   const int bn_r = columns_of(r, r, true), bn_x = columns_of(j.R, j.C, false);
   auto product = [&](int64_t m, int64_t n, int64_t depth, int BN, bool lower, Mode mode) {
@@ -716,7 +803,6 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
     g.status = status;
     return g;
   };
-  nmd_status st;
   for (int i = 0; i < steps; ++i) {
     // A = X X^T: 2^24 a in the sums, 2^12 a in the pieces
     Gemm g = product(r, r, M, plan.BN, true, plan.splits > 1 ? kPartial : kSymmetric);
@@ -730,8 +816,9 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
     st = wide ? launch<false, false>(plan.BN, X, X, g, s) : launch<true, true>(plan.BN, X, X, g, s);
     if (st != NMD_OK) return st;
     if (plan.splits > 1) {
-      join_kernel<<<(unsigned)(plan.tiles * kBM * (plan.BN / 32)), kThreads, 0, s>>>(g, plan.BN);
-      if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
+      st = plan.splits > 16 ? start(join_kernel<true>, plan.tiles * kBM * (plan.BN / 32), kThreads, 0, s, g, plan.BN)
+                            : start(join_kernel<false>, plan.tiles * (kBM / 32) * (plan.BN / 32), kThreads, 0, s, g, plan.BN);
+      if (st != NMD_OK) return st;
     }
     // P = a I + b A + c A A
     g = product(r, r, r, bn_r, true, kSymmetric);
