@@ -14,79 +14,23 @@
 // the sum so far per addition; so the two small products of 64 columns come first,
 // and after each 64 columns the sum leaves TMEM and goes on in the epilogue's
 // registers, rounded to nearest.
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <cmath>
 
-#include "nmd_internal.cuh"
-#include "tc_pipe.cuh"
-#include "tc_ptx.cuh"
+#include "muon.cuh"
 
 namespace nmd {
 namespace {
 
 using namespace tc;
+using namespace muon;
 
 constexpr int64_t kMostSide = 16384;
 constexpr int kThreads = 256;
 constexpr int kParts = 608;          // CTAs of the norm's pass: four per SM
 constexpr int kSms = 152;            // the splitting of sums goes by this number, not by the device, for equal bits
-constexpr float kUnit = 4096.f;      // pieces hold 2^12 x
-
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ float as_float(bf16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ void from_float(float v, float* x) { *x = v; }
-__device__ __forceinline__ void from_float(float v, bf16* x) { *x = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void from_float(float v, __half* x) { *x = __float2half_rn(v); }
-
-struct Matrix {   // elements at i rs + j cs
-  void* x;
-  int dtype;
-  int64_t rs, cs;
-  template <class T>
-  __device__ __forceinline__ T& at(int64_t i, int64_t j) const {
-    return ((T*)x)[i * rs + j * cs];
-  }
-};
-
-// What becomes of the update: an R x C matrix, C the side whose elements are
-// adjacent in memory (or nearer).
-struct Job {
-  int64_t R, C;
-  Matrix grad, momentum, out;   // out: the result, or the weights
-  int step;                     // 1: a training step (momentum and weights)
-  float beta, rest;             // rest = 1 - beta
-  int nesterov;
-  float keep, lr;               // 1 - lr weight_decay, lr scale
-  double eps;
-};
-
-// Two fp16 pieces of an R x C matrix: plane 0 hi, plane 1 lo, rows of ld elements
-struct Pieces {
-  __half* hi;
-  int64_t rows, cols, ld;
-  __host__ __device__ int64_t plane() const { return rows * ld; }
-};
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  const __half2 h = __floats2half2_rn(a, b);
-  const float2 f = __half22float2(h);
-  const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
-  hi = *(const uint32_t*)&h;
-  lo = *(const uint32_t*)&l;
-}
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-  hi = __float2half_rn(v);
-  lo = __float2half_rn(v - __half2float(hi));   // an overflow leaves infinities of both signs: NaN in the next product
-}
 
 // ------------------------------------------------------------------ the update and its norm
-
-// Every kernel here lets the next one start and waits for the one before to have ended
-// before it touches memory, so that launches and set-up overlap.
-__device__ __forceinline__ void ready_for_next() { asm volatile("griddepcontrol.launch_dependents;"); }
-__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // fp32 squares of a few values, in fp64 where they leave fp32's range or come near its ends
 template <int N>
@@ -134,7 +78,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, in
   __shared__ double red[kThreads / 32];
   ready_for_next();
   after_previous();   // the kernels of an earlier call have done with the workspace
-  if (blockIdx.x == 0 && threadIdx.x < 2) status[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < kShift) status[threadIdx.x] = 0;
   double sum = 0.0;
   const Walk w = walk_of(j.R, j.C);
   for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
@@ -166,14 +110,15 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, in
   }
 }
 
-// X = update / (norm + eps) in pieces
-// shift: t of X before each step and after the last
-template <class G, class M, bool STEP>
-__global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
-                                                          int grows) {
+// What a value of the update is multiplied by, 2^(12 + t) / (norm + eps): a number near 1 and a power of two
+// in two halves, so that norms of 1e-40 and 1e38 do.  By a whole CTA; the first one of the grid writes the
+// shifts, t of X before each step and after the last.
+struct Factor3 {
+  float f, p, q;
+  __device__ __forceinline__ float of(float u) const { return u * p * q * f; }
+};
+__device__ __forceinline__ Factor3 factor_of(const double* parts, int count, double eps, int* shift, int steps, int grows) {
   __shared__ double red[kThreads / 32];
-  ready_for_next();
-  after_previous();
   double sum = 0.0;
   for (int i = threadIdx.x; i < count; i += kThreads) sum += parts[i];
 #pragma unroll
@@ -183,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const
   sum = 0.0;
   for (int i = 0; i < kThreads / 32; ++i) sum += red[i];
   // |X| = 2^-t at most; `grows`: a step takes a small X to 2^grows times itself at most
-  const double norm = sqrt(sum), size = norm / (norm + j.eps);
+  const double norm = sqrt(sum), size = norm / (norm + eps);
   const int small = size > 0.0 && size < 0x1p-8 ? min(100, -ilogb(size) - 1) : 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     int t = small;
@@ -192,11 +137,22 @@ __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const
       t = t < 8 ? 0 : max(0, t - grows);
     }
   }
-  // 2^(12 + t) / (norm + eps) as a number near 1 and a power of two in two halves, so that norms of 1e-40 and 1e38 do
   int e = 0;
-  const float f = (float)frexp((double)kUnit / (norm + j.eps), &e);
+  Factor3 r;
+  r.f = (float)frexp((double)kUnit / (norm + eps), &e);
   e = max(-280, min(280, e + small));
-  const float p = ldexpf(1.f, e / 2), q = ldexpf(1.f, e - e / 2);
+  r.p = ldexpf(1.f, e / 2);
+  r.q = ldexpf(1.f, e - e / 2);
+  return r;
+}
+
+// X = update / (norm + eps) in pieces
+template <class G, class M, bool STEP>
+__global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
+                                                          int grows) {
+  ready_for_next();
+  after_previous();
+  const Factor3 f = factor_of(parts, count, j.eps, shift, steps, grows);
   const Walk w = walk_of(j.R, j.C);
   for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
     G g[kEach];
@@ -206,10 +162,49 @@ __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const
     each(w, j, at, [&](int i, int64_t r, int64_t c) {
       const float u = STEP ? update_of(j, as_float(m[i]), as_float(g[i])) : as_float(g[i]);
       __half hi, lo;
-      split(u * p * q * f, hi, lo);
+      split(f.of(u), hi, lo);
       X.hi[r * X.ld + c] = hi;
       X.hi[X.plane() + r * X.ld + c] = lo;
     });
+  }
+}
+
+// The same of a wide update turned over: row c of X is column c of the update, 64
+// columns.  A lane reads 32 elements of its column, adjacent lanes adjacent columns, and
+// writes them as vectors.
+template <class G, class M, bool STEP>
+__global__ void __launch_bounds__(kThreads) turned_kernel(Job j, Pieces X, const double* parts, int count, int* shift, int steps,
+                                                          int grows) {
+  ready_for_next();
+  after_previous();
+  const Factor3 f = factor_of(parts, count, j.eps, shift, steps, grows);
+  const int64_t half = (j.R + 31) / 32, work = (j.C + 31) / 32 * half;
+  for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < work; at += gridDim.x * (kThreads / 32)) {
+    const int64_t c = at / half * 32 + (threadIdx.x & 31), r0 = at % half * 32;
+    if (c >= j.C) continue;
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+      G g[8];
+      M m[8];
+      float u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + q * 8 + i;
+        if (r < j.R) g[i] = j.grad.at<G>(r, c);
+        if (STEP && r < j.R) m[i] = j.momentum.at<M>(r, c);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        u[i] = r0 + q * 8 + i < j.R ? f.of(STEP ? update_of(j, as_float(m[i]), as_float(g[i])) : as_float(g[i])) : 0.f;
+      uint4 h, l;
+      split2(u[0], u[1], h.x, l.x);
+      split2(u[2], u[3], h.y, l.y);
+      split2(u[4], u[5], h.z, l.z);
+      split2(u[6], u[7], h.w, l.w);
+      __half* to = X.hi + c * X.ld + r0 + q * 8;
+      *(uint4*)to = h;
+      *(uint4*)(to + X.plane()) = l;
+    }
   }
 }
 
@@ -645,17 +640,6 @@ __global__ void __launch_bounds__(kThreads) join_kernel(Gemm p, int BN) {
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// boxes of 64 columns x `rows` rows x both pieces
-bool map_of(const Pieces& x, int rows, CUtensorMap* m) {
-  const auto encode = encode_fn();
-  if (!encode) return false;
-  const cuuint64_t dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2};
-  const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane() * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)rows, 2}, one[3] = {1, 1, 1};
-  return encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.hi, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int sm_count() {
   static std::atomic<int> sms[kMaxDevices];
   return per_device(sms, [] {
@@ -730,6 +714,7 @@ GramPlan gram_plan(int64_t r, int64_t M) {
 struct Layout {
   size_t status, parts, X[2], A, P, part, bytes;
   int64_t R, C, ldx, r, ldr;
+  bool strip;
 };
 Layout layout_of(int64_t R, int64_t C) {
   Layout l;
@@ -739,6 +724,7 @@ Layout layout_of(int64_t R, int64_t C) {
   l.r = std::min(R, C);
   l.ldr = (l.r + 63) / 64 * 64;
   const GramPlan g = gram_plan(l.r, std::max(R, C));
+  l.strip = l.r <= kStripSide;
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -747,6 +733,12 @@ Layout layout_of(int64_t R, int64_t C) {
   };
   l.status = take(256);
   l.parts = take(kParts * sizeof(double));
+  if (l.strip) {
+    l.X[0] = take((size_t)std::max(R, C) * 64 * 4);
+    l.part = take(strip_bytes(std::max(R, C)));
+    l.bytes = at;
+    return l;
+  }
   for (size_t& x : l.X) x = take((size_t)R * l.ldx * 4);
   l.A = take((size_t)l.r * l.ldr * 4);
   l.P = take((size_t)l.r * l.ldr * 4);
@@ -766,9 +758,11 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
   const Layout l = layout_of(j.R, j.C);
   char* w = (char*)ws;
   int* status = (int*)(w + l.status);
-  int* shift = status + 4;   // steps + 1 of them
+  int* shift = status + kShift;
   double* parts = (double*)(w + l.parts);
   Pieces X{(__half*)(w + l.X[0]), j.R, j.C, l.ldx}, Y{(__half*)(w + l.X[1]), j.R, j.C, l.ldx};
+  const bool turned = l.strip && j.R <= j.C;
+  if (l.strip) X = Pieces{X.hi, std::max(j.R, j.C), l.r, 64};
   const Pieces A{(__half*)(w + l.A), l.r, l.r, l.ldr}, P{(__half*)(w + l.P), l.r, l.r, l.ldr};
   const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
   const int64_t r = l.r, M = std::max(j.R, j.C);
@@ -783,11 +777,12 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
         st = start(norm, grid, kThreads, 0, s, j, parts, status);
         if (st == NMD_OK) st = start(pieces, grid, kThreads, 0, s, j, X, (const double*)parts, grid, shift, steps, grows);
       };
-      if (j.step) both(norm_kernel<G, M, true>, pieces_kernel<G, M, true>);
-      else both(norm_kernel<G, G, false>, pieces_kernel<G, G, false>);
+      if (j.step) both(norm_kernel<G, M, true>, turned ? turned_kernel<G, M, true> : pieces_kernel<G, M, true>);
+      else both(norm_kernel<G, G, false>, turned ? turned_kernel<G, G, false> : pieces_kernel<G, G, false>);
     });
   });
   if (st != NMD_OK) return st;
+  if (l.strip) return strip_run(j, X, steps, k, status, w + l.part, s);
   const GramPlan plan = gram_plan(r, M);
   const int bn_r = columns_of(r, r, true), bn_x = columns_of(j.R, j.C, false);
   auto product = [&](int64_t m, int64_t n, int64_t depth, int BN, bool lower, Mode mode) {

@@ -1,0 +1,431 @@
+// All Newton-Schulz steps of an update with a short side of at most 64 in one kernel
+// (mathematics, pieces and scales: muon.cu).
+//
+// X is M x 64, M the long side, in tiles of 128 rows; a CTA per SM holds its tiles in
+// shared memory from the first step to the last (five of them; of more it keeps two and
+// passes the others through three buffers).  A step is one pass over them,
+//   X <- X P  (128 x 64 by 64 x 64),  Z += X^T X,
+// and between passes the CTAs' sums Z are added up and every CTA forms
+//   A = Z,  P = a I + b A + c A A
+// for itself.  So nothing of X moves between steps, and a step costs two barriers of the
+// grid instead of four launches.
+//
+// Pieces are put side by side, so that one product of the tensor cores takes two:
+//   X P:    columns [hi P_hi | hi P_lo + lo P_hi],  128 x 128;
+//   X^T X:  rows [hi^T hi; lo^T hi], 128 x 64.  With Z = hi^T hi / 2 + lo^T hi the Gram
+//           matrix is Z + Z^T, which is as symmetric in its bits as in the formula;
+//   A A:    likewise.
+// The small products have accumulators of their own, and Z leaves TMEM after every tile.
+//
+// A tile is stored as rows of 64 columns, 128 bytes in the 128-byte swizzle, hi and lo
+// one after the other: K-major for X P, MN-major for X^T X.
+#include <algorithm>
+
+#include "muon.cuh"
+
+namespace nmd {
+namespace muon {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 256, kSms = 152;
+constexpr int kRows = 128, kSide = 64;
+constexpr int kBuffers = 5, kKept = 2;                      // tiles in shared memory; kept of more than that
+constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
+constexpr int kSquare = 2 * kSide * kSide * 2;              // both pieces of a 64 x 64 matrix
+constexpr int kZ = kSide + 1;                               // row stride of Z in shared memory
+constexpr size_t kOffP = (size_t)kBuffers * kTile, kOffA = kOffP + kSquare, kOffZ = kOffA + kSquare,
+                 kOffBars = kOffZ + (kSide * kZ * 4 + 255) / 256 * 256;
+constexpr size_t kSmem = 1024 + kOffBars + 128;
+static_assert(kSmem <= 227 * 1024, "shared memory");
+constexpr uint32_t kColD = 0, kColZ = 256, kTmem = 512;     // two X P, two Z
+
+struct Strip {
+  Job j;
+  Pieces x;            // X; tiles that are not kept go back there
+  int64_t M;
+  int turned;          // the result's columns are X's rows
+  int tiles, steps;
+  float a, b, c;
+  int* ints;
+  float* part;         // the CTAs' Z, 64 x 64 each
+  float* sum;          // 64 x 64
+};
+
+// the 16-byte vector q (0 .. 7) of row m in a tile's piece
+__device__ __forceinline__ uint32_t vector_at(int m, int q) { return (uint32_t)(m * 128 + ((q ^ (m & 7)) << 4)); }
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// All CTAs' writes before are seen by all after.  `target`: arrivals of all barriers up to
+// this one.  A wait that runs out (2 s) raises the abort flag; the kernel then goes on
+// without waiting and its result is NaN.
+__device__ __forceinline__ void grid_barrier(int* count, int target, volatile int* abort_flag, int* status) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    atomicAdd(count, 1);
+    const uint64_t t0 = globaltimer_ns();
+    for (;;) {
+      int n;
+      asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(n) : "l"(count) : "memory");
+      if (n >= target || *abort_flag) break;
+      if (globaltimer_ns() - t0 > kTimeoutNs) {
+        *abort_flag = 1;
+        record(status, NMD_ERR_TIMEOUT, 10);
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+}
+
+// A tile of the result from its fp32 rows in shared memory ([m][j ^ (m & 31)])
+template <class T>
+__device__ __forceinline__ void put_tile(const Strip& p, const float* stage, int64_t m0, float fill) {
+  const int r = (int)p.x.cols, rows = (int)min((int64_t)kRows, p.M - m0);
+#pragma unroll 1
+  for (int i = 0; i < kRows * kSide / kThreads; i += 8) {
+    T* at[8];
+    T w[8];
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      // adjacent threads, adjacent elements of the result
+      const int e = (i + k) * kThreads + threadIdx.x, m = p.turned ? e & (kRows - 1) : e / kSide, j = p.turned ? e / kRows : e & (kSide - 1);
+      at[k] = m < rows && j < r ? (p.turned ? &p.j.out.at<T>(j, m0 + m) : &p.j.out.at<T>(m0 + m, j)) : nullptr;
+      x[k] = stage[m * kSide + (j ^ (m & 31))] + fill;
+    }
+    if (p.j.step) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (at[k]) w[k] = *at[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (at[k]) from_float(p.j.step ? fmaf(-p.j.lr, x[k], p.j.keep * as_float(w[k])) : x[k], at[k]);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ Strip p) {
+  extern __shared__ char smem_raw[];
+  char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  float* Z = (float*)(smem + kOffZ);
+  const uint32_t base = smem_u32(smem), sP = base + kOffP, sA = base + kOffA, bars = base + kOffBars;
+  const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16;
+  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 4));
+  volatile int* abort_flag = (volatile int*)(slot + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int quad = warp & 3, half = warp >> 2;     // TMEM lanes and columns of this warp
+  const int row = quad * 32 + lane;                // of a tile, or of [hi; lo]
+  const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+  int* status = p.ints;
+  const int* shift = p.ints + kShift;
+  const int G = gridDim.x, T = (p.tiles - (int)blockIdx.x + G - 1) / G, kept = T <= kBuffers ? T : kKept;
+  auto tile_row = [&](int t) { return ((int64_t)blockIdx.x + (int64_t)t * G) * kRows; };
+  auto buffer_of = [&](int t) { return t < kept ? t : kKept + (t - kept) % (kBuffers - kKept); };
+
+  if (tid == 0) {
+    prefetch_tmap(&tx);
+    for (int i = 0; i < kBuffers + 4; ++i) mbar_init(bars + 8 * i, 1);
+    fence_mbar_init();
+    *abort_flag = 0;
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(slot), kTmem);
+    tmem_relinquish();
+  }
+  after_previous();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)slot;
+
+  uint32_t ph_full = 0, ph_xp = 0, ph_z = 0;   // parities of the next waits
+  auto wait = [&](uint32_t bar, uint32_t& ph, int i, int where) {
+    wait_bar(bar + 8 * i, ph >> i & 1u, abort_flag, status, where);
+    ph ^= 1u << i;
+    __syncwarp();
+  };
+  auto load = [&](int t) {   // by one thread
+    const int b = buffer_of(t);
+    mbar_expect_tx(b_full + 8 * b, kTile);
+    tma_load_3d(base + b * kTile, &tx, b_full + 8 * b, 0, (int)tile_row(t), 0);
+  };
+  // X P of a tile, by one thread
+  auto issue_xp = [&](int t) {
+    constexpr uint32_t wide = idesc_fp16(128, 128, false, false), narrow = idesc_fp16(128, 64, false, false);
+    const uint64_t x = sdesc(base + buffer_of(t) * kTile, 16, 1024, SWZ_128B), P = sdesc(sP, 16, 1024, SWZ_128B);
+    const uint32_t d = tmem + kColD + (t & 1) * 128;
+    fence_after();
+#pragma unroll
+    for (int q = 0; q < kSide / 16; ++q) mma_ss(d, x + (q * 32 >> 4), P + (q * 32 >> 4), wide, q > 0);
+#pragma unroll
+    for (int q = 0; q < kSide / 16; ++q) mma_ss(d + 64, x + ((kPiece + q * 32) >> 4), P + (q * 32 >> 4), narrow, 1);
+    commit(b_xp + 8 * (t & 1));
+  };
+  // X^T X of a tile
+  auto issue_z = [&](int t) {
+    constexpr uint32_t idesc = idesc_fp16(128, 64, true, true);
+    const uint64_t x = sdesc(base + buffer_of(t) * kTile, kPiece, 1024, SWZ_128B);
+    const uint32_t d = tmem + kColZ + (t & 1) * 64;
+    fence_after();
+#pragma unroll
+    for (int q = 0; q < kRows / 16; ++q) mma_ss(d, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
+    commit(b_z + 8 * (t & 1));
+  };
+  float z[32];   // this thread's part of [hi^T hi; lo^T hi]: its row, 32 columns
+  auto add_z = [&](int t) {
+    wait(b_z, ph_z, t & 1, 3);
+    fence_after();
+    uint32_t v[32];
+    tmem_ld32(tmem + lanes + kColZ + (t & 1) * 64 + half * 32, v);
+    tmem_wait_ld(v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] += __uint_as_float(v[i]);
+    fence_before();
+  };
+  // Z = top / 2 + bottom of 128 x 64 values, a row and 32 columns of a thread
+  auto fold = [&](const float (&v)[32]) {
+    if (quad < 2)
+#pragma unroll
+      for (int i = 0; i < 32; ++i) Z[row * kZ + half * 32 + i] = 0.5f * v[i];
+    __syncthreads();
+    if (quad >= 2)
+#pragma unroll
+      for (int i = 0; i < 32; ++i) Z[(row - 64) * kZ + half * 32 + i] += v[i];
+    __syncthreads();
+  };
+
+  // the first Z
+#pragma unroll
+  for (int i = 0; i < 32; ++i) z[i] = 0.f;
+  if (tid == 0)
+    for (int t = 0; t < min(T, kBuffers); ++t) load(t);
+#pragma unroll 1
+  for (int t = 0; t < T; ++t) {
+    wait(b_full, ph_full, buffer_of(t), 1);
+    if (tid == 0) issue_z(t);
+    add_z(t);
+    __syncthreads();
+    if (tid == 0 && t >= kept && t + kBuffers - kKept < T) load(t + kBuffers - kKept);
+  }
+
+  int barriers = 0;
+#pragma unroll 1
+  for (int step = 0; step < p.steps; ++step) {
+    const bool last = step + 1 == p.steps;
+    // Z of all CTAs
+    fold(z);
+    if (G > 1) {
+      float* mine = p.part + (size_t)blockIdx.x * kSide * kSide;
+#pragma unroll
+      for (int i = 0; i < kSide * kSide / kThreads; ++i) {
+        const int e = i * kThreads + tid;
+        __stcg(mine + e, Z[(e / kSide) * kZ + e % kSide]);
+      }
+      grid_barrier(p.ints + kBarrier, ++barriers * G, abort_flag, status);
+      // 32 elements of the sum at a time: eight warps take every eighth part each, in order
+      for (int e0 = blockIdx.x * 32; e0 < kSide * kSide; e0 += G * 32) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int q = warp; q < G; q += 8) s += __ldcg(p.part + (size_t)q * kSide * kSide + e0 + lane);
+        Z[warp * 32 + lane] = s;
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+          for (int q = 1; q < 8; ++q) s += Z[q * 32 + lane];
+          __stcg(p.sum + e0 + lane, s);
+        }
+        __syncthreads();
+      }
+      grid_barrier(p.ints + kBarrier, ++barriers * G, abort_flag, status);
+#pragma unroll
+      for (int i = 0; i < kSide * kSide / kThreads; ++i) {
+        const int e = i * kThreads + tid;
+        Z[(e / kSide) * kZ + e % kSide] = __ldcg(p.sum + e);
+      }
+      __syncthreads();
+    }
+    // A in pieces, [hi; lo]; a thread has 16 columns of a row
+    const int i = tid >> 2, j0 = (tid & 3) * 16, t0 = shift[step], t1 = shift[step + 1];
+    auto put_square = [&](uint32_t at, const float (&v)[16]) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint4 h, l;
+        split2(v[8 * q], v[8 * q + 1], h.x, l.x);
+        split2(v[8 * q + 2], v[8 * q + 3], h.y, l.y);
+        split2(v[8 * q + 4], v[8 * q + 5], h.z, l.z);
+        split2(v[8 * q + 6], v[8 * q + 7], h.w, l.w);
+        char* to = smem + (at - base) + vector_at(i, (tid & 3) * 2 + q);
+        *(uint4*)to = h;
+        *(uint4*)(to + kSquare / 2) = l;
+      }
+    };
+    float A[16];
+    const float to_a = ldexpf(1.f / kUnit, -2 * t0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) A[e] = to_a * (Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i]);
+    put_square(sA, A);
+    fence_async();
+    fence_before();
+    __syncthreads();
+    if (tid == 0) {
+      constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
+      const uint64_t a = sdesc(sA, 16, 1024, SWZ_128B);
+      fence_after();
+#pragma unroll
+      for (int q = 0; q < kSide / 16; ++q) mma_ss(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
+      commit(b_xp);
+    }
+    wait(b_xp, ph_xp, 0, 2);
+    fence_after();
+    {
+      uint32_t v[32];
+      tmem_ld32(tmem + lanes + kColD + half * 32, v);
+      tmem_wait_ld(v);
+      fence_before();
+#pragma unroll
+      for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]);
+    }
+    fold(z);
+    // P = a I + b A + c A A
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float aa = Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i];
+      A[e] = fmaf(p.b, A[e], p.c / kUnit * aa) + (i == j0 + e ? p.a * kUnit : 0.f);
+    }
+    put_square(sP, A);
+    fence_async();
+    __syncthreads();
+
+    // X <- X P and its Z
+    const float to_x = last ? ldexpf(1.f / (kUnit * kUnit), -t0) : ldexpf(1.f / kUnit, t1 - t0);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) z[e] = 0.f;
+    if (T > kBuffers && tid == 0)
+      for (int t = kept; t < kBuffers; ++t) load(t);
+    if (tid == 0) issue_xp(0);
+#pragma unroll 1
+    for (int t = 0; t < T; ++t) {
+      if (t + 1 < T) {
+        if (t + 1 >= kept) wait(b_full, ph_full, buffer_of(t + 1), 1);
+        if (tid == 0) issue_xp(t + 1);
+      }
+      wait(b_xp, ph_xp, t & 1, 2);
+      fence_after();
+      float y[32];
+      {
+        uint32_t v[32], w[32];
+        tmem_ld32(tmem + lanes + kColD + (t & 1) * 128 + half * 32, v);
+        tmem_ld32(tmem + lanes + kColD + (t & 1) * 128 + 64 + half * 32, w);
+        tmem_wait_ld(v);
+        tmem_wait_ld(w);
+        fence_before();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) y[e] = to_x * (__uint_as_float(v[e]) + __uint_as_float(w[e]));
+      }
+      char* tile = smem + buffer_of(t) * kTile;
+      const int64_t m0 = tile_row(t);
+      if (!last) {   // in its place: the product that read it has ended
+        __half* back = p.x.hi + (m0 + row) * p.x.ld + half * 32;
+        const bool away = t >= kept && m0 + row < p.M;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint4 h, l;
+          split2(y[8 * q], y[8 * q + 1], h.x, l.x);
+          split2(y[8 * q + 2], y[8 * q + 3], h.y, l.y);
+          split2(y[8 * q + 4], y[8 * q + 5], h.z, l.z);
+          split2(y[8 * q + 6], y[8 * q + 7], h.w, l.w);
+          char* to = tile + vector_at(row, half * 4 + q);
+          *(uint4*)to = h;
+          *(uint4*)(to + kPiece) = l;
+          if (away) {
+            *(uint4*)(back + q * 8) = h;
+            *(uint4*)(back + p.x.plane() + q * 8) = l;
+          }
+        }
+        fence_async();
+        __syncthreads();
+        if (tid == 0) issue_z(t);
+        if (t > 0) add_z(t - 1);
+      } else {
+        float* stage = (float*)tile;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) stage[row * kSide + ((half * 32 + e) ^ (row & 31))] = y[e];
+        __syncthreads();
+        const float fill = *abort_flag ? NAN : 0.f;   // the result of a wait that ran out shows
+        if (p.j.out.dtype == NMD_DT_FP32) put_tile<float>(p, stage, m0, fill);
+        else if (p.j.out.dtype == NMD_DT_BF16) put_tile<bf16>(p, stage, m0, fill);
+        else put_tile<__half>(p, stage, m0, fill);
+        fence_async();
+      }
+      // the tile before this one is done with: the one after the next goes to its buffer
+      if (t > kept && t + 2 < T) {
+        __syncthreads();
+        if (tid == 0) load(t + 2);
+      }
+    }
+    if (!last) add_z(T - 1);
+    fence_before();
+    __syncthreads();
+  }
+  fence_after();
+  if (warp == 0) tmem_dealloc(tmem, kTmem);
+}
+
+int grid_of(int64_t tiles) {   // the fewest CTAs with the fewest tiles each
+  const int64_t each = (tiles + kSms - 1) / kSms;
+  return (int)((tiles + each - 1) / each);
+}
+
+}  // namespace
+
+size_t strip_bytes(int64_t M) {
+  const int G = grid_of((M + kRows - 1) / kRows);
+  return G > 1 ? (size_t)(G + 1) * kSide * kSide * 4 : 0;
+}
+
+nmd_status strip_run(const Job& j, const Pieces& X, int steps, const double* k, int* ints, void* ws, cudaStream_t s) {
+  static std::atomic<int> ready[kMaxDevices];
+  if (!per_device(ready, [] {
+        return cudaFuncSetAttribute(strip_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) == cudaSuccess;
+      }))
+    return NMD_ERR_CUDA;
+  Strip p{};
+  p.j = j;
+  p.x = X;
+  p.M = X.rows;
+  p.turned = j.R <= j.C;
+  p.tiles = (int)((X.rows + kRows - 1) / kRows);
+  p.steps = steps;
+  p.a = (float)k[0];
+  p.b = (float)k[1];
+  p.c = (float)k[2];
+  p.ints = ints;
+  const int G = grid_of(p.tiles);
+  p.part = (float*)ws;
+  p.sum = p.part + (size_t)G * kSide * kSide;
+  CUtensorMap tx;
+  if (!map_of(X, kRows, &tx)) return NMD_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  if (G > 1) {   // its CTAs wait for one another
+    attr.id = cudaLaunchAttributeCooperative;
+    attr.val.cooperative = 1;
+  } else {
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.gridDim = dim3((unsigned)G);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, strip_kernel, tx, p) == cudaSuccess ? NMD_OK : NMD_ERR_CUDA;
+}
+
+}  // namespace muon
+}  // namespace nmd
