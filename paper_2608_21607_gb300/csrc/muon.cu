@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, in
   __shared__ double red[kThreads / 32];
   ready_for_next();
   after_previous();   // the kernels of an earlier call have done with the workspace
-  if (blockIdx.x == 0 && threadIdx.x < kShift) status[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < kInts) status[threadIdx.x] = 0;
   double sum = 0.0;
   const Walk w = walk_of(j.R, j.C);
   for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
@@ -724,14 +724,14 @@ Layout layout_of(int64_t R, int64_t C) {
   l.r = std::min(R, C);
   l.ldr = (l.r + 63) / 64 * 64;
   const GramPlan g = gram_plan(l.r, std::max(R, C));
-  l.strip = l.r <= kStripSide;
+  l.strip = l.r <= kStripSide && std::max(R, C) <= kStripMost;
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
     at += align256(n);
     return here;
   };
-  l.status = take(256);
+  l.status = take(kInts * sizeof(int));
   l.parts = take(kParts * sizeof(double));
   if (l.strip) {
     l.X[0] = take((size_t)std::max(R, C) * 64 * 4);

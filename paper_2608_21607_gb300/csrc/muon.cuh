@@ -76,13 +76,14 @@ inline bool map_of(const Pieces& x, int rows, CUtensorMap* m) {
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// ints at the start of a call's workspace: status, its detail, a barrier's count, and
-// the shift t of X before each step and after the last
-constexpr int kBarrier = 2, kShift = 4;
+// ints at the start of a call's workspace: status and its detail, the shift t of X before
+// each step and after the last, and on lines of their own a barrier's count and its flag
+constexpr int kShift = 4, kBarrier = 32, kFlag = 64, kInts = 96;
 
-// Updates of at most 64 rows or columns: all steps in one kernel (muon_strip.cu).  X
-// comes in pieces, a row per row of the long side and 64 columns.  `ws`: strip_bytes.
-constexpr int64_t kStripSide = 64;
+// Updates with a short side of at most 64, and a long one that fits on chip: all steps in
+// one kernel (muon_strip.cu).  X comes in pieces, a row per row of the long side and 64
+// columns.  `ws`: strip_bytes.
+constexpr int64_t kStripSide = 64, kStripMost = 152 * 8 * 128;
 size_t strip_bytes(int64_t M);
 nmd_status strip_run(const Job& j, const Pieces& X, int steps, const double* k, int* ints, void* ws, cudaStream_t s);
 

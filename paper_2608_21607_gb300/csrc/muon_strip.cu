@@ -1,9 +1,10 @@
 // All Newton-Schulz steps of an update with a short side of at most 64 in one kernel
 // (mathematics, pieces and scales: muon.cu).
 //
-// X is M x 64, M the long side, in tiles of 128 rows; a CTA per SM holds its tiles in
-// shared memory from the first step to the last (five of them; of more it keeps two and
-// passes the others through three buffers).  A step is one pass over them,
+// X is M x 64, M the long side, in tiles of 128 rows; a CTA per SM holds its tiles on
+// chip from the first step to the last: up to six in shared memory, or five there and up
+// to three in TMEM, which pass through the sixth buffer on their way into Z.  A step is
+// one pass over them,
 //   X <- X P  (128 x 64 by 64 x 64),  Z += X^T X,
 // and between passes the CTAs' sums Z are added up and every CTA forms
 //   A = Z,  P = a I + b A + c A A
@@ -31,19 +32,20 @@ using namespace tc;
 
 constexpr int kThreads = 256, kSms = 152;
 constexpr int kRows = 128, kSide = 64;
-constexpr int kBuffers = 5, kKept = 2;                      // tiles in shared memory; kept of more than that
+constexpr int kBuffers = 6;                                 // tiles in shared memory
 constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
 constexpr int kSquare = 2 * kSide * kSide * 2;              // both pieces of a 64 x 64 matrix
 constexpr int kZ = kSide + 1;                               // row stride of Z in shared memory
-constexpr size_t kOffP = (size_t)kBuffers * kTile, kOffA = kOffP + kSquare, kOffZ = kOffA + kSquare,
+constexpr size_t kOffP = (size_t)kBuffers * kTile, kOffZ = kOffP + kSquare,
                  kOffBars = kOffZ + (kSide * kZ * 4 + 255) / 256 * 256;
 constexpr size_t kSmem = 1024 + kOffBars + 128;
-static_assert(kSmem <= 227 * 1024, "shared memory");
-constexpr uint32_t kColD = 0, kColZ = 256, kTmem = 512;     // two X P, two Z
+static_assert(kSmem <= 227 * 1024 && kSms % 8 == 0, "shared memory");
+// TMEM: two X P, Z, tiles (32 columns of hi, 32 of lo each)
+constexpr uint32_t kColD = 0, kColZ = 256, kColX = 320, kTmem = 512;
 
 struct Strip {
   Job j;
-  Pieces x;            // X; tiles that are not kept go back there
+  Pieces x;            // X to start with
   int64_t M;
   int turned;          // the result's columns are X's rows
   int tiles, steps;
@@ -59,24 +61,27 @@ __device__ __forceinline__ uint32_t vector_at(int m, int q) { return (uint32_t)(
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
 // All CTAs' writes before are seen by all after.  `target`: arrivals of all barriers up to
-// this one.  A wait that runs out (2 s) raises the abort flag; the kernel then goes on
+// this one; the CTA that comes last raises the flag that the others look at, apart from
+// the count.  A wait that runs out (2 s) raises the abort flag; the kernel then goes on
 // without waiting and its result is NaN.
-__device__ __forceinline__ void grid_barrier(int* count, int target, volatile int* abort_flag, int* status) {
+__device__ __forceinline__ void grid_barrier(int* ints, int target, volatile int* abort_flag, int* status) {
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    atomicAdd(count, 1);
-    const uint64_t t0 = globaltimer_ns();
-    for (;;) {
-      int n;
-      asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(n) : "l"(count) : "memory");
-      if (n >= target || *abort_flag) break;
-      if (globaltimer_ns() - t0 > kTimeoutNs) {
-        *abort_flag = 1;
-        record(status, NMD_ERR_TIMEOUT, 10);
+    int n;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(ints + kBarrier) : "memory");
+    if (n + 1 == target) {
+      asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(ints + kFlag), "r"(target) : "memory");
+    } else {
+      const uint64_t t0 = globaltimer_ns();
+      for (;;) {
+        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(n) : "l"(ints + kFlag) : "memory");
+        if (n >= target || *abort_flag) break;
+        if (globaltimer_ns() - t0 > kTimeoutNs) {
+          *abort_flag = 1;
+          record(status, NMD_ERR_TIMEOUT, 10);
+        }
       }
     }
-    __threadfence();
   }
   __syncthreads();
 }
@@ -112,9 +117,9 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   extern __shared__ char smem_raw[];
   char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float* Z = (float*)(smem + kOffZ);
-  const uint32_t base = smem_u32(smem), sP = base + kOffP, sA = base + kOffA, bars = base + kOffBars;
+  const uint32_t base = smem_u32(smem), sP = base + kOffP, bars = base + kOffBars;
   const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16;
-  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 4));
+  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 3));
   volatile int* abort_flag = (volatile int*)(slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;     // TMEM lanes and columns of this warp
@@ -122,13 +127,17 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   const uint32_t lanes = (uint32_t)(quad * 32) << 16;
   int* status = p.ints;
   const int* shift = p.ints + kShift;
-  const int G = gridDim.x, T = (p.tiles - (int)blockIdx.x + G - 1) / G, kept = T <= kBuffers ? T : kKept;
+  const int G = gridDim.x, T = (p.tiles - (int)blockIdx.x + G - 1) / G;
   auto tile_row = [&](int t) { return ((int64_t)blockIdx.x + (int64_t)t * G) * kRows; };
-  auto buffer_of = [&](int t) { return t < kept ? t : kKept + (t - kept) % (kBuffers - kKept); };
+  // Of more than six tiles the second, fourth and sixth lie in TMEM, so that one in shared
+  // memory comes between two that need the sixth buffer.
+  const int away = max(0, T - kBuffers + (T > kBuffers ? 1 : 0));
+  auto place_of = [&](int t) { return (t & 1) && t / 2 < away ? t / 2 : -1; };   // in TMEM
+  auto buffer_of = [&](int t) { return place_of(t) >= 0 ? kBuffers - 1 : t - min(t / 2 + (t & 1), away); };
 
   if (tid == 0) {
     prefetch_tmap(&tx);
-    for (int i = 0; i < kBuffers + 4; ++i) mbar_init(bars + 8 * i, 1);
+    for (int i = 0; i < kBuffers + 3; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
     *abort_flag = 0;
   }
@@ -156,31 +165,39 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   // X P of a tile, by one thread
   auto issue_xp = [&](int t) {
     constexpr uint32_t wide = idesc_fp16(128, 128, false, false), narrow = idesc_fp16(128, 64, false, false);
-    const uint64_t x = sdesc(base + buffer_of(t) * kTile, 16, 1024, SWZ_128B), P = sdesc(sP, 16, 1024, SWZ_128B);
+    const uint64_t P = sdesc(sP, 16, 1024, SWZ_128B);
     const uint32_t d = tmem + kColD + (t & 1) * 128;
     fence_after();
+    if (place_of(t) >= 0) {
+      const uint32_t x = tmem + kColX + place_of(t) * 64;
 #pragma unroll
-    for (int q = 0; q < kSide / 16; ++q) mma_ss(d, x + (q * 32 >> 4), P + (q * 32 >> 4), wide, q > 0);
+      for (int q = 0; q < kSide / 16; ++q) mma_ts(d, x + q * 8, P + (q * 32 >> 4), wide, q > 0);
 #pragma unroll
-    for (int q = 0; q < kSide / 16; ++q) mma_ss(d + 64, x + ((kPiece + q * 32) >> 4), P + (q * 32 >> 4), narrow, 1);
+      for (int q = 0; q < kSide / 16; ++q) mma_ts(d + 64, x + 32 + q * 8, P + (q * 32 >> 4), narrow, 1);
+    } else {
+      const uint64_t x = sdesc(base + buffer_of(t) * kTile, 16, 1024, SWZ_128B);
+#pragma unroll
+      for (int q = 0; q < kSide / 16; ++q) mma_ss(d, x + (q * 32 >> 4), P + (q * 32 >> 4), wide, q > 0);
+#pragma unroll
+      for (int q = 0; q < kSide / 16; ++q) mma_ss(d + 64, x + ((kPiece + q * 32) >> 4), P + (q * 32 >> 4), narrow, 1);
+    }
     commit(b_xp + 8 * (t & 1));
   };
   // X^T X of a tile
   auto issue_z = [&](int t) {
     constexpr uint32_t idesc = idesc_fp16(128, 64, true, true);
     const uint64_t x = sdesc(base + buffer_of(t) * kTile, kPiece, 1024, SWZ_128B);
-    const uint32_t d = tmem + kColZ + (t & 1) * 64;
     fence_after();
 #pragma unroll
-    for (int q = 0; q < kRows / 16; ++q) mma_ss(d, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
-    commit(b_z + 8 * (t & 1));
+    for (int q = 0; q < kRows / 16; ++q) mma_ss(tmem + kColZ, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
+    commit(b_z);
   };
   float z[32];   // this thread's part of [hi^T hi; lo^T hi]: its row, 32 columns
-  auto add_z = [&](int t) {
-    wait(b_z, ph_z, t & 1, 3);
+  auto add_z = [&] {   // of the last tile that went into it
+    wait(b_z, ph_z, 0, 3);
     fence_after();
     uint32_t v[32];
-    tmem_ld32(tmem + lanes + kColZ + (t & 1) * 64 + half * 32, v);
+    tmem_ld32(tmem + lanes + kColZ + half * 32, v);
     tmem_wait_ld(v);
 #pragma unroll
     for (int i = 0; i < 32; ++i) z[i] += __uint_as_float(v[i]);
@@ -192,24 +209,47 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
 #pragma unroll
       for (int i = 0; i < 32; ++i) Z[row * kZ + half * 32 + i] = 0.5f * v[i];
     __syncthreads();
-    if (quad >= 2)
+    if (quad >= 2) {
+      float u[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) Z[(row - 64) * kZ + half * 32 + i] += v[i];
+      for (int i = 0; i < 32; ++i) u[i] = Z[(row - 64) * kZ + half * 32 + i];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) Z[(row - 64) * kZ + half * 32 + i] = u[i] + v[i];
+    }
     __syncthreads();
+  };
+  // a tile's row of this thread into TMEM, as the tensor cores take it
+  auto keep = [&](int t, const uint4 (&h)[4], const uint4 (&l)[4]) {
+    const uint32_t at = tmem + lanes + kColX + place_of(t) * 64 + half * 16;
+    tmem_st16(at, (const uint32_t(&)[16])h);
+    tmem_st16(at + 32, (const uint32_t(&)[16])l);
+    tmem_wait_st();
   };
 
   // the first Z
 #pragma unroll
   for (int i = 0; i < 32; ++i) z[i] = 0.f;
   if (tid == 0)
-    for (int t = 0; t < min(T, kBuffers); ++t) load(t);
+    for (int t = 0; t < T; ++t)
+      if (place_of(t) <= 0) load(t);
 #pragma unroll 1
   for (int t = 0; t < T; ++t) {
     wait(b_full, ph_full, buffer_of(t), 1);
     if (tid == 0) issue_z(t);
-    add_z(t);
+    if (place_of(t) >= 0) {
+      const char* tile = smem + buffer_of(t) * kTile;
+      uint4 h[4], l[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        h[q] = *(const uint4*)(tile + vector_at(row, half * 4 + q));
+        l[q] = *(const uint4*)(tile + kPiece + vector_at(row, half * 4 + q));
+      }
+      __syncwarp();
+      keep(t, h, l);
+    }
+    add_z();
     __syncthreads();
-    if (tid == 0 && t >= kept && t + kBuffers - kKept < T) load(t + kBuffers - kKept);
+    if (tid == 0 && place_of(t) >= 0 && t + 2 < T && place_of(t + 2) >= 0) load(t + 2);
   }
 
   int barriers = 0;
@@ -225,12 +265,15 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         const int e = i * kThreads + tid;
         __stcg(mine + e, Z[(e / kSide) * kZ + e % kSide]);
       }
-      grid_barrier(p.ints + kBarrier, ++barriers * G, abort_flag, status);
+      grid_barrier(p.ints, ++barriers * G, abort_flag, status);
       // 32 elements of the sum at a time: eight warps take every eighth part each, in order
       for (int e0 = blockIdx.x * 32; e0 < kSide * kSide; e0 += G * 32) {
-        float s = 0.f;
-#pragma unroll 8
-        for (int q = warp; q < G; q += 8) s += __ldcg(p.part + (size_t)q * kSide * kSide + e0 + lane);
+        float v[kSms / 8], s = 0.f;   // all loads under way together
+#pragma unroll
+        for (int q = 0; q < kSms / 8; ++q)
+          v[q] = warp + 8 * q < G ? __ldcg(p.part + (size_t)(warp + 8 * q) * kSide * kSide + e0 + lane) : 0.f;
+#pragma unroll
+        for (int q = 0; q < kSms / 8; ++q) s += v[q];
         Z[warp * 32 + lane] = s;
         __syncthreads();
         if (warp == 0) {
@@ -240,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         }
         __syncthreads();
       }
-      grid_barrier(p.ints + kBarrier, ++barriers * G, abort_flag, status);
+      grid_barrier(p.ints, ++barriers * G, abort_flag, status);
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) {
         const int e = i * kThreads + tid;
@@ -250,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     }
     // A in pieces, [hi; lo]; a thread has 16 columns of a row
     const int i = tid >> 2, j0 = (tid & 3) * 16, t0 = shift[step], t1 = shift[step + 1];
-    auto put_square = [&](uint32_t at, const float (&v)[16]) {
+    auto put_square = [&](const float (&v)[16]) {   // A, and later P, side by side in the same place
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         uint4 h, l;
@@ -258,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         split2(v[8 * q + 2], v[8 * q + 3], h.y, l.y);
         split2(v[8 * q + 4], v[8 * q + 5], h.z, l.z);
         split2(v[8 * q + 6], v[8 * q + 7], h.w, l.w);
-        char* to = smem + (at - base) + vector_at(i, (tid & 3) * 2 + q);
+        char* to = smem + kOffP + vector_at(i, (tid & 3) * 2 + q);
         *(uint4*)to = h;
         *(uint4*)(to + kSquare / 2) = l;
       }
@@ -267,13 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     const float to_a = ldexpf(1.f / kUnit, -2 * t0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) A[e] = to_a * (Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i]);
-    put_square(sA, A);
+    put_square(A);
     fence_async();
     fence_before();
     __syncthreads();
     if (tid == 0) {
       constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
-      const uint64_t a = sdesc(sA, 16, 1024, SWZ_128B);
+      const uint64_t a = sdesc(sP, 16, 1024, SWZ_128B);
       fence_after();
 #pragma unroll
       for (int q = 0; q < kSide / 16; ++q) mma_ss(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
@@ -296,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
       const float aa = Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i];
       A[e] = fmaf(p.b, A[e], p.c / kUnit * aa) + (i == j0 + e ? p.a * kUnit : 0.f);
     }
-    put_square(sP, A);
+    put_square(A);
     fence_async();
     __syncthreads();
 
@@ -304,15 +347,10 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     const float to_x = last ? ldexpf(1.f / (kUnit * kUnit), -t0) : ldexpf(1.f / kUnit, t1 - t0);
 #pragma unroll
     for (int e = 0; e < 32; ++e) z[e] = 0.f;
-    if (T > kBuffers && tid == 0)
-      for (int t = kept; t < kBuffers; ++t) load(t);
     if (tid == 0) issue_xp(0);
 #pragma unroll 1
     for (int t = 0; t < T; ++t) {
-      if (t + 1 < T) {
-        if (t + 1 >= kept) wait(b_full, ph_full, buffer_of(t + 1), 1);
-        if (tid == 0) issue_xp(t + 1);
-      }
+      if (t + 1 < T && tid == 0) issue_xp(t + 1);
       wait(b_xp, ph_xp, t & 1, 2);
       fence_after();
       float y[32];
@@ -329,27 +367,23 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
       char* tile = smem + buffer_of(t) * kTile;
       const int64_t m0 = tile_row(t);
       if (!last) {   // in its place: the product that read it has ended
-        __half* back = p.x.hi + (m0 + row) * p.x.ld + half * 32;
-        const bool away = t >= kept && m0 + row < p.M;
+        uint4 h[4], l[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint4 h, l;
-          split2(y[8 * q], y[8 * q + 1], h.x, l.x);
-          split2(y[8 * q + 2], y[8 * q + 3], h.y, l.y);
-          split2(y[8 * q + 4], y[8 * q + 5], h.z, l.z);
-          split2(y[8 * q + 6], y[8 * q + 7], h.w, l.w);
+          split2(y[8 * q], y[8 * q + 1], h[q].x, l[q].x);
+          split2(y[8 * q + 2], y[8 * q + 3], h[q].y, l[q].y);
+          split2(y[8 * q + 4], y[8 * q + 5], h[q].z, l[q].z);
+          split2(y[8 * q + 6], y[8 * q + 7], h[q].w, l[q].w);
           char* to = tile + vector_at(row, half * 4 + q);
-          *(uint4*)to = h;
-          *(uint4*)(to + kPiece) = l;
-          if (away) {
-            *(uint4*)(back + q * 8) = h;
-            *(uint4*)(back + p.x.plane() + q * 8) = l;
-          }
+          *(uint4*)to = h[q];
+          *(uint4*)(to + kPiece) = l[q];
         }
+        if (place_of(t) >= 0) keep(t, h, l);
+        if (t > 0) add_z();
         fence_async();
+        fence_before();
         __syncthreads();
         if (tid == 0) issue_z(t);
-        if (t > 0) add_z(t - 1);
       } else {
         float* stage = (float*)tile;
 #pragma unroll
@@ -359,15 +393,9 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         if (p.j.out.dtype == NMD_DT_FP32) put_tile<float>(p, stage, m0, fill);
         else if (p.j.out.dtype == NMD_DT_BF16) put_tile<bf16>(p, stage, m0, fill);
         else put_tile<__half>(p, stage, m0, fill);
-        fence_async();
-      }
-      // the tile before this one is done with: the one after the next goes to its buffer
-      if (t > kept && t + 2 < T) {
-        __syncthreads();
-        if (tid == 0) load(t + 2);
       }
     }
-    if (!last) add_z(T - 1);
+    if (!last) add_z();
     fence_before();
     __syncthreads();
   }

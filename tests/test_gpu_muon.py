@@ -332,3 +332,10 @@ def test_refusals():
                dict(lr=0.1, weight_decay=-1.0), dict(lr=0.1, scale=float("inf")), dict(lr=0.1, steps=0), dict(lr=0.1, eps=0.0)):
         refused(t.muon_step, W, G, M, **kw)
     assert torch.equal(W, x) and torch.equal(M, x) and (flat == 1).all()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(100000, 64, "fp32"), (64, 130000, "fp32"), (117000, 33, "bf16"), (155648, 17, "fp32"),
+                                             (155649, 17, "fp32"), (40, 97281, "fp16"), (58369, 50, "fp32")])
+def test_orthogonalize_tall(rows, cols, dtype):
+    """Long sides at which the tiles of a CTA no longer fit shared memory, or no longer fit on chip."""
+    check(place(gradient(rows, cols, 9), dtype))
