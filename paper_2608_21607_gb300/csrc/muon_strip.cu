@@ -35,9 +35,12 @@ constexpr int kRows = 128, kSide = 64;
 constexpr int kBuffers = 6;                                 // tiles in shared memory
 constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
 constexpr int kSquare = 2 * kSide * kSide * 2;              // both pieces of a 64 x 64 matrix
-constexpr int kZ = kSide + 1;                               // row stride of Z in shared memory
+// Z in shared memory: two halves of 32 columns, so placed that eight rows by columns 16
+// apart, and the same transposed, lie in 32 banks
+constexpr int kZ = 4248;
+__device__ __forceinline__ int z_at(int i, int j) { return (j >> 5) * 2120 + i * 33 + (i >> 5) * 8 + (j & 31); }
 constexpr size_t kOffP = (size_t)kBuffers * kTile, kOffZ = kOffP + kSquare,
-                 kOffBars = kOffZ + (kSide * kZ * 4 + 255) / 256 * 256;
+                 kOffBars = kOffZ + (kZ * 4 + 255) / 256 * 256;
 constexpr size_t kSmem = 1024 + kOffBars + 128;
 static_assert(kSmem <= 227 * 1024 && kSms % 8 == 0, "shared memory");
 // TMEM: two X P, Z, tiles (32 columns of hi, 32 of lo each)
@@ -207,14 +210,14 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   auto fold = [&](const float (&v)[32]) {
     if (quad < 2)
 #pragma unroll
-      for (int i = 0; i < 32; ++i) Z[row * kZ + half * 32 + i] = 0.5f * v[i];
+      for (int i = 0; i < 32; ++i) Z[z_at(row, half * 32 + i)] = 0.5f * v[i];
     __syncthreads();
     if (quad >= 2) {
       float u[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) u[i] = Z[(row - 64) * kZ + half * 32 + i];
+      for (int i = 0; i < 32; ++i) u[i] = Z[z_at(row - 64, half * 32 + i)];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) Z[(row - 64) * kZ + half * 32 + i] = u[i] + v[i];
+      for (int i = 0; i < 32; ++i) Z[z_at(row - 64, half * 32 + i)] = u[i] + v[i];
     }
     __syncthreads();
   };
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) {
         const int e = i * kThreads + tid;
-        __stcg(mine + e, Z[(e / kSide) * kZ + e % kSide]);
+        __stcg(mine + e, Z[z_at(e / kSide, e % kSide)]);
       }
       grid_barrier(p.ints, ++barriers * G, abort_flag, status);
       // 32 elements of the sum at a time: eight warps take every eighth part each, in order
@@ -284,11 +287,11 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         __syncthreads();
       }
       grid_barrier(p.ints, ++barriers * G, abort_flag, status);
+      float v[kSide * kSide / kThreads];
 #pragma unroll
-      for (int i = 0; i < kSide * kSide / kThreads; ++i) {
-        const int e = i * kThreads + tid;
-        Z[(e / kSide) * kZ + e % kSide] = __ldcg(p.sum + e);
-      }
+      for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] = __ldcg(p.sum + i * kThreads + tid);
+#pragma unroll
+      for (int i = 0; i < kSide * kSide / kThreads; ++i) Z[z_at((i * kThreads + tid) / kSide, tid % kSide)] = v[i];
       __syncthreads();
     }
     // A in pieces, [hi; lo]; a thread has 16 columns of a row
@@ -309,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     float A[16];
     const float to_a = ldexpf(1.f / kUnit, -2 * t0);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) A[e] = to_a * (Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i]);
+    for (int e = 0; e < 16; ++e) A[e] = to_a * (Z[z_at(i, j0 + e)] + Z[z_at(j0 + e, i)]);
     put_square(A);
     fence_async();
     fence_before();
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     // P = a I + b A + c A A
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float aa = Z[i * kZ + j0 + e] + Z[(j0 + e) * kZ + i];
+      const float aa = Z[z_at(i, j0 + e)] + Z[z_at(j0 + e, i)];
       A[e] = fmaf(p.b, A[e], p.c / kUnit * aa) + (i == j0 + e ? p.a * kUnit : 0.f);
     }
     put_square(A);
