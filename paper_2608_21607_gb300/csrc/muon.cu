@@ -72,6 +72,67 @@ __device__ __forceinline__ void each(const Walk& w, const Job& j, int64_t at, F 
     if (r0 + i * w.down < j.R && c0 + i * w.step < j.C) f(i, r0 + i * w.down, c0 + i * w.step);
 }
 
+// Matrices whose elements fill memory row by row from a 16-byte boundary are read eight
+// elements at a time, whatever their rows' length: the window from element f on comes out
+// of the vectors that hold it.
+__device__ __forceinline__ void window(const uint32_t* base, int64_t f, int64_t n, uint32_t (&w)[8]) {   // 8 of 32 bits
+  const int s = (int)(f & 3);
+  const uint4* v = (const uint4*)base + (f >> 2);
+  if (f - s + 12 > n) {   // near the end: no vector beyond it
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = f + i < n ? base[f + i] : 0u;
+    return;
+  }
+  const uint4 a = v[0], b = v[1];
+  uint32_t u[11] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, 0u, 0u, 0u};
+  if (s != 0) {
+    const uint4 c = v[2];
+    u[8] = c.x;
+    u[9] = c.y;
+    u[10] = c.z;
+  }
+#pragma unroll
+  for (int i = 0; i < 9; ++i) u[i] = s & 2 ? u[i + 2] : u[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = s & 1 ? u[i + 1] : u[i];
+}
+__device__ __forceinline__ void window(const uint16_t* base, int64_t f, int64_t n, uint32_t (&w)[4]) {   // 8 of 16 bits
+  const int s = (int)(f & 7);
+  const uint4* v = (const uint4*)base + (f >> 3);
+  if (f - s + 16 > n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (f + 2 * i < n ? base[f + 2 * i] : 0u) | (f + 2 * i + 1 < n ? (uint32_t)base[f + 2 * i + 1] << 16 : 0u);
+    return;
+  }
+  const uint4 a = v[0];
+  uint32_t u[8] = {a.x, a.y, a.z, a.w, 0u, 0u, 0u, 0u};
+  if (s != 0) {
+    const uint4 b = v[1];
+    u[4] = b.x;
+    u[5] = b.y;
+    u[6] = b.z;
+    u[7] = b.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 6; ++i) u[i] = s & 4 ? u[i + 2] : u[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) u[i] = s & 2 ? u[i + 1] : u[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = s & 1 ? __funnelshift_r(u[i], u[i + 1], 16) : u[i];
+}
+template <class T>
+struct Eight {   // elements of a thread
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* base, int64_t f, int64_t n) {
+    if constexpr (sizeof(T) == 4) window((const uint32_t*)base, f, n, w);
+    else window((const uint16_t*)base, f, n, w);
+  }
+  __device__ __forceinline__ float get(int i) const { return as_float(((const T*)w)[i]); }
+  __device__ __forceinline__ void set(int i, float v) { from_float(v, (T*)w + i); }
+};
+__host__ __device__ inline bool filled(const Matrix& m, int64_t C) { return m.cs == 1 && m.rs == C && ((uintptr_t)m.x & 15) == 0; }
+
 // M <- beta M + (1 - beta) G, and the sum of squares of the update
 template <class G, class M, bool STEP>
 __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, int* status) {
@@ -80,8 +141,39 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Job j, double* parts, in
   after_previous();   // the kernels of an earlier call have done with the workspace
   if (blockIdx.x == 0 && threadIdx.x < kInts) status[threadIdx.x] = 0;
   double sum = 0.0;
+  if (j.flat) {
+    const int64_t n = j.R * j.C, vectors = (n + 7) / 8;
+#pragma unroll 2
+    for (int64_t v = blockIdx.x * (int64_t)kThreads + threadIdx.x; v < vectors; v += (int64_t)gridDim.x * kThreads) {
+      Eight<G> g;
+      Eight<M> m;
+      float u[8];
+      g.load((const G*)j.grad.x, v * 8, n);
+      if (STEP) m.load((const M*)j.momentum.x, v * 8, n);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u[i] = g.get(i);
+        if (STEP) {
+          m.set(i, fmaf(j.beta, m.get(i), j.rest * u[i]));
+          u[i] = update_of(j, m.get(i), u[i]);   // of the momentum as it is stored
+        }
+      }
+      if (STEP) {
+        M* to = (M*)j.momentum.x + v * 8;
+        if (v * 8 + 8 <= n) {
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(M) / 2; ++i) ((uint4*)to)[i] = ((const uint4*)m.w)[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (v * 8 + i < n) to[i] = ((const M*)m.w)[i];
+        }
+      }
+      sum += squares(u);   // (what is past the end is 0 in all of them)
+    }
+  }
   const Walk w = walk_of(j.R, j.C);
-  for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
+  for (int64_t at = j.flat ? w.work : blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
     G g[kEach];
     M m[kEach];
     float u[kEach];
@@ -153,6 +245,30 @@ __global__ void __launch_bounds__(kThreads) pieces_kernel(Job j, Pieces X, const
   ready_for_next();
   after_previous();
   const Factor3 f = factor_of(parts, count, j.eps, shift, steps, grows);
+  if (j.flat) {   // by vectors of what is written
+    const int64_t n = j.R * j.C, across = X.ld / 8, vectors = j.R * across;
+#pragma unroll 2
+    for (int64_t v = blockIdx.x * (int64_t)kThreads + threadIdx.x; v < vectors; v += (int64_t)gridDim.x * kThreads) {
+      const int64_t r = vectors >> 31 ? v / across : (int64_t)((uint32_t)v / (uint32_t)across), c = (v - r * across) * 8;
+      if (c >= j.C) continue;
+      Eight<G> g;
+      Eight<M> m;
+      g.load((const G*)j.grad.x, r * j.C + c, n);
+      if (STEP) m.load((const M*)j.momentum.x, r * j.C + c, n);
+      float u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = f.of(STEP ? update_of(j, m.get(i), g.get(i)) : g.get(i));   // (past the row's end: padding)
+      uint4 h, l;
+      split2(u[0], u[1], h.x, l.x);
+      split2(u[2], u[3], h.y, l.y);
+      split2(u[4], u[5], h.z, l.z);
+      split2(u[6], u[7], h.w, l.w);
+      __half* to = X.hi + r * X.ld + c;
+      *(uint4*)to = h;
+      *(uint4*)(to + X.plane()) = l;
+    }
+    return;
+  }
   const Walk w = walk_of(j.R, j.C);
   for (int64_t at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < w.work; at += gridDim.x * (kThreads / 32)) {
     G g[kEach];
@@ -754,7 +870,7 @@ void with_type(int dtype, F f) {
   else f(__half{});
 }
 
-nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t s) {
+nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
   const Layout l = layout_of(j.R, j.C);
   char* w = (char*)ws;
   int* status = (int*)(w + l.status);
@@ -762,11 +878,13 @@ nmd_status run(const Job& j, int steps, const double* k, void* ws, cudaStream_t 
   double* parts = (double*)(w + l.parts);
   Pieces X{(__half*)(w + l.X[0]), j.R, j.C, l.ldx}, Y{(__half*)(w + l.X[1]), j.R, j.C, l.ldx};
   const bool turned = l.strip && j.R <= j.C;
+  j.flat = filled(j.grad, j.C) && (!j.step || filled(j.momentum, j.C));
   if (l.strip) X = Pieces{X.hi, std::max(j.R, j.C), l.r, 64};
   const Pieces A{(__half*)(w + l.A), l.r, l.r, l.ldr}, P{(__half*)(w + l.P), l.r, l.r, l.ldr};
   const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
   const int64_t r = l.r, M = std::max(j.R, j.C);
-  const int grid = (int)std::min<int64_t>((walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
+  const int grid = (int)std::min<int64_t>(j.flat ? (j.R * j.C + 8 * kThreads - 1) / (8 * kThreads)
+                                                 : (walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
   const int grows = (int)std::ceil(std::log2(std::max(1.0, 1.001 * std::fabs(k[0]))));
   nmd_status st = NMD_OK;
   with_type(j.grad.dtype, [&](auto g) {

@@ -40,6 +40,7 @@ struct Job {
   int nesterov;
   float keep, lr;               // 1 - lr weight_decay, lr scale
   double eps;
+  int flat;                     // the update's matrices fill memory row by row, from 16-byte boundaries
 };
 
 // Two fp16 pieces of an R x C matrix: plane 0 hi, plane 1 lo, rows of ld elements
