@@ -30,7 +30,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 256, kSms = 152;
+constexpr int kThreads = 256, kSms = 152;                  // threads that work; one warp more issues the products
 constexpr int kRows = 128, kSide = 64;
 constexpr int kBuffers = 6;                                 // tiles in shared memory
 constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
@@ -61,14 +61,16 @@ struct Strip {
 // the 16-byte vector q (0 .. 7) of row m in a tile's piece
 __device__ __forceinline__ uint32_t vector_at(int m, int q) { return (uint32_t)(m * 128 + ((q ^ (m & 7)) << 4)); }
 
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// the working threads
+__device__ __forceinline__ void sync_workers() { named_bar_sync(1, kThreads); }
 
 // All CTAs' writes before are seen by all after.  `target`: arrivals of all barriers up to
 // this one; the CTA that comes last raises the flag that the others look at, apart from
 // the count.  A wait that runs out (2 s) raises the abort flag; the kernel then goes on
 // without waiting and its result is NaN.
 __device__ __forceinline__ void grid_barrier(int* ints, int target, volatile int* abort_flag, int* status) {
-  __syncthreads();
+  sync_workers();
   if (threadIdx.x == 0) {
     int n;
     asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(ints + kBarrier) : "memory");
@@ -86,7 +88,7 @@ __device__ __forceinline__ void grid_barrier(int* ints, int target, volatile int
       }
     }
   }
-  __syncthreads();
+  sync_workers();
 }
 
 // A tile of the result from its fp32 rows in shared memory ([m][j ^ (m & 31)])
@@ -116,13 +118,13 @@ __device__ __forceinline__ void put_tile(const Strip& p, const float* stage, int
   }
 }
 
-__global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ Strip p) {
+__global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ Strip p) {
   extern __shared__ char smem_raw[];
   char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float* Z = (float*)(smem + kOffZ);
   const uint32_t base = smem_u32(smem), sP = base + kOffP, bars = base + kOffBars;
-  const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16;
-  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 3));
+  const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16, b_done = b_z + 8;
+  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 5));
   volatile int* abort_flag = (volatile int*)(slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;     // TMEM lanes and columns of this warp
@@ -141,6 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   if (tid == 0) {
     prefetch_tmap(&tx);
     for (int i = 0; i < kBuffers + 3; ++i) mbar_init(bars + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(b_done + 8 * i, kThreads / 32);
     fence_mbar_init();
     *abort_flag = 0;
   }
@@ -154,11 +157,10 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   fence_after();
   const uint32_t tmem = *(volatile uint32_t*)slot;
 
-  uint32_t ph_full = 0, ph_xp = 0, ph_z = 0;   // parities of the next waits
+  uint32_t ph_full = 0, ph_xp = 0, ph_z = 0, turn = 0;   // parities of the next waits
   auto wait = [&](uint32_t bar, uint32_t& ph, int i, int where) {
     wait_bar(bar + 8 * i, ph >> i & 1u, abort_flag, status, where);
     ph ^= 1u << i;
-    __syncwarp();
   };
   auto load = [&](int t) {   // by one thread
     const int b = buffer_of(t);
@@ -195,23 +197,74 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
     for (int q = 0; q < kRows / 16; ++q) mma_ss(tmem + kColZ, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
     commit(b_z);
   };
+  if (warp == kThreads / 32) {
+    // ---- one thread issues all loads and products.  The workers say after each of their
+    // pieces of work that they have done with it, on two barriers in turn: the next but one
+    // needs something that is issued after this one.
+    if (lane == 0) {
+      uint32_t n = 0;
+      auto done = [&] {
+        wait_bar(b_done + 8 * (n & 1), n >> 1 & 1u, abort_flag, status, 4);
+        ++n;
+      };
+      for (int t = 0; t < T; ++t)
+        if (place_of(t) <= 0) load(t);
+      for (int t = 0; t < T; ++t) {
+        wait(b_full, ph_full, buffer_of(t), 1);
+        issue_z(t);
+        done();
+        if (place_of(t) >= 0 && t + 2 < T && place_of(t + 2) >= 0) load(t + 2);
+      }
+      for (int step = 0; step < p.steps; ++step) {
+        done();   // A is there
+        constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
+        const uint64_t a = sdesc(sP, 16, 1024, SWZ_128B);
+        fence_after();
+#pragma unroll
+        for (int q = 0; q < kSide / 16; ++q) mma_ss(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
+        commit(b_xp);
+        done();   // P is there
+        issue_xp(0);
+        if (T > 1) issue_xp(1);
+        for (int t = 0; t < T; ++t) {
+          done();
+          if (step + 1 < p.steps) issue_z(t);
+          if (t + 2 < T) issue_xp(t + 2);
+        }
+      }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    return;
+  }
+  auto done = [&] {   // what was written is there for the tensor cores, what was read may be overwritten
+    fence_async();
+    fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(b_done + 8 * (turn & 1));
+    ++turn;
+  };
+  auto wait_warp = [&](uint32_t bar, uint32_t& ph, int i, int where) {
+    wait(bar, ph, i, where);
+    __syncwarp();
+    fence_after();
+  };
   float z[32];   // this thread's part of [hi^T hi; lo^T hi]: its row, 32 columns
   auto add_z = [&] {   // of the last tile that went into it
-    wait(b_z, ph_z, 0, 3);
-    fence_after();
+    wait_warp(b_z, ph_z, 0, 3);
     uint32_t v[32];
     tmem_ld32(tmem + lanes + kColZ + half * 32, v);
     tmem_wait_ld(v);
 #pragma unroll
     for (int i = 0; i < 32; ++i) z[i] += __uint_as_float(v[i]);
-    fence_before();
   };
   // Z = top / 2 + bottom of 128 x 64 values, a row and 32 columns of a thread
   auto fold = [&](const float (&v)[32]) {
     if (quad < 2)
 #pragma unroll
       for (int i = 0; i < 32; ++i) Z[z_at(row, half * 32 + i)] = 0.5f * v[i];
-    __syncthreads();
+    sync_workers();
     if (quad >= 2) {
       float u[32];
 #pragma unroll
@@ -219,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
 #pragma unroll
       for (int i = 0; i < 32; ++i) Z[z_at(row - 64, half * 32 + i)] = u[i] + v[i];
     }
-    __syncthreads();
+    sync_workers();
   };
   // a tile's row of this thread into TMEM, as the tensor cores take it
   auto keep = [&](int t, const uint4 (&h)[4], const uint4 (&l)[4]) {
@@ -232,14 +285,10 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
   // the first Z
 #pragma unroll
   for (int i = 0; i < 32; ++i) z[i] = 0.f;
-  if (tid == 0)
-    for (int t = 0; t < T; ++t)
-      if (place_of(t) <= 0) load(t);
 #pragma unroll 1
   for (int t = 0; t < T; ++t) {
-    wait(b_full, ph_full, buffer_of(t), 1);
-    if (tid == 0) issue_z(t);
     if (place_of(t) >= 0) {
+      wait_warp(b_full, ph_full, buffer_of(t), 1);
       const char* tile = smem + buffer_of(t) * kTile;
       uint4 h[4], l[4];
 #pragma unroll
@@ -247,12 +296,10 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         h[q] = *(const uint4*)(tile + vector_at(row, half * 4 + q));
         l[q] = *(const uint4*)(tile + kPiece + vector_at(row, half * 4 + q));
       }
-      __syncwarp();
       keep(t, h, l);
     }
     add_z();
-    __syncthreads();
-    if (tid == 0 && place_of(t) >= 0 && t + 2 < T && place_of(t + 2) >= 0) load(t + 2);
+    done();
   }
 
   int barriers = 0;
@@ -278,13 +325,13 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
 #pragma unroll
         for (int q = 0; q < kSms / 8; ++q) s += v[q];
         Z[warp * 32 + lane] = s;
-        __syncthreads();
+        sync_workers();
         if (warp == 0) {
 #pragma unroll
           for (int q = 1; q < 8; ++q) s += Z[q * 32 + lane];
           __stcg(p.sum + e0 + lane, s);
         }
-        __syncthreads();
+        sync_workers();
       }
       grid_barrier(p.ints, ++barriers * G, abort_flag, status);
       float v[kSide * kSide / kThreads];
@@ -292,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
       for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] = __ldcg(p.sum + i * kThreads + tid);
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) Z[z_at((i * kThreads + tid) / kSide, tid % kSide)] = v[i];
-      __syncthreads();
+      sync_workers();
     }
     // A in pieces, [hi; lo]; a thread has 16 columns of a row
     const int i = tid >> 2, j0 = (tid & 3) * 16, t0 = shift[step], t1 = shift[step + 1];
@@ -314,24 +361,12 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
 #pragma unroll
     for (int e = 0; e < 16; ++e) A[e] = to_a * (Z[z_at(i, j0 + e)] + Z[z_at(j0 + e, i)]);
     put_square(A);
-    fence_async();
-    fence_before();
-    __syncthreads();
-    if (tid == 0) {
-      constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
-      const uint64_t a = sdesc(sP, 16, 1024, SWZ_128B);
-      fence_after();
-#pragma unroll
-      for (int q = 0; q < kSide / 16; ++q) mma_ss(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
-      commit(b_xp);
-    }
-    wait(b_xp, ph_xp, 0, 2);
-    fence_after();
+    done();
+    wait_warp(b_xp, ph_xp, 0, 2);
     {
       uint32_t v[32];
       tmem_ld32(tmem + lanes + kColD + half * 32, v);
       tmem_wait_ld(v);
-      fence_before();
 #pragma unroll
       for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]);
     }
@@ -343,19 +378,15 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
       A[e] = fmaf(p.b, A[e], p.c / kUnit * aa) + (i == j0 + e ? p.a * kUnit : 0.f);
     }
     put_square(A);
-    fence_async();
-    __syncthreads();
+    done();
 
     // X <- X P and its Z
     const float to_x = last ? ldexpf(1.f / (kUnit * kUnit), -t0) : ldexpf(1.f / kUnit, t1 - t0);
 #pragma unroll
     for (int e = 0; e < 32; ++e) z[e] = 0.f;
-    if (tid == 0) issue_xp(0);
 #pragma unroll 1
     for (int t = 0; t < T; ++t) {
-      if (t + 1 < T && tid == 0) issue_xp(t + 1);
-      wait(b_xp, ph_xp, t & 1, 2);
-      fence_after();
+      wait_warp(b_xp, ph_xp, t & 1, 2);
       float y[32];
       {
         uint32_t v[32], w[32];
@@ -363,7 +394,6 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         tmem_ld32(tmem + lanes + kColD + (t & 1) * 128 + 64 + half * 32, w);
         tmem_wait_ld(v);
         tmem_wait_ld(w);
-        fence_before();
 #pragma unroll
         for (int e = 0; e < 32; ++e) y[e] = to_x * (__uint_as_float(v[e]) + __uint_as_float(w[e]));
       }
@@ -383,26 +413,24 @@ __global__ void __launch_bounds__(kThreads, 1) strip_kernel(const __grid_constan
         }
         if (place_of(t) >= 0) keep(t, h, l);
         if (t > 0) add_z();
-        fence_async();
-        fence_before();
-        __syncthreads();
-        if (tid == 0) issue_z(t);
+        done();
       } else {
         float* stage = (float*)tile;
 #pragma unroll
         for (int e = 0; e < 32; ++e) stage[row * kSide + ((half * 32 + e) ^ (row & 31))] = y[e];
-        __syncthreads();
+        sync_workers();
         const float fill = *abort_flag ? NAN : 0.f;   // the result of a wait that ran out shows
         if (p.j.out.dtype == NMD_DT_FP32) put_tile<float>(p, stage, m0, fill);
         else if (p.j.out.dtype == NMD_DT_BF16) put_tile<bf16>(p, stage, m0, fill);
         else put_tile<__half>(p, stage, m0, fill);
+        done();
       }
     }
     if (!last) add_z();
-    fence_before();
-    __syncthreads();
   }
   fence_after();
+  fence_before();
+  __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, kTmem);
 }
 
@@ -450,7 +478,7 @@ nmd_status strip_run(const Job& j, const Pieces& X, int steps, const double* k, 
     attr.val.programmaticStreamSerializationAllowed = 1;
   }
   cfg.gridDim = dim3((unsigned)G);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kThreads + 32);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
   cfg.attrs = &attr;
