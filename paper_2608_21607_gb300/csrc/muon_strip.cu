@@ -162,12 +162,14 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
     wait_bar(bar + 8 * i, ph >> i & 1u, abort_flag, status, where);
     ph ^= 1u << i;
   };
-  auto load = [&](int t) {   // by one thread
+  // the rest of this block by the converged issuing warp: what is uniform stays in uniform registers
+  auto load = [&](int t) {
+    if (lane != 0) return;
     const int b = buffer_of(t);
     mbar_expect_tx(b_full + 8 * b, kTile);
     tma_load_3d(base + b * kTile, &tx, b_full + 8 * b, 0, (int)tile_row(t), 0);
   };
-  // X P of a tile, by one thread
+  // X P of a tile
   auto issue_xp = [&](int t) {
     constexpr uint32_t wide = idesc_fp16(128, 128, false, false), narrow = idesc_fp16(128, 64, false, false);
     const uint64_t P = sdesc(sP, 16, 1024, SWZ_128B);
@@ -176,17 +178,17 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
     if (place_of(t) >= 0) {
       const uint32_t x = tmem + kColX + place_of(t) * 64;
 #pragma unroll
-      for (int q = 0; q < kSide / 16; ++q) mma_ts(d, x + q * 8, P + (q * 32 >> 4), wide, q > 0);
+      for (int q = 0; q < kSide / 16; ++q) mma_ts_elect(d, x + q * 8, P + (q * 32 >> 4), wide, q > 0);
 #pragma unroll
-      for (int q = 0; q < kSide / 16; ++q) mma_ts(d + 64, x + 32 + q * 8, P + (q * 32 >> 4), narrow, 1);
+      for (int q = 0; q < kSide / 16; ++q) mma_ts_elect(d + 64, x + 32 + q * 8, P + (q * 32 >> 4), narrow, 1);
     } else {
       const uint64_t x = sdesc(base + buffer_of(t) * kTile, 16, 1024, SWZ_128B);
 #pragma unroll
-      for (int q = 0; q < kSide / 16; ++q) mma_ss(d, x + (q * 32 >> 4), P + (q * 32 >> 4), wide, q > 0);
+      for (int q = 0; q < kSide / 16; ++q) mma_ss_elect(d, x + (q * 32 >> 4), P + (q * 32 >> 4), wide, q > 0);
 #pragma unroll
-      for (int q = 0; q < kSide / 16; ++q) mma_ss(d + 64, x + ((kPiece + q * 32) >> 4), P + (q * 32 >> 4), narrow, 1);
+      for (int q = 0; q < kSide / 16; ++q) mma_ss_elect(d + 64, x + ((kPiece + q * 32) >> 4), P + (q * 32 >> 4), narrow, 1);
     }
-    commit(b_xp + 8 * (t & 1));
+    commit_elect(b_xp + 8 * (t & 1));
   };
   // X^T X of a tile
   auto issue_z = [&](int t) {
@@ -194,46 +196,45 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
     const uint64_t x = sdesc(base + buffer_of(t) * kTile, kPiece, 1024, SWZ_128B);
     fence_after();
 #pragma unroll
-    for (int q = 0; q < kRows / 16; ++q) mma_ss(tmem + kColZ, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
-    commit(b_z);
+    for (int q = 0; q < kRows / 16; ++q) mma_ss_elect(tmem + kColZ, x + (q * 16 * 128 >> 4), x + (q * 16 * 128 >> 4), idesc, q > 0);
+    commit_elect(b_z);
   };
   if (warp == kThreads / 32) {
-    // ---- one thread issues all loads and products.  The workers say after each of their
-    // pieces of work that they have done with it, on two barriers in turn: the next but one
-    // needs something that is issued after this one.
-    if (lane == 0) {
-      uint32_t n = 0;
-      auto done = [&] {
-        wait_bar(b_done + 8 * (n & 1), n >> 1 & 1u, abort_flag, status, 4);
-        ++n;
-      };
-      for (int t = 0; t < T; ++t)
-        if (place_of(t) <= 0) load(t);
-      for (int t = 0; t < T; ++t) {
-        wait(b_full, ph_full, buffer_of(t), 1);
-        issue_z(t);
-        done();
-        if (place_of(t) >= 0 && t + 2 < T && place_of(t + 2) >= 0) load(t + 2);
-      }
-      for (int step = 0; step < p.steps; ++step) {
-        done();   // A is there
-        constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
-        const uint64_t a = sdesc(sP, 16, 1024, SWZ_128B);
-        fence_after();
+    // ---- loads and products.  The workers say after each of their pieces of work that they
+    // have done with it, on two barriers in turn: the next but one needs something that is
+    // issued after this one.
+    uint32_t n = 0;
+    auto done = [&] {
+      conv_wait(b_done + 8 * (n & 1), n >> 1 & 1u, abort_flag, status, 4);
+      ++n;
+    };
+    for (int t = 0; t < T; ++t)
+      if (place_of(t) <= 0) load(t);
+    for (int t = 0; t < T; ++t) {
+      const int b = buffer_of(t);
+      conv_wait(b_full + 8 * b, ph_full >> b & 1u, abort_flag, status, 1);
+      ph_full ^= 1u << b;
+      issue_z(t);
+      done();
+      if (place_of(t) >= 0 && t + 2 < T && place_of(t + 2) >= 0) load(t + 2);
+    }
+    for (int step = 0; step < p.steps; ++step) {
+      done();   // A is there
+      constexpr uint32_t idesc = idesc_fp16(128, 64, false, false);
+      const uint64_t a = sdesc(sP, 16, 1024, SWZ_128B);
+      fence_after();
 #pragma unroll
-        for (int q = 0; q < kSide / 16; ++q) mma_ss(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
-        commit(b_xp);
-        done();   // P is there
-        issue_xp(0);
-        if (T > 1) issue_xp(1);
-        for (int t = 0; t < T; ++t) {
-          done();
-          if (step + 1 < p.steps) issue_z(t);
-          if (t + 2 < T) issue_xp(t + 2);
-        }
+      for (int q = 0; q < kSide / 16; ++q) mma_ss_elect(tmem + kColD, a + (q * 32 >> 4), a + (q * 32 >> 4), idesc, q > 0);
+      commit_elect(b_xp);
+      done();   // P is there
+      issue_xp(0);
+      if (T > 1) issue_xp(1);
+      for (int t = 0; t < T; ++t) {
+        done();
+        if (step + 1 < p.steps) issue_z(t);
+        if (t + 2 < T) issue_xp(t + 2);
       }
     }
-    __syncwarp();
     fence_before();
     __syncthreads();
     return;
