@@ -885,6 +885,7 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
   const int64_t r = l.r, M = std::max(j.R, j.C);
   const int grid = (int)std::min<int64_t>(j.flat ? (j.R * j.C + 8 * kThreads - 1) / (8 * kThreads)
                                                  : (walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
+  const int grid_x = (int)std::min<int64_t>((X.rows * X.ld / 8 + kThreads - 1) / kThreads, kParts);
   const int grows = (int)std::ceil(std::log2(std::max(1.0, 1.001 * std::fabs(k[0]))));
   nmd_status st = NMD_OK;
   with_type(j.grad.dtype, [&](auto g) {
@@ -893,7 +894,7 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
       typedef decltype(m) M;
       auto both = [&](auto norm, auto pieces) {
         st = start(norm, grid, kThreads, 0, s, j, parts, status);
-        if (st == NMD_OK) st = start(pieces, grid, kThreads, 0, s, j, X, (const double*)parts, grid, shift, steps, grows);
+        if (st == NMD_OK) st = start(pieces, grid_x, kThreads, 0, s, j, X, (const double*)parts, grid, shift, steps, grows);
       };
       if (j.step) both(norm_kernel<G, M, true>, turned ? turned_kernel<G, M, true> : pieces_kernel<G, M, true>);
       else both(norm_kernel<G, G, false>, turned ? turned_kernel<G, G, false> : pieces_kernel<G, G, false>);

@@ -91,30 +91,78 @@ __device__ __forceinline__ void grid_barrier(int* ints, int target, volatile int
   sync_workers();
 }
 
-// A tile of the result from its fp32 rows in shared memory ([m][j ^ (m & 31)])
+// fp32 rows of a tile in shared memory: groups of four columns, group g of row m where
+// rows by eight lanes and groups by sixteen lie in different banks
+__device__ __forceinline__ int group_at(int m, int g) { return m * kSide + ((g ^ (m & 15)) << 2); }
+
+template <class T>
+struct __align__(4 * sizeof(T)) Four {
+  T x[4];
+};
+// A tile of the result.  Rows of the result that are X's rows: a thread takes four
+// columns of every sixteenth row, in one store where the result's rows allow it.
+// Rows that are X's columns: one row of X, adjacent to its neighbours' everywhere.
 template <class T>
 __device__ __forceinline__ void put_tile(const Strip& p, const float* stage, int64_t m0, float fill) {
-  const int r = (int)p.x.cols, rows = (int)min((int64_t)kRows, p.M - m0);
+  const int r = (int)p.x.cols, rows = (int)min((int64_t)kRows, p.M - m0), tid = threadIdx.x;
+  auto mix = [&](float x, T w) { return p.j.step ? fmaf(-p.j.lr, x, p.j.keep * as_float(w)) : x; };
+  if (!p.turned) {
+    const int j = (tid & 15) * 4, first = tid >> 4;
+    const int64_t rs = p.j.out.rs, cs = p.j.out.cs;
+    T* at = &p.j.out.at<T>(m0 + first, j);
+    const bool whole = cs == 1 && j + 4 <= r && (((uintptr_t)at | (uintptr_t)(rs * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+    if (whole) {
 #pragma unroll 1
-  for (int i = 0; i < kRows * kSide / kThreads; i += 8) {
-    T* at[8];
-    T w[8];
-    float x[8];
+      for (int m = first; m < rows; m += 32, at += 32 * rs) {   // two at a time
+        Four<T> w[2];
+        const bool second = m + 16 < rows;
+        if (p.j.step) {
+          w[0] = *(const Four<T>*)at;
+          if (second) w[1] = *(const Four<T>*)(at + 16 * rs);
+        }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      // adjacent threads, adjacent elements of the result
-      const int e = (i + k) * kThreads + threadIdx.x, m = p.turned ? e & (kRows - 1) : e / kSide, j = p.turned ? e / kRows : e & (kSide - 1);
-      at[k] = m < rows && j < r ? (p.turned ? &p.j.out.at<T>(j, m0 + m) : &p.j.out.at<T>(m0 + m, j)) : nullptr;
-      x[k] = stage[m * kSide + (j ^ (m & 31))] + fill;
+        for (int k = 0; k < 2; ++k) {
+          if (k == 1 && !second) break;
+          const float4 x = *(const float4*)(stage + group_at(m + 16 * k, tid & 15));
+          from_float(mix(x.x + fill, w[k].x[0]), &w[k].x[0]);
+          from_float(mix(x.y + fill, w[k].x[1]), &w[k].x[1]);
+          from_float(mix(x.z + fill, w[k].x[2]), &w[k].x[2]);
+          from_float(mix(x.w + fill, w[k].x[3]), &w[k].x[3]);
+          *(Four<T>*)(at + 16 * k * rs) = w[k];
+        }
+      }
+      return;
     }
+#pragma unroll 1
+    for (int m = first; m < rows; m += 16, at += 16 * rs) {
+      const float4 x = *(const float4*)(stage + group_at(m, tid & 15));
+      T w[4];
+      if (p.j.step) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < r) w[e] = at[e * cs];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < r) from_float(mix((e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w) + fill, w[e]), at + e * cs);
+    }
+    return;
+  }
+  const int m = tid & (kRows - 1), j0 = tid / kRows;
+  if (m >= rows) return;
+  const int64_t rs = p.j.out.rs;
+  T* at = &p.j.out.at<T>(j0, m0 + m);
+#pragma unroll 1
+  for (int j = j0; j < r; j += 8, at += 8 * rs) {   // every second row, four at a time
+    T w[4];
     if (p.j.step) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (at[k]) w[k] = *at[k];
+      for (int k = 0; k < 4; ++k)
+        if (j + 2 * k < r) w[k] = at[2 * k * rs];
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (at[k]) from_float(p.j.step ? fmaf(-p.j.lr, x[k], p.j.keep * as_float(w[k])) : x[k], at[k]);
+    for (int k = 0; k < 4; ++k)
+      if (j + 2 * k < r) from_float(mix(stage[group_at(m, (j + 2 * k) >> 2) + ((j + 2 * k) & 3)] + fill, w[k]), at + 2 * k * rs);
   }
 }
 
@@ -418,7 +466,8 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
       } else {
         float* stage = (float*)tile;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) stage[row * kSide + ((half * 32 + e) ^ (row & 31))] = y[e];
+        for (int q = 0; q < 8; ++q)
+          *(float4*)(stage + group_at(row, half * 8 + q)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
         sync_workers();
         const float fill = *abort_flag ? NAN : 0.f;   // the result of a wait that ran out shows
         if (p.j.out.dtype == NMD_DT_FP32) put_tile<float>(p, stage, m0, fill);
