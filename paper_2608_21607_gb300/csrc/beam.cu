@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostBeams = 64, kMostWidth = 128, kMostCluster = 8;
+constexpr int kSmallRow = 1024;   // columns of a row that a warp takes
 constexpr int kDepth = 2;   // groups of four vectors under way
 
 struct Select {
@@ -103,22 +104,25 @@ struct Best {
     const int n = min(*count, room);
     if (threadIdx.x == 0 && *count > room) *lost = 1;
     __syncthreads();
-    // a warp per entry: its rank among the others by a vote on 32 of them at a time
-    const int lane = threadIdx.x & 31;
-    if (n <= 32) {
+    if (n <= 32) {   // a warp per entry: its rank among the others by a vote
+      const int lane = threadIdx.x & 31;
       const entry_t mine = lane < n ? list[lane] : 0;
       for (int i = threadIdx.x >> 5; i < n; i += kThreads / 32) {
         const entry_t e = list[i];
         const int rank = __popc(__ballot_sync(0xffffffffu, mine > e));
         if (lane == 0 && rank < width) sorted[rank] = e;
       }
-    } else {
-      for (int i = threadIdx.x >> 5; i < n; i += kThreads / 32) {
+    } else {   // a thread per entry, two others at a time
+      for (int i = threadIdx.x; i < n; i += kThreads) {
         const entry_t e = list[i];
-        int rank = 0;
-        for (int k = lane; k < n; k += 32) rank += list[k] > e;
-        rank = __reduce_add_sync(0xffffffffu, rank);
-        if (lane == 0 && rank < width) sorted[rank] = e;
+        int rank = 0, k = 0;
+#pragma unroll 4
+        for (; k + 1 < n; k += 2) {
+          const ulonglong2 u = *(const ulonglong2*)(list + k);
+          rank += (u.x > e) + (u.y > e);
+        }
+        if (k < n) rank += list[k] > e;
+        if (rank < width) sorted[rank] = e;
       }
     }
     __syncthreads();
@@ -133,18 +137,18 @@ struct Best {
 };
 
 // A first bar: the width-th largest of the maxima of groups of elements that threads
-// have in hand, as at least that many elements are not below it.  Up to 32 wide the
-// groups are those of eight threads, and every warp ranks all 32 of them; beyond,
-// those of single threads.
+// have in hand, as at least that many elements are not below it.  Where there are as
+// many groups of eight threads, every warp ranks all 32 of them; otherwise they are
+// those of single threads.  `vectors`: of the segment.
 template <class T, class G>
-__device__ __forceinline__ entry_t first_bar(G get, const Best& best, entry_t* bests) {
+__device__ __forceinline__ entry_t first_bar(G get, int vectors, const Best& best, entry_t* bests) {
   float m = Vec<T>::top(get(0));
 #pragma unroll
   for (int q = 1; q < 4; ++q) m = max_nan(m, Vec<T>::top(get(q)));
   uint32_t o = order_of(m);
   const int lane = threadIdx.x & 31;
   entry_t bar = *best.least;
-  if (best.width <= 32) {
+  if (8 * best.width <= min(vectors, kThreads)) {
 #pragma unroll
     for (int d = 1; d < 8; d *= 2) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
     uint32_t* all = (uint32_t*)bests;
@@ -163,13 +167,18 @@ __device__ __forceinline__ entry_t first_bar(G get, const Best& best, entry_t* b
     if (lane == 0) *best.least = bar;   // every warp the same
     __syncwarp();
   } else {
+    if (vectors < best.width) return bar;   // the same for all
     const entry_t mine = (entry_t)o << 32 | threadIdx.x;
     bests[threadIdx.x] = mine;
     __syncthreads();
     int rank = 0;
-#pragma unroll 8
-    for (int k = 0; k < kThreads; ++k) rank += bests[k] > mine;
-    if (rank == best.width - 1) *best.least = max(bar, (entry_t)o << 32);
+    const int some = min((vectors + 1) & ~1, kThreads);   // (of the others o is that of -inf)
+#pragma unroll 4
+    for (int k = 0; k < some; k += 2) {
+      const ulonglong2 u = *(const ulonglong2*)(bests + k);
+      rank += (u.x > mine) + (u.y > mine);
+    }
+    if (threadIdx.x < some && rank == best.width - 1) *best.least = max(bar, (entry_t)o << 32);
     __syncthreads();
     bar = *best.least;
   }
@@ -223,15 +232,16 @@ __device__ __noinline__ void again(Best best, entry_t* bests, const uint4* xv, i
 
 // Dynamic shared memory: slots, then the lists
 struct Shape {
-  int cluster, limit, room;
+  int cluster, limit, room, small;
   size_t off_list, off_sorted, off_all, off_places, bytes;
 };
-Shape shape_of(int64_t K, int width, int cluster) {
+Shape shape_of(int64_t K, int width, int cluster, bool small = false) {
   Shape s;
+  s.small = small;
   s.cluster = cluster;
   s.limit = 2 * width;
   s.room = s.limit + 36 * width;
-  s.off_list = (size_t)kDepth * 4 * kThreads * 16;
+  s.off_list = (size_t)kDepth * 4 * kThreads * 16;   // (16-byte aligned, as the pairs that are read of it)
   s.off_sorted = s.off_list + (size_t)s.room * 8;
   s.off_all = s.off_sorted + (size_t)width * 8;
   const size_t offers = ((size_t)(K + cluster) * width + K) * 8;   // the segments' lists and finished beams, in the first CTA
@@ -323,8 +333,63 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
   const uint4* mine = slots + tid;
   bool waited = csize == 1;
 
+  // Short rows: a warp each, in fp32 in its part of the slots; the largest is taken `width`
+  // times, a lane keeping the largest of its own columns l, l + 32, ...
+  if (shape.small) {
+    float* x = (float*)slots + warp * kSmallRow;
+    const int V = (int)a.V;
+#pragma unroll 1
+    for (int r = warp; r < R; r += kThreads / 32) {
+      const T* from_row = (const T*)a.x + (b * a.K + row_beam[r]) * a.ld;
+      float m = -INFINITY;
+#pragma unroll 8
+      for (int v = lane; v < V; v += 32) {
+        const float f = Vec<T>::get(from_row[v]);
+        x[v] = f;
+        m = max_nan(m, f);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const bool near = is_near(m, a.c), some = m > -INFINITY && m < INFINITY;
+      const float ref = near ? ref_of(m, a.c) : 0.f;
+      float S = 0.f;
+      entry_t top = 0;
+      if (some) {
+#pragma unroll 4
+        for (int v = lane; v < V; v += 32) {
+          const float f = x[v];
+          S += near ? ex2(fmaf(f, a.c.hi, -ref) + f * a.c.lo) : power(f, m, a.c);
+          top = max(top, entry_of(f, v));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+      }
+      const entry_t bar = entry_of(-INFINITY, 0);
+      int n = 0;
+#pragma unroll 1
+      for (; some && n < a.width; ++n) {
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32));
+        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32) == hi ? (uint32_t)top : 0u);
+        const entry_t e = (entry_t)hi << 32 | lo;
+        if (e <= bar) break;
+        if (top == e) {   // one lane: its next
+          all[r * a.width + n] = e;
+          x[column_of(e)] = -INFINITY;
+          top = 0;
+#pragma unroll 4
+          for (int v = lane; v < V; v += 32) top = max(top, entry_of(x[v], v));
+        }
+        __syncwarp();
+      }
+      if (lane == 0) {
+        stats[r] = Stat{m, S};
+        counts[r] = n;
+      }
+      __syncwarp();
+    }
+  }
   int row = 0;
-  for (int64_t at = from; at < to;) {
+  for (int64_t at = shape.small ? to : from; at < to;) {
     while (at >= (row + 1) * a.V) ++row;
     const int64_t e0 = at - row * a.V, e1 = min(a.V, to - row * a.V);
     at = row * a.V + e1;
@@ -362,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       copy_wait<kDepth - 1>();
       const float group = run.add(get, a.c);
       // What has to be passed only rises; an older value lets more through, not less
-      const entry_t bar = i == 0 ? first_bar<T>(get, best, bests) : *(volatile entry_t*)&least;
+      const entry_t bar = i == 0 ? first_bar<T>(get, n, best, bests) : *(volatile entry_t*)&least;
       const float bar_x = value_of(bar);
       const float power = ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo);
       // (0.99: far more than the sum's rounding.)  The warp looks at a thread's elements
@@ -488,6 +553,46 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     if (tid >= there && tid < a.width) put(tid, 0, 0);
     return;
   }
+  // More offers: only those not below the width-th largest of the threads' largest ones
+  {
+    entry_t mine_top = 0;
+    for (int i = tid; i < offers; i += kThreads) mine_top = max(mine_top, all[i]);
+    bests[tid] = mine_top;
+    if (tid == 0) count = 0, least = 1;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 4
+    for (int k = 0; k < kThreads; k += 2) {
+      const ulonglong2 u = *(const ulonglong2*)(bests + k);
+      rank += (u.x > mine_top || (u.x == mine_top && k < tid)) + (u.y > mine_top || (u.y == mine_top && k + 1 < tid));
+    }
+    if (rank == a.width - 1 && mine_top != 0) least = mine_top;
+    __syncthreads();
+    const entry_t bar = least;
+    int* which = (int*)best.list;
+    for (int i = tid; i < offers; i += kThreads)
+      if (all[i] >= bar) {
+        const int q = atomicAdd(&count, 1);
+        if (q < shape.room) which[q] = i;
+      }
+    __syncthreads();
+    const int n = count;
+    if (n <= min(shape.room, 2 * kThreads)) {
+      for (int i = tid; i < n; i += kThreads) {
+        const entry_t v = all[which[i]], place = places[which[i]];
+        int better = 0;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+          const entry_t u = all[which[k]];
+          better += u > v;
+          if (u == v && k != i) better += places[which[k]] < place;
+        }
+        if (better < a.width) put(better, v, place);
+      }
+      for (int i = n + tid; i < a.width; i += kThreads) put(i, 0, 0);
+      return;
+    }
+  }
   if (warp != 0) return;
 
   // Lists are in order: the best of their heads is the next offer.  Lane l has lists l,
@@ -562,18 +667,28 @@ __device__ __forceinline__ void move(const State& s, int64_t slice, int64_t b, i
   const char* in = s.in + o * s.in_outer + b * a.K * s.in_row + slice * a.per;
   char* out = s.out + o * s.out_outer + b * a.width * s.out_row + slice * a.per;
   U* buf = (U*)smem;
-  for (int u = u0; u < n; u += across) {
+  if constexpr (sizeof(U) >= 4) {
+    for (int u = u0; u < n; u += across) {
 #pragma unroll 4
-    for (int k = k0; k < a.K; k += rows)
-      if (needed >> k & 1) {
-        const U* from = (const U*)(in + k * s.in_row) + u;
-        if (sizeof(U) == 16) copy_async(tc::smem_u32(buf + k * per + u), from);
-        else buf[k * per + u] = *from;
-      }
-  }
-  if (sizeof(U) == 16) {
+      for (int k = k0; k < a.K; k += rows)
+        if (needed >> k & 1) copy_async<sizeof(U)>(tc::smem_u32(buf + k * per + u), (const U*)(in + k * s.in_row) + u);
+    }
     copy_commit();
     copy_wait<0>();
+  } else {   // loads of a thread eight at a time
+    for (int k = k0; k < a.K; k += rows) {
+      if (!(needed >> k & 1)) continue;
+      const U* from = (const U*)(in + k * s.in_row);
+      for (int u = u0; u < n; u += 8 * across) {
+        U v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (u + i * across < n) v[i] = from[u + i * across];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (u + i * across < n) buf[k * per + u + i * across] = v[i];
+      }
+    }
   }
   __syncthreads();
   for (int u = u0; u < n; u += across) {
@@ -622,8 +737,10 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
 template <class T>
 nmd_status launch_select(const Select& a, int64_t B, cudaStream_t s) {
   int cluster = 1;
-  while (cluster < kMostCluster && B * cluster < 456 && a.K * a.V > (int64_t)cluster * 4 * kThreads * Vec<T>::N) cluster *= 2;
-  const Shape shape = shape_of(a.K, a.width, cluster);
+  // Short rows go to warps, unless very many of their columns are wanted one by one
+  const bool small = a.V <= kSmallRow && std::min<int64_t>(a.width, a.V) <= 48;
+  while (!small && cluster < kMostCluster && B * cluster < 456 && a.K * a.V > (int64_t)cluster * 4 * kThreads * Vec<T>::N) cluster *= 2;
+  const Shape shape = shape_of(a.K, a.width, cluster, small);
   static std::atomic<int> ready[kMaxDevices];
   auto kernel = select_kernel<T>;
   if (!per_device(ready, [&] {
@@ -740,8 +857,8 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
     a.K = (int)K;
     a.width = (int)width;
     a.parents = d_parents;
-    a.per = 4096;
-    while (a.per * K > 32768) a.per /= 2;
+    a.per = 16384;
+    while (a.per > 512 && a.per * K > 32768) a.per /= 2;
     for (; k < count && a.count < kStates; ++k) {
       const nmd_beam_state& s = states[k];
       if (s.outer == 0 || s.bytes == 0 || B == 0) continue;

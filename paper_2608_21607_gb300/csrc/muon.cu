@@ -331,7 +331,7 @@ enum Mode { kSymmetric, kPartial, kMatrix, kResult };
 struct Gemm {
   int64_t M, N;             // D is M x N
   int kblocks, splits;      // blocks of 64 of the sum; parts of it that are tiles of their own
-  int tiles_n, items;       // tiles across; tiles x splits
+  int tiles_m, tiles_n, items;   // tiles down and across; tiles x splits
   int lower;                // 1: D is symmetric, tiles below and on the diagonal only
   int mode;
   float alpha, beta, diag;  // D = alpha 2^(*up - times *down) (sum) + beta C + diag I, in pieces
@@ -379,8 +379,14 @@ __device__ __forceinline__ Item item_of(const Gemm& p, int w, int BN) {
     }
     t.j = left;
   } else {
-    t.i = tile / p.tiles_n;
-    t.j = tile - t.i * p.tiles_n;
+    // the shorter side first: tiles that read the same part of the longer operand run together
+    if (p.tiles_m < p.tiles_n) {
+      t.j = tile / p.tiles_m;
+      t.i = tile - t.j * p.tiles_m;
+    } else {
+      t.i = tile / p.tiles_n;
+      t.j = tile - t.i * p.tiles_n;
+    }
   }
   t.k0 = (int)((int64_t)p.kblocks * part / p.splits);
   t.k1 = (int)((int64_t)p.kblocks * (part + 1) / p.splits);
@@ -910,6 +916,7 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
     g.N = n;
     g.kblocks = (int)((depth + kBK - 1) / kBK);
     g.splits = 1;
+    g.tiles_m = (int)((m + kBM - 1) / kBM);
     g.tiles_n = (int)((n + BN - 1) / BN);
     g.items = (int)tiles_of(m, n, BN, lower);
     g.lower = lower;

@@ -309,23 +309,26 @@ def beam_select(logits, scores, *, width: Optional[int] = None, finished=None, e
     return Beams(out, parents, tokens, done)
 
 
-def _rows_of(x, dim: int, name: str):
-    """(outer count, outer stride, row stride, bytes of a row) of a tensor whose dimension ``dim`` counts the rows."""
-    shape, strides, size = x.shape, x.stride(), x.element_size()
+@functools.lru_cache(maxsize=1024)
+def _rows_of(shape, strides, dim: int, size: int):
+    """(what is not rows, rows, outer count, outer stride, row stride, bytes of a row) of a tensor whose dimension
+    ``dim`` counts the rows, strides in bytes; or what is wrong with it."""
+    if not 0 <= dim < len(shape):
+        return "a dimension %d of rows is wanted" % dim
     want = 1
     for n, s in zip(reversed(shape[dim + 1:]), reversed(strides[dim + 1:])):
         if n > 1 and s != want:
-            _invalid("%s: the elements of a row have to be adjacent" % name)
+            return "the elements of a row have to be adjacent"
         want *= n
     outer, stride = 1, 0
     for n, s in zip(reversed(shape[:dim]), reversed(strides[:dim])):
         if n > 1:
             if outer > 1 and s != stride * outer:
-                _invalid("%s: the dimensions before the rows have to lie at one distance" % name)
+                return "the dimensions before the rows have to lie at one distance"
             if outer == 1:
                 stride = s
         outer *= n
-    return outer, stride * size, strides[dim] * size, want * size
+    return shape[:dim] + shape[dim + 1:], shape[dim], outer, stride * size, strides[dim] * size, want * size
 
 
 def beam_reorder(states, parents, *, dim: int = 0, out=None):
@@ -342,31 +345,28 @@ def beam_reorder(states, parents, *, dim: int = 0, out=None):
             or not parents.is_cuda or not all(isinstance(x, torch.Tensor) for x in xs + ys) or len(xs) != len(ys):
         _invalid("states, parents, out: tensors, an int64 CUDA matrix and as many tensors are wanted")
     B, w = parents.shape
-    device, index = parents.device, parents.get_device()
+    index = parents.get_device()
     if not xs:
         return states if out is None else out
-    K, table = None, (nmd.nmd_beam_state * len(xs))()
-    for t, x, y in zip(table, xs, ys):
-        if x.device != device or y.device != device or y.dtype != x.dtype:
-            _invalid("states, out: tensors on %s, of one type each, are wanted" % device)
-        if not 0 <= dim < x.dim() or y.dim() != x.dim() or x.shape[:dim] != y.shape[:dim] \
-                or x.shape[dim + 1:] != y.shape[dim + 1:]:
-            _invalid("states, out: tensors with a dimension %d of rows, alike apart from it, are wanted" % dim)
-        rows = x.shape[dim]
+    K, table = None, array.array("q")   # nmd_beam_state, eight fields of 64 bits
+    for x, y in zip(xs, ys):
+        here = _rows_of(x.shape, x.stride(), dim, x.element_size())
+        there = here if y is x else _rows_of(y.shape, y.stride(), dim, y.element_size())
+        for problem in (here, there):
+            if isinstance(problem, str):
+                _invalid("states, out: " + problem)
+        rest, rows, outer, stride, row, nbytes = here
+        if x.get_device() != index or y is not x and (y.get_device() != index or y.dtype != x.dtype or rest != there[0]):
+            _invalid("states, out: tensors on cuda:%d, of one type each and alike apart from the rows, are wanted" % index)
         k = rows // B if B else w
-        if rows != B * k or y.shape[dim] != B * w or (K is not None and k != K):
+        if rows != B * k or there[1] != B * w or (K is not None and k != K):
             _invalid("states, out: B x K rows and B x width rows for parents of %d x %d are wanted" % (B, w))
         K = k
-        t.outer, t.in_outer, t.in_row, t.bytes = _rows_of(x, dim, "states")
-        t.in_, t.out = x.data_ptr(), y.data_ptr()
-        if y is x:
-            t.out_outer, t.out_row = t.in_outer, t.in_row
-        else:
-            _, t.out_outer, t.out_row, _ = _rows_of(y, dim, "out")
+        table.extend((x.data_ptr(), y.data_ptr(), outer, stride, there[3], row, there[4], nbytes))
     if not 1 <= K <= 64 or not 1 <= w <= 128 or (out is None and K != w):
         _invalid("states, parents: 1 to 64 beams and a width of 1 to 128, the same in place, are wanted")
     parents = parents if parents.is_contiguous() else parents.contiguous()
-    _call(index, "nmd_beam_reorder", len(xs), C.addressof(table), B, K, w, parents.data_ptr())
+    _call(index, "nmd_beam_reorder", len(xs), table.buffer_info()[0], B, K, w, parents.data_ptr())
     torch.autograd.graph.increment_version(ys)
     return states if out is None else out
 

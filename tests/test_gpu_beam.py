@@ -97,7 +97,8 @@ def check(rows, scores, done, width, end=None, temperature=1.0, got=None):
 @pytest.mark.parametrize("B,K,V,width", [
     (1, 1, 1, 1), (1, 1, 2, 2), (3, 2, 7, 5), (2, 5, 3, 20), (4, 3, 1, 7), (5, 4, 255, 4), (2, 8, 1000, 16),
     (3, 64, 33, 128), (1, 64, 700, 64), (7, 1, 4097, 3), (2, 3, 20011, 6), (1, 4, 139255, 4), (1, 1, 70001, 128),
-    (40, 5, 513, 5), (1, 32, 9001, 64)])
+    (40, 5, 513, 5), (1, 32, 9001, 64), (6, 14, 312, 14), (2, 3, 1024, 48), (2, 3, 1025, 48), (3, 33, 34, 66), (2, 22, 461, 44),
+    (1, 16, 1142, 16), (2, 64, 1000, 128), (1, 64, 1024, 40), (1, 8, 64, 128)])
 def test_select(dtype, B, K, V, width):
     check(*make(B * 7 + K, B, K, V, dtype), width)
 
