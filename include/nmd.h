@@ -504,7 +504,7 @@ nmd_status nmd_beam_select(const void* d_logits, int32_t dtype, int64_t B, int64
  * (o, b K + d_parents[b width + k]) of in was.  A parent outside [0, K) leaves
  * its row of out as it is.  in == out (with equal strides and width == K): in
  * place.  Otherwise no memory of any out lies between the first and the last byte
- * of any other in or out of the call.  In place, states that lie between each
+ * of any other in or out of the call; nor do the parents lie there.  In place, states that lie between each
  * other's bytes are dealt with one after another, in the order of the array.
  * Rows of one state lie apart.  `states` is a host array, read before the call
  * returns.  B, K, width as above. */
@@ -528,11 +528,12 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
  * with X = G / (|G|_F + eps), `steps` (1 to 16) times
  *   A = X X^T,  X <- a X + (b A + c A^2) X      (A of the smaller side),
  * (a, b, c) = coefficients, which maps every singular value s to
- * a s + b s^3 + c s^5 and leaves the singular vectors.  X is held to 22 bits or
- * more, sums to fp32; the result is rounded once to its own type.  Singular
- * values on the way and |a| + |b| s^2 + |c| s^4 have to stay below 15, or the result is not
- * finite; so is that of a G with NaN or infinities.  G = 0 gives 0.  eps > 0.
- * Equal calls give equal bits. */
+ * a s + b s^3 + c s^5 and leaves the singular vectors.  Each element of X is held
+ * to 22 bits, or to 2^-37 of |X|_F where that is more, sums are fp32; the result is
+ * rounded once to its own type.  Singular values on the way have to stay below
+ * 3.8 and |a + b s^2 + c s^4| below 15, or the result is not finite; neither is
+ * that of a G with NaN or infinities, or of a wait in the kernels that runs out
+ * (2 s).  G = 0 gives 0.  eps > 0.  Equal calls give equal bits. */
 nmd_status nmd_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
 nmd_status nmd_orthogonalize(const void* d_update, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride,
                              int64_t col_stride, int32_t steps, const double* coefficients, double eps, void* d_out,

@@ -841,6 +841,7 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
     if (!place) *end++ = Range{(uintptr_t)s.in, (uintptr_t)s.in + (uintptr_t)in, kRead};
     *end++ = Range{(uintptr_t)s.out, (uintptr_t)s.out + (uintptr_t)out, place ? kPlace : kWritten};
   }
+  *end++ = Range{(uintptr_t)d_parents, (uintptr_t)d_parents + (uintptr_t)(B * width * 8), kRead};
   std::sort(ranges.get(), end, [](const Range& x, const Range& y) { return x.from < y.from; });
   uintptr_t to[3] = {0, 0, 0};
   for (const Range* q = ranges.get(); q < end; ++q) {

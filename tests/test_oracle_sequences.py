@@ -105,7 +105,7 @@ def test_beam_select_of_no_groups(L):
     assert select(L, B=0, logits=None) == N.NMD_OK
 
 
-def reorder(L, states, B=2, K=3, width=3, parents=P):
+def reorder(L, states, B=2, K=3, width=3, parents=8 * P):
     table = (N.nmd_beam_state * len(states))(*[N.nmd_beam_state(*s) for s in states])
     return L.nmd_beam_reorder(len(states), C.addressof(table), B, K, width, parents, None)
 
@@ -122,6 +122,7 @@ def reorder(L, states, B=2, K=3, width=3, parents=P):
     ([(P, P + 100, 1, 0, 0, 8, 8, 8), (P + 60, P + 130, 1, 0, 0, 8, 8, 8)], {}),
     ([(P, P + 200, 1, 0, 0, 8, 8, 8), (P + 220, P + 220, 1, 0, 0, 8, 8, 8)], {}),
     ([(P, P + 200, 1, 0, 0, 8, 8, 8), (P + 8, P + 8, 1, 0, 0, 8, 8, 8)], {}),
+    ([(P, P, 1, 0, 0, 8, 8, 8)], dict(parents=P + 40)), ([(2 * P, P, 1, 0, 0, 8, 8, 8)], dict(parents=P - 40)),
     ([(P, P, 1, 0, 0, 8, 8, 8)], dict(parents=None)), ([(P, P, 1, 0, 0, 8, 8, 8)], dict(B=-1)),
     ([(P, P, 1, 0, 0, 8, 8, 8)], dict(K=65, width=65)), ([(P, P, 1, 0, 0, 8, 8, 8)], dict(K=0, width=0)),
     ([(P, P, 1 << 45, 1 << 45, 1 << 45, 8, 8, 8)], {})])
@@ -133,7 +134,7 @@ def test_beam_reorder_of_nothing(L):
     assert reorder(L, []) == N.NMD_OK
     assert reorder(L, [(None, None, 1, 0, 0, 8, 8, 0), (None, None, 0, 0, 0, 8, 8, 8)]) == N.NMD_OK
     assert reorder(L, [(None, None, 1, 0, 0, 8, 8, 8)], B=0) == N.NMD_OK
-    assert L.nmd_beam_reorder(1, None, 2, 3, 3, P, None) == N.NMD_ERR_INVALID
+    assert L.nmd_beam_reorder(1, None, 2, 3, 3, 8 * P, None) == N.NMD_ERR_INVALID
     assert L.nmd_beam_reorder(-1, None, 2, 3, 3, P, None) == N.NMD_ERR_INVALID
 
 
