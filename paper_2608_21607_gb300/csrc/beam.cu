@@ -138,8 +138,8 @@ struct Best {
 
 // A first bar: the width-th largest of the maxima of groups of elements that threads
 // have in hand, as at least that many elements are not below it.  Where there are as
-// many groups of eight threads, every warp ranks all 32 of them; otherwise they are
-// those of single threads.  `vectors`: of the segment.
+// many of 32 groups of threads, every warp ranks them; otherwise they are those of
+// single threads.  `vectors`: of the segment.
 template <class T, class G>
 __device__ __forceinline__ entry_t first_bar(G get, int vectors, const Best& best, entry_t* bests) {
   float m = Vec<T>::top(get(0));
@@ -148,11 +148,12 @@ __device__ __forceinline__ entry_t first_bar(G get, int vectors, const Best& bes
   uint32_t o = order_of(m);
   const int lane = threadIdx.x & 31;
   entry_t bar = *best.least;
-  if (8 * best.width <= min(vectors, kThreads)) {
+  constexpr int kGroup = kThreads / 32;
+  if (kGroup * best.width <= min(vectors, kThreads)) {
 #pragma unroll
-    for (int d = 1; d < 8; d *= 2) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
+    for (int d = 1; d < kGroup; d *= 2) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
     uint32_t* all = (uint32_t*)bests;
-    if ((lane & 7) == 0) all[threadIdx.x >> 3] = o;
+    if (lane % kGroup == 0) all[threadIdx.x / kGroup] = o;
     __syncthreads();
     o = all[lane];
     int rank = 0;
