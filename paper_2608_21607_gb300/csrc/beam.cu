@@ -25,7 +25,7 @@ namespace nmd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostBeams = 64, kMostWidth = 128, kMostCluster = 16;
+constexpr int kMostBeams = 64, kMostWidth = 128, kMostCluster = 8;
 constexpr int kSmallRow = 1024;   // columns of a row that a warp takes
 constexpr int kDepth = 2;   // groups of four vectors under way
 
@@ -735,50 +735,18 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
 
 // CTAs of a group: enough that the groups give every SM three, and none with less than
 // a round of its own.
-constexpr int kFewGroups = 8;
-template <class F>
-int most_cluster(F kernel, const Shape& largest) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)largest.bytes) != cudaSuccess ||
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    cudaGetLastError();
-    return 8;
-  }
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = 16;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.gridDim = dim3(16);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = largest.bytes;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-    cudaGetLastError();
-    n = 0;
-  }
-  return n >= 1 ? 16 : 8;
-}
-
 template <class T>
 nmd_status launch_select(const Select& a, int64_t B, cudaStream_t s) {
   int cluster = 1;
   // Short rows go to warps, unless very many of their columns are wanted one by one
   const bool small = a.V <= kSmallRow && std::min<int64_t>(a.width, a.V) <= 48;
-  while (!small && cluster < 8 && B * cluster < 456 && a.K * a.V > (int64_t)cluster * 4 * kThreads * Vec<T>::N) cluster *= 2;
-  // a few groups of long rows: sixteen, if the device has room for such clusters (one
-  // group of four rows of 139,255 bf16 columns: 17.5 us with eight)
-  const Shape largest = shape_of(kMostBeams, kMostWidth, 8);
-  static std::atomic<int> most[kMaxDevices];
-  if (cluster == 8 && B <= kFewGroups && a.K * a.V > 16 * 4 * kThreads * Vec<T>::N &&
-      shape_of(a.K, a.width, 16).bytes <= largest.bytes)
-    cluster = per_device(most, [&] { return most_cluster(select_kernel<T>, largest); });
+  while (!small && cluster < kMostCluster && B * cluster < 456 && a.K * a.V > (int64_t)cluster * 4 * kThreads * Vec<T>::N) cluster *= 2;
   const Shape shape = shape_of(a.K, a.width, cluster, small);
   static std::atomic<int> ready[kMaxDevices];
   auto kernel = select_kernel<T>;
   if (!per_device(ready, [&] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)largest.bytes) == cudaSuccess;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)shape_of(kMostBeams, kMostWidth, kMostCluster).bytes) == cudaSuccess;
       }))
     return NMD_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
