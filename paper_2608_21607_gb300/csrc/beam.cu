@@ -260,7 +260,12 @@ __device__ __forceinline__ void put_remote(uint32_t at, entry_t v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
 }
 
-// Bound by HBM; one group by the launch, two barriers of the cluster and the merge.
+// Bound by HBM where there is much to read: 128 groups of four rows of 139,255 bf16
+// columns (a tenth of the beams finished) take 40 us, of which 20 are the rows at 6.4
+// TB/s and the rest the start, the last cut and the merge, which nothing covers as all
+// CTAs run at a time (twice as many CTAs: 49 us).  64 groups of eight rows of 50,001 fp16
+// columns 30 us; one group of four rows of 139,255 18 us, eight CTAs' latency.  A bar that
+// needs every element compared, or a list per warp, cost as much again as the sums.
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_constant__ Select a, const __grid_constant__ Shape shape) {
   constexpr int N = Vec<T>::N;
@@ -703,8 +708,11 @@ __device__ __forceinline__ void move(const State& s, int64_t slice, int64_t b, i
 
 // A CTA takes a piece of all K rows of a group at a time: what is needed of it is in
 // shared memory before any row is written, so that rows may change places.  In place,
-// rows that stay are not written, and those that nothing goes on from not read.
-__global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant__ States a) {
+// rows that stay are not written, and those that nothing goes on from not read.  Bound by
+// HBM: 16 tensors of 512 rows of 64 KB (groups of eight, parents at random) take 142 us,
+// 5.8 TB/s over what moves; with four CTAs an SM 154 us, and 179 us where the grid is
+// larger than what fits at a time.
+__global__ void __launch_bounds__(kThreads, 6) reorder_kernel(const __grid_constant__ States a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ int parent[kMostWidth];
   __shared__ unsigned long long needed;
@@ -884,7 +892,7 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
       a.work += t.slices * B * s.outer;
     }
     if (a.count == 0) break;
-    reorder_kernel<<<(unsigned)std::min<int64_t>(a.work, 152 * 6), kThreads, a.per * K, (cudaStream_t)stream>>>(a);
+    reorder_kernel<<<(unsigned)std::min<int64_t>(a.work, 152 * 12), kThreads, a.per * K, (cudaStream_t)stream>>>(a);
     if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
   }
   return NMD_OK;
