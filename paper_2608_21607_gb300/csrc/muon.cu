@@ -415,39 +415,55 @@ __device__ __forceinline__ float& in_square(float* sq, int r, int c) { return sq
 // 32 rows x 32 columns of D in pieces, from row0 and col0 on: alpha (the square, or with
 // `turned` its transpose) + beta C + diag I.  Four lanes write 64 adjacent bytes of a row.
 // Rows past the last are not written; columns up to the row's stride are.
+template <bool WIDE>
 __device__ __forceinline__ void put_block(const Gemm& p, float alpha, float* sq, int64_t row0, int64_t col0, bool turned, bool lower) {
   const int lane = threadIdx.x & 31, c = (lane & 3) * 8;
-#pragma unroll 2
-  for (int i = 0; i < 4; ++i) {
-    const int r = i * 8 + (lane >> 2);
-    const int64_t row = row0 + r, col = col0 + c;
-    if (row >= p.M) return;
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // on the diagonal what is above it is what is below it, in every bit
-      const bool swap = turned || (lower && c + e > r);
-      v[e] = alpha * (swap ? in_square(sq, c + e, r) : in_square(sq, r, c + e));
-    }
+  // C, all of it under way together where a thread has the registers
+  constexpr int kAhead = WIDE ? 1 : 4;
+#pragma unroll 1
+  for (int i0 = 0; i0 < 4; i0 += kAhead) {
+    uint4 ch[kAhead], cl[kAhead];
     if (p.beta != 0.f) {
-      const __half* at = p.c.hi + row * p.c.ld + col;
-      const uint4 a = *(const uint4*)at, b = *(const uint4*)(at + p.c.plane());
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, __half2float(((const __half*)&a)[e]) + __half2float(((const __half*)&b)[e]), v[e]);
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t row = row0 + (i0 + i) * 8 + (lane >> 2);
+        if (row >= p.M) break;
+        const __half* at = p.c.hi + row * p.c.ld + col0 + c;
+        ch[i] = *(const uint4*)at;
+        cl[i] = *(const uint4*)(at + p.c.plane());
+      }
     }
-    if (lower) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e == r) v[e] += p.diag;
+    for (int i = 0; i < kAhead; ++i) {
+      const int r = (i0 + i) * 8 + (lane >> 2);
+      const int64_t row = row0 + r, col = col0 + c;
+      if (row >= p.M) return;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        // on the diagonal what is above it is what is below it, in every bit
+        const bool swap = turned || (lower && c + e > r);
+        v[e] = alpha * (swap ? in_square(sq, c + e, r) : in_square(sq, r, c + e));
+      }
+      if (p.beta != 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = fmaf(p.beta, __half2float(((const __half*)&ch[i])[e]) + __half2float(((const __half*)&cl[i])[e]), v[e]);
+      }
+      if (lower) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e == r) v[e] += p.diag;
+      }
+      uint4 h, l;
+      split2(v[0], v[1], h.x, l.x);
+      split2(v[2], v[3], h.y, l.y);
+      split2(v[4], v[5], h.z, l.z);
+      split2(v[6], v[7], h.w, l.w);
+      __half* to = p.d.hi + row * p.d.ld + col;
+      *(uint4*)to = h;
+      *(uint4*)(to + p.d.plane()) = l;
     }
-    uint4 h, l;
-    split2(v[0], v[1], h.x, l.x);
-    split2(v[2], v[3], h.y, l.y);
-    split2(v[4], v[5], h.z, l.z);
-    split2(v[6], v[7], h.w, l.w);
-    __half* to = p.d.hi + row * p.d.ld + col;
-    *(uint4*)to = h;
-    *(uint4*)(to + p.d.plane()) = l;
   }
 }
 
@@ -503,12 +519,10 @@ __device__ __forceinline__ void put_rows_of(const Gemm& p, float alpha, const fl
   }
 }
 // the square of rows from row0 and columns from col0 on, by the kernel's mode
-__device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq, int64_t row0, int64_t col0, float* part, int BN) {
+template <bool WIDE>
+__device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq, int64_t row0, int64_t col0) {
   const int lane = threadIdx.x & 31;
-  if (p.mode == kPartial) {
-#pragma unroll 4
-    for (int r = 0; r < 32; ++r) part[r * BN + lane] = in_square(sq, r, lane);
-  } else if (p.mode == kResult) {
+  if (p.mode == kResult) {
     if (col0 + lane >= p.N) return;
     const Matrix& o = p.out.out;
     const int rows = (int)min((int64_t)32, p.M - row0);
@@ -517,9 +531,9 @@ __device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq
     else put_rows<__half>(p, alpha, row0, rows, col0 + lane, sq);
   } else if (col0 < p.d.ld) {
     if (p.mode == kSymmetric && col0 > row0) return;   // above the diagonal
-    put_block(p, alpha, sq, row0, col0, false, p.mode == kSymmetric && col0 == row0);
+    put_block<WIDE>(p, alpha, sq, row0, col0, false, p.mode == kSymmetric && col0 == row0);
     if (p.mode == kSymmetric && col0 < row0 && row0 < p.M) {
-      put_block(p, alpha, sq, col0, row0, true, false);
+      put_block<WIDE>(p, alpha, sq, col0, row0, true, false);
     }
   }
 }
@@ -703,10 +717,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           put_rows_of(p, alpha, v, square, r, (int64_t)t.j * BN + col);
           continue;
         }
+        if (p.mode == kPartial) {
+          float4* at = (float4*)(p.part + ((int64_t)w * kBM + row + lane) * BN + col);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) at[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < 32; ++i) in_square(square, lane, i) = ok ? v[i] : NAN;   // the result of a wait that ran out shows
         __syncwarp();
-        put_square(p, alpha, square, r, (int64_t)t.j * BN + col, p.part + ((int64_t)w * kBM + row) * BN + col, BN);
+        put_square<(BN > 64)>(p, alpha, square, r, (int64_t)t.j * BN + col);
       }
     }
   }
@@ -841,6 +861,12 @@ struct GramPlan {
 GramPlan gram_plan(int64_t r, int64_t M) {
   GramPlan g;
   const int64_t blocks = (M + kBK - 1) / kBK;
+  if (blocks <= 20) {   // the sum of 20 blocks takes what adding parts up would (8 us)
+    g.BN = columns_of(r, r, true);
+    g.tiles = tiles_of(r, r, g.BN, true);
+    g.splits = 1;
+    return g;
+  }
   g.BN = r <= 64 ? 64 : 128;
   g.tiles = tiles_of(r, r, g.BN, true);
   g.splits = std::max<int64_t>(1, std::min<int64_t>(kSms / g.tiles, blocks / 2));
