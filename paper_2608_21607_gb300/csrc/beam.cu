@@ -706,6 +706,55 @@ __device__ __forceinline__ void move(const State& s, int64_t slice, int64_t b, i
   }
 }
 
+// The same for rows that start at any multiple of two bytes: whole words are loaded as
+// they lie, and stored as they are to lie, each out of the two words that hold it.
+__device__ __forceinline__ void move_halves(const State& s, int64_t slice, int64_t b, int64_t o, const States& a, char* smem,
+                                            const int* parent, unsigned long long needed) {
+  const int stride = a.per / 4 + 1;   // words of a row here
+  const int n = (int)min((int64_t)a.per, s.units * 2 - slice * a.per);   // bytes
+  const char* in = s.in + o * s.in_outer + b * a.K * s.in_row + slice * a.per;
+  char* out = s.out + o * s.out_outer + b * a.width * s.out_row + slice * a.per;
+  uint32_t* buf = (uint32_t*)smem;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int across = min(stride, kThreads) > 128 ? kThreads / 32 : 1;   // warps to a row
+  for (int k = warp / across; k < a.K; k += kThreads / 32 / across) {
+    if (!(needed >> k & 1)) continue;
+    const char* from = in + k * s.in_row;
+    const int odd = (int)((uintptr_t)from & 2), words = (odd + n + 3) / 4;
+    const char* base = from - odd;
+    for (int i = warp % across * 32 + lane; i < words; i += 32 * across) {
+      const int at = 4 * i - odd;   // of the row's bytes
+      if (at >= 0 && at + 4 <= n) {
+        copy_async<4>(tc::smem_u32(buf + k * stride + i), base + 4 * i);
+      } else {   // a word that the row has half of
+        uint16_t* half = (uint16_t*)(buf + k * stride + i);
+        if (at >= 0 && at < n) half[0] = *(const uint16_t*)(from + at);
+        if (at + 2 >= 0 && at + 2 < n) half[1] = *(const uint16_t*)(from + at + 2);
+      }
+    }
+  }
+  copy_commit();
+  copy_wait<0>();
+  __syncthreads();
+  for (int k = warp / across; k < a.width; k += kThreads / 32 / across) {
+    const int p = parent[k];
+    if (p < 0) continue;
+    char* to = out + k * s.out_row;
+    const int odd = (int)((uintptr_t)to & 2), from_odd = (int)((uintptr_t)(in + p * s.in_row) & 2), words = (odd + n + 3) / 4;
+    const uint32_t* row = buf + p * stride;
+    for (int i = warp % across * 32 + lane; i < words; i += 32 * across) {
+      const int at = 4 * i - odd, w = (at + from_odd) >> 2;   // the word that holds byte `at`
+      if (at >= 0 && at + 4 <= n) {
+        *(uint32_t*)(to + at) = (at + from_odd) & 2 ? __funnelshift_r(row[w], row[w + 1], 16) : row[w];
+      } else {
+        const uint16_t* half = (const uint16_t*)row;
+        if (at >= 0 && at < n) *(uint16_t*)(to + at) = half[(at + from_odd) >> 1];
+        if (at + 2 >= 0 && at + 2 < n) *(uint16_t*)(to + at + 2) = half[(at + 2 + from_odd) >> 1];
+      }
+    }
+  }
+}
+
 // A CTA takes a piece of all K rows of a group at a time: what is needed of it is in
 // shared memory before any row is written, so that rows may change places.  In place,
 // rows that stay are not written, and those that nothing goes on from not read.  Bound by
@@ -735,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 6) reorder_kernel(const __grid_const
       case 16: move<uint4>(s, slice, b, o, a, smem, parent, needed); break;
       case 8: move<uint2>(s, slice, b, o, a, smem, parent, needed); break;
       case 4: move<uint32_t>(s, slice, b, o, a, smem, parent, needed); break;
-      case 2: move<uint16_t>(s, slice, b, o, a, smem, parent, needed); break;
+      case 2: move_halves(s, slice, b, o, a, smem, parent, needed); break;
       default: move<uint8_t>(s, slice, b, o, a, smem, parent, needed);
     }
   }
@@ -892,7 +941,7 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
       a.work += t.slices * B * s.outer;
     }
     if (a.count == 0) break;
-    reorder_kernel<<<(unsigned)std::min<int64_t>(a.work, 152 * 12), kThreads, a.per * K, (cudaStream_t)stream>>>(a);
+    reorder_kernel<<<(unsigned)std::min<int64_t>(a.work, 152 * 12), kThreads, (a.per + 4) * K, (cudaStream_t)stream>>>(a);
     if (cudaGetLastError() != cudaSuccess) return NMD_ERR_CUDA;
   }
   return NMD_OK;

@@ -230,9 +230,14 @@ __device__ __forceinline__ Factor3 factor_of(const double* parts, int count, dou
   __syncthreads();
   sum = 0.0;
   for (int i = 0; i < kThreads / 32; ++i) sum += red[i];
+  // norm = s 2^h with s in [1, 2), so that one fp64 product and fp32 do for the rest
+  const bool usual = sum > 0.0 && sum < INFINITY;
+  const int h = usual ? (ilogb(sum) >> 1) : 0;
+  const float s = usual ? sqrtf((float)ldexp(sum, -2 * h)) : (float)sum;
+  const float both = s + (float)ldexp(eps, -h);
   // |X| = 2^-t at most; `grows`: a step takes a small X to 2^grows times itself at most
-  const double norm = sqrt(sum), size = norm / (norm + eps);
-  const int small = size > 0.0 && size < 0x1p-8 ? min(100, -ilogb(size) - 1) : 0;
+  const float size = s / both;
+  const int small = size > 0.f && size < 0x1p-8f ? min(100, -ilogbf(size) - 1) : 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     int t = small;
     for (int i = 0; i <= steps; ++i) {
@@ -242,8 +247,8 @@ __device__ __forceinline__ Factor3 factor_of(const double* parts, int count, dou
   }
   int e = 0;
   Factor3 r;
-  r.f = (float)frexp((double)kUnit / (norm + eps), &e);
-  e = max(-280, min(280, e + small));
+  r.f = frexpf(sum == 0.0 ? 0.f : kUnit / both, &e);   // (an eps below fp32's range is 0 in it)
+  e = max(-280, min(280, e - h + small));
   r.p = ldexpf(1.f, e / 2);
   r.q = ldexpf(1.f, e - e / 2);
   return r;
@@ -849,9 +854,13 @@ int64_t tiles_of(int64_t M, int64_t N, int BN, bool lower) {
   for (int64_t i = 0; i < tm; ++i) n += std::min<int64_t>((kBM * (i + 1) - 1) / BN + 1, tn);
   return n;
 }
-// Tiles of 128 columns where they give every SM one, of 64 otherwise.  (Of 256, half
-// the operand traffic per product, do not leave the epilogue's threads the registers.)
-int columns_of(int64_t M, int64_t N, bool lower) { return N > 64 && tiles_of(M, N, 128, lower) >= kSms ? 128 : 64; }
+// Tiles of 128 columns or of 64: those whose rounds over the SMs take less, at 1250 and
+// 940 cycles a block of the sum.  (Of 256, half the operand traffic per product, do not
+// leave the epilogue's threads the registers.)
+int columns_of(int64_t M, int64_t N, bool lower) {
+  const int64_t wide = (tiles_of(M, N, 128, lower) + kSms - 1) / kSms, narrow = (tiles_of(M, N, 64, lower) + kSms - 1) / kSms;
+  return N > 64 && 125 * wide <= 94 * narrow ? 128 : 64;
+}
 
 // The sums of a Gram matrix run over the long side: tiles, and parts of the sum where there are few of them
 struct GramPlan {

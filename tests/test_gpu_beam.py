@@ -297,6 +297,25 @@ def test_reorder_several_views(shift):
     assert torch.equal(flat[:shift], before[4][:shift]) and torch.equal(flat[shift + B * K * 77:], before[4][shift + B * K * 77:])
 
 
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("inner", [1, 2, 3, 127, 8191, 8193, 20001])
+@pytest.mark.parametrize("K", [2, 7, 64])
+def test_reorder_rows_of_any_phase(shift, inner, K):
+    """16-bit rows that start at every multiple of two bytes; what lies around them stays."""
+    rng = np.random.default_rng(inner)
+    parents = rng.integers(0, K, (3, K))
+    flat = values((3 * K * (inner + 1) + 9,), torch.bfloat16, inner)
+    rows = flat[shift:shift + 3 * K * (inner + 1)].view(3 * K, inner + 1)[:, :inner]
+    want, before = moved(rows, parents), flat.clone()
+    tuning().beam_reorder(rows, cuda(parents))
+    assert torch.equal(rows.double(), want)
+    before[shift:shift + 3 * K * (inner + 1)].view(3 * K, inner + 1)[:, :inner] = want.to(torch.bfloat16)
+    assert torch.equal(flat, before)
+    other = torch.zeros(3 * K, inner, device="cuda", dtype=torch.bfloat16)
+    tuning().beam_reorder(rows, cuda(parents), out=other)
+    assert torch.equal(other.double(), moved(rows, parents))
+
+
 def test_reorder_the_same_state_twice():
     parents = cuda([[1, 2, 0, 0]])
     x = torch.arange(4, device="cuda")[:, None].repeat(1, 999)

@@ -175,6 +175,7 @@ def test_orthogonalize_zero_and_sizes(dtype, rows, cols):
     t = tuning()
     zero = torch.zeros(rows, cols, device="cuda", dtype=DTYPES[dtype])
     assert torch.equal(t.orthogonalize(zero), zero)
+    assert torch.equal(t.orthogonalize(zero, eps=1e-300), zero)
     g = gradient(rows, cols, 5, size=1.0)
     for size in ((1e-30, 1e-5, 1e15, 1e36) if dtype != "fp16" else (1e-3, 1e3)):
         check(place(size * g, dtype))
@@ -339,3 +340,20 @@ def test_refusals():
 def test_orthogonalize_tall(rows, cols, dtype):
     """Long sides at which the tiles of a CTA no longer fit shared memory, or no longer fit on chip."""
     check(place(gradient(rows, cols, 9), dtype))
+
+
+def test_several_streams_at_once():
+    """Steps that each want more than half of the SMs at a time, on three streams."""
+    t = tuning()
+    Gs = [place(gradient(rows, cols, k), "fp32") for k, (rows, cols) in enumerate(((20000, 64), (30000, 33), (64, 25000)))]
+    want = [t.orthogonalize(G) for G in Gs]
+    streams = [torch.cuda.Stream() for _ in Gs]
+    torch.cuda.synchronize()
+    got = [[], [], []]
+    for _ in range(10):
+        for k, (G, s) in enumerate(zip(Gs, streams)):
+            with torch.cuda.stream(s):
+                got[k].append(t.orthogonalize(G))
+    torch.cuda.synchronize()
+    for k in range(3):
+        assert all(torch.equal(x, want[k]) for x in got[k])
