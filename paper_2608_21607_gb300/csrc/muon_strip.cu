@@ -9,11 +9,12 @@
 // and between passes the CTAs' sums Z are added up and every CTA forms
 //   A = Z,  P = a I + b A + c A A
 // for itself.  So nothing of X moves between steps, and a step costs two barriers of the
-// grid instead of four launches.  139,255 x 64 in fp32 takes 85 us of the call's 120 (the
-// rest is the norm and the pieces): a step 15 us, of which the pass over eight tiles is
-// 6, the two barriers 4, A and P 2.  64 x 64 takes 26 us, a chain of latencies; a 32 x
-// 20,000 step 62 us.  (As separate launches: 263, 92 and 164 us a call; tiles that did not
-// fit passed through global memory: 175 us instead of 85.)
+// grid (one among up to eight CTAs) instead of four launches.  139,255 x 64 in fp32 takes
+// 85 us of the call's 115 (the rest is the norm and the pieces): a step 15 us, of which
+// the pass over eight tiles is 6, the two barriers 4, A and P 2.  64 x 64 takes 26 us, a
+// chain of latencies; a 32 x 20,000 step 62 us.  (As separate launches: 263, 92 and 164
+// us a call; tiles that did not fit passed through global memory: 175 us instead of 85;
+// 129 x 64 with the second barrier and each sum by one CTA at a time: 142 us, now 42.)
 //
 // Pieces are put side by side, so that one product of the tensor cores takes two:
 //   X P:    columns [hi P_hi | hi P_lo + lo P_hi],  128 x 128;
@@ -36,6 +37,7 @@ using namespace tc;
 
 constexpr int kThreads = 256, kSms = 152;                  // threads that work; one warp more issues the products
 constexpr int kRows = 128, kSide = 64;
+constexpr int kFew = 8;                                     // CTAs that add up each other's Z without a second barrier
 constexpr int kBuffers = 6;                                 // tiles in shared memory
 constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
 constexpr int kSquare = 2 * kSide * kSide * 2;              // both pieces of a 64 x 64 matrix
@@ -58,7 +60,7 @@ struct Strip {
   int tiles, steps;
   float a, b, c;
   int* ints;
-  float* part;         // the CTAs' Z, 64 x 64 each
+  float* part;         // the CTAs' Z, 64 x 64 each, of two steps
   float* sum;          // 64 x 64
 };
 
@@ -362,34 +364,53 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
     // Z of all CTAs
     fold(z);
     if (G > 1) {
-      float* mine = p.part + (size_t)blockIdx.x * kSide * kSide;
+      // in two places in turn: a CTA may write the next step's while another still reads these
+      const float* parts = p.part + (size_t)(step & 1) * G * kSide * kSide;
+      float* mine = p.part + ((size_t)(step & 1) * G + blockIdx.x) * kSide * kSide;
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) {
         const int e = i * kThreads + tid;
         __stcg(mine + e, Z[z_at(e / kSide, e % kSide)]);
       }
       grid_barrier(p.ints, ++barriers * G, abort_flag, status);
-      // 32 elements of the sum at a time: eight warps take every eighth part each, in order
-      for (int e0 = blockIdx.x * 32; e0 < kSide * kSide; e0 += G * 32) {
-        float v[kSms / 8], s = 0.f;   // all loads under way together
-#pragma unroll
-        for (int q = 0; q < kSms / 8; ++q)
-          v[q] = warp + 8 * q < G ? __ldcg(p.part + (size_t)(warp + 8 * q) * kSide * kSide + e0 + lane) : 0.f;
-#pragma unroll
-        for (int q = 0; q < kSms / 8; ++q) s += v[q];
-        Z[warp * 32 + lane] = s;
-        sync_workers();
-        if (warp == 0) {
-#pragma unroll
-          for (int q = 1; q < 8; ++q) s += Z[q * 32 + lane];
-          __stcg(p.sum + e0 + lane, s);
-        }
-        sync_workers();
-      }
-      grid_barrier(p.ints, ++barriers * G, abort_flag, status);
       float v[kSide * kSide / kThreads];
+      if (G <= kFew) {   // every CTA adds up all of them
 #pragma unroll
-      for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] = __ldcg(p.sum + i * kThreads + tid);
+        for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] = 0.f;
+#pragma unroll 1
+        for (int q = 0; q < G; ++q)
+#pragma unroll
+          for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] += __ldcg(parts + (size_t)q * kSide * kSide + i * kThreads + tid);
+      } else {
+        if (G <= 32) {   // 32 elements by a warp
+          for (int e0 = (blockIdx.x * 8 + warp) * 32; e0 < kSide * kSide; e0 += G * 8 * 32) {
+            float s = 0.f;
+#pragma unroll 16
+            for (int q = 0; q < G; ++q) s += __ldcg(parts + (size_t)q * kSide * kSide + e0 + lane);
+            __stcg(p.sum + e0 + lane, s);
+          }
+        } else {   // by eight warps, every eighth part each, in order
+          for (int e0 = blockIdx.x * 32; e0 < kSide * kSide; e0 += G * 32) {
+            float u[kSms / 8], s = 0.f;   // all loads under way together
+#pragma unroll
+            for (int q = 0; q < kSms / 8; ++q)
+              u[q] = warp + 8 * q < G ? __ldcg(parts + (size_t)(warp + 8 * q) * kSide * kSide + e0 + lane) : 0.f;
+#pragma unroll
+            for (int q = 0; q < kSms / 8; ++q) s += u[q];
+            Z[warp * 32 + lane] = s;
+            sync_workers();
+            if (warp == 0) {
+#pragma unroll
+              for (int q = 1; q < 8; ++q) s += Z[q * 32 + lane];
+              __stcg(p.sum + e0 + lane, s);
+            }
+            sync_workers();
+          }
+        }
+        grid_barrier(p.ints, ++barriers * G, abort_flag, status);
+#pragma unroll
+        for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] = __ldcg(p.sum + i * kThreads + tid);
+      }
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) Z[z_at((i * kThreads + tid) / kSide, tid % kSide)] = v[i];
       sync_workers();
@@ -497,7 +518,7 @@ int grid_of(int64_t tiles) {   // the fewest CTAs with the fewest tiles each
 
 size_t strip_bytes(int64_t M) {
   const int G = grid_of((M + kRows - 1) / kRows);
-  return G > 1 ? (size_t)(G + 1) * kSide * kSide * 4 : 0;
+  return G > 1 ? (size_t)(2 * G + 1) * kSide * kSide * 4 : 0;
 }
 
 nmd_status strip_run(const Job& j, const Pieces& X, int steps, const double* k, int* ints, void* ws, cudaStream_t s) {
@@ -519,7 +540,7 @@ nmd_status strip_run(const Job& j, const Pieces& X, int steps, const double* k, 
   p.ints = ints;
   const int G = grid_of(p.tiles);
   p.part = (float*)ws;
-  p.sum = p.part + (size_t)G * kSide * kSide;
+  p.sum = p.part + (size_t)2 * G * kSide * kSide;
   CUtensorMap tx;
   if (!map_of(X, kRows, &tx)) return NMD_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
