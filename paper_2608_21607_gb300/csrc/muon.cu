@@ -349,7 +349,7 @@ struct Gemm {
   int kblocks, splits;      // blocks of 64 of the sum; parts of it that are tiles of their own
   int chunk;                // blocks whose sum stays in TMEM
   int tiles_m, tiles_n, items;   // tiles down and across; tiles x splits
-  int lower;                // 1: D is symmetric, tiles below and on the diagonal only
+  int lower;                // 1: D is symmetric (B is A), tiles below and on the diagonal only
   int mode;
   float alpha, beta, diag;  // D = alpha 2^(*up - times *down) (sum) + beta C + diag I, in pieces
   const int *up, *down;     // or nullptr
@@ -604,14 +604,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           const int s = (int)(n % C::NS);
           if (!(ok = wait_bar(b_empty + 8 * s, (uint32_t)((n / C::NS) & 1) ^ 1u, abort_flag, p.status, 1))) break;
           const uint32_t full = b_full + 8 * s, dst = stage0 + s * C::STAGE;
-          mbar_expect_tx(full, C::STAGE);
+          const bool once = BN == kBM && p.lower && t.i == t.j;   // on the diagonal both operands are one
+          mbar_expect_tx(full, once ? C::A_BYTES : C::STAGE);
           if (AMN) {
 #pragma unroll
             for (int q = 0; q < kBM / 64; ++q) tma_load_3d(dst + q * 2 * kBK * 128, &ta, full, t.i * kBM + q * 64, k * kBK, 0);
           } else {
             tma_load_3d(dst, &ta, full, k * kBK, t.i * kBM, 0);
           }
-          if (BMN) {
+          if (once) {
+          } else if (BMN) {
 #pragma unroll
             for (int q = 0; q < BN / 64; ++q)
               tma_load_3d(dst + C::A_BYTES + q * 2 * kBK * 128, &tb, full, t.j * BN + q * 64, k * kBK, 0);
@@ -644,7 +646,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (in == 0 && !(ok = conv_wait(b_tempty + 8 * buf, (uint32_t)((ch >> 1) & 1) ^ 1u, abort_flag, p.status, 2))) break;
           if (!(ok = conv_wait(b_full + 8 * s, (uint32_t)((n / C::NS) & 1), abort_flag, p.status, 3))) break;
           fence_after();
-          const uint32_t a0 = stage0 + s * C::STAGE, b0 = a0 + C::A_BYTES, d = tmem + buf * BN;
+          const bool once = BN == kBM && p.lower && t.i == t.j;
+          const uint32_t a0 = stage0 + s * C::STAGE, b0 = once ? a0 : a0 + C::A_BYTES, d = tmem + buf * BN;
           const uint64_t ah = AMN ? sdesc(a0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(a0, 16, 1024, SWZ_128B);
           const uint64_t bh = BMN ? sdesc(b0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(b0, 16, 1024, SWZ_128B);
           // the small products first: what an addition loses is a part of the sum so far
