@@ -357,3 +357,14 @@ def test_several_streams_at_once():
     torch.cuda.synchronize()
     for k in range(3):
         assert all(torch.equal(x, want[k]) for x in got[k])
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(70, 240001, "fp32"), (129, 131000, "bf16"), (515, 33001, "fp16"), (2000, 8400, "fp32")])
+@pytest.mark.parametrize("layout", ["rows", "columns"])
+def test_orthogonalize_wide(rows, cols, dtype, layout):
+    """Long sides split over many CTAs, by rows and by columns in memory; a step is its update."""
+    G = place(gradient(rows, cols, 13), dtype, layout)
+    check(G)
+    W, M = torch.zeros_like(G), torch.zeros_like(G)
+    tuning().muon_step(W, G, M, lr=1.0, beta=0.0, nesterov=False, scale=1.0)
+    assert torch.equal(W, -tuning().orthogonalize(G))
