@@ -73,12 +73,14 @@ __device__ __forceinline__ void sync_workers() { named_bar_sync(1, kThreads); }
 
 // All CTAs' writes before are seen by all after.  `target`: arrivals of all barriers up to
 // this one; the CTA that comes last raises the flag that the others look at, apart from
-// the count.  A wait that runs out (2 s) raises the abort flag; the kernel then goes on
-// without waiting and its result is NaN.
+// the count.  A wait that runs out (2 s) raises the abort flag; the CTA then goes on
+// without waiting.  Its status is there before what it adds up is: the result of every CTA
+// that took part in sums from then on is NaN.
 __device__ __forceinline__ void grid_barrier(int* ints, int target, volatile int* abort_flag, int* status) {
   sync_workers();
   if (threadIdx.x == 0) {
     int n;
+    if (*abort_flag) record(status, NMD_ERR_TIMEOUT, 10);
     asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(ints + kBarrier) : "memory");
     if (n + 1 == target) {
       asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(ints + kFlag), "r"(target) : "memory");
@@ -177,9 +179,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
   char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float* Z = (float*)(smem + kOffZ);
   const uint32_t base = smem_u32(smem), sP = base + kOffP, bars = base + kOffBars;
-  const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16, b_done = b_z + 8;
-  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 5));
+  const uint32_t b_full = bars, b_xp = bars + 8 * kBuffers, b_z = b_xp + 16, b_done = b_z + 8, b_drain = b_done + 16;
+  uint32_t* slot = (uint32_t*)(smem + kOffBars + 8 * (kBuffers + 6));
   volatile int* abort_flag = (volatile int*)(slot + 1);
+  volatile int* others = (volatile int*)(slot + 2);   // another CTA's wait ran out
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;     // TMEM lanes and columns of this warp
   const int row = quad * 32 + lane;                // of a tile, or of [hi; lo]
@@ -198,8 +201,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
     prefetch_tmap(&tx);
     for (int i = 0; i < kBuffers + 3; ++i) mbar_init(bars + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(b_done + 8 * i, kThreads / 32);
+    mbar_init(b_drain, 1);
     fence_mbar_init();
     *abort_flag = 0;
+    *others = 0;
   }
   if (warp == 0) {
     tmem_alloc(smem_u32(slot), kTmem);
@@ -288,6 +293,20 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
         if (step + 1 < p.steps) issue_z(t);
         if (t + 2 < T) issue_xp(t + 2);
       }
+    }
+    __syncwarp();
+    if (*abort_flag) {   // copies and products that nothing waited for land before this memory is given back
+      commit_elect(b_drain);
+      if (lane == 0) {
+        const uint64_t t0 = globaltimer_ns();
+        auto drain = [&](uint32_t bar, uint32_t parity) {
+          while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 < 200000000ull) {
+          }
+        };
+        for (int t = 0; t < T; ++t) drain(b_full + 8 * buffer_of(t), (ph_full >> buffer_of(t) & 1u) ^ 1u);
+        drain(b_drain, 0);
+      }
+      __syncwarp();
     }
     fence_before();
     __syncthreads();
@@ -413,6 +432,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
       }
 #pragma unroll
       for (int i = 0; i < kSide * kSide / kThreads; ++i) Z[z_at((i * kThreads + tid) / kSide, tid % kSide)] = v[i];
+      if (last && tid == 0) *others = *(volatile int*)status;
       sync_workers();
     }
     // A in pieces, [hi; lo]; a thread has 16 columns of a row
@@ -494,7 +514,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
         for (int q = 0; q < 8; ++q)
           *(float4*)(stage + group_at(row, half * 8 + q)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
         sync_workers();
-        const float fill = *abort_flag ? NAN : 0.f;   // the result of a wait that ran out shows
+        const float fill = *abort_flag || *others ? NAN : 0.f;   // the result of a wait that ran out shows
         if (p.j.out.dtype == NMD_DT_FP32) put_tile<float>(p, stage, m0, fill);
         else if (p.j.out.dtype == NMD_DT_BF16) put_tile<bf16>(p, stage, m0, fill);
         else put_tile<__half>(p, stage, m0, fill);
