@@ -19,11 +19,11 @@
 //
 // A step is three products: the Gram matrix (half of its tiles, the sum split where there
 // are few), the polynomial (likewise half), and the update.  4096 x 4096 in bf16 takes
-// 3.4 ms: 0.18 + 0.20 + 0.29 ms a step, the update at 1.4 PFLOP/s of MMAs, 0.74 of the
-// measured burst rate.  There the operands' way bounds it: a stage of 64 KB is written to
-// shared memory and its tiles read three times for 768 cycles of products (tensor cores
-// busy in 0.64 of the cycles).  256 x 139,255 in bf16 takes 0.69 ms: its pieces, 142 MB,
-// do not stay in L2 and are read twice and written once a step.  Small matrices are bound
+// 3.2 ms: 0.16 + 0.18 + 0.29 ms a step, the update at 1.44 PFLOP/s of MMAs, 0.76 of the
+// measured burst rate.  There the operands' way bounds it, at about 52 bytes a cycle from
+// L2 to an SM, and the last round of tiles (512 on 152 SMs).
+// 256 x 139,255 in bf16 takes 0.69 ms: its pieces, 142 MB, do not stay in L2 and are read
+// twice and written once a step.  Small matrices are bound
 // by the launches, 4 us each (2047 x 1001 in 0.31 ms).  Short sides up to 64: muon_strip.cu.
 #include <algorithm>
 #include <cmath>
@@ -346,8 +346,8 @@ enum Mode { kSymmetric, kPartial, kMatrix, kResult };
 
 struct Gemm {
   int64_t M, N;             // D is M x N
-  int kblocks, splits;      // blocks of 64 of the sum; parts of it that are tiles of their own
-  int chunk;                // blocks whose sum stays in TMEM
+  int kblocks, splits;      // stages of the sum; parts of it that are tiles of their own
+  int chunk;                // stages whose sum stays in TMEM
   int tiles_m, tiles_n, items;   // tiles down and across; tiles x splits
   int lower;                // 1: D is symmetric (B is A), tiles below and on the diagonal only
   int mode;
@@ -361,13 +361,15 @@ struct Gemm {
 };
 
 constexpr int kBM = 128, kBK = 64;   // rows of a tile, products of a stage
-constexpr int kEpilogue = 256, kProducer = 8, kIssuer = 9, kGemmThreads = 320;
+// (of tiles of 256 columns half as many, four stages: 3.13 ms for 4096 x 4096, in two 3.30)
+__host__ __device__ constexpr int depth_of(int BN) { return BN > 128 ? kBK / 2 : kBK; }
 template <int BN>
 struct Cfg {
-  static constexpr int A_BYTES = 2 * kBM * kBK * 2, B_BYTES = 2 * BN * kBK * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr int BK = depth_of(BN), A_BYTES = 2 * kBM * BK * 2, B_BYTES = 2 * BN * BK * 2, STAGE = A_BYTES + B_BYTES;
   static constexpr int NS = 196608 / STAGE;
   static constexpr int TMEM = 2 * BN;
-  static constexpr size_t OFF_TURN = (size_t)NS * STAGE;                // a 32 x 32 square per epilogue warp
+  static constexpr int EPILOGUE = BN > 128 ? 16 : 8, PRODUCER = EPILOGUE, ISSUER = EPILOGUE + 1, THREADS = 32 * (EPILOGUE + 2);   // warps
+  static constexpr size_t OFF_TURN = (size_t)NS * STAGE;                // eight 32 x 32 squares for the epilogue's warps
   static constexpr size_t OFF_BARS = OFF_TURN + 8 * 4096;
   static constexpr int NBAR = 2 * NS + 5;
   static constexpr size_t SMEM = 1024 + OFF_BARS + NBAR * 8 + 16;
@@ -554,9 +556,11 @@ __device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq
 // Work items (tile, part of the sum) are dealt to one CTA per SM in turn; two TMEM
 // buffers and the ring of stages run on from one item to the next.
 template <int BN, bool AMN, bool BMN>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Gemm p) {
   using C = Cfg<BN>;
+  constexpr int BK = C::BK;
+  constexpr uint32_t kAlong = BK == 64 ? SWZ_128B : SWZ_64B;   // of an operand whose sum runs along its rows
   extern __shared__ char smem_raw[];
   char* smem = (char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const uint32_t stage0 = smem_u32(smem);
@@ -577,13 +581,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(b_tfull + 8 * b, 1);
-      mbar_init(b_tempty + 8 * b, kEpilogue / 32);
+      mbar_init(b_tempty + 8 * b, C::EPILOGUE);
     }
     mbar_init(b_drain, 1);
     fence_mbar_init();
     *abort_flag = 0;
   }
-  if (warp == kIssuer) {
+  if (warp == C::ISSUER) {
     tmem_alloc(smem_u32(slot), C::TMEM);
     tmem_relinquish();
   }
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   fence_after();
   const uint32_t tmem = *(volatile uint32_t*)slot;
   const bool dead = *dead_word != 0;
-  if (warp == kProducer) {
+  if (warp == C::PRODUCER) {
     if (lane == 0 && !dead) {
       int64_t n = 0;
       bool ok = true;
@@ -608,17 +612,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           mbar_expect_tx(full, once ? C::A_BYTES : C::STAGE);
           if (AMN) {
 #pragma unroll
-            for (int q = 0; q < kBM / 64; ++q) tma_load_3d(dst + q * 2 * kBK * 128, &ta, full, t.i * kBM + q * 64, k * kBK, 0);
+            for (int q = 0; q < kBM / 64; ++q) tma_load_3d(dst + q * 2 * BK * 128, &ta, full, t.i * kBM + q * 64, k * BK, 0);
           } else {
-            tma_load_3d(dst, &ta, full, k * kBK, t.i * kBM, 0);
+            tma_load_3d(dst, &ta, full, k * BK, t.i * kBM, 0);
           }
           if (once) {
           } else if (BMN) {
 #pragma unroll
             for (int q = 0; q < BN / 64; ++q)
-              tma_load_3d(dst + C::A_BYTES + q * 2 * kBK * 128, &tb, full, t.j * BN + q * 64, k * kBK, 0);
+              tma_load_3d(dst + C::A_BYTES + q * 2 * BK * 128, &tb, full, t.j * BN + q * 64, k * BK, 0);
           } else {
-            tma_load_3d(dst + C::A_BYTES, &tb, full, k * kBK, t.j * BN, 0);
+            tma_load_3d(dst + C::A_BYTES, &tb, full, k * BK, t.j * BN, 0);
           }
         }
       }
@@ -630,11 +634,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
     }
     __syncwarp();
-  } else if (warp == kIssuer) {
+  } else if (warp == C::ISSUER) {
     if (!dead) {
       constexpr uint32_t idesc = idesc_fp16(kBM, BN, AMN, BMN);
       // between the hi and the lo tile of a stage, and between steps of 16 products
-      constexpr uint32_t A_LO = AMN ? kBK * 128 : kBM * 128, B_LO = BMN ? kBK * 128 : BN * 128;
+      constexpr uint32_t A_LO = AMN ? BK * 128 : kBM * BK * 2, B_LO = BMN ? BK * 128 : BN * BK * 2;
       constexpr uint32_t A_STEP = AMN ? 16 * 128 : 32, B_STEP = BMN ? 16 * 128 : 32;
       int64_t n = 0, ch = 0;
       bool ok = true;
@@ -648,17 +652,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           fence_after();
           const bool once = BN == kBM && p.lower && t.i == t.j;
           const uint32_t a0 = stage0 + s * C::STAGE, b0 = once ? a0 : a0 + C::A_BYTES, d = tmem + buf * BN;
-          const uint64_t ah = AMN ? sdesc(a0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(a0, 16, 1024, SWZ_128B);
-          const uint64_t bh = BMN ? sdesc(b0, 2 * kBK * 128, 1024, SWZ_128B) : sdesc(b0, 16, 1024, SWZ_128B);
+          const uint64_t ah = AMN ? sdesc(a0, 2 * BK * 128, 1024, SWZ_128B) : sdesc(a0, 16, BK * 16, kAlong);
+          const uint64_t bh = BMN ? sdesc(b0, 2 * BK * 128, 1024, SWZ_128B) : sdesc(b0, 16, BK * 16, kAlong);
           // the small products first: what an addition loses is a part of the sum so far
 #pragma unroll
-          for (int q = 0; q < kBK / 16; ++q) {
+          for (int q = 0; q < BK / 16; ++q) {
             const uint64_t a = ah + ((q * A_STEP) >> 4), b = bh + ((q * B_STEP) >> 4);
             mma_ss_elect(d, a + (A_LO >> 4), b, idesc, q > 0 || in > 0);
             mma_ss_elect(d, a, b + (B_LO >> 4), idesc, 1);
           }
 #pragma unroll
-          for (int q = 0; q < kBK / 16; ++q) mma_ss_elect(d, ah + ((q * A_STEP) >> 4), bh + ((q * B_STEP) >> 4), idesc, 1);
+          for (int q = 0; q < BK / 16; ++q) mma_ss_elect(d, ah + ((q * A_STEP) >> 4), bh + ((q * B_STEP) >> 4), idesc, 1);
           commit_elect(b_empty + 8 * s);
           if (in == p.chunk - 1 || k + 1 == t.k1) {
             commit_elect(b_tfull + 8 * buf);
@@ -674,11 +678,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       __syncwarp();
     }
-  } else if (warp < kEpilogue / 32) {
-    constexpr int G = BN / 64;   // groups of 32 columns of a warpgroup
+  } else if (warp < C::EPILOGUE) {
+    constexpr int G = BN / 8 / C::EPILOGUE;   // groups of 32 columns of a warpgroup
+    constexpr bool kShared = C::EPILOGUE > 8;   // two warps of the same rows use a square in turn
     const int part = warp >> 2, row = (warp & 3) * 32;
     const uint32_t lanes = (uint32_t)row << 16;
-    float* square = (float*)(smem + C::OFF_TURN) + warp * 1024;
+    float* square = (float*)(smem + C::OFF_TURN) + (warp & 7) * 1024;
     const float alpha = scale_of_sum(p);
     int64_t ch = 0;
     bool ok = !dead;
@@ -694,25 +699,40 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const int buf = (int)(ch & 1);
         if (!(ok = warp_wait(b_tfull + 8 * buf, (uint32_t)((ch >> 1) & 1), abort_flag, p.status, 4))) break;
         fence_after();
-        uint32_t v[G][32];   // all loads, and the buffer is free again
+        if constexpr (kShared) {   // (96 registers a thread: half a group at a time)
 #pragma unroll
-        for (int g = 0; g < G; ++g) tmem_ld32(tmem + lanes + buf * BN + (part * G + g) * 32, v[g]);
+          for (int h = 0; h < 2 * G; ++h) {
+            uint32_t v[16];
+            tmem_ld16(tmem + lanes + buf * BN + part * G * 32 + h * 16, v);
+            tmem_wait_ld(v);
 #pragma unroll
-        for (int g = 0; g < G; ++g) tmem_wait_ld(v[g]);
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b_tempty + 8 * buf);
+            for (int i = 0; i < 16; ++i) acc[h / 2][h % 2 * 16 + i] += __uint_as_float(v[i]);
+          }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_tempty + 8 * buf);
+        } else {
+          uint32_t v[G][32];   // all loads, and the buffer is free again
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+          for (int g = 0; g < G; ++g) tmem_ld32(tmem + lanes + buf * BN + (part * G + g) * 32, v[g]);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[g][i] += __uint_as_float(v[g][i]);
+          for (int g = 0; g < G; ++g) tmem_wait_ld(v[g]);
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_tempty + 8 * buf);
+#pragma unroll
+          for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[g][i] += __uint_as_float(v[g][i]);
+        }
       }
-      if (!ok && p.mode != kResult) break;
+      if (!ok && p.mode != kResult && !kShared) break;   // (two warps that share a square meet to the end)
       const int64_t r = (int64_t)t.i * kBM + row;
       if (r >= p.M && p.mode != kPartial) continue;
-#pragma unroll 1
+#pragma unroll(kShared ? G : 1)
       for (int g = 0; g < G; ++g) {
         const int col = (part * G + g) * 32;
+        if (kShared && part >= 2) named_bar_sync(1 + (warp & 7), 64);
         __syncwarp();
         float v[32];
 #pragma unroll
@@ -723,24 +743,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
         if (p.mode == kMatrix) {
           put_rows_of(p, alpha, v, square, r, (int64_t)t.j * BN + col);
-          continue;
-        }
-        if (p.mode == kPartial) {
+        } else if (p.mode == kPartial) {
           float4* at = (float4*)(p.part + ((int64_t)w * kBM + row + lane) * BN + col);
 #pragma unroll
           for (int q = 0; q < 8; ++q) at[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-          continue;
-        }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) in_square(square, lane, i) = ok ? v[i] : NAN;   // the result of a wait that ran out shows
-        __syncwarp();
-        put_square<(BN > 64)>(p, alpha, square, r, (int64_t)t.j * BN + col);
+          for (int i = 0; i < 32; ++i) in_square(square, lane, i) = ok ? v[i] : NAN;   // the result of a wait that ran out shows
+          __syncwarp();
+          put_square<(BN > 64)>(p, alpha, square, r, (int64_t)t.j * BN + col);
+        }
+        if (kShared) {
+          named_bar_sync(1 + (warp & 7), 64);
+          if (part < 2) named_bar_sync(1 + (warp & 7), 64);
+        }
       }
     }
   }
   fence_before();
   __syncthreads();
-  if (warp == kIssuer) {
+  if (warp == C::ISSUER) {
     fence_after();
     tmem_dealloc(tmem, C::TMEM);
   }
@@ -839,13 +861,15 @@ nmd_status launch_bn(const Pieces& a, const Pieces& b, const Gemm& g, cudaStream
       }))
     return NMD_ERR_CUDA;
   CUtensorMap ta, tb;
-  if (!map_of(a, AMN ? 64 : kBM, &ta) || !map_of(b, BMN ? 64 : BN, &tb)) return NMD_ERR_CUDA;
+  constexpr int BK = Cfg<BN>::BK;
+  if (!map_of(a, AMN ? BK : kBM, &ta, AMN ? 64 : BK) || !map_of(b, BMN ? BK : BN, &tb, BMN ? 64 : BK)) return NMD_ERR_CUDA;
   const int sms = sm_count();
   if (sms == 0) return NMD_ERR_CUDA;
-  return start(kernel, std::min(g.items, sms), kGemmThreads, Cfg<BN>::SMEM, s, ta, tb, g);
+  return start(kernel, std::min(g.items, sms), Cfg<BN>::THREADS, Cfg<BN>::SMEM, s, ta, tb, g);
 }
 template <bool AMN, bool BMN>
 nmd_status launch(int BN, const Pieces& a, const Pieces& b, const Gemm& g, cudaStream_t s) {
+  if (BN == 256) return launch_bn<256, AMN, BMN>(a, b, g, s);
   if (BN == 128) return launch_bn<128, AMN, BMN>(a, b, g, s);
   return launch_bn<64, AMN, BMN>(a, b, g, s);
 }
@@ -857,12 +881,27 @@ int64_t tiles_of(int64_t M, int64_t N, int BN, bool lower) {
   for (int64_t i = 0; i < tm; ++i) n += std::min<int64_t>((kBM * (i + 1) - 1) / BN + 1, tn);
   return n;
 }
-// Tiles of 128 columns or of 64: those whose rounds over the SMs take less, at 1250 and
-// 940 cycles a block of the sum.  (Of 256, half the operand traffic per product, do not
-// leave the epilogue's threads the registers.)
-int columns_of(int64_t M, int64_t N, bool lower) {
-  const int64_t wide = (tiles_of(M, N, 128, lower) + kSms - 1) / kSms, narrow = (tiles_of(M, N, 64, lower) + kSms - 1) / kSms;
-  return N > 64 && 125 * wide <= 94 * narrow ? 128 : 64;
+// Tiles of 256, 128 or 64 columns: those whose rounds over the SMs take least, at 2200,
+// 1250 and 940 cycles a block of the sum.  Tiles of 256 read a quarter less per product,
+// but take twice as long after their last one, and lose where a sum leaves TMEM every 64
+// columns: `wide` for 16-bit results and deep sums.  With them 4096 x 4096 in bf16 takes
+// 3.17 instead of 3.33 ms, 8192 x 2560 2.22 instead of 2.39, 11008 x 4096 7.1 instead of
+// 7.5; sums of 512 (16384 x 512) 416 instead of 405 us, fp32 4096 x 4096 4.02 instead of
+// 3.88 ms.  (Pairs of CTAs that share the second operand, 256 x 256 by both: 3.21 ms in
+// three stages, 3.39 in six of half the depth.)
+constexpr int64_t kWideDepth = 1280;
+int columns_of(int64_t M, int64_t N, bool lower, bool wide) {
+  int best = 64;
+  int64_t least = INT64_MAX;
+  for (const int BN : {256, 128, 64}) {
+    if ((BN > 64 && N <= BN / 2) || (BN > 128 && !wide)) continue;
+    const int64_t cycles = (tiles_of(M, N, BN, lower) + kSms - 1) / kSms * (BN == 256 ? 2200 : BN == 128 ? 1250 : 940);
+    if (cycles < least) {
+      least = cycles;
+      best = BN;
+    }
+  }
+  return best;
 }
 
 // The sums of a Gram matrix run over the long side: tiles, and parts of the sum where there are few of them
@@ -870,11 +909,11 @@ struct GramPlan {
   int BN;
   int64_t tiles, splits;
 };
-GramPlan gram_plan(int64_t r, int64_t M) {
+GramPlan gram_plan(int64_t r, int64_t M, bool wide) {
   GramPlan g;
   const int64_t blocks = (M + kBK - 1) / kBK;
   if (blocks <= 20) {   // the sum of 20 blocks takes what adding parts up would (8 us)
-    g.BN = columns_of(r, r, true);
+    g.BN = columns_of(r, r, true, wide);
     g.tiles = tiles_of(r, r, g.BN, true);
     g.splits = 1;
     return g;
@@ -882,6 +921,10 @@ GramPlan gram_plan(int64_t r, int64_t M) {
   g.BN = r <= 64 ? 64 : 128;
   g.tiles = tiles_of(r, r, g.BN, true);
   g.splits = std::max<int64_t>(1, std::min<int64_t>(kSms / g.tiles, blocks / 2));
+  if (g.splits == 1) {
+    g.BN = columns_of(r, r, true, wide);
+    g.tiles = tiles_of(r, r, g.BN, true);
+  }
   return g;
 }
 
@@ -898,7 +941,7 @@ Layout layout_of(int64_t R, int64_t C) {
   l.ldx = (C + 63) / 64 * 64;
   l.r = std::min(R, C);
   l.ldr = (l.r + 63) / 64 * 64;
-  const GramPlan g = gram_plan(l.r, std::max(R, C));
+  const GramPlan g = gram_plan(l.r, std::max(R, C), false);
   l.strip = l.r <= kStripSide && std::max(R, C) <= kStripMost;
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -961,13 +1004,14 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
   });
   if (st != NMD_OK) return st;
   if (l.strip) return strip_run(j, X, steps, k, status, w + l.part, s);
-  const GramPlan plan = gram_plan(r, M);
-  const int bn_r = columns_of(r, r, true), bn_x = columns_of(j.R, j.C, false);
+  auto wide_tiles = [&](int64_t depth) { return j.out.dtype != NMD_DT_FP32 && depth >= kWideDepth; };
+  const GramPlan plan = gram_plan(r, M, wide_tiles(M));
+  const int bn_r = columns_of(r, r, true, wide_tiles(r)), bn_x = columns_of(j.R, j.C, false, wide_tiles(r));
   auto product = [&](int64_t m, int64_t n, int64_t depth, int BN, bool lower, Mode mode) {
     Gemm g{};
     g.M = m;
     g.N = n;
-    g.kblocks = (int)((depth + kBK - 1) / kBK);
+    g.kblocks = (int)((depth + depth_of(BN) - 1) / depth_of(BN));
     g.splits = 1;
     g.tiles_m = (int)((m + kBM - 1) / kBM);
     g.tiles_n = (int)((n + BN - 1) / BN);
@@ -978,7 +1022,7 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
     // A 16-bit result does not see what sums of 256 lean by (5e-7), and a whole sum of that
     // length in TMEM lets the epilogue work beside the next tile's products (256 x 139,255
     // bf16: 760 us with sums of 64)
-    g.chunk = j.out.dtype == NMD_DT_FP32 ? 1 : 4;
+    g.chunk = (j.out.dtype == NMD_DT_FP32 ? 64 : 256) / depth_of(BN);
     return g;
   };
   for (int i = 0; i < steps; ++i) {

@@ -66,15 +66,15 @@ __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
 __device__ __forceinline__ void ready_for_next() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// boxes of 64 columns x `rows` rows x both pieces
-inline bool map_of(const Pieces& x, int rows, CUtensorMap* m) {
+// boxes of 64 (or 32) columns x `rows` rows x both pieces
+inline bool map_of(const Pieces& x, int rows, CUtensorMap* m, int cols = 64) {
   const auto encode = tc::encode_fn();
   if (!encode) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2};
   const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane() * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)rows, 2}, one[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)cols, (cuuint32_t)rows, 2}, one[3] = {1, 1, 1};
   return encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.hi, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // ints at the start of a call's workspace: status and its detail, the shift t of X before

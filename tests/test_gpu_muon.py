@@ -368,3 +368,14 @@ def test_orthogonalize_wide(rows, cols, dtype, layout):
     W, M = torch.zeros_like(G), torch.zeros_like(G)
     tuning().muon_step(W, G, M, lr=1.0, beta=0.0, nesterov=False, scale=1.0)
     assert torch.equal(W, -tuning().orthogonalize(G))
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(1400, 3000, "bf16"), (2433, 2500, "fp16"), (1290, 20001, "bf16"), (1281, 2300, "fp32")])
+@pytest.mark.parametrize("layout", ["rows", "columns"])
+def test_orthogonalize_large(rows, cols, dtype, layout):
+    """Tiles of 256 columns: the update's of 16-bit results, and at (2433, 2500) the symmetric products' too."""
+    G = place(gradient(rows, cols, 17), dtype, layout)
+    check(G)
+    W, M = torch.zeros_like(G), torch.zeros_like(G)
+    tuning().muon_step(W, G, M, lr=1.0, beta=0.0, nesterov=False, scale=1.0)
+    assert torch.equal(W, -tuning().orthogonalize(G))
