@@ -19,9 +19,10 @@
 //
 // A step is three products: the Gram matrix (half of its tiles, the sum split where there
 // are few), the polynomial (likewise half), and the update.  4096 x 4096 in bf16 takes
-// 3.2 ms: 0.16 + 0.18 + 0.29 ms a step, the update at 1.44 PFLOP/s of MMAs, 0.76 of the
-// measured burst rate.  There the operands' way bounds it, at about 52 bytes a cycle from
-// L2 to an SM, and the last round of tiles (512 on 152 SMs).
+// 3.2 ms: 0.16 + 0.18 + 0.29 ms a step, the update at 1.41 PFLOP/s of MMAs, 0.75 of the
+// measured burst rate.  There the operands' way bounds it: shared memory takes a block of
+// 64 KB and gives three reads of its tiles for 768 cycles of products, 160 KB at 128 bytes
+// a cycle (1240 cycles measured); call after call it is the power limit (3.45 ms at 1,370 W).
 // 256 x 139,255 in bf16 takes 0.69 ms: its pieces, 142 MB, do not stay in L2 and are read
 // twice and written once a step.  Small matrices are bound
 // by the launches, 4 us each (2047 x 1001 in 0.31 ms).  Short sides up to 64: muon_strip.cu.
@@ -882,8 +883,8 @@ int64_t tiles_of(int64_t M, int64_t N, int BN, bool lower) {
   return n;
 }
 // Tiles of 256, 128 or 64 columns: those whose rounds over the SMs take least, at 2200,
-// 1250 and 940 cycles a block of the sum.  Tiles of 256 read a quarter less per product,
-// but take twice as long after their last one, and lose where a sum leaves TMEM every 64
+// 1250 and 940 cycles a block of the sum.  Tiles of 256 move a quarter less per product
+// through shared memory (1875 cycles for 1536 of products), but take twice as long after their last one, and lose where a sum leaves TMEM every 64
 // columns: `wide` for 16-bit results and deep sums.  With them 4096 x 4096 in bf16 takes
 // 3.17 instead of 3.33 ms, 8192 x 2560 2.22 instead of 2.39, 11008 x 4096 7.1 instead of
 // 7.5; sums of 512 (16384 x 512) 416 instead of 405 us, fp32 4096 x 4096 4.02 instead of
