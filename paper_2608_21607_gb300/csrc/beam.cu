@@ -11,8 +11,9 @@
 //
 // What is largest is found on the way at the cost of one comparison per four vectors:
 // a group of elements whose sum of powers is below the power of the width-th largest
-// so far holds nothing that could displace it.  (The elements themselves are looked at
-// in the few groups that pass.)
+// so far holds nothing that could displace it.  Of the groups that pass, all of them
+// where a row is flat, the largest element is compared; the elements themselves are
+// looked at in the few that still pass.
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -137,49 +138,52 @@ struct Best {
 };
 
 // A first bar: the width-th largest of the maxima of groups of elements that threads
-// have in hand, as at least that many elements are not below it.  Where there are as
-// many of 32 groups of threads, every warp ranks them; otherwise they are those of
-// single threads.  `vectors`: of the segment.
+// have in hand, as at least that many elements are not below it.  A maximum's column is
+// taken to be the last of the vector that has it, so that rows of equal values offer few.
+// Where there are as many of 32 groups of threads, every warp ranks them; otherwise they
+// are those of single threads.  `vectors`: of the segment, from column `col0` on.
 template <class T, class G>
-__device__ __forceinline__ entry_t first_bar(G get, int vectors, const Best& best, entry_t* bests) {
+__device__ __forceinline__ entry_t first_bar(G get, int64_t col0, int vectors, const Best& best, entry_t* bests) {
   float m = Vec<T>::top(get(0));
+  int at = 0;
 #pragma unroll
-  for (int q = 1; q < 4; ++q) m = max_nan(m, Vec<T>::top(get(q)));
-  uint32_t o = order_of(m);
+  for (int q = 1; q < 4; ++q) {
+    const float f = Vec<T>::top(get(q));
+    if (f > m) at = q;
+    m = max_nan(m, f);
+  }
+  entry_t o = entry_of(m, col0 + (int64_t)(at * kThreads + threadIdx.x + 1) * Vec<T>::N - 1);   // no two are equal
   const int lane = threadIdx.x & 31;
   entry_t bar = *best.least;
   constexpr int kGroup = kThreads / 32;
   if (kGroup * best.width <= min(vectors, kThreads)) {
 #pragma unroll
     for (int d = 1; d < kGroup; d *= 2) o = max(o, __shfl_xor_sync(0xffffffffu, o, d));
-    uint32_t* all = (uint32_t*)bests;
-    if (lane % kGroup == 0) all[threadIdx.x / kGroup] = o;
+    if (lane % kGroup == 0) bests[threadIdx.x / kGroup] = o;
     __syncthreads();
-    o = all[lane];
+    o = bests[lane];
     int rank = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint4 u = ((const uint4*)all)[k];
-      rank += (u.x > o) + (u.y > o) + (u.z > o) + (u.w > o);
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+      const ulonglong2 u = ((const ulonglong2*)bests)[k];
+      rank += (u.x > o) + (u.y > o);
     }
-    rank += __popc(__match_any_sync(0xffffffffu, o) & ((1u << lane) - 1));   // equal ones in the order of the lanes
     o = __shfl_sync(0xffffffffu, o, __ffs(__ballot_sync(0xffffffffu, rank == best.width - 1)) - 1);
-    bar = max(bar, (entry_t)o << 32);
+    bar = max(bar, o - 1);
     if (lane == 0) *best.least = bar;   // every warp the same
     __syncwarp();
   } else {
     if (vectors < best.width) return bar;   // the same for all
-    const entry_t mine = (entry_t)o << 32 | threadIdx.x;
-    bests[threadIdx.x] = mine;
+    bests[threadIdx.x] = o;
     __syncthreads();
     int rank = 0;
     const int some = min((vectors + 1) & ~1, kThreads);   // (of the others o is that of -inf)
 #pragma unroll 4
     for (int k = 0; k < some; k += 2) {
       const ulonglong2 u = *(const ulonglong2*)(bests + k);
-      rank += (u.x > mine) + (u.y > mine);
+      rank += (u.x > o) + (u.y > o);
     }
-    if (threadIdx.x < some && rank == best.width - 1) *best.least = max(bar, (entry_t)o << 32);
+    if (threadIdx.x < some && rank == best.width - 1) *best.least = max(bar, o - 1);
     __syncthreads();
     bar = *best.least;
   }
@@ -189,7 +193,7 @@ __device__ __forceinline__ entry_t first_bar(G get, int vectors, const Best& bes
 // A segment's largest entries again, where there were more offers than room: one
 // vector of a thread at a time, and where more than `width` threads have something to
 // offer, the width-th of their largest entries is the bar first.  A round adds at most
-// 8 width entries.  Rows that rise from column to column, and rows of few values.
+// 8 width entries.  Rows that rise from column to column.
 template <class T>
 __device__ __noinline__ void again(Best best, entry_t* bests, const uint4* xv, int n, int64_t col0, T xs, int64_t scalar) {
   constexpr int N = Vec<T>::N;
@@ -241,7 +245,7 @@ Shape shape_of(int64_t K, int width, int cluster, bool small = false) {
   s.small = small;
   s.cluster = cluster;
   s.limit = 2 * width;
-  s.room = s.limit + 36 * width;
+  s.room = s.limit + (width <= 32 ? 64 : 36) * width;   // (in rows of equal values a first round offers eight vectors for each)
   s.off_list = (size_t)kDepth * 4 * kThreads * 16;   // (16-byte aligned, as the pairs that are read of it)
   s.off_sorted = s.off_list + (size_t)s.room * 8;
   s.off_all = s.off_sorted + (size_t)width * 8;
@@ -265,7 +269,10 @@ __device__ __forceinline__ void put_remote(uint32_t at, entry_t v) {
 // TB/s and the rest the start, the last cut and the merge, which nothing covers as all
 // CTAs run at a time (twice as many CTAs: 49 us).  64 groups of eight rows of 50,001 fp16
 // columns 30 us; one group of four rows of 139,255 18 us, eight CTAs' latency.  A bar that
-// needs every element compared, or a list per warp, cost as much again as the sums.
+// needs every element compared, or a list per warp, cost as much again as the sums.  The
+// 128 groups with logits of standard deviation one take 42 us (108 without the groups'
+// maxima), and with all logits equal 51 (205 with a first bar that is a value alone, whose
+// offers run over).
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_constant__ Select a, const __grid_constant__ Shape shape) {
   constexpr int N = Vec<T>::N;
@@ -394,34 +401,42 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       __syncwarp();
     }
   }
-  int row = 0;
-  for (int64_t at = shape.small ? to : from; at < to;) {
+  // A segment: its row, its vectors, and the element before or after the row's vectors that
+  // this thread has.  What comes first of it is under way before the one before is finished.
+  int row = 0, n = 0, ahead = 0;
+  int64_t at = shape.small ? to : from, col0 = 0, scalar = -1;   // col0: of its first vector
+  const uint4* xv = nullptr;
+  T xs = Vec<T>::put(0.f);
+  auto load = [&](int slot) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q, ahead += kThreads)
+      if (ahead < n) copy_async(tc::smem_u32(mine + (slot * 4 + q) * kThreads), xv + ahead);
+      else slots[(slot * 4 + q) * kThreads + tid] = Vec<T>::none();   // -inf past the segment's end
+    copy_commit();
+  };
+  auto begin = [&] {   // the segment at `at`
     while (at >= (row + 1) * a.V) ++row;
     const int64_t e0 = at - row * a.V, e1 = min(a.V, to - row * a.V);
     at = row * a.V + e1;
     const T* x = (const T*)a.x + (b * a.K + row_beam[row]) * a.ld;
     const Span sp = span_of(x, a.V);
-    // this segment's vectors; the cut between two CTAs falls on the same vector for both
+    // the cut between two CTAs falls on the same vector for both
     auto vector_at = [&](int64_t e) { return e == 0 ? (int64_t)0 : e == a.V ? sp.nvec : min(sp.nvec, max((int64_t)0, (e - sp.head) / N)); };
     const int64_t v0 = vector_at(e0);
-    const int n = (int)(vector_at(e1) - v0);
-    const uint4* xv = (const uint4*)(x + sp.head) + v0;
-    // elements before and after the row's vectors
-    int64_t scalar = -1;
+    n = (int)(vector_at(e1) - v0);
+    xv = (const uint4*)(x + sp.head) + v0;
+    col0 = sp.head + v0 * N;
+    scalar = -1;
     if (e0 == 0 && tid < sp.head) scalar = tid;
     if (e1 == a.V && tid >= 32 && tid - 32 < sp.tail) scalar = sp.head + sp.nvec * N + tid - 32;
-
-    int ahead = tid;
-    auto load = [&](int slot) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q, ahead += kThreads)
-        if (ahead < n) copy_async(tc::smem_u32(mine + (slot * 4 + q) * kThreads), xv + ahead);
-        else slots[(slot * 4 + q) * kThreads + tid] = Vec<T>::none();   // -inf past the segment's end
-      copy_commit();
-    };
+    ahead = tid;
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) load(d);
-    const T xs = scalar >= 0 ? x[scalar] : Vec<T>::put(0.f);
+    if (scalar >= 0) xs = x[scalar];
+  };
+  bool more = at < to;
+  if (more) begin();
+  while (more) {
     if (tid == 0) best.clear();
     __syncthreads();
 
@@ -433,12 +448,20 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       copy_wait<kDepth - 1>();
       const float group = run.add(get, a.c);
       // What has to be passed only rises; an older value lets more through, not less
-      const entry_t bar = i == 0 ? first_bar<T>(get, n, best, bests) : *(volatile entry_t*)&least;
+      const entry_t bar = i == 0 ? first_bar<T>(get, col0, n, best, bests) : *(volatile entry_t*)&least;
       const float bar_x = value_of(bar);
       const float power = ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo);
-      // (0.99: far more than the sum's rounding.)  The warp looks at a thread's elements
-      // together, one or none a lane.
+      // (0.99: far more than the sum's rounding.)  In flat rows most sums pass; there the
+      // largest element says whether there is something.  The warp looks at a thread's
+      // elements together, one or none a lane.
       unsigned look = __ballot_sync(0xffffffffu, !(group < 0.99f * power));
+      if (look != 0) {
+        float m = Vec<T>::top(get(0));
+#pragma unroll
+        for (int q = 1; q < 4; ++q) m = max_nan(m, Vec<T>::top(get(q)));
+        // (after the first round what is equal to the bar comes after it)
+        look &= __ballot_sync(0xffffffffu, i == 0 ? !(m < bar_x) : !(m <= bar_x));
+      }
       if (look != 0) {
         __syncwarp();   // the copies of all lanes have landed
         do {
@@ -448,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
           entry_t e = 0;
           if (q < 4) {   // (-inf past the segment's end is below every bar)
             const T* its = (const T*)(slots + (d * 4 + q) * kThreads + warp * 32 + from);
-            e = entry_of(Vec<T>::get(its[lane % N]), sp.head + (v0 + vec) * N + lane % N);
+            e = entry_of(Vec<T>::get(its[lane % N]), col0 + (int64_t)vec * N + lane % N);
           }
           best.offer_warp(e, bar);
         } while (look != 0);
@@ -472,16 +495,19 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
     const Stat st = merge_lanes<32>(run.s, a.c);
     if (lane == 0) red[warp] = st;
     __syncthreads();
-    if (*(volatile int*)&count > shape.room || lost) {   // more offers than there is room for (rising rows, many equal values)
+    if (*(volatile int*)&count > shape.room || lost) {   // more offers than there is room for (rising rows)
       __syncthreads();
-      again<T>(best, bests, xv, n, sp.head + v0 * N, xs, scalar);
+      again<T>(best, bests, xv, n, col0, xs, scalar);
     }
+    const int seg = row + (int)rank;
+    more = at < to;
+    if (more) begin();
     best.cut();
     if (!waited) {
       cluster_wait();
       waited = true;
     }
-    const int seg = row + (int)rank, kept = count;
+    const int kept = count;
     const uint32_t to_list = first_cta(all + (int64_t)seg * a.width);
     for (int i = tid; i < kept; i += kThreads) put_remote(to_list + i * 8, best.sorted[i]);
     if (warp == 0) {

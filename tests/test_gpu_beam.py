@@ -151,6 +151,26 @@ def test_select_rising_and_falling_rows(dtype, V):
     check(rows, np.array([[-1.0, -1.25], [-3.0, -2.0]], np.float32), None, 40)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V,shift", [(1100, 0), (9001, 3), (50000, 1), (139255, 0)])
+@pytest.mark.parametrize("width", [1, 4, 32, 33, 128])
+def test_select_equal_and_flat_rows(dtype, V, shift, width):
+    """Rows of one value, of three, and of nearly one: nothing but the columns tells many offers apart."""
+    g = torch.Generator(device="cuda").manual_seed(V + width)
+    store = torch.zeros(4 * V + shift, device="cuda", dtype=DTYPES[dtype])
+    rows = store[shift:].view(4, V)
+    rows[1] = torch.randint(0, 3, (V,), device="cuda", generator=g).to(rows.dtype) / 2
+    rows[2] = torch.randint(0, 2, (V,), device="cuda", generator=g).to(rows.dtype)
+    rows[2, V // 2:] = 1.0 + 1 / 128
+    rows[3] = (1 + 1e-3 * torch.randn(V, device="cuda", generator=g)).to(rows.dtype)
+    got = tuning().beam_select(rows, torch.zeros(4, 1, device="cuda"), width=width)
+    assert (got.parents == 0).all()
+    for i in range(4):   # in each row the order of the logits, of equal ones that of the columns
+        want = torch.sort(rows[i].float(), descending=True, stable=True).indices[:width]
+        assert torch.equal(got.tokens[i], want)
+    check(rows, np.array([[-1.0, -1.25], [-3.0, -2.0]], np.float32), None, width)
+
+
 def test_select_masked_values():
     """Rows masked with the type's lowest value, +inf and NaN, banned altogether, and tiny temperatures."""
     for dtype in DTYPES:
