@@ -452,10 +452,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       const float bar_x = value_of(bar);
       const float power = ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo);
       // (0.99: far more than the sum's rounding.)  In flat rows most sums pass; there the
-      // largest element says whether there is something.  The warp looks at a thread's
-      // elements together, one or none a lane.
+      // largest element says whether there is something (for four threads that costs more
+      // than it saves).  The warp looks at a thread's elements together, one or none a lane.
       unsigned look = __ballot_sync(0xffffffffu, !(group < 0.99f * power));
-      if (look != 0) {
+      if (__popc(look) > 4) {
         float m = Vec<T>::top(get(0));
 #pragma unroll
         for (int q = 1; q < 4; ++q) m = max_nan(m, Vec<T>::top(get(q)));
