@@ -11,9 +11,9 @@
 //
 // What is largest is found on the way at the cost of one comparison per four vectors:
 // a group of elements whose sum of powers is below the power of the width-th largest
-// so far holds nothing that could displace it.  Of the groups that pass, all of them
-// where a row is flat, the largest element is compared; the elements themselves are
-// looked at in the few that still pass.
+// so far (where that is not too small for a sum in fp32) holds nothing that could
+// displace it.  Of the groups that pass, all of them where a row is flat, the largest
+// element is compared; the elements themselves are looked at in the few that still pass.
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -451,10 +451,12 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const __grid_consta
       const entry_t bar = i == 0 ? first_bar<T>(get, col0, n, best, bests) : *(volatile entry_t*)&least;
       const float bar_x = value_of(bar);
       const float power = ex2(fmaf(bar_x, a.c.hi, -run.r) + bar_x * a.c.lo);
-      // (0.99: far more than the sum's rounding.)  In flat rows most sums pass; there the
+      // (0.99: far more than the sum's rounding.  Below 2^-124 a sum has lost half of its
+      // elements, which are taken 2^-2 smaller: beside a dominating column it says nothing,
+      // and everything passes well before that.)  In flat rows most sums pass; there the
       // largest element says whether there is something (for four threads that costs more
       // than it saves).  The warp looks at a thread's elements together, one or none a lane.
-      unsigned look = __ballot_sync(0xffffffffu, !(group < 0.99f * power));
+      unsigned look = __ballot_sync(0xffffffffu, !(power >= 0x1p-120f && group < 0.99f * power));
       if (__popc(look) > 4) {
         float m = Vec<T>::top(get(0));
 #pragma unroll
