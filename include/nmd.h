@@ -533,7 +533,9 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
  * rounded once to its own type.  Singular values on the way have to stay below
  * 3.8 and |a + b s^2 + c s^4| below 15, or the result is not finite; neither is
  * that of a G with NaN or infinities, or of a wait in the kernels that runs out
- * (2 s).  G = 0 gives 0.  eps > 0.  Equal calls give equal bits. */
+ * (2 s).  G = 0 gives 0.  eps > 0.  Equal calls give equal bits (short sides up to
+ * 64 in a context that does not have enough of the SMs are taken another way, with
+ * bits of its own). */
 nmd_status nmd_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
 nmd_status nmd_orthogonalize(const void* d_update, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride,
                              int64_t col_stride, int32_t steps, const double* coefficients, double eps, void* d_out,

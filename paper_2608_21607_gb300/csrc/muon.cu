@@ -952,16 +952,13 @@ Layout layout_of(int64_t R, int64_t C) {
   };
   l.status = take(kInts * sizeof(int));
   l.parts = take(kParts * sizeof(double));
-  if (l.strip) {
-    l.X[0] = take((size_t)std::max(R, C) * 64 * 4);
-    l.part = take(strip_bytes(std::max(R, C)));
-    l.bytes = at;
-    return l;
-  }
-  for (size_t& x : l.X) x = take((size_t)R * l.ldx * 4);
+  // A strip's X in pieces, a row per row of the long side; the rest where the products take its place
+  const size_t x_bytes = l.strip ? (size_t)std::max(R, C) * 64 * 4 : (size_t)R * l.ldx * 4;
+  for (size_t& x : l.X) x = take(x_bytes);
   l.A = take((size_t)l.r * l.ldr * 4);
   l.P = take((size_t)l.r * l.ldr * 4);
-  l.part = take(g.splits > 1 ? (size_t)(g.tiles * g.splits) * kBM * g.BN * 4 : 0);
+  l.part = take(std::max(g.splits > 1 ? (size_t)(g.tiles * g.splits) * kBM * g.BN * 4 : 0,
+                         l.strip ? strip_bytes(std::max(R, C)) : 0));
   l.bytes = at;
   return l;
 }
@@ -971,6 +968,11 @@ void with_type(int dtype, F f) {
   if (dtype == NMD_DT_FP32) f(0.f);
   else if (dtype == NMD_DT_BF16) f(bf16{});
   else f(__half{});
+}
+
+void turn(Job* j) {   // the transpose of every matrix: the steps are the same
+  std::swap(j->R, j->C);
+  for (Matrix* m : {&j->grad, &j->momentum, &j->out}) std::swap(m->rs, m->cs);
 }
 
 nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
@@ -984,7 +986,6 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
   j.flat = filled(j.grad, j.C) && (!j.step || filled(j.momentum, j.C));
   if (l.strip) X = Pieces{X.hi, std::max(j.R, j.C), l.r, 64};
   const Pieces A{(__half*)(w + l.A), l.r, l.r, l.ldr}, P{(__half*)(w + l.P), l.r, l.r, l.ldr};
-  const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
   const int64_t r = l.r, M = std::max(j.R, j.C);
   const int grid = (int)std::min<int64_t>(j.flat ? (j.R * j.C + 8 * kThreads - 1) / (8 * kThreads)
                                                  : (walk_of(j.R, j.C).work + kThreads / 32 - 1) / (kThreads / 32), kParts);
@@ -1004,7 +1005,16 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
     });
   });
   if (st != NMD_OK) return st;
-  if (l.strip) return strip_run(j, X, steps, k, status, w + l.part, s);
+  if (l.strip) {
+    if (strip_run(j, X, steps, k, status, w + l.part, s) == NMD_OK) return NMD_OK;
+    // Its CTAs wait for one another and are launched only if all can run at a time, which a
+    // context with a part of the SMs does not give.  The momentum is on its way, so the
+    // products below, which wait for none, take X as it is.
+    (void)cudaGetLastError();
+    if (turned) turn(&j);
+    Y = Pieces{Y.hi, X.rows, X.cols, X.ld};
+  }
+  const bool wide = j.R <= j.C;   // X is r x M; otherwise M x r
   auto wide_tiles = [&](int64_t depth) { return j.out.dtype != NMD_DT_FP32 && depth >= kWideDepth; };
   const GramPlan plan = gram_plan(r, M, wide_tiles(M));
   const int bn_r = columns_of(r, r, true, wide_tiles(r)), bn_x = columns_of(j.R, j.C, false, wide_tiles(r));
@@ -1100,10 +1110,6 @@ bool check(const void* x, int dtype, int64_t rows, int64_t cols, int64_t rs, int
 // whether the rows' elements lie further apart than the columns'
 bool columns_apart(int64_t rows, int64_t cols, int64_t rs, int64_t cs) {
   return rows > 1 && (cols <= 1 || rs < cs);
-}
-void turn(Job* j) {   // the transpose of every matrix: the steps are the same
-  std::swap(j->R, j->C);
-  for (Matrix* m : {&j->grad, &j->momentum, &j->out}) std::swap(m->rs, m->cs);
 }
 bool sizes_ok(int64_t rows, int64_t cols) {
   return rows >= 0 && cols >= 0 && rows < ((int64_t)1 << 31) && cols < ((int64_t)1 << 31) && std::min(rows, cols) <= kMostSide &&

@@ -23,6 +23,9 @@
 //   A A:    likewise.
 // The small products have accumulators of their own, and Z leaves TMEM after every tile.
 //
+// Where the grid cannot run all at a time the launch is refused, and muon.cu's products
+// take its place.
+//
 // A tile is stored as rows of 64 columns, 128 bytes in the 128-byte swizzle, hi and lo
 // one after the other: K-major for X P, MN-major for X^T X.
 #include <algorithm>
