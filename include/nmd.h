@@ -518,9 +518,9 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
 
 /* ---------------------------------------------------------------------------
  * The training step on the gradients of the factors, or of other matrices.
- * Matrices are rows x cols (at most 2^31 - 1 each, 0 allowed), element (i, j) at
- * i row_stride + j col_stride (elements; >= 0), of any of the three types.  The
- * smaller side is at most 16384.  The elements of a matrix that is written lie
+ * Matrices are rows x cols (at most 2^31 - 1 each and 2^36 elements, 0 allowed),
+ * element (i, j) at i row_stride + j col_stride (elements; >= 0, and a side times its
+ * stride at most 2^44), of any of the three types.  The smaller side is at most 16384.  The elements of a matrix that is written lie
  * apart (NMD_ERR_INVALID), and it overlaps no other one, except that d_out may be
  * d_update itself with its strides.
  *

@@ -1077,20 +1077,23 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
   return NMD_OK;
 }
 
-// Whether the elements of a matrix lie apart, and the bytes from its first to its last
-bool apart(int64_t rows, int64_t cols, int64_t rs, int64_t cs, int64_t es, int64_t* reach) {
-  if (rs < 0 || cs < 0 || rs > ((int64_t)1 << 40) || cs > ((int64_t)1 << 40)) return false;
+// How far the elements of a matrix reach (a stride may be 0), and whether they lie apart; false where
+// that is no distance in memory
+constexpr int64_t kMostReach = (int64_t)1 << 44;   // elements
+bool reach_of(int64_t rows, int64_t cols, int64_t rs, int64_t cs, int64_t* reach, bool* apart) {
+  if (rs < 0 || cs < 0 || rs > kMostReach || cs > kMostReach) return false;
   int64_t n[2] = {rows, cols}, st[2] = {rs, cs};
   if (n[0] > 1 && n[1] > 1 && st[0] < st[1]) std::swap(n[0], n[1]), std::swap(st[0], st[1]);
   int64_t span = 1;
-  bool ok = true;
+  *apart = true;
   for (int i = 1; i >= 0; --i) {
     if (n[i] <= 1) continue;
-    ok &= st[i] >= span;
+    if (st[i] > kMostReach / n[i]) return false;
+    *apart &= st[i] >= span;
     span += (n[i] - 1) * st[i];
   }
-  *reach = span * es;
-  return ok;
+  *reach = span;
+  return true;
 }
 inline int64_t size_of(int dtype) { return dtype == NMD_DT_FP32 ? 4 : 2; }
 
@@ -1102,9 +1105,9 @@ struct Range {
 bool check(const void* x, int dtype, int64_t rows, int64_t cols, int64_t rs, int64_t cs, bool unique, Range* at) {
   if (dtype < NMD_DT_FP32 || dtype > NMD_DT_FP16 || !x || ((uintptr_t)x & (uintptr_t)(size_of(dtype) - 1))) return false;
   int64_t reach = 0;
-  const bool ok = apart(rows, cols, rs, cs, size_of(dtype), &reach);
-  if ((unique && !ok) || rs < 0 || cs < 0 || rs > ((int64_t)1 << 40) || cs > ((int64_t)1 << 40)) return false;
-  *at = Range{(uintptr_t)x, (uintptr_t)x + (uintptr_t)reach};
+  bool apart = false;
+  if (!reach_of(rows, cols, rs, cs, &reach, &apart) || (unique && !apart)) return false;
+  *at = Range{(uintptr_t)x, (uintptr_t)x + (uintptr_t)(reach * size_of(dtype))};
   return true;
 }
 // whether the rows' elements lie further apart than the columns'
