@@ -358,6 +358,8 @@ def beam_reorder(states, parents, *, dim: int = 0, out=None):
         rest, rows, outer, stride, row, nbytes = here
         if x.get_device() != index or y is not x and (y.get_device() != index or y.dtype != x.dtype or rest != there[0]):
             _invalid("states, out: tensors on cuda:%d, of one type each and alike apart from the rows, are wanted" % index)
+        if y is not x and (x.is_conj() != y.is_conj() or x.is_neg() != y.is_neg()):
+            _invalid("states, out: both or none of them conjugated or negated on reading are wanted")
         k = rows // B if B else w
         if rows != B * k or there[1] != B * w or (K is not None and k != K):
             _invalid("states, out: B x K rows and B x width rows for parents of %d x %d are wanted" % (B, w))
@@ -376,6 +378,8 @@ def _update_matrix(x, name: str, shape=None, device=None) -> int:
         _invalid("%s: a two-dimensional float32, bfloat16 or float16 CUDA tensor is wanted" % name)
     if shape is not None and (x.shape != shape or x.device != device):
         _invalid("%s: %d x %d on %s is wanted" % (name, *shape, device))
+    if x.is_neg():   # (the imaginary part of a conjugate: memory holds its negative)
+        _invalid("%s: a tensor that is not negated on reading is wanted (resolve_neg)" % name)
     return _DTYPES[x.dtype]
 
 
