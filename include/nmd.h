@@ -529,8 +529,14 @@ nmd_status nmd_beam_reorder(int64_t count, const nmd_beam_state* states, int64_t
  *   A = X X^T,  X <- a X + (b A + c A^2) X      (A of the smaller side),
  * (a, b, c) = coefficients, which maps every singular value s to
  * a s + b s^3 + c s^5 and leaves the singular vectors.  Each element of X is held
- * to 22 bits, or to 2^-37 of |X|_F where that is more, sums are fp32; the result is
- * rounded once to its own type.  Singular values on the way have to stay below
+ * to 22 bits, or to 2^-37 where that is more.  (A first X of less than 2^-8 in norm is
+ * kept larger by a power of two, up to 2^100: |G|_F below 2^-100 eps loses bits, and
+ * below 2^-126 eps the result may be 0.)  Sums are fp32: of 64 products, or 256 for
+ * 16-bit results, on the tensor cores, which round towards zero, and of these sums to
+ * nearest.  Results in fp32 are as far from the definition as steps in fp32 products
+ * leave them, or some times that (about 1e-6 of the norm for a few strong directions
+ * over noise), 16-bit ones up to ten times before they are rounded once to their own
+ * type.  Singular values on the way have to stay below
  * 3.8 and |a + b s^2 + c s^4| below 15, or the result is not finite; neither is
  * that of a G with NaN or infinities, or of a wait in the kernels that runs out
  * (2 s).  G = 0 gives 0.  eps > 0.  Equal calls give equal bits (short sides up to
