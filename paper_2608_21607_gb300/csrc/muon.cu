@@ -3,9 +3,9 @@
 //
 // The products run on the tcgen05 tensor cores.  Every matrix on the way (X, A =
 // X X^T, P = a I + b A + c A^2) is kept as two fp16 pieces of 2^12 x, hi =
-// fp16(v), lo = fp16(v - hi): 22 bits, and an absolute error below 2^-37 however
-// small the element (|X|_F starts at 1).  (Where eps is most of the divisor, X starts
-// much smaller and is kept 2^t larger, t falling to 0 as the steps raise it.)  A product
+// fp16(v), lo = fp16(v - hi): 22 bits, or an absolute error below 2^-37 where that is
+// more.  (|X|_F starts at 1, or less where eps is much of the divisor; below 2^-8 X is
+// kept 2^t larger, t at most 100 and falling to 0 as the steps raise it.)  A product
 // is hi hi + hi lo + lo hi, three MMAs; what lo lo would add is below 2^-22.  In fp32
 // throughout the errors of early steps grow by up to a per step just the same, and the
 // two come out equally far from the definition (a gradient of 139,255 x 64: 7.6e-7, fp32
@@ -14,8 +14,8 @@
 // alone a 16-bit result by up to twice its rounding.
 // The tensor cores add in fp32 but round towards zero, which leans by up to a unit of
 // the sum so far per addition; so the two small products of 64 columns come first,
-// and after each 64 columns the sum leaves TMEM and goes on in the epilogue's
-// registers, rounded to nearest.
+// and after each 64 columns (256 for 16-bit results, see run()) the sum leaves TMEM and
+// goes on in the epilogue's registers, rounded to nearest.
 //
 // A step is three products: the Gram matrix (half of its tiles, the sum split where there
 // are few), the polynomial (likewise half), and the update.  4096 x 4096 in bf16 takes
@@ -547,13 +547,15 @@ __device__ __forceinline__ void put_square(const Gemm& p, float alpha, float* sq
 }
 
 // D = A B^T in tiles of 128 x BN.  An operand whose sum runs along its rows in memory
-// (AMN = false: A[m][k]) comes in tiles of 64 adjacent k; one whose sum runs
+// (AMN = false: A[m][k]) comes in tiles of 64 adjacent k (32 for BN = 256); one whose sum runs
 // across them (AMN: A[k][m]) in panels of 64 adjacent m, and the tensor cores take
 // it as MN-major.  Hi and lo pieces are the two planes of one tensor map.
-//   warps 0-7   epilogue: a sum's chunks from TMEM (lane = row, two halves of the
-//               columns), added up in registers, then written
-//   warp 8      loads, one elected lane
-//   warp 9      issues the products
+//   epilogue    8 warps, or 16 for tiles of 256 columns: a sum's chunks from TMEM (a
+//               lane a row; two or four parts of the columns), added up in registers,
+//               then written; of 16, the two warps of the same rows share a square of
+//               shared memory and use it in turn
+//   one warp    loads, one elected lane
+//   one warp    issues the products
 // Work items (tile, part of the sum) are dealt to one CTA per SM in turn; two TMEM
 // buffers and the ring of stages run on from one item to the next.
 template <int BN, bool AMN, bool BMN>
@@ -913,7 +915,10 @@ struct GramPlan {
 GramPlan gram_plan(int64_t r, int64_t M, bool wide) {
   GramPlan g;
   const int64_t blocks = (M + kBK - 1) / kBK;
-  if (blocks <= 20) {   // the sum of 20 blocks takes what adding parts up would (8 us)
+  // A sum of 20 blocks takes what adding parts up would (8 us).  Five steps with whole sums and
+  // with parts: 318 x 1280 185 and 182 us, x 1920 215 and 203, x 2560 246 and 185; 556 x 960
+  // 194 and 213, x 1280 211 and 233, x 1920 248 and 238; 1001 x 1280 278 and 298.
+  if (blocks <= 20) {
     g.BN = columns_of(r, r, true, wide);
     g.tiles = tiles_of(r, r, g.BN, true);
     g.splits = 1;
@@ -1030,9 +1035,12 @@ nmd_status run(Job j, int steps, const double* k, void* ws, cudaStream_t s) {
     g.lower = lower;
     g.mode = mode;
     g.status = status;
-    // A 16-bit result does not see what sums of 256 lean by (5e-7), and a whole sum of that
-    // length in TMEM lets the epilogue work beside the next tile's products (256 x 139,255
-    // bf16: 760 us with sums of 64)
+    // Sums of 256 lean more than those of 64: before its rounding (1.66e-3 of the norm in
+    // bf16) a result of 256 x 139,255 is 1.5e-5 off instead of 3.1e-6, of 4096 x 4096 3.8e-6
+    // instead of 1.3e-6, so that single elements round to a neighbour (2.7e-4 and 1.1e-4
+    // from the rounded definition instead of 1.2e-4 and 7e-5).  A whole sum of that length
+    // in TMEM lets the epilogue work beside the next tile's products: 706 instead of 808 us,
+    // 3.46 instead of 4.13 ms.  (Sums of 128: 7.3e-6 and 2.0e-6, 722 us and 3.72 ms.)
     g.chunk = (j.out.dtype == NMD_DT_FP32 ? 64 : 256) / depth_of(BN);
     return g;
   };

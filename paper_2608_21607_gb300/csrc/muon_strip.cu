@@ -40,7 +40,10 @@ using namespace tc;
 
 constexpr int kThreads = 256, kSms = 152;                  // threads that work; one warp more issues the products
 constexpr int kRows = 128, kSide = 64;
-constexpr int kFew = 8;                                     // CTAs that add up each other's Z without a second barrier
+// CTAs that add up each other's Z without a second barrier (M x 64, five steps, one barrier
+// and two: 2 CTAs 43 and 64 us, 4 46 and 64, 8 57 and 72, 12 62 and 78, 16 69 and 56, 24 81
+// and 66; 9 to 15 share the elements unevenly and would gain from one)
+constexpr int kFew = 8;
 constexpr int kBuffers = 6;                                 // tiles in shared memory
 constexpr int kPiece = kRows * kSide * 2, kTile = 2 * kPiece;   // bytes
 constexpr int kSquare = 2 * kSide * kSide * 2;              // both pieces of a 64 x 64 matrix
@@ -404,7 +407,9 @@ __global__ void __launch_bounds__(kThreads + 32, 1) strip_kernel(const __grid_co
 #pragma unroll
           for (int i = 0; i < kSide * kSide / kThreads; ++i) v[i] += __ldcg(parts + (size_t)q * kSide * kSide + i * kThreads + tid);
       } else {
-        if (G <= 32) {   // 32 elements by a warp
+        // 32 elements by a warp, or by eight (16 CTAs 56 and 72 us, 24 66 and 68, 32 58 and 64,
+        // 47 76 and 64, 152 88 and 68)
+        if (G <= 32) {
           for (int e0 = (blockIdx.x * 8 + warp) * 32; e0 < kSide * kSide; e0 += G * 8 * 32) {
             float s = 0.f;
 #pragma unroll 16
