@@ -786,7 +786,7 @@ __device__ __forceinline__ void move_halves(const State& s, int64_t slice, int64
 // A CTA takes a piece of all K rows of a group at a time: what is needed of it is in
 // shared memory before any row is written, so that rows may change places.  In place,
 // rows that stay are not written, and those that nothing goes on from not read.  Bound by
-// HBM: 16 tensors of 512 rows of 64 KB (groups of eight, parents at random) take 142 us,
+// HBM: 16 tensors of 512 rows of 64 KB (groups of eight, parents at random) take 138 us,
 // 5.8 TB/s over what moves; with four CTAs an SM 154 us, and 179 us where the grid is
 // larger than what fits at a time.
 __global__ void __launch_bounds__(kThreads, 6) reorder_kernel(const __grid_constant__ States a) {
